@@ -525,6 +525,135 @@ int dflare_weighted_ce(const float* logits, const int32_t* labels, int32_t rows,
 int dflare_weighted_ce_noalloc(const float* logits, const int32_t* labels, int32_t rows, int32_t V, int32_t B,
                                float gamma, float* loss, float* row_ce, float* dlogits, void* stream);
 
+/*
+ * ---- The rest of a draft layer's training step (no handle) ----
+ * Norms, rotary positions, the LM head with its loss, and the gradients' norm: what surrounds the
+ * anchor attention.  Tensors are DEVICE memory, row-major and contiguous where no strides are given,
+ * aligned to their elements (to 16 bytes where said); DFLARE_F32 and DFLARE_BF16 name their types.
+ * Every call is asynchronous on `stream` (hipStream_t, NULL = default), which must belong to the current device
+ * (else INVALID_ARG), allocates nothing, can be captured into a graph, and gives the same bits when it
+ * is repeated.  A workspace belongs to one call at a time; its contents need not be kept.
+ */
+enum { DFLARE_F32 = 0, DFLARE_BF16 = 1 };
+
+/*
+ * dflare_rope_frequencies -- the inverse frequencies of a rotary embedding, on the HOST, in double:
+ * f_m = base^(-2 m / rotary_dim) for m < rotary_dim / 2, stretched for longer contexts by `method`:
+ *   DFLARE_ROPE_PLAIN   as they are (factor and original_len are not read)
+ *   DFLARE_ROPE_LINEAR  f_m / factor (positions interpolated)
+ *   DFLARE_ROPE_NTK     base factor^(d / (d - 2)) in the place of base, d = rotary_dim (d = 2: as they are)
+ *   DFLARE_ROPE_YARN    f_m (k + (1 - k) / factor), k = clamp((original_len f_m / 2 pi - 1) / 31, 0, 1): pairs that turn
+ *                       more than 32 times within the original context stay, those that turn less
+ *                       than once are interpolated (Peng et al., "YaRN", 2023); *scale = 0.1 ln(factor) + 1
+ *   inv_freq  HOST double [rotary_dim / 2], out;  scale  HOST float out, or NULL: the factor on cosines and
+ *             sines (1 except for YARN).
+ * rotary_dim odd or below 2, base <= 0, factor < 1, original_len <= 0 or a value that is not finite: INVALID_ARG.
+ */
+enum { DFLARE_ROPE_PLAIN = 0, DFLARE_ROPE_LINEAR = 1, DFLARE_ROPE_NTK = 2, DFLARE_ROPE_YARN = 3 };
+int dflare_rope_frequencies(int32_t rotary_dim, double base, int32_t method, double factor, double original_len,
+                            double* inv_freq, float* scale);
+
+/*
+ * dflare_rope -- rotary positions of one or two tensors whose rows have the same positions (queries and
+ * keys), in one launch.  Element pair m of a head at position p becomes
+ *   (a cos - b sin, b cos + a sin) scale,  angle p f_m,
+ * a, b = elements m, m + rotary_dim / 2 (DFLARE_ROPE_HALF) or 2 m, 2 m + 1 (DFLARE_ROPE_INTERLEAVED); elements from
+ * rotary_dim on are copied.  Angles are formed in double, products in fp32, each result is rounded once.
+ *   tensors     HOST [n_tensors], 1 or 2: x [rows, n_heads, head_dim] and y of the same shape, with strides in
+ *               elements from row to row and from head to head (a head's elements are contiguous).  y may
+ *               be x with the same strides (in place); otherwise nothing written may overlap anything else.
+ *   positions   DEVICE int32 [ceil(rows / B)] or NULL: row r sits at positions[r / B] + r % B (B = 1: a position
+ *               per row; blocks anchored at positions: B rows each); NULL: at r.
+ *   inv_freq    DEVICE double [rotary_dim / 2], as dflare_rope_frequencies gives them.
+ *   inverse     0, or not 0: turns by the opposite angle, which maps the output's gradient to x's.
+ * rows = 0 does nothing.  head_dim > 1,024 or n_heads head_dim > 2^20: UNSUPPORTED.  Any alignment and strides; 16-byte
+ * accesses where all of them allow it.
+ */
+enum { DFLARE_ROPE_HALF = 0, DFLARE_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t x_row, x_head, y_row, y_head; /* strides, in elements */
+  int32_t n_heads;
+} dflare_rope_tensor;
+int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int32_t* positions, const double* inv_freq,
+                int32_t rows, int32_t B, int32_t head_dim, int32_t rotary_dim, int32_t dtype, int32_t layout,
+                float scale, int32_t inverse, void* stream);
+
+/*
+ * dflare_norm_fwd -- y = (h - mean) rstd gain + bias over rows of H values, with h = x, or h = x + residual
+ * rounded to the tensors' type and written to sum (the residual stream).
+ *   kind     DFLARE_NORM_RMS: mean = 0, rstd = 1 / sqrt(mean of h^2 + eps), no bias (must be NULL);
+ *            DFLARE_NORM_LAYER: rstd = 1 / sqrt(mean of (h - mean)^2 + eps).
+ *   x, residual (or NULL), gain (or NULL: ones), bias (or NULL: zeros), sum (read only with a residual), y: of
+ *            type dtype, [rows, H] or [H].  sum and y may be x or residual, not each other.
+ *   mean     fp32 [rows] out (LAYER; not written for RMS);  rstd  fp32 [rows] out.
+ * Statistics and products in fp32.  rows = 0 does nothing; H > 16,384: UNSUPPORTED.
+ */
+enum { DFLARE_NORM_RMS = 0, DFLARE_NORM_LAYER = 1 };
+int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const void* bias, int32_t rows, int32_t H,
+                    int32_t dtype, int32_t kind, float eps, void* sum, void* y, float* mean, float* rstd, void* stream);
+
+/*
+ * dflare_norm_bwd -- gradients of the above for the output gradient dy:
+ *   h        the normalised rows (x, or sum where there was a residual);  mean, rstd  of the forward pass
+ *   dsum     gradient of sum from its other uses, added to dx, or NULL
+ *   dx       [rows, H] of type dtype out: the gradient of h (of x and of residual alike); may be dy or dsum
+ *   dgain    fp32 [H] out;  dbias  fp32 [H] out (LAYER) or NULL: summed over the rows in a fixed order in fp32
+ *   workspace  16-byte aligned, at least dflare_norm_bwd_workspace(rows, H, kind) bytes
+ * rows = 0 writes zeros to dgain and dbias.
+ */
+size_t dflare_norm_bwd_workspace(int32_t rows, int32_t H, int32_t kind);
+int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float* mean, const float* rstd,
+                    const void* dsum, int32_t rows, int32_t H, int32_t dtype, int32_t kind, void* dx, float* dgain,
+                    float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dflare_linear_ce -- the LM head and dflare_weighted_ce in one: logits z = hidden head^T are formed piece by
+ * piece and never kept, and the gradients are those of hidden and head.  Row r is position b = r % B of its
+ * block; rows with b = 0 or a label outside [0, V) carry no loss, take no part in any product (they may hold
+ * anything) and get zeros; the others have weight w = exp(-(b - 1) / gamma), and the loss is sum w CE / sum w.
+ *   hidden   bf16 [rows, H];  head  bf16 [V, H];  labels  int32 [rows]
+ *   loss     fp32 [1] out;  row_ce  fp32 [rows] out (CE per row, 0 where no loss)
+ *   dhidden  bf16 [rows, H] out, or NULL: not wanted;  dhead  bf16 [V, H] out, or NULL
+ *   workspace  at least dflare_linear_ce_workspace(rows, V, H, dhidden wanted, dhead wanted) bytes; it grows
+ *            with rows, V and H, not with rows x V
+ * hidden, head, dhidden, dhead and workspace 16-byte aligned.  rows not a multiple of B, gamma <= 0 or not finite:
+ * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows or about 2^39 logits: UNSUPPORTED (the
+ * workspace is then 0 bytes).  Products run on the bf16 matrix cores with fp32 sums; the logits' gradient is
+ * rounded to bf16 as their operand, each gradient once more where it is written.  NaN or infinities in a row
+ * that takes part, or in head, make results NaN.
+ */
+size_t dflare_linear_ce_workspace(int32_t rows, int32_t V, int32_t H, int32_t dhidden, int32_t dhead);
+int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels, int32_t rows, int32_t V, int32_t H,
+                     int32_t B, float gamma, float* loss, float* row_ce, void* dhidden, void* dhead, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/*
+ * dflare_grad_norm -- the global 2-norm of n gradient tensors: *sumsq = sum of all squares, formed and added
+ * in double in a fixed order; *norm = its root in fp32.  Ranks that hold parts of the gradients add their
+ * sumsq before they clip.
+ *   tensors    HOST [n], read before the call returns; `out` is not read.  Empty tensors (n = 0) and n = 0 are allowed.
+ *   sumsq      DEVICE double [1] out;  norm  DEVICE fp32 [1] out or NULL
+ *   workspace  8-byte aligned, at least dflare_grad_norm_workspace(n) bytes
+ * dflare_clip_grads -- out = data max_norm / norm where norm = sqrt(*sumsq) is above max_norm, out = data
+ * otherwise; also where *sumsq is NaN or infinite (the caller sees it there and drops the step).
+ *   out        of each tensor: where the clipped values go, NULL: data itself.  No tensor that is written may
+ *              overlap another one (INVALID_ARG).
+ *   max_norm   >= 0; infinite: nothing is clipped.
+ * More than 2^36 elements in one tensor: UNSUPPORTED.
+ */
+typedef struct {
+  void* data;
+  void* out;
+  int64_t n;     /* elements */
+  int32_t dtype;
+} dflare_grad_tensor;
+size_t dflare_grad_norm_workspace(int32_t n);
+int dflare_grad_norm(const dflare_grad_tensor* tensors, int32_t n, double* sumsq, float* norm, void* workspace,
+                     size_t workspace_bytes, void* stream);
+int dflare_clip_grads(const dflare_grad_tensor* tensors, int32_t n, const double* sumsq, float max_norm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

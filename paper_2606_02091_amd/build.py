@@ -13,7 +13,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libdflare.so")
-SOURCES = ["kernels.hip", "batched.hip", "runtime.hip", "training.hip"]
+SOURCES = ["kernels.hip", "batched.hip", "runtime.hip", "training.hip", "train_ops.hip",
+           "linear_ce.hip"]
 ARCH = os.environ.get("DFLARE_OFFLOAD_ARCH", "gfx950")
 
 

@@ -1,0 +1,589 @@
+// The LM head with the position-weighted cross-entropy (Sec. 3.3, Sec. 4.3, Eq. 5) and its gradients,
+// without logits in memory.  With z = h W^T over the rows that carry a loss, c_r = w_r / sum w,
+//   ce_r = lse(z_r) - z_r[y_r],  loss = sum c ce,  dz = c (softmax(z) - onehot(y)),
+//   dh = dz W,  dW = dz^T h.
+// The rows with a loss are gathered first (the others take no part in any product).  One product gives
+// every row's maximum and sum per 256 words, from which its log-sum-exp follows; for the gradients the
+// vocabulary is walked in pieces: the product again, its epilogue writes the piece's dz in bf16, and this
+// feeds the products for dh (added up in fp32 over the pieces) and dW.
+// Bound by the matrix cores: 2 rows V H operations for the loss, 4 more for dh, 2 more for dW.
+#include <hip/hip_runtime.h>
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "device_common.h"
+#include "dflare.h"
+
+namespace dflare {
+
+namespace {
+
+constexpr int kT = 512;     // threads of a product's work-group: 8 waves
+constexpr int kTile = 256;  // output tile: 256 x 256, a wave 128 x 64
+constexpr int kBK = 64;     // k of a stage
+constexpr int kOpBytes = kTile * kBK * 2;
+constexpr float kL2E = 1.4426950408889634f;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_w __attribute__((ext_vector_type(2)));
+typedef float f32x2_w __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                 0, 0);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {  // to bf16, nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_w{a, b}), bf16x2_w));
+}
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct Lce {
+  const uint16_t *hidden, *head;
+  const int32_t* labels;
+  float *loss, *row_ce;
+  uint16_t *dhidden, *dhead;
+  int rows, V, H, B;
+  float gamma;
+  // workspace; i counts the rows with a loss, Mp = rows rounded up to whole tiles
+  int* count;     // [1] rows with a loss
+  int* src;       // [Mp] i -> row
+  int* pos;       // [rows] row -> i, -1 without a loss
+  float* c;       // [Mp] w / sum w, 0 past the last
+  uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
+  float2* part;   // [words / 256][Mp] (max, sum of exp(z - max))
+  float* zlab;    // [Mp] z at the label
+  float* lse2;    // [Mp] log2-domain log-sum-exp
+  uint16_t* dz;   // [Mp][Vp] dz of a piece of the vocabulary
+  float* dacc;    // [KS][Mp][H] dh of the pieces so far, in KS parts
+  int Mp, ldh, Vp, KS;
+};
+
+// ---- rows with a loss, in order; their weights; work-group of 1,024 threads ----
+__global__ __launch_bounds__(1024) void k_lce_rows(Lce a) {
+  __shared__ int wc[16];
+  __shared__ double ws[16];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  int n = 0;
+  double sum = 0.0;
+  for (int base = 0; base < a.rows; base += 1024) {
+    const int r = base + tid;
+    const int b = r % a.B, y = r < a.rows ? a.labels[r] : -1;
+    const bool on = b > 0 && y >= 0 && y < a.V;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(on);
+    if (lane == 0) wc[wv] = __builtin_popcountll(m);
+    __syncthreads();
+    int i = n + __builtin_popcountll(m & ((1ull << lane) - 1));
+    for (int k = 0; k < 16; ++k) {
+      if (k < wv) i += wc[k];
+      n += wc[k];
+    }
+    __syncthreads();
+    if (on) {
+      const float w = expf(-(float)(b - 1) / a.gamma);
+      sum += w;
+      a.src[i] = r;
+      a.c[i] = w;
+    }
+    if (r < a.rows) {
+      a.pos[r] = on ? i : -1;
+      if (!on) a.row_ce[r] = 0.f;
+    }
+  }
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+  if (lane == 0) ws[wv] = sum;
+  __syncthreads();
+  sum = 0.0;
+  for (int k = 0; k < 16; ++k) sum += ws[k];
+  const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
+  const int np = min((n + kTile - 1) / kTile * kTile, a.Mp);
+  for (int i = tid; i < np; i += 1024) a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
+  if (tid == 0) a.count[0] = n;
+}
+
+__global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
+  const int n = a.count[0], i = blockIdx.x;
+  if (i >= (n + kTile - 1) / kTile * kTile) return;
+  const u32x4 z = {0u, 0u, 0u, 0u};
+  const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)(i < n ? a.src[i] : 0) * a.H);
+  u32x4* to = reinterpret_cast<u32x4*>(a.hc + (long)i * a.ldh);
+  for (int p = threadIdx.x; p < a.ldh / 8; p += 256) to[p] = i < n && p < a.H / 8 ? from[p] : z;
+}
+
+// ---- products.  D[n][m] = sum over k of A[m, k] B[n, k] for a tile of 256 m x 256 n.  An operand lies in memory
+// either with k along its rows (plain) or with k down its columns (across); both go to LDS as they lie, 16-byte
+// pieces permuted by an xor so that the reads are free of bank conflicts, and the `across` ones are transposed
+// by the LDS read (ds_read_b64_tr_b16):
+//   plain   256 rows x 64 k, 128 bytes a row: piece c of row r at c ^ (r / 2 mod 8)
+//   across  64 k x 256 columns, 512 bytes a row: piece c of row k at c ^ 4 (k mod 4)
+// m runs along A so that a lane holds, of one n (a token's row), 4 consecutive m at a time: sums over the words
+// of a row stay within a lane. ----
+struct Operand {
+  const uint16_t* p;  // first element of the tile's rows (plain) or columns (across)
+  long ld;
+  int valid;  // rows (plain) or columns (across) of the tile that exist; past them the last is repeated
+  int kend;   // plain: k that exist (past them the row's k = 0 of the stage again, to meet zeros of the other operand)
+};
+
+template <bool ACROSS>
+struct Loader {
+  const char* base;
+  uint32_t off[4], back[4];  // byte offset of the wave's four pieces of a lane; what takes it back to k = 0
+  long step;
+  int kl[4];  // first k of the piece
+  __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
+    base = reinterpret_cast<const char*>(o.p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (!ACROSS) {
+        const int row = (4 * w + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+        off[j] = (uint32_t)(min(row, o.valid - 1) * o.ld * 2 + c * 16);
+        back[j] = c * 16;
+        kl[j] = c * 8;
+      } else {
+        const int row = (4 * w + j) * 2 + (lane >> 5), c = (lane & 31) ^ ((row & 3) << 2);
+        off[j] = (uint32_t)(row * o.ld * 2 + min(c * 8, o.valid - 8) * 2);
+        back[j] = (uint32_t)(row * o.ld * 2);
+        kl[j] = row;
+      }
+    }
+    step = ACROSS ? o.ld * kBK * 2 : kBK * 2;
+  }
+  // the wave's share of a stage; left: k that exist from the stage's first on
+  __device__ __forceinline__ void issue(char* dst, int w, int kt, int left) const {
+    const char* b = base + kt * step;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t o = kl[j] < left ? off[j] : off[j] - back[j];
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(b + o), (LDSP char*)(dst + (4 * w + j) * 1024), 16, 0, 0);
+    }
+  }
+};
+
+template <bool ACROSS>
+struct Reader {
+  uint32_t off[4];
+  // tile0: first 32-row (or 32-column) tile of the wave
+  __device__ __forceinline__ void init(int tile0, int lane) {
+    const int h = lane >> 5;
+    if constexpr (!ACROSS) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        off[ks] = (tile0 * 32 + (lane & 31)) * 128 + (((2 * ks + h) ^ ((lane >> 1) & 7)) << 4);
+    } else {
+      const int i = lane & 15, g = (lane >> 4) & 1, f = i >> 2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        off[j] = (8 * h + f) * 512 + ((4 * ((tile0 + j) ^ f) + 2 * g + ((i & 3) >> 1)) << 4) + (i & 1) * 8;
+    }
+  }
+  __device__ __forceinline__ u32x4 get(const char* op, int ks, int j) const {
+    if constexpr (!ACROSS) return *reinterpret_cast<const u32x4*>(op + off[ks] + j * 4096);
+    else {
+      const char* p = op + off[j] + ks * 16 * 512;
+      const u32x2 lo = tr(p), hi = tr(p + 4 * 512);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+  }
+  static __device__ __forceinline__ u32x2 tr(const char* p) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDSP s16x4*)(LDSP char*)const_cast<char*>(p)));
+  }
+};
+
+typedef f32x16 Acc[4][2];
+
+// acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
+// something finite
+template <bool XA, bool XB>
+__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc& acc) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Loader<XA> la;
+  Loader<XB> lb;
+  la.init(oa, w, lane);
+  lb.init(ob, w, lane);
+  Reader<XA> ra;
+  Reader<XB> rb;
+  ra.init((w & 1) * 4, lane);
+  rb.init((w >> 1) * 2, lane);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  const int nk = (K + kBK - 1) / kBK;
+  auto issue = [&](int kt) {
+    char* st = lds + (kt & 1) * 2 * kOpBytes;
+    la.issue(st, w, kt, oa.kend - kt * kBK);
+    lb.issue(st + kOpBytes, w, kt, ob.kend - kt * kBK);
+  };
+  if (nk > 0) issue(0);
+  for (int kt = 0; kt < nk; ++kt) {
+    wait_vm();
+    __syncthreads();
+    if (kt + 1 < nk) issue(kt + 1);
+    const char* st = lds + (kt & 1) * 2 * kOpBytes;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      u32x4 fa[4], fb[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fa[i] = ra.get(st, ks, i);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) fb[j] = rb.get(st + kOpBytes, ks, j);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] = mfma32(fa[i], fb[j], acc[i][j]);
+    }
+  }
+  __syncthreads();
+}
+
+// Output tile t of TA x TB, so that the work-groups that run together on an XCD (ids are dealt to the 8 XCDs
+// in turn) share operand tiles in its L2: an XCD takes a contiguous part of the tiles, in groups of 4 A tiles by
+// all B tiles.  false past the last tile.
+__device__ __forceinline__ bool tile_of(int id, int TA, int TB, int& ta, int& tb) {
+  const int total = TA * TB, per = (total + 7) / 8;
+  const int t = id % 8 * per + id / 8;
+  if (id / 8 >= per || t >= total) return false;
+  const int g = t / (4 * TB), w = min(4, TA - 4 * g), r = t - g * 4 * TB;
+  ta = 4 * g + r % w;
+  tb = r / w;
+  return true;
+}
+
+// bf16 tile from LDS to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
+__device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long ld, int nv, int mv) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll 4
+  for (int it = 0; it < 16; ++it) {
+    const int n = w * 32 + it * 2 + (lane >> 5), p = lane & 31;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + n * 512 + ((p ^ (n & 31)) << 4));
+    if (n < nv && p * 8 < mv) *reinterpret_cast<u32x4*>(to + n * ld + p * 8) = v;
+  }
+}
+
+enum { kStats, kDz, kDh, kDw };
+
+// One tile of a product and its epilogue:
+//   kStats  z tile (256 words x 256 rows) -> part, zlab
+//   kDz     z tile of the piece from word v0 on -> dz
+//   kDh     dacc (+)= dz W over the piece's words, in KS parts (z of the grid)
+//   kDw     dhead rows of the piece = dz^T h
+template <int MODE>
+__global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int first) {
+  __shared__ __attribute__((aligned(1024))) char lds[4 * kOpBytes];
+  const int n = a.count[0], nb = (n + kTile - 1) / kTile;  // rows with a loss, tiles of them
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, wm = w & 1, wn = w >> 1;
+  Acc acc;
+  int ta, tb;
+  if constexpr (MODE == kStats || MODE == kDz) {
+    if (!tile_of(blockIdx.x, (nv + kTile - 1) / kTile, nb, ta, tb)) return;
+    const int vt = v0 + ta * kTile, r0 = tb * kTile;
+    product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTile), a.H},
+                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTile, a.ldh}, a.H, lds, acc);
+    const int vw = vt + wm * 128;  // the wave's first word
+    float* red = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int rl = wn * 64 + j * 32 + (lane & 31), i = r0 + rl;
+      // the label's place among the wave's words, if it is there
+      const int rel = i < n ? a.labels[a.src[i]] - vw : -1;
+      const bool here = rel >= 0 && rel < 128 && ((rel >> 2) & 1) == h;
+      const int le = here ? (rel >> 5) * 16 + ((rel & 31) >> 3) * 4 + (rel & 3) : -1;  // its (tile, element) of this lane
+      auto each = [&](auto f) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float z = acc[t][j][e];
+            f(t, e, z);
+            acc[t][j][e] = z;
+          }
+      };
+      if (vw + 128 > a.V)  // words past the last do not take part
+        each([&](int t, int e, float& z) {
+          if (vw + t * 32 + 8 * (e >> 2) + 4 * h + (e & 3) >= a.V) z = -INFINITY;
+        });
+      if constexpr (MODE == kStats) {
+        if (__builtin_amdgcn_ballot_w64(here)) {
+          float zl = 0.f;
+          each([&](int t, int e, float& z) { zl = t * 16 + e == le ? z : zl; });
+          if (here) a.zlab[i] = zl;
+        }
+        float m = -FLT_MAX, s = 0.f;
+        each([&](int, int, float& z) { m = fmaxf(m, z); });
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float ml = fmaxf(m * kL2E, -FLT_MAX);  // (finite where the wave has no words: they add 0)
+        each([&](int, int, float& z) { s += ex2(fmaf(z, kL2E, -ml)); });
+        s += __shfl_xor(s, 32);
+        if (h == 0) {
+          red[(wm * 256 + rl) * 2] = m;
+          red[(wm * 256 + rl) * 2 + 1] = s;
+        }
+      } else {
+        const float c = a.c[i], l = a.lse2[i];
+        each([&](int t, int e, float& z) {
+          z = c * ex2(fmaf(z, kL2E, -l));
+          if (t * 16 + e == le) z -= c;
+          if (c == 0.f) z = 0.f;
+        });
+        // columns m of row rl: piece (m / 8) at (m / 8) ^ (rl mod 32)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x16& z = acc[t][j];
+            const int p = wm * 16 + t * 4 + q;
+            const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
+            *reinterpret_cast<uint2*>(lds + rl * 512 + ((p ^ (rl & 31)) << 4) + h * 8) = v;
+          }
+      }
+    }
+    __syncthreads();
+    if constexpr (MODE == kStats) {
+      if (threadIdx.x < kTile) {
+        const float m0 = red[threadIdx.x * 2], m1 = red[(256 + threadIdx.x) * 2];
+        const float m = fmaxf(m0, m1);
+        const float s = red[threadIdx.x * 2 + 1] * ex2((m0 - m) * kL2E) + red[(256 + threadIdx.x) * 2 + 1] * ex2((m1 - m) * kL2E);
+        a.part[(long)(vt / kTile) * a.Mp + r0 + threadIdx.x] = make_float2(m, s);
+      }
+    } else {
+      store_tile(lds, a.dz + (long)r0 * a.Vp + ta * kTile, a.Vp, kTile, kTile);
+    }
+  } else if constexpr (MODE == kDh) {
+    if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, nb, ta, tb)) return;
+    const int m0 = ta * kTile, r0 = tb * kTile;
+    // this part's words: whole stages
+    const int stages = (nv + kBK - 1) / kBK, ks = blockIdx.y;
+    const int k0 = (int)((long)stages * ks / a.KS) * kBK, k1 = min((int)((long)stages * (ks + 1) / a.KS) * kBK, nv);
+    product<true, false>(Operand{a.head + (long)(v0 + k0) * a.H + m0, a.H, min(a.H - m0, kTile), k1 - k0},
+                         Operand{a.dz + (long)r0 * a.Vp + k0, a.Vp, kTile, a.Vp}, k1 - k0, lds, acc);
+    float* out = a.dacc + (long)ks * a.Mp * a.H;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float* row = out + (long)(r0 + wn * 64 + j * 32 + (lane & 31)) * a.H;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int m = m0 + wm * 128 + t * 32 + q * 8 + 4 * h;
+          if (m >= a.H) continue;
+          f32x4* at = reinterpret_cast<f32x4*>(row + m);
+          const f32x4 v = {acc[t][j][4 * q], acc[t][j][4 * q + 1], acc[t][j][4 * q + 2], acc[t][j][4 * q + 3]};
+          *at = first ? v : *at + v;
+        }
+    }
+  } else {
+    if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, (nv + kTile - 1) / kTile, ta, tb)) return;
+    const int m0 = ta * kTile, n0 = tb * kTile;
+    product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTile), a.Mp},
+                        Operand{a.dz + n0, a.Vp, kTile, a.Mp}, n, lds, acc);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int nl = wn * 64 + j * 32 + (lane & 31);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x16& z = acc[t][j];
+          const int p = wm * 16 + t * 4 + q;
+          const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
+          *reinterpret_cast<uint2*>(lds + nl * 512 + ((p ^ (nl & 31)) << 4) + h * 8) = v;
+        }
+    }
+    __syncthreads();
+    store_tile(lds, a.dhead + (long)(v0 + n0) * a.H + m0, a.H, min(nv - n0, kTile), min(a.H - m0, kTile));
+  }
+}
+
+// log-sum-exp of every row from its parts (16 rows by 16 groups of parts), and its cross-entropy
+__global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
+  __shared__ float2 sh[16][17];
+  const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
+  if ((int)blockIdx.x * 16 >= n) return;
+  float m = -FLT_MAX, s = 0.f;
+#pragma unroll 4
+  for (int p = g; p < parts; p += 16) {
+    const float2 v = a.part[(long)p * a.Mp + i];
+    const float mn = fmaxf(m, v.x);
+    s = s * ex2((m - mn) * kL2E) + v.y * ex2((v.x - mn) * kL2E);
+    m = mn;
+  }
+  sh[g][l] = make_float2(m, s);
+  __syncthreads();
+  if (g != 0 || i >= n) return;
+  for (int k = 1; k < 16; ++k) {
+    const float2 v = sh[k][l];
+    const float mn = fmaxf(m, v.x);
+    s = s * ex2((m - mn) * kL2E) + v.y * ex2((v.x - mn) * kL2E);
+    m = mn;
+  }
+  const float ls = log2f(s);
+  a.lse2[i] = m * kL2E + ls;
+  a.row_ce[a.src[i]] = (m - a.zlab[i]) + ls * 0.6931471805599453f;
+}
+
+// loss = sum of c ce in 64 bits, in a fixed order
+__global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
+  __shared__ double ws[16];
+  const int n = a.count[0];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 1024) s += (double)a.c[i] * a.row_ce[a.src[i]];
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) s += ws[k];
+    a.loss[0] = (float)s;
+  }
+}
+
+// dhidden rows: the parts' sum, rounded once; zeros without a loss
+__global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
+  const int i = a.pos[blockIdx.x];
+  u32x4* to = reinterpret_cast<u32x4*>(a.dhidden + (long)blockIdx.x * a.H);
+  for (int p = threadIdx.x; p < a.H / 8; p += 256) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    if (i >= 0)
+      for (int k = 0; k < a.KS; ++k) {
+        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * a.Mp + i) * a.H) + 2 * p;
+        x += from[0];
+        y += from[1];
+      }
+    to[p] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
+  }
+}
+
+// ---- host side ----
+constexpr size_t kDzBytes = 256u << 20;  // room for dz of a piece of the vocabulary
+
+struct LceLayout {
+  size_t count, src, pos, c, hc, part, zlab, lse2, dz, dacc, total;
+  int Mp, ldh, Vp, KS;
+};
+
+LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
+  LceLayout L{};
+  auto al = [](size_t x) { return (x + 255) / 256 * 256; };
+  const int nb = (rows + kTile - 1) / kTile, na = (H + kTile - 1) / kTile;
+  L.Mp = nb * kTile;
+  L.ldh = (H + kBK - 1) / kBK * kBK;
+  const int words = (int)((V + (long)kTile - 1) / kTile);  // tiles of the vocabulary
+  // pieces of equal numbers of tiles
+  const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kTile * 2)));
+  const int pieces = (words + most - 1) / most;
+  L.Vp = (words + pieces - 1) / pieces * kTile;
+  // dh in parts over the words where there are few tiles for 256 CUs
+  L.KS = std::max(1, std::min({(256 + nb * na - 1) / (nb * na), 16, L.Vp / 1024}));
+  size_t o = 0;
+  auto take = [&](size_t& at, size_t bytes) {
+    at = o;
+    o = al(o + bytes);
+  };
+  take(L.count, 4);
+  take(L.src, (size_t)L.Mp * 4);
+  take(L.pos, (size_t)rows * 4);
+  take(L.c, (size_t)L.Mp * 4);
+  take(L.hc, (size_t)L.Mp * L.ldh * 2);
+  take(L.part, (size_t)words * L.Mp * 8);
+  take(L.zlab, (size_t)L.Mp * 4);
+  take(L.lse2, (size_t)L.Mp * 4);
+  if (dhidden || dhead) take(L.dz, (size_t)L.Mp * L.Vp * 2);
+  if (dhidden) take(L.dacc, (size_t)L.KS * L.Mp * H * 4);
+  L.total = o;
+  return L;
+}
+
+int lce_check(int rows, int V, int H, int B) {
+  if (rows < 1 || V < 1 || H < 1 || B < 1 || rows % B) return DFLARE_ERR_INVALID_ARG;
+  if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
+  // a launch has less than 2^32 threads
+  if ((long)((rows + kTile - 1) / kTile) * ((V + (long)kTile - 1) / kTile) >= (1l << 23) - 8) return DFLARE_ERR_UNSUPPORTED;
+  return DFLARE_OK;
+}
+
+}  // namespace
+
+}  // namespace dflare
+
+using namespace dflare;
+
+extern "C" {
+
+size_t dflare_linear_ce_workspace(int32_t rows, int32_t V, int32_t H, int32_t dhidden, int32_t dhead) {
+  if (lce_check(rows, V, H, 1) != DFLARE_OK) return 0;
+  return lce_layout(rows, V, H, dhidden != 0, dhead != 0).total;
+}
+
+int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels, int32_t rows, int32_t V, int32_t H,
+                     int32_t B, float gamma, float* loss, float* row_ce, void* dhidden, void* dhead, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  const int rc = lce_check(rows, V, H, B);
+  if (rc != DFLARE_OK) return rc;
+  if (!hidden || !head || !labels || !loss || !row_ce || !workspace || !(gamma > 0.f) || !isfinite(gamma))
+    return DFLARE_ERR_INVALID_ARG;
+  for (const void* p : {hidden, head, (const void*)dhidden, (const void*)dhead, (const void*)workspace})
+    if ((uintptr_t)p & 15) return DFLARE_ERR_INVALID_ARG;
+  const LceLayout L = lce_layout(rows, V, H, dhidden != nullptr, dhead != nullptr);
+  if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  if (st) {
+    int dev = -1, sdev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || hipStreamGetDevice(st, &sdev) != hipSuccess) return DFLARE_ERR_HIP;
+    if (dev != sdev) return DFLARE_ERR_INVALID_ARG;
+  }
+  char* w = static_cast<char*>(workspace);
+  Lce a{};
+  a.hidden = (const uint16_t*)hidden;
+  a.head = (const uint16_t*)head;
+  a.labels = labels;
+  a.loss = loss;
+  a.row_ce = row_ce;
+  a.dhidden = (uint16_t*)dhidden;
+  a.dhead = (uint16_t*)dhead;
+  a.rows = rows;
+  a.V = V;
+  a.H = H;
+  a.B = B;
+  a.gamma = gamma;
+  a.count = (int*)(w + L.count);
+  a.src = (int*)(w + L.src);
+  a.pos = (int*)(w + L.pos);
+  a.c = (float*)(w + L.c);
+  a.hc = (uint16_t*)(w + L.hc);
+  a.part = (float2*)(w + L.part);
+  a.zlab = (float*)(w + L.zlab);
+  a.lse2 = (float*)(w + L.lse2);
+  a.dz = (uint16_t*)(w + L.dz);
+  a.dacc = (float*)(w + L.dacc);
+  a.Mp = L.Mp;
+  a.ldh = L.ldh;
+  a.Vp = L.Vp;
+  a.KS = L.KS;
+  const int nb = L.Mp / kTile, na = (H + kTile - 1) / kTile, words = (int)((V + (long)kTile - 1) / kTile);
+  auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
+  hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a);
+  hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_lce_product<kStats>), dim3(grid((long)words * nb)), dim3(kT), 0, st, a, 0, V, 0);
+  hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, words);
+  hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
+  if (dhidden || dhead)
+    for (long at = 0; at < V; at += L.Vp) {
+      const int v0 = (int)at, nv = std::min(V - v0, L.Vp);
+      const long wt = (nv + kTile - 1) / kTile;
+      hipLaunchKernelGGL((k_lce_product<kDz>), dim3(grid(wt * nb)), dim3(kT), 0, st, a, v0, nv, 0);
+      if (dhidden)
+        hipLaunchKernelGGL((k_lce_product<kDh>), dim3(grid((long)na * nb), L.KS), dim3(kT), 0, st, a, v0, nv, v0 == 0);
+      if (dhead)
+        hipLaunchKernelGGL((k_lce_product<kDw>), dim3(grid(wt * na)), dim3(kT), 0, st, a, v0, nv, 0);
+    }
+  if (dhidden) hipLaunchKernelGGL(k_lce_dhidden, dim3(rows), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR_HIP;
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@ has not been built -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -29,6 +30,9 @@ EXPORTED = (
     "dflare_context_len_seq", "dflare_debug_read_seq", "dflare_set_sampling", "dflare_accept", "dflare_accept_async",
     "dflare_anchor_attention_workspace", "dflare_anchor_attention_fwd", "dflare_anchor_attention_bwd",
     "dflare_weighted_ce_workspace", "dflare_weighted_ce", "dflare_weighted_ce_noalloc", "dflare_read_probe",
+    "dflare_rope_frequencies", "dflare_rope", "dflare_norm_fwd", "dflare_norm_bwd_workspace", "dflare_norm_bwd",
+    "dflare_linear_ce_workspace", "dflare_linear_ce", "dflare_grad_norm_workspace", "dflare_grad_norm",
+    "dflare_clip_grads",
 )
 K_QKV, K_ATTN, K_O, K_GATE_UP, K_DOWN, K_LM_HEAD, K_FUSE, K_KV_T, K_DRAFT = range(1, 10)
 (K_B_QKV, K_B_ATTN, K_B_O, K_B_GATE_UP, K_B_DOWN, K_B_LM_HEAD, K_B_KV_T, K_B_EPI, K_B_FUSE, K_B_DRAFT,
@@ -60,6 +64,15 @@ WEIGHT_FIELDS = ("embed", "lm_head", "final_norm", "fuse_norm", "attn_norm", "ml
 
 class dflare_weights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in WEIGHT_FIELDS]
+
+
+class dflare_rope_tensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_row", ctypes.c_int64), ("x_head", ctypes.c_int64),
+                ("y_row", ctypes.c_int64), ("y_head", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+
+class dflare_grad_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -110,6 +123,18 @@ def lib() -> ctypes.CDLL:
         "dflare_weighted_ce_noalloc": ([vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, vp,
                                         vp, vp, vp], ctypes.c_int),
         "dflare_read_probe": ([vp, i64, vp, vp], ctypes.c_int),
+        "dflare_rope_frequencies": ([i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
+                                     ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)], ctypes.c_int),
+        "dflare_rope": ([ctypes.POINTER(dflare_rope_tensor), i32, vp, vp] + [i32] * 6 + [ctypes.c_float, i32, vp],
+                        ctypes.c_int),
+        "dflare_norm_fwd": ([vp] * 4 + [i32] * 4 + [ctypes.c_float] + [vp] * 5, ctypes.c_int),
+        "dflare_norm_bwd_workspace": ([i32] * 3, ctypes.c_size_t),
+        "dflare_norm_bwd": ([vp] * 6 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_linear_ce_workspace": ([i32] * 5, ctypes.c_size_t),
+        "dflare_linear_ce": ([vp] * 3 + [i32] * 4 + [ctypes.c_float] + [vp] * 5 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_grad_norm_workspace": ([i32], ctypes.c_size_t),
+        "dflare_grad_norm": ([ctypes.POINTER(dflare_grad_tensor), i32, vp, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_clip_grads": ([ctypes.POINTER(dflare_grad_tensor), i32, vp, ctypes.c_float, vp], ctypes.c_int),
         "dflare_context_len_seq": ([vp, i32, ctypes.POINTER(i32)], ctypes.c_int),
         "dflare_debug_read_seq": ([vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
                                    i64], ctypes.c_int),
@@ -295,6 +320,220 @@ def weighted_ce_noalloc(logits, labels, B: int, gamma: float, loss, row_ce, dlog
     _train_check(lib().dflare_weighted_ce_noalloc(_ptr(logits), _ptr(labels), rows, V, B, float(gamma), _ptr(loss),
                                                   _ptr(row_ce), _ptr(dlogits), _stream(stream)),
                  "weighted ce (no allocation)")
+
+
+# ---- the rest of a draft layer's training step (no handle) ----
+
+F32, BF16 = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = range(4)
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
+
+
+def _dtype(t: torch.Tensor) -> int:
+    """Type code of a tensor; 16-bit integer tensors hold bf16 bit patterns."""
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        return BF16
+    raise TypeError(f"expected a bf16 or fp32 tensor, got {t.dtype}")
+
+
+def _like(t, name: str, shape, ref, dtype=None) -> None:
+    """t (or None) is a contiguous tensor of this shape on ref's device, of dtype, or of ref's type."""
+    if t is None:
+        return
+    _ptr(t)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != ref.device:
+        raise ValueError(f"{name} is on {t.device}, expected {ref.device}")
+    if t.dtype != dtype if dtype is not None else _dtype(t) != _dtype(ref):
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype or ref.dtype}")
+
+
+@contextlib.contextmanager
+def _place(t: torch.Tensor, stream):
+    """Inside, t's device is current and so is the stream of the call (the current one of that device by
+    default), so that what the binding allocates belongs to it.  Gives the raw stream."""
+    with torch.cuda.device(t.device):
+        raw = _stream(stream)
+        if raw == torch.cuda.current_stream().cuda_stream:
+            yield raw
+        else:
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(raw)):
+                yield raw
+
+
+def rope_frequencies(rotary_dim: int, base: float, method: int = ROPE_PLAIN, factor: float = 1.0,
+                     original_len: float = 0.0, device="cuda"):
+    """Inverse frequencies of a rotary embedding (include/dflare.h): (fp64 tensor [rotary_dim / 2] on the device,
+    the factor on cosines and sines)."""
+    f = np.empty(max(int(rotary_dim) // 2, 1), dtype=np.float64)
+    scale = ctypes.c_float()
+    _train_check(lib().dflare_rope_frequencies(int(rotary_dim), float(base), int(method), float(factor),
+                                               float(original_len), f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                               ctypes.byref(scale)), "rope frequencies")
+    return torch.from_numpy(f).to(device), scale.value
+
+
+def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = ROPE_HALF, scale: float = 1.0,
+         inverse: bool = False, out=None, stream=None):
+    """Rotary positions (include/dflare.h) of x [rows, n_heads, head_dim], or of a pair of such tensors with the same
+    rows (queries and keys).  The last dimension is contiguous, the others may be strided.  Row r sits at
+    positions[r // B] + r % B (positions int32 [ceil(rows / B)]), or at r.  inverse: the gradient's rotation.
+    out: where the result goes (x itself: in place); by default new tensors.  Returns out."""
+    xs = x if isinstance(x, (tuple, list)) else (x,)
+    if not 1 <= len(xs) <= 2:
+        raise ValueError("expected one tensor or a pair")
+    for t in xs:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError("expected a device tensor")
+        if t.dim() != 3 or t.shape[0] != xs[0].shape[0] or t.shape[2] != xs[0].shape[2]:
+            raise ValueError("expected [rows, n_heads, head_dim] tensors with the same rows and head_dim")
+    rows, _, hd = xs[0].shape
+    if int(B) < 1:
+        raise ValueError("B must be positive")
+    _ptr(inv_freq)
+    _like(inv_freq, "inv_freq", (inv_freq.numel(),), xs[0], torch.float64)
+    _like(positions, "positions", (-(-rows // int(B)),), xs[0], torch.int32)
+    with _place(xs[0], stream) as raw:
+        if out is None:
+            outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs)
+        else:
+            outs = out if isinstance(out, (tuple, list)) else (out,)
+        if len(outs) != len(xs):
+            raise ValueError("out and x differ in number")
+        tab = (dflare_rope_tensor * len(xs))()
+        for e, t, y in zip(tab, xs, outs):
+            if not isinstance(y, torch.Tensor) or not y.is_cuda:
+                raise TypeError("expected a device tensor")
+            if y.shape != t.shape or y.dtype != t.dtype or _dtype(t) != _dtype(xs[0]) or \
+                    {t.device, y.device} != {xs[0].device}:
+                raise ValueError("x and out differ in shape, type or device")
+            if any(v.numel() and v.shape[2] > 1 and v.stride(2) != 1 for v in (t, y)):
+                raise ValueError("the last dimension must be contiguous")
+            e.x, e.y, e.n_heads = t.data_ptr(), y.data_ptr(), t.shape[1]
+            e.x_row, e.x_head, e.y_row, e.y_head = t.stride(0), t.stride(1), y.stride(0), y.stride(1)
+        _train_check(lib().dflare_rope(tab, len(xs), _ptr(positions), _ptr(inv_freq), rows, int(B), hd,
+                                       2 * inv_freq.numel(), _dtype(xs[0]), int(layout), float(scale),
+                                       int(bool(inverse)), raw), "rope")
+    return outs if isinstance(x, (tuple, list)) else outs[0]
+
+
+def norm_fwd(x, gain=None, bias=None, residual=None, kind: int = NORM_RMS, eps: float = 1e-6, stream=None):
+    """RMSNorm or LayerNorm of the rows of x [rows, H] (plus residual): returns (y, h, mean, rstd) with h = x, or x +
+    residual as stored; mean is None for RMSNorm (include/dflare.h)."""
+    _ptr(x)
+    if x.dim() != 2:
+        raise ValueError("expected a [rows, H] tensor")
+    rows, H = x.shape
+    _like(residual, "residual", x.shape, x)
+    _like(gain, "gain", (H,), x)
+    _like(bias, "bias", (H,), x)
+    with _place(x, stream) as raw:
+        h = x if residual is None else torch.empty_like(x)
+        y = torch.empty_like(x)
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device) if kind == NORM_LAYER else None
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        _train_check(lib().dflare_norm_fwd(_ptr(x), _ptr(residual), _ptr(gain), _ptr(bias), rows, H, _dtype(x), int(kind),
+                                           float(eps), None if residual is None else _ptr(h), _ptr(y), _ptr(mean),
+                                           _ptr(rstd), raw), "norm fwd")
+    return y, h, mean, rstd
+
+
+def norm_bwd(dy, h, gain, mean, rstd, dsum=None, kind: int = NORM_RMS, stream=None):
+    """Backward of norm_fwd: returns (dx, dgain fp32 [H], dbias fp32 [H], None for RMSNorm); dsum is the gradient
+    that reaches h from its other uses."""
+    _ptr(h)
+    if h.dim() != 2:
+        raise ValueError("expected a [rows, H] tensor")
+    rows, H = h.shape
+    _like(dy, "dy", h.shape, h)
+    _like(dsum, "dsum", h.shape, h)
+    _like(gain, "gain", (H,), h)
+    _like(rstd, "rstd", (rows,), h, torch.float32)
+    _like(mean, "mean", (rows,), h, torch.float32)
+    with _place(h, stream) as raw:
+        dx = torch.empty_like(h)
+        dgain = torch.empty(H, dtype=torch.float32, device=h.device)
+        dbias = torch.empty(H, dtype=torch.float32, device=h.device) if kind == NORM_LAYER else None
+        ws_bytes = lib().dflare_norm_bwd_workspace(rows, H, int(kind))
+        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=h.device)
+        _train_check(lib().dflare_norm_bwd(_ptr(dy), _ptr(h), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dsum), rows, H,
+                                           _dtype(h), int(kind), _ptr(dx), _ptr(dgain), _ptr(dbias), _ptr(ws), ws_bytes,
+                                           raw), "norm bwd")
+    return dx, dgain, dbias
+
+
+def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = True, need_dhead: bool = False,
+              stream=None):
+    """LM head and position-weighted cross-entropy without logits in memory (include/dflare.h): hidden bf16 [rows, H],
+    head bf16 [V, H], labels int32 [rows].  Returns (loss fp32 [1], row_ce fp32 [rows], dhidden, dhead), gradients in
+    bf16, None where not wanted."""
+    _ptr(hidden)
+    _ptr(head)
+    if hidden.dim() != 2 or head.dim() != 2 or _dtype(hidden) != BF16:
+        raise ValueError("expected bf16 tensors hidden [rows, H] and head [V, H]")
+    rows, H = hidden.shape
+    V = head.shape[0]
+    _like(head, "head", (V, H), hidden)
+    _like(labels, "labels", (rows,), hidden, torch.int32)
+    ws_bytes = lib().dflare_linear_ce_workspace(rows, V, H, int(need_dhidden), int(need_dhead))
+    if ws_bytes == 0:
+        raise DFlareError(ERR_UNSUPPORTED if rows and V and H else ERR_INVALID_ARG, "linear ce: shape")
+    with _place(hidden, stream) as raw:
+        loss = torch.empty(1, dtype=torch.float32, device=hidden.device)
+        ce = torch.empty(rows, dtype=torch.float32, device=hidden.device)
+        dhidden = torch.empty_like(hidden) if need_dhidden else None
+        dhead = torch.empty_like(head) if need_dhead else None
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=hidden.device)
+        _train_check(lib().dflare_linear_ce(_ptr(hidden), _ptr(head), _ptr(labels), rows, V, H, int(B), float(gamma),
+                                            _ptr(loss), _ptr(ce), _ptr(dhidden), _ptr(dhead), _ptr(ws), ws_bytes, raw),
+                     "linear ce")
+    return loss, ce, dhidden, dhead
+
+
+def _grad_table(grads, out=None):
+    tab = (dflare_grad_tensor * len(grads))()
+    if out is not None and len(out) != len(grads):
+        raise ValueError("out and grads differ in number")
+    for i, (e, t) in enumerate(zip(tab, grads)):
+        e.data, e.n, e.dtype = _ptr(t), t.numel(), _dtype(t)
+        if t.device != grads[0].device:
+            raise ValueError("the gradients are on different devices")
+        if out is not None:
+            _like(out[i], "out", t.shape, t)
+            e.out = _ptr(out[i])
+    return tab
+
+
+def grad_norm(grads, stream=None):
+    """Global 2-norm of a list of gradient tensors (bf16 or fp32, contiguous): (norm fp32 [1], sumsq fp64 [1])."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("expected at least one gradient")
+    tab = _grad_table(grads)
+    dev = grads[0].device
+    with _place(grads[0], stream) as raw:
+        sumsq = torch.empty(1, dtype=torch.float64, device=dev)
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        ws_bytes = lib().dflare_grad_norm_workspace(len(grads))
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        _train_check(lib().dflare_grad_norm(tab, len(grads), _ptr(sumsq), _ptr(norm), _ptr(ws), ws_bytes, raw), "grad norm")
+    return norm, sumsq
+
+
+def clip_grads(grads, sumsq: torch.Tensor, max_norm: float, out=None, stream=None) -> None:
+    """Scale gradients whose squares add up to sumsq (fp64 [1], grad_norm's) to the norm max_norm where theirs is
+    larger; in place, or into the tensors `out`."""
+    grads = list(grads)
+    if not grads:
+        return
+    tab = _grad_table(grads, None if out is None else list(out))
+    _like(sumsq, "sumsq", (1,), grads[0], torch.float64)
+    with _place(grads[0], stream) as raw:
+        _train_check(lib().dflare_clip_grads(tab, len(grads), _ptr(sumsq), float(max_norm), raw), "clip grads")
 
 
 def dflare_set_sampling(h: int, temperature: float, seed: int = 0) -> None:

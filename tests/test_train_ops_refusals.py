@@ -1,0 +1,146 @@
+"""What the entry points of the training step's operators refuse, at the C ABI, before any GPU call; and the
+frequencies of the rotary embedding, which are computed on the host."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from paper_2606_02091_amd import dflare as dfl
+
+P = 0x1000  # an aligned address that no refused call reads
+INV, UNS, OK = dfl.ERR_INVALID_ARG, dfl.ERR_UNSUPPORTED, dfl.OK
+INF, NAN = float("inf"), float("nan")
+
+
+def lce(rows=32, V=100, H=64, B=4, gamma=4.5, ws=1 << 40, hidden=P, head=P, labels=P, loss=P, ce=P, dh=P, dw=P, work=P):
+    return dfl.lib().dflare_linear_ce(hidden, head, labels, rows, V, H, B, gamma, loss, ce, dh, dw, work, ws, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=0), INV), (dict(rows=-4), INV), (dict(V=0), INV), (dict(H=0), INV), (dict(B=0), INV), (dict(rows=33), INV),
+    (dict(gamma=0.0), INV), (dict(gamma=-1.0), INV), (dict(gamma=NAN), INV), (dict(gamma=INF), INV), (dict(ws=64), INV),
+    (dict(hidden=None), INV), (dict(head=None), INV), (dict(labels=None), INV), (dict(loss=None), INV), (dict(ce=None), INV),
+    (dict(work=None), INV), (dict(hidden=P + 8), INV), (dict(head=P + 2), INV), (dict(dh=P + 4), INV), (dict(dw=P + 8), INV),
+    (dict(work=P + 8), INV), (dict(H=60), UNS), (dict(H=16392), UNS), (dict(rows=(1 << 22) + 4), UNS),
+    (dict(rows=1 << 22, V=1 << 20), UNS)])
+def test_linear_ce_refuses(kw, code):
+    assert lce(**kw) == code
+
+
+def test_linear_ce_workspace():
+    ws = dfl.lib().dflare_linear_ce_workspace
+    assert ws(0, 10, 8, 0, 0) == 0 and ws(8, 10, 12, 0, 0) == 0 and ws(8, 0, 8, 0, 0) == 0
+    # without logits: far below rows x V floats, and more where more is asked for
+    a, b, c = ws(8192, 151936, 4096, 0, 0), ws(8192, 151936, 4096, 1, 0), ws(8192, 151936, 4096, 1, 1)
+    assert 0 < a < b <= c < 8192 * 151936 * 4 // 8
+    need = ws(32, 100, 64, 1, 1)
+    assert lce(ws=need - 1) == INV
+
+
+def rope(n=1, rows=4, B=1, hd=64, rot=64, dtype=dfl.BF16, layout=0, scale=1.0, pos=P, freq=P, x=P, y=2 * P, heads=2,
+         strides=(128, 64, 128, 64), tab=True):
+    t = (dfl.dflare_rope_tensor * 2)(*[dfl.dflare_rope_tensor(x, y, *strides, heads)] * 2)
+    return dfl.lib().dflare_rope(t if tab else None, n, pos, freq, rows, B, hd, rot, dtype, layout, scale, 0, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), INV), (dict(n=3), INV), (dict(tab=False), INV), (dict(rows=-1), INV), (dict(B=0), INV), (dict(hd=1), INV),
+    (dict(rot=0), INV), (dict(rot=63), INV), (dict(rot=66), INV), (dict(dtype=2), INV), (dict(dtype=-1), INV),
+    (dict(layout=2), INV), (dict(scale=NAN), INV), (dict(scale=INF), INV), (dict(freq=None), INV), (dict(freq=P + 4), INV),
+    (dict(pos=P + 2), INV), (dict(x=None), INV), (dict(y=None), INV), (dict(x=P + 1), INV), (dict(y=P + 2, dtype=dfl.F32), INV),
+    (dict(heads=-1), INV), (dict(y=P, strides=(128, 64, 256, 64)), INV), (dict(hd=1026), UNS), (dict(heads=1 << 15), UNS),
+    (dict(rows=0), OK), (dict(heads=0, x=None, y=None), OK)])
+def test_rope_refuses(kw, code):
+    assert rope(**kw) == code
+
+
+def norm_fwd(rows=4, H=64, dtype=dfl.BF16, kind=0, eps=1e-6, x=P, res=None, gain=P, bias=None, sum_=None, y=P, mean=P, rstd=P):
+    return dfl.lib().dflare_norm_fwd(x, res, gain, bias, rows, H, dtype, kind, eps, sum_, y, mean, rstd, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=-1), INV), (dict(H=0), INV), (dict(dtype=7), INV), (dict(kind=2), INV), (dict(eps=-1.0), INV), (dict(eps=NAN), INV),
+    (dict(eps=INF), INV), (dict(bias=P), INV), (dict(x=None), INV), (dict(y=None), INV), (dict(rstd=None), INV),
+    (dict(kind=1, mean=None), INV), (dict(res=P), INV), (dict(x=P + 1), INV), (dict(gain=P + 2, dtype=dfl.F32), INV),
+    (dict(H=16385), UNS), (dict(rows=0, x=None, y=None, rstd=None), OK)])
+def test_norm_fwd_refuses(kw, code):
+    assert norm_fwd(**kw) == code
+
+
+def norm_bwd(rows=4, H=64, dtype=dfl.BF16, kind=0, dy=P, h=P, gain=P, mean=P, rstd=P, dsum=None, dx=P, dgain=P, dbias=None,
+             work=P, ws=1 << 30):
+    return dfl.lib().dflare_norm_bwd(dy, h, gain, mean, rstd, dsum, rows, H, dtype, kind, dx, dgain, dbias, work, ws, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=-1), INV), (dict(H=0), INV), (dict(dtype=2), INV), (dict(kind=-1), INV), (dict(dy=None), INV), (dict(h=None), INV),
+    (dict(rstd=None), INV), (dict(kind=1, mean=None), INV), (dict(dx=None), INV), (dict(dgain=None), INV), (dict(dbias=P), INV),
+    (dict(work=None), INV), (dict(work=P + 4), INV), (dict(ws=100), INV), (dict(dsum=P + 1), INV), (dict(H=20000), UNS)])
+def test_norm_bwd_refuses(kw, code):
+    assert norm_bwd(**kw) == code
+
+
+def tensors(*items):
+    return (dfl.dflare_grad_tensor * max(1, len(items)))(*[dfl.dflare_grad_tensor(*t) for t in items])
+
+
+def grad_norm(items, n=None, sumsq=P, work=P, ws=1 << 30, tab=True):
+    return dfl.lib().dflare_grad_norm(tensors(*items) if tab else None, len(items) if n is None else n, sumsq, None, work, ws, None)
+
+
+def clip(items, n=None, sumsq=P, max_norm=1.0):
+    return dfl.lib().dflare_clip_grads(tensors(*items), len(items) if n is None else n, sumsq, max_norm, None)
+
+
+GOOD = (P, None, 64, dfl.F32)
+
+
+@pytest.mark.parametrize("items,kw,code", [
+    ([GOOD], dict(n=-1), INV), ([GOOD], dict(tab=False), INV), ([GOOD], dict(sumsq=None), INV), ([GOOD], dict(sumsq=P + 4), INV),
+    ([GOOD], dict(work=None), INV), ([GOOD], dict(work=P + 4), INV), ([GOOD], dict(ws=100), INV), ([(None, None, 1, 0)], {}, INV),
+    ([(P + 2, None, 1, 0)], {}, INV), ([(P + 1, None, 1, 1)], {}, INV), ([(P, None, -1, 0)], {}, INV), ([(P, None, 1, 2)], {}, INV),
+    ([(P, None, (1 << 36) + 1, 0)], {}, UNS)])
+def test_grad_norm_refuses(items, kw, code):
+    assert grad_norm(items, **kw) == code
+
+
+@pytest.mark.parametrize("items,kw,code", [
+    ([GOOD], dict(sumsq=None), INV), ([GOOD], dict(max_norm=-1.0), INV), ([GOOD], dict(max_norm=NAN), INV), ([GOOD, GOOD], {}, INV),
+    ([GOOD, (P + 252, None, 4, 0)], {}, INV), ([(P, 2 * P, 64, 0), (2 * P + 8, None, 4, 0)], {}, INV),
+    ([(P, 2 * P, 64, 0), (3 * P, 2 * P, 4, 0)], {}, INV), ([(P, P + 4, 64, 0)], {}, INV), ([(P, 2 * P + 2, 64, 0)], {}, INV)])
+def test_clip_refuses(items, kw, code):
+    assert clip(items, **kw) == code
+
+
+def freqs(d, base, method=0, factor=1.0, length=0.0):
+    f, s = np.zeros(max(d // 2, 1)), ctypes.c_float()
+    rc = dfl.lib().dflare_rope_frequencies(d, base, method, factor, length, f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                           ctypes.byref(s))
+    return rc, f, s.value
+
+
+@pytest.mark.parametrize("args", [(0, 1e4), (3, 1e4), (-2, 1e4), (64, 0.0), (64, -1.0), (64, NAN), (64, INF), (64, 1e4, 4), (64, 1e4, -1),
+                                  (64, 1e4, 1, 0.5), (64, 1e4, 2, NAN), (64, 1e4, 3, INF, 100.0), (64, 1e4, 3, 2.0, 0.0), (64, 1e4, 3, 2.0, NAN)])
+def test_frequencies_refuse(args):
+    assert freqs(*args)[0] == INV
+
+
+@pytest.mark.parametrize("d,base", [(2, 1e4), (64, 1e4), (128, 1e6)])
+def test_frequencies(d, base):
+    m = np.arange(d // 2)
+    plain = base ** (-2.0 * m / d)
+    rc, f, s = freqs(d, base)
+    assert rc == OK and s == 1.0 and np.allclose(f, plain, rtol=1e-14)
+    assert np.allclose(freqs(d, base, dfl.ROPE_LINEAR, 4.0)[1], plain / 4, rtol=1e-14)
+    rc, f, s = freqs(d, base, dfl.ROPE_NTK, 4.0)
+    assert rc == OK and s == 1.0 and f[0] == 1.0
+    if d > 2:  # the slowest pair is stretched by the whole factor
+        assert np.isclose(f[-1], plain[-1] / 4, rtol=1e-12)
+    rc, f, s = freqs(d, base, dfl.ROPE_YARN, 8.0, 4096.0)
+    assert rc == OK and np.isclose(s, 0.1 * math.log(8.0) + 1, rtol=1e-6)
+    turns = 4096 * plain / (2 * math.pi)
+    assert np.allclose(f[turns >= 32], plain[turns >= 32], rtol=1e-14)
+    assert np.allclose(f[turns <= 1], plain[turns <= 1] / 8, rtol=1e-14)
+    mid = (turns > 1) & (turns < 32)
+    assert np.all((f[mid] < plain[mid]) & (f[mid] > plain[mid] / 8))
