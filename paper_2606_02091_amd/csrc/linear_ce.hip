@@ -9,6 +9,7 @@
 // Bound by the matrix cores: 2 rows V H operations for the loss, 4 more for dh, 2 more for dW.
 #include <hip/hip_runtime.h>
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -57,10 +58,28 @@ struct Lce {
   float2* part;   // [words / 256][Mp] (max, sum of exp(z - max))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
-  uint16_t* dz;   // [Mp][Vp] dz of a piece of the vocabulary
-  float* dacc;    // [KS][Mp][H] dh of the pieces so far, in KS parts
-  int Mp, ldh, Vp, KS;
+  uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
+  float* dacc;    // [parts][tiles of rows x 256][H] dh of the pieces so far
+  int Mp, ldh, Vp;
+  int stages;     // stages of k of the first (longest) piece
 };
+
+// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for 256 CUs: the number
+// with the least time, a round of work-groups costing its stages of k and about 30 more for its start and its
+// sums in memory (measured: 0.9 us a stage, 27 us).  More than one part makes at most 512 work-groups.  The number
+// depends on the rows with a loss, so that it is chosen on the device.
+__host__ __device__ inline int dh_parts(int nb, int na, int stages) {
+  int best = 1, cost = 0x7fffffff;
+  for (int k = 1; k <= 16; ++k) {
+    if (k > 1 && (nb * na * k > 512 || stages < 8 * k)) break;
+    const int c = (nb * na * k + 255) / 256 * ((stages + k - 1) / k + 30);
+    if (c < cost) {
+      best = k;
+      cost = c;
+    }
+  }
+  return best;
+}
 
 // ---- rows with a loss, in order; their weights; work-group of 1,024 threads ----
 __global__ __launch_bounds__(1024) void k_lce_rows(Lce a) {
@@ -125,7 +144,10 @@ struct Operand {
   const uint16_t* p;  // first element of the tile's rows (plain) or columns (across)
   long ld;
   int valid;  // rows (plain) or columns (across) of the tile that exist; past them the last is repeated
-  int kend;   // plain: k that exist (past them the row's k = 0 of the stage again, to meet zeros of the other operand)
+  int kend;   // k that exist (past them the stage's first again, to meet zeros of the other operand)
+  // plain: 256 k lie side by side, the next 256 `block` bytes on (512: rows of any length); first stage
+  long block = 512;
+  int s0 = 0;
 };
 
 template <bool ACROSS>
@@ -133,6 +155,7 @@ struct Loader {
   const char* base;
   uint32_t off[4], back[4];  // byte offset of the wave's four pieces of a lane; what takes it back to k = 0
   long step;
+  int s0;
   int kl[4];  // first k of the piece
   __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
     base = reinterpret_cast<const char*>(o.p);
@@ -150,11 +173,13 @@ struct Loader {
         kl[j] = row;
       }
     }
-    step = ACROSS ? o.ld * kBK * 2 : kBK * 2;
+    step = ACROSS ? o.ld * kBK * 2 : o.block;
+    s0 = o.s0;
   }
   // the wave's share of a stage; left: k that exist from the stage's first on
   __device__ __forceinline__ void issue(char* dst, int w, int kt, int left) const {
-    const char* b = base + kt * step;
+    const int st = s0 + kt;
+    const char* b = ACROSS ? base + kt * step : base + (st >> 2) * step + (st & 3) * (kBK * 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t o = kl[j] < left ? off[j] : off[j] - back[j];
@@ -271,7 +296,7 @@ enum { kStats, kDz, kDh, kDw };
 // One tile of a product and its epilogue:
 //   kStats  z tile (256 words x 256 rows) -> part, zlab
 //   kDz     z tile of the piece from word v0 on -> dz
-//   kDh     dacc (+)= dz W over the piece's words, in KS parts (z of the grid)
+//   kDh     dacc (+)= dz W over the piece's words, in parts
 //   kDw     dhead rows of the piece = dz^T h
 template <int MODE>
 __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int first) {
@@ -353,17 +378,20 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         a.part[(long)(vt / kTile) * a.Mp + r0 + threadIdx.x] = make_float2(m, s);
       }
     } else {
-      store_tile(lds, a.dz + (long)r0 * a.Vp + ta * kTile, a.Vp, kTile, kTile);
+      store_tile(lds, a.dz + ((long)ta * a.Mp + r0) * kTile, kTile, kTile, kTile);
     }
   } else if constexpr (MODE == kDh) {
-    if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, nb, ta, tb)) return;
-    const int m0 = ta * kTile, r0 = tb * kTile;
+    const int na = (a.H + kTile - 1) / kTile, stages = (nv + kBK - 1) / kBK, parts = dh_parts(nb, na, a.stages);
+    int unit;
+    if (!tile_of(blockIdx.x, na * parts, nb, unit, tb)) return;
+    ta = unit % na;
+    const int ks = unit / na, m0 = ta * kTile, r0 = tb * kTile;
     // this part's words: whole stages
-    const int stages = (nv + kBK - 1) / kBK, ks = blockIdx.y;
-    const int k0 = (int)((long)stages * ks / a.KS) * kBK, k1 = min((int)((long)stages * (ks + 1) / a.KS) * kBK, nv);
-    product<true, false>(Operand{a.head + (long)(v0 + k0) * a.H + m0, a.H, min(a.H - m0, kTile), k1 - k0},
-                         Operand{a.dz + (long)r0 * a.Vp + k0, a.Vp, kTile, a.Vp}, k1 - k0, lds, acc);
-    float* out = a.dacc + (long)ks * a.Mp * a.H;
+    const int s0 = (int)((long)stages * ks / parts), s1 = (int)((long)stages * (ks + 1) / parts);
+    const int words = min(s1 * kBK, nv) - s0 * kBK;
+    product<true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, kTile), words},
+                         Operand{a.dz + (long)r0 * kTile, kTile, kTile, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc);
+    float* out = a.dacc + (long)ks * nb * kTile * a.H;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float* row = out + (long)(r0 + wn * 64 + j * 32 + (lane & 31)) * a.H;
@@ -382,7 +410,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
     if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, (nv + kTile - 1) / kTile, ta, tb)) return;
     const int m0 = ta * kTile, n0 = tb * kTile;
     product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTile), a.Mp},
-                        Operand{a.dz + n0, a.Vp, kTile, a.Mp}, n, lds, acc);
+                        Operand{a.dz + (long)tb * a.Mp * kTile, kTile, kTile, a.Mp}, n, lds, acc);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int nl = wn * 64 + j * 32 + (lane & 31);
@@ -445,13 +473,14 @@ __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
 
 // dhidden rows: the parts' sum, rounded once; zeros without a loss
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
+  const int nb = (a.count[0] + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
   const int i = a.pos[blockIdx.x];
   u32x4* to = reinterpret_cast<u32x4*>(a.dhidden + (long)blockIdx.x * a.H);
   for (int p = threadIdx.x; p < a.H / 8; p += 256) {
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
     if (i >= 0)
-      for (int k = 0; k < a.KS; ++k) {
-        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * a.Mp + i) * a.H) + 2 * p;
+      for (int k = 0; k < parts; ++k) {
+        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * nb * kTile + i) * a.H) + 2 * p;
         x += from[0];
         y += from[1];
       }
@@ -460,17 +489,17 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
 }
 
 // ---- host side ----
-constexpr size_t kDzBytes = 256u << 20;  // room for dz of a piece of the vocabulary
+constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
 
 struct LceLayout {
   size_t count, src, pos, c, hc, part, zlab, lse2, dz, dacc, total;
-  int Mp, ldh, Vp, KS;
+  int Mp, ldh, Vp;
 };
 
 LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   LceLayout L{};
   auto al = [](size_t x) { return (x + 255) / 256 * 256; };
-  const int nb = (rows + kTile - 1) / kTile, na = (H + kTile - 1) / kTile;
+  const int nb = (rows + kTile - 1) / kTile;
   L.Mp = nb * kTile;
   L.ldh = (H + kBK - 1) / kBK * kBK;
   const int words = (int)((V + (long)kTile - 1) / kTile);  // tiles of the vocabulary
@@ -478,8 +507,6 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kTile * 2)));
   const int pieces = (words + most - 1) / most;
   L.Vp = (words + pieces - 1) / pieces * kTile;
-  // dh in parts over the words where there are few tiles for 256 CUs
-  L.KS = std::max(1, std::min({(256 + nb * na - 1) / (nb * na), 16, L.Vp / 1024}));
   size_t o = 0;
   auto take = [&](size_t& at, size_t bytes) {
     at = o;
@@ -493,8 +520,10 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.part, (size_t)words * L.Mp * 8);
   take(L.zlab, (size_t)L.Mp * 4);
   take(L.lse2, (size_t)L.Mp * 4);
-  if (dhidden || dhead) take(L.dz, (size_t)L.Mp * L.Vp * 2);
-  if (dhidden) take(L.dacc, (size_t)L.KS * L.Mp * H * 4);
+  // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
+  const size_t tile = (size_t)kTile * kTile;
+  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kTile * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kTile * 2)));
+  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)16 * L.Mp * H, 512 * tile)) * 4);
   L.total = o;
   return L;
 }
@@ -564,7 +593,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.Mp = L.Mp;
   a.ldh = L.ldh;
   a.Vp = L.Vp;
-  a.KS = L.KS;
+  a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
   const int nb = L.Mp / kTile, na = (H + kTile - 1) / kTile, words = (int)((V + (long)kTile - 1) / kTile);
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
   hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a);
@@ -578,7 +607,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
       const long wt = (nv + kTile - 1) / kTile;
       hipLaunchKernelGGL((k_lce_product<kDz>), dim3(grid(wt * nb)), dim3(kT), 0, st, a, v0, nv, 0);
       if (dhidden)
-        hipLaunchKernelGGL((k_lce_product<kDh>), dim3(grid((long)na * nb), L.KS), dim3(kT), 0, st, a, v0, nv, v0 == 0);
+        hipLaunchKernelGGL((k_lce_product<kDh>), dim3(grid(std::max((long)na * nb, std::min(16l * na * nb, 512l)))), dim3(kT),
+                           0, st, a, v0, nv, v0 == 0);
       if (dhead)
         hipLaunchKernelGGL((k_lce_product<kDw>), dim3(grid(wt * na)), dim3(kT), 0, st, a, v0, nv, 0);
     }
