@@ -2,11 +2,17 @@
 // without logits in memory.  With z = h W^T over the rows that carry a loss, c_r = w_r / sum w,
 //   ce_r = lse(z_r) - z_r[y_r],  loss = sum c ce,  dz = c (softmax(z) - onehot(y)),
 //   dh = dz W,  dW = dz^T h.
-// The rows with a loss are gathered first (the others take no part in any product).  One product gives
-// every row's maximum and sum per 256 words, from which its log-sum-exp follows; for the gradients the
-// vocabulary is walked in pieces: the product again, its epilogue writes the piece's dz in bf16, and this
-// feeds the products for dh (added up in fp32 over the pieces) and dW.
-// Bound by the matrix cores: 2 rows V H operations for the loss, 4 more for dh, 2 more for dW.
+// The rows with a loss are gathered first (the others take no part in any product).
+// The loss alone is one product, whose epilogue leaves every row's maximum and sum per 256 words.
+// With dh alone the vocabulary is walked once, in pieces, as one pass of a softmax: a piece's product leaves
+// 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
+// product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
+// fp32, so that R need not be the maximum: only logits more than 2^80 above it (which a piece's 128 words
+// then take as their own reference, raise a flag and have the row rescaled) move it.  The label's word is left out
+// of both and added at the end, as the difference 1 - p is lost where p is rounded.
+// With dW, which needs dz of all words of a row at its final scale, the maxima and sums come first, and each
+// piece's logits are formed again: 2 rows V H operations more.
+// Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with dW alone, 8 with both.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -55,9 +61,12 @@ struct Lce {
   int* pos;       // [rows] row -> i, -1 without a loss
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
-  float2* part;   // [words / 256][Mp] (max, sum of exp(z - max))
+  float2* part;   // [words / 256][Mp] (max, sum of exp(z - max)); one pass: [words / 128][Mp] (R, sum of 2^(z log2 e - R))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
+  // one pass: the rows' references R (log2 domain), c / sum and c (1 - p of the label) at the end; flags of the pieces
+  float *ref, *fac, *lab;
+  int* flag;
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
   float* dacc;    // [parts][tiles of rows x 256][H] dh of the pieces so far
   int Mp, ldh, Vp;
@@ -82,7 +91,7 @@ __host__ __device__ inline int dh_parts(int nb, int na, int stages) {
 }
 
 // ---- rows with a loss, in order; their weights; work-group of 1,024 threads ----
-__global__ __launch_bounds__(1024) void k_lce_rows(Lce a) {
+__global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
   __shared__ int wc[16];
   __shared__ double ws[16];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -120,16 +129,45 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a) {
   const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
   const int np = min((n + kTile - 1) / kTile * kTile, a.Mp);
   for (int i = tid; i < np; i += 1024) a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
+  if (a.flag)
+    for (int i = tid; i < pieces; i += 1024) a.flag[i] = 0;
   if (tid == 0) a.count[0] = n;
 }
 
+// a row of hc; one pass: also the label's logit and the first reference
 __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
+  __shared__ float red[4];
   const int n = a.count[0], i = blockIdx.x;
   if (i >= (n + kTile - 1) / kTile * kTile) return;
   const u32x4 z = {0u, 0u, 0u, 0u};
-  const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)(i < n ? a.src[i] : 0) * a.H);
+  const int row = i < n ? a.src[i] : 0;
+  const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)row * a.H);
   u32x4* to = reinterpret_cast<u32x4*>(a.hc + (long)i * a.ldh);
-  for (int p = threadIdx.x; p < a.ldh / 8; p += 256) to[p] = i < n && p < a.H / 8 ? from[p] : z;
+  const bool dot = a.ref && i < n;
+  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (dot ? (long)a.labels[row] * a.H : 0));
+  float s = 0.f;
+  for (int p = threadIdx.x; p < a.ldh / 8; p += 256) {
+    const bool in = i < n && p < a.H / 8;
+    const u32x4 v = in ? from[p] : z;
+    to[p] = v;
+    if (dot && in) {
+      const u32x4 x = word[p];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s = fmaf(__uint_as_float(v[e] << 16), __uint_as_float(x[e] << 16), s);
+        s = fmaf(__uint_as_float(v[e] & 0xFFFF0000u), __uint_as_float(x[e] & 0xFFFF0000u), s);
+      }
+    }
+  }
+  if (!a.ref) return;
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = (red[0] + red[1]) + (red[2] + red[3]);
+    a.zlab[i] = s;
+    a.ref[i] = s * kL2E;
+  }
 }
 
 // ---- products.  D[n][m] = sum over k of A[m, k] B[n, k] for a tile of 256 m x 256 n.  An operand lies in memory
@@ -152,10 +190,11 @@ struct Operand {
 
 // 1 KB from base + off (16 bytes per lane) to LDS, asynchronously.  In asm, and waited for by wait_vm_barrier: with the
 // builtin the compiler waits for every such load before a transposing LDS read, which has a stage wait
-// for the next one's data (dh 2.3 us a stage against 1.6).
+// for the next one's data (dh 2.3 us a stage against 1.8).  m0 needs no saving: the compiler sets it before each
+// use of its own.
 __device__ __forceinline__ void load_lds(const char* base, uint32_t off, const char* dst) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)const_cast<char*>(dst));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
 }
 
 template <bool ACROSS>
@@ -298,22 +337,24 @@ __device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long l
   }
 }
 
-enum { kStats, kDz, kDh, kDw };
+enum { kStats, kDz, kExp, kDh, kDw };
+constexpr float kRise = 80.f;  // how far above its reference (log2) a row's values may lie: 2^80 times 2^24 words fit fp32
 
 // One tile of a product and its epilogue:
 //   kStats  z tile (256 words x 256 rows) -> part, zlab
 //   kDz     z tile of the piece from word v0 on -> dz
+//   kExp    the same -> 2^(z log2 e - R) in the place of dz, part
 //   kDh     dacc (+)= dz W over the piece's words, in parts
 //   kDw     dhead rows of the piece = dz^T h
 template <int MODE>
-__global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int first) {
+__global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int piece) {
   __shared__ __attribute__((aligned(1024))) char lds[4 * kOpBytes];
   const int n = a.count[0], nb = (n + kTile - 1) / kTile;  // rows with a loss, tiles of them
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, wm = w & 1, wn = w >> 1;
   Acc acc;
   int ta, tb;
-  if constexpr (MODE == kStats || MODE == kDz) {
+  if constexpr (MODE <= kExp) {
     if (!tile_of(blockIdx.x, (nv + kTile - 1) / kTile, nb, ta, tb)) return;
     const int vt = v0 + ta * kTile, r0 = tb * kTile;
     product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTile), a.H},
@@ -358,12 +399,28 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
           red[(wm * 256 + rl) * 2 + 1] = s;
         }
       } else {
-        const float c = a.c[i], l = a.lse2[i];
-        each([&](int t, int e, float& z) {
-          z = c * ex2(fmaf(z, kL2E, -l));
-          if (t * 16 + e == le) z -= c;
-          if (c == 0.f) z = 0.f;
-        });
+        if constexpr (MODE == kDz) {
+          const float c = a.c[i], l = a.lse2[i];
+          each([&](int t, int e, float& z) {
+            z = c * ex2(fmaf(z, kL2E, -l));
+            if (t * 16 + e == le) z -= c;
+            if (c == 0.f) z = 0.f;
+          });
+        } else {
+          if (__builtin_amdgcn_ballot_w64(here)) each([&](int t, int e, float& z) { z = t * 16 + e == le ? -INFINITY : z; });
+          float m = -FLT_MAX, s = 0.f, r = a.ref[i];
+          each([&](int, int, float& z) { m = fmaxf(m, z); });
+          m = fmaxf(m, __shfl_xor(m, 32)) * kL2E;
+          const bool over = m > r + kRise;
+          if (__builtin_amdgcn_ballot_w64(over) && lane == 0) a.flag[piece] = 1;
+          r = over ? m : r;
+          each([&](int, int, float& z) {
+            z = ex2(fmaf(z, kL2E, -r));
+            s += z;
+          });
+          s += __shfl_xor(s, 32);
+          if (h == 0) a.part[(long)(vw / 128) * a.Mp + i] = make_float2(r, s);
+        }
         // columns m of row rl: piece (m / 8) at (m / 8) ^ (rl mod 32)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -410,7 +467,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
           if (m >= a.H) continue;
           f32x4* at = reinterpret_cast<f32x4*>(row + m);
           const f32x4 v = {acc[t][j][4 * q], acc[t][j][4 * q + 1], acc[t][j][4 * q + 2], acc[t][j][4 * q + 3]};
-          *at = first ? v : *at + v;
+          *at = piece == 0 ? v : *at + v;
         }
     }
   } else {
@@ -463,6 +520,66 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
   a.row_ce[a.src[i]] = (m - a.zlab[i]) + ls * 0.6931471805599453f;
 }
 
+// A piece in which some words took a reference of their own: the row's reference becomes the highest of them, and
+// what was written under others, dh of the pieces before it included, is scaled to it.
+__global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece) {
+  __shared__ float red[4];
+  if (a.flag[piece] == 0) return;
+  const int n = a.count[0], nb = (n + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
+  const int groups = (nv + kTile - 1) / kTile * 2;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const float2* p = a.part + (long)(v0 / 128) * a.Mp + i;
+    const float old = a.ref[i];
+    float r = old;
+    for (int g = threadIdx.x; g < groups; g += 256) r = fmaxf(r, p[(long)g * a.Mp].x);
+    for (int off = 32; off > 0; off >>= 1) r = fmaxf(r, __shfl_xor(r, off));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = r;
+    __syncthreads();
+    r = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if (!(r > old)) continue;
+    for (int e = threadIdx.x; e < groups * 16; e += 256) {  // 8 words each
+      const int g = e >> 4;
+      const float f = ex2(p[(long)g * a.Mp].x - r);
+      if (f == 1.f) continue;
+      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(g >> 1) * a.Mp + i) * kTile + (g & 1) * 128) + (e & 15);
+      u32x4 v = *at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
+      *at = v;
+    }
+    if (piece > 0)
+      for (int k = 0; k < parts; ++k) {
+        float* d = a.dacc + ((long)k * nb * kTile + i) * a.H;
+        for (int m = threadIdx.x; m < a.H; m += 256) d[m] *= ex2(old - r);
+      }
+    if (threadIdx.x == 0) a.ref[i] = r;
+  }
+}
+
+// one pass: the rows' sums from their parts, their cross-entropy and the factors of dh
+__global__ __launch_bounds__(256) void k_lce_close(Lce a, int parts) {
+  __shared__ float sh[16][17];
+  const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
+  if ((int)blockIdx.x * 16 >= n) return;
+  const float r = a.ref[i];
+  float s = 0.f;
+#pragma unroll 4
+  for (int p = g; p < parts; p += 16) {
+    const float2 v = a.part[(long)p * a.Mp + i];
+    s += v.y * ex2(v.x - r);
+  }
+  sh[g][l] = s;
+  __syncthreads();
+  if (g != 0 || i >= n) return;
+  for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
+  const float y = a.zlab[i] * kL2E - r, ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey);
+  a.fac[i] = c * inv;
+  a.lab[i] = c * (s * inv);
+  // log((s + ey) / ey); far below the reference ey may be 0
+  a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
+}
+
 // loss = sum of c ce in 64 bits, in a fixed order
 __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
   __shared__ double ws[16];
@@ -482,6 +599,8 @@ __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
   const int nb = (a.count[0] + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
   const int i = a.pos[blockIdx.x];
+  const float f = a.ref && i >= 0 ? a.fac[i] : 1.f, fl = a.ref && i >= 0 ? a.lab[i] : 0.f;
+  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (fl != 0.f ? (long)a.labels[blockIdx.x] * a.H : 0));
   u32x4* to = reinterpret_cast<u32x4*>(a.dhidden + (long)blockIdx.x * a.H);
   for (int p = threadIdx.x; p < a.H / 8; p += 256) {
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
@@ -491,15 +610,24 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
         x += from[0];
         y += from[1];
       }
+    x *= f;
+    y *= f;
+    if (fl != 0.f) {
+      const u32x4 v = word[p];
+      x -= fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
+      y -= fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
+    }
     to[p] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
   }
 }
 
 // ---- host side ----
+template <int N>
+using mode_c = std::integral_constant<int, N>;
 constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
 
 struct LceLayout {
-  size_t count, src, pos, c, hc, part, zlab, lse2, dz, dacc, total;
+  size_t count, src, pos, c, hc, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -524,9 +652,13 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.pos, (size_t)rows * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
-  take(L.part, (size_t)words * L.Mp * 8);
+  take(L.part, (size_t)words * L.Mp * 16);
   take(L.zlab, (size_t)L.Mp * 4);
   take(L.lse2, (size_t)L.Mp * 4);
+  take(L.ref, (size_t)L.Mp * 4);
+  take(L.fac, (size_t)L.Mp * 4);
+  take(L.lab, (size_t)L.Mp * 4);
+  take(L.flag, (size_t)words * 4);
   // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
   const size_t tile = (size_t)kTile * kTile;
   if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kTile * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kTile * 2)));
@@ -602,23 +734,39 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.Vp = L.Vp;
   a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
   const int nb = L.Mp / kTile, na = (H + kTile - 1) / kTile, words = (int)((V + (long)kTile - 1) / kTile);
+  const int pieces = (words + L.Vp / kTile - 1) / (L.Vp / kTile);
+  const bool one_pass = dhidden && !dhead;
+  if (one_pass) {
+    a.ref = (float*)(w + L.ref);
+    a.fac = (float*)(w + L.fac);
+    a.lab = (float*)(w + L.lab);
+    a.flag = (int*)(w + L.flag);
+  }
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
-  hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a);
+  auto product = [&](auto mode, long tiles, int v0, int nv, int piece) {
+    hipLaunchKernelGGL((k_lce_product<decltype(mode)::value>), dim3(grid(tiles)), dim3(kT), 0, st, a, v0, nv, piece);
+  };
+  hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a, pieces);
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
-  hipLaunchKernelGGL((k_lce_product<kStats>), dim3(grid((long)words * nb)), dim3(kT), 0, st, a, 0, V, 0);
-  hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, words);
-  hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
+  if (!one_pass) {
+    product(mode_c<kStats>{}, (long)words * nb, 0, V, 0);
+    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, words);
+  }
   if (dhidden || dhead)
-    for (long at = 0; at < V; at += L.Vp) {
-      const int v0 = (int)at, nv = std::min(V - v0, L.Vp);
+    for (int piece = 0; piece < pieces; ++piece) {
+      const int v0 = piece * L.Vp, nv = std::min(V - v0, L.Vp);
       const long wt = (nv + kTile - 1) / kTile;
-      hipLaunchKernelGGL((k_lce_product<kDz>), dim3(grid(wt * nb)), dim3(kT), 0, st, a, v0, nv, 0);
-      if (dhidden)
-        hipLaunchKernelGGL((k_lce_product<kDh>), dim3(grid(std::max((long)na * nb, std::min(16l * na * nb, 512l)))), dim3(kT),
-                           0, st, a, v0, nv, v0 == 0);
-      if (dhead)
-        hipLaunchKernelGGL((k_lce_product<kDw>), dim3(grid(wt * na)), dim3(kT), 0, st, a, v0, nv, 0);
+      if (one_pass) {
+        product(mode_c<kExp>{}, wt * nb, v0, nv, piece);
+        hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece);
+      } else {
+        product(mode_c<kDz>{}, wt * nb, v0, nv, piece);
+      }
+      if (dhidden) product(mode_c<kDh>{}, std::max((long)na * nb, std::min(16l * na * nb, 512l)), v0, nv, piece);
+      if (dhead) product(mode_c<kDw>{}, wt * na, v0, nv, piece);
     }
+  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(256), 0, st, a, 2 * words);
+  hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
   if (dhidden) hipLaunchKernelGGL(k_lce_dhidden, dim3(rows), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR_HIP;
 }

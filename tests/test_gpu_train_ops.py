@@ -81,11 +81,11 @@ def lce_check(h, head, y, B, gamma, got):
 
 
 # (blocks, B, V, H): one word, one row; widths below, at and past a stage of 64; vocabularies around a tile of 256; 255,
-# 256 and 257 rows with a loss at ignored = 0; 4,096 x 40,000: several pieces of the vocabulary
+# 256 and 257 rows with a loss at ignored = 0; 4,096 x 70,000: two pieces of the vocabulary
 @pytest.mark.parametrize("n,B,V,H,ignored", [
     (1, 2, 1, 8, 0), (1, 2, 2, 8, 0), (2, 2, 255, 64, 0), (3, 5, 256, 72, 0.1), (7, 3, 257, 56, 0.1),
     (17, 16, 1000, 512, 0), (128, 3, 515, 128, 0), (257, 2, 300, 200, 0), (23, 9, 32003, 264, 0.1),
-    (40, 16, 5000, 2880, 0.5), (1, 700, 2049, 1024, 0.2), (256, 16, 40000, 64, 0.05), (5, 13, 3001, 4096, 0.1)])
+    (40, 16, 5000, 2880, 0.5), (1, 700, 2049, 1024, 0.2), (256, 16, 70000, 64, 0.05), (5, 13, 3001, 4096, 0.1)])
 def test_linear_ce(n, B, V, H, ignored):
     print(f"[train ops] linear ce {(n, B, V, H)}", flush=True)
     h, head, y = lce_inputs(n, B, V, H, seed=n + V, ignored=ignored)
@@ -121,6 +121,17 @@ def test_linear_ce_far_outlier_words():
             w[v, 0] = 4.0 + 3.0 * k
         for dw in (False, True):
             lce_check(h, w, y, 4, 4.5, dfl.linear_ce(h, w, y, 4, 4.5, need_dhead=dw))
+
+
+def test_linear_ce_outlier_words_of_two_pieces():
+    """Rows whose largest logit rises by hundreds within a piece and again in the next one, and rows that stay."""
+    h, head, y = lce_inputs(256, 16, 70000, 64, seed=6, lean=0.0)
+    h[:, 0] = torch.where(torch.arange(4096, device="cuda") % 3 == 0, 100.0, 0.0).to(BF)
+    for words in ((69999,), (5, 69000), (30000, 34000, 40000), (35071, 35072)):
+        w = head.clone()
+        for k, v in enumerate(words):
+            w[v, 0] = 4.0 + 3.0 * k
+        lce_check(h, w, y, 16, 4.5, dfl.linear_ce(h, w, y, 16, 4.5))
 
 
 def test_linear_ce_rows_without_a_loss_may_hold_anything():
