@@ -8,10 +8,11 @@
 // 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
 // product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
 // fp32, so that R need not be the maximum: only logits more than 2^80 above it (which a piece's 128 words
-// then take as their own reference, raise a flag and have the row rescaled) move it.  The label's word is left out
-// of both and added at the end, as the difference 1 - p is lost where p is rounded.
+// then take as their own reference, raise a flag and have the row rescaled) move it.
 // With dW, which needs dz of all words of a row at its final scale, the maxima and sums come first, and each
 // piece's logits are formed again: 2 rows V H operations more.
+// The label's word is left out of dz: its -c (1 - p), the largest value of its row, goes into dh and dW in fp32
+// (rounded to bf16 with the others it would be 0.7 of the gradients' whole error).
 // Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with dW alone, 8 with both.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -59,13 +60,15 @@ struct Lce {
   int* count;     // [1] rows with a loss
   int* src;       // [Mp] i -> row
   int* pos;       // [rows] row -> i, -1 without a loss
+  int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
   float2* part;   // [words / 256][Mp] (max, sum of exp(z - max)); one pass: [words / 128][Mp] (R, sum of 2^(z log2 e - R))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
-  // one pass: the rows' references R (log2 domain), c / sum and c (1 - p of the label) at the end; flags of the pieces
-  float *ref, *fac, *lab;
+  float* lab;     // [Mp] c (1 - p of the label)
+  // one pass: the rows' references R (log2 domain) and c / sum at the end; flags of the pieces
+  float *ref, *fac;
   int* flag;
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
   float* dacc;    // [parts][tiles of rows x 256][H] dh of the pieces so far
@@ -114,6 +117,7 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
       const float w = expf(-(float)(b - 1) / a.gamma);
       sum += w;
       a.src[i] = r;
+      a.word[i] = y;
       a.c[i] = w;
     }
     if (r < a.rows) {
@@ -128,7 +132,10 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
   for (int k = 0; k < 16; ++k) sum += ws[k];
   const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
   const int np = min((n + kTile - 1) / kTile * kTile, a.Mp);
-  for (int i = tid; i < np; i += 1024) a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
+  for (int i = tid; i < np; i += 1024) {
+    a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
+    if (i >= n) a.word[i] = -1;
+  }
   if (a.flag)
     for (int i = tid; i < pieces; i += 1024) a.flag[i] = 0;
   if (tid == 0) a.count[0] = n;
@@ -144,7 +151,7 @@ __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)row * a.H);
   u32x4* to = reinterpret_cast<u32x4*>(a.hc + (long)i * a.ldh);
   const bool dot = a.ref && i < n;
-  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (dot ? (long)a.labels[row] * a.H : 0));
+  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (dot ? (long)a.word[i] * a.H : 0));
   float s = 0.f;
   for (int p = threadIdx.x; p < a.ldh / 8; p += 256) {
     const bool in = i < n && p < a.H / 8;
@@ -268,9 +275,9 @@ struct Reader {
 typedef f32x16 Acc[4][2];
 
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
-// something finite
-template <bool XA, bool XB>
-__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc& acc) {
+// something finite.  start(acc) runs while the first stage is on its way.
+template <bool XA, bool XB, typename F>
+__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc& acc, F&& start) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Loader<XA> la;
   Loader<XB> lb;
@@ -293,6 +300,7 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     lb.issue(st + kOpBytes, w, kt, ob.kend - kt * kBK);
   };
   if (nk > 0) issue(0);
+  start(acc);
   for (int kt = 0; kt < nk; ++kt) {
     wait_vm_barrier<0>();
     if (kt + 1 < nk) issue(kt + 1);
@@ -358,14 +366,14 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
     if (!tile_of(blockIdx.x, (nv + kTile - 1) / kTile, nb, ta, tb)) return;
     const int vt = v0 + ta * kTile, r0 = tb * kTile;
     product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTile), a.H},
-                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTile, a.ldh}, a.H, lds, acc);
+                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTile, a.ldh}, a.H, lds, acc, [](Acc&) {});
     const int vw = vt + wm * 128;  // the wave's first word
     float* red = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int rl = wn * 64 + j * 32 + (lane & 31), i = r0 + rl;
       // the label's place among the wave's words, if it is there
-      const int rel = i < n ? a.labels[a.src[i]] - vw : -1;
+      const int rel = i < n ? a.word[i] - vw : -1;
       const bool here = rel >= 0 && rel < 128 && ((rel >> 2) & 1) == h;
       const int le = here ? (rel >> 5) * 16 + ((rel & 31) >> 3) * 4 + (rel & 3) : -1;  // its (tile, element) of this lane
       auto each = [&](auto f) {
@@ -403,8 +411,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
           const float c = a.c[i], l = a.lse2[i];
           each([&](int t, int e, float& z) {
             z = c * ex2(fmaf(z, kL2E, -l));
-            if (t * 16 + e == le) z -= c;
-            if (c == 0.f) z = 0.f;
+            if (t * 16 + e == le || c == 0.f) z = 0.f;
           });
         } else {
           if (__builtin_amdgcn_ballot_w64(here)) each([&](int t, int e, float& z) { z = t * 16 + e == le ? -INFINITY : z; });
@@ -454,7 +461,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
     const int s0 = (int)((long)stages * ks / parts), s1 = (int)((long)stages * (ks + 1) / parts);
     const int words = min(s1 * kBK, nv) - s0 * kBK;
     product<true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, kTile), words},
-                         Operand{a.dz + (long)r0 * kTile, kTile, kTile, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc);
+                         Operand{a.dz + (long)r0 * kTile, kTile, kTile, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc, [](Acc&) {});
     float* out = a.dacc + (long)ks * nb * kTile * a.H;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -474,7 +481,43 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
     if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, (nv + kTile - 1) / kTile, ta, tb)) return;
     const int m0 = ta * kTile, n0 = tb * kTile;
     product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTile), a.Mp},
-                        Operand{a.dz + (long)tb * a.Mp * kTile, kTile, kTile, a.Mp}, n, lds, acc);
+                        Operand{a.dz + (long)tb * a.Mp * kTile, kTile, kTile, a.Mp}, n, lds, acc, [&](Acc& d) {
+      // the label terms: the rows whose label is one of the wave's 64 words, in order
+      const int word0 = v0 + n0 + wn * 64;
+      const uint16_t* col = a.hc + m0 + wm * 128 + 4 * h;
+      const int most = a.ldh - 4 - (m0 + wm * 128 + 4 * h);  // (columns past the last are not kept)
+      for (int i0 = 0; i0 < n; i0 += 256) {
+        int y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + 64 * k + lane;
+          y[k] = i < n ? a.word[i] - word0 : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < 64u);
+          while (hit) {
+            const int b = __builtin_ctzll(hit), i = i0 + 64 * k + b, wl = __builtin_amdgcn_readlane(y[k], b);
+            hit &= hit - 1;
+            const float f = (lane & 31) == (wl & 31) ? -a.lab[i] : 0.f;
+            const uint16_t* row = col + (long)i * a.ldh;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const u32x2 v = *reinterpret_cast<const u32x2*>(row + min(t * 32 + q * 8, most));
+                const f32x4 x = {__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u),
+                                 __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if (wl < 32) d[t][0][4 * q + e] = fmaf(f, x[e], d[t][0][4 * q + e]);
+                  else d[t][1][4 * q + e] = fmaf(f, x[e], d[t][1][4 * q + e]);
+                }
+              }
+          }
+        }
+      }
+    });
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int nl = wn * 64 + j * 32 + (lane & 31);
@@ -516,8 +559,10 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
     m = mn;
   }
   const float ls = log2f(s);
+  const float ce = (m - a.zlab[i]) + ls * 0.6931471805599453f;
   a.lse2[i] = m * kL2E + ls;
-  a.row_ce[a.src[i]] = (m - a.zlab[i]) + ls * 0.6931471805599453f;
+  a.lab[i] = a.c[i] * -expm1f(-ce);
+  a.row_ce[a.src[i]] = ce;
 }
 
 // A piece in which some words took a reference of their own: the row's reference becomes the highest of them, and
@@ -599,8 +644,8 @@ __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
   const int nb = (a.count[0] + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
   const int i = a.pos[blockIdx.x];
-  const float f = a.ref && i >= 0 ? a.fac[i] : 1.f, fl = a.ref && i >= 0 ? a.lab[i] : 0.f;
-  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (fl != 0.f ? (long)a.labels[blockIdx.x] * a.H : 0));
+  const float f = a.ref && i >= 0 ? a.fac[i] : 1.f, fl = i >= 0 ? a.lab[i] : 0.f;
+  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (i >= 0 ? (long)a.word[i] * a.H : 0));
   u32x4* to = reinterpret_cast<u32x4*>(a.dhidden + (long)blockIdx.x * a.H);
   for (int p = threadIdx.x; p < a.H / 8; p += 256) {
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
@@ -612,7 +657,7 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
       }
     x *= f;
     y *= f;
-    if (fl != 0.f) {
+    if (i >= 0) {
       const u32x4 v = word[p];
       x -= fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
       y -= fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
@@ -627,7 +672,7 @@ using mode_c = std::integral_constant<int, N>;
 constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
 
 struct LceLayout {
-  size_t count, src, pos, c, hc, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
+  size_t count, src, pos, word, c, hc, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -650,6 +695,7 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.count, 4);
   take(L.src, (size_t)L.Mp * 4);
   take(L.pos, (size_t)rows * 4);
+  take(L.word, (size_t)L.Mp * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
   take(L.part, (size_t)words * L.Mp * 16);
@@ -722,7 +768,9 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.count = (int*)(w + L.count);
   a.src = (int*)(w + L.src);
   a.pos = (int*)(w + L.pos);
+  a.word = (int*)(w + L.word);
   a.c = (float*)(w + L.c);
+  a.lab = (float*)(w + L.lab);
   a.hc = (uint16_t*)(w + L.hc);
   a.part = (float2*)(w + L.part);
   a.zlab = (float*)(w + L.zlab);
@@ -739,7 +787,6 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   if (one_pass) {
     a.ref = (float*)(w + L.ref);
     a.fac = (float*)(w + L.fac);
-    a.lab = (float*)(w + L.lab);
     a.flag = (int*)(w + L.flag);
   }
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
