@@ -3,7 +3,7 @@
 //   ce_r = lse(z_r) - z_r[y_r],  loss = sum c ce,  dz = c (softmax(z) - onehot(y)),
 //   dh = dz W,  dW = dz^T h.
 // The rows with a loss are gathered first (the others take no part in any product).
-// The loss alone is one product, whose epilogue leaves every row's maximum and sum per 256 words.
+// The loss alone is one product, whose epilogue leaves every row's maximum and sum per 128 words.
 // With dh alone the vocabulary is walked once, in pieces, as one pass of a softmax: a piece's product leaves
 // 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
 // product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
@@ -29,10 +29,12 @@ namespace dflare {
 
 namespace {
 
-constexpr int kT = 512;     // threads of a product's work-group: 8 waves
-constexpr int kTile = 256;  // output tile: 256 x 256, a wave 128 x 64
+constexpr int kT = 512;     // threads of a product's work-group: 8 waves, 2 (m) x 4 (n)
+constexpr int kWaves = kT / 64;
+constexpr int kTM = 256;    // output tile: 256 m x 256 n, a wave 128 x 64
+constexpr int kTN = 256;
 constexpr int kBK = 64;     // k of a stage
-constexpr int kOpBytes = kTile * kBK * 2;
+constexpr int kABytes = kTM * kBK * 2, kBBytes = kTN * kBK * 2, kStageBytes = kABytes + kBBytes;
 constexpr float kL2E = 1.4426950408889634f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -63,7 +65,7 @@ struct Lce {
   int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
-  float2* part;   // [words / 256][Mp] (max, sum of exp(z - max)); one pass: [words / 128][Mp] (R, sum of 2^(z log2 e - R))
+  float2* part;   // [words / 128][Mp] (max log2 e, sum of exp(z - max)); one pass: (R, sum of 2^(z log2 e - R))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
   float* lab;     // [Mp] c (1 - p of the label)
@@ -76,14 +78,15 @@ struct Lce {
   int stages;     // stages of k of the first (longest) piece
 };
 
-// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for 256 CUs: the number
-// with the least time, a round of work-groups costing its stages of k and about 30 more for its start and its
-// sums in memory (measured: 0.9 us a stage, 27 us).  More than one part makes at most 512 work-groups.  The number
-// depends on the rows with a loss, so that it is chosen on the device.
+// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for 256 CUs: the
+// number with the least time, a round of work-groups costing its stages of k and about 30
+// more for its start and its sums in memory (measured: 0.9 us a stage, 27 us).  More than one part makes at
+// most 512 work-groups.  The number depends on the rows with a loss, so that it is chosen on the device.
+constexpr int kMostUnits = 512, kMostParts = 16;
 __host__ __device__ inline int dh_parts(int nb, int na, int stages) {
   int best = 1, cost = 0x7fffffff;
-  for (int k = 1; k <= 16; ++k) {
-    if (k > 1 && (nb * na * k > 512 || stages < 8 * k)) break;
+  for (int k = 1; k <= kMostParts; ++k) {
+    if (k > 1 && (nb * na * k > kMostUnits || stages < 8 * k)) break;
     const int c = (nb * na * k + 255) / 256 * ((stages + k - 1) / k + 30);
     if (c < cost) {
       best = k;
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
   sum = 0.0;
   for (int k = 0; k < 16; ++k) sum += ws[k];
   const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
-  const int np = min((n + kTile - 1) / kTile * kTile, a.Mp);
+  const int np = min((n + kTN - 1) / kTN * kTN, a.Mp);
   for (int i = tid; i < np; i += 1024) {
     a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
     if (i >= n) a.word[i] = -1;
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
 __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   __shared__ float red[4];
   const int n = a.count[0], i = blockIdx.x;
-  if (i >= (n + kTile - 1) / kTile * kTile) return;
+  if (i >= (n + kTN - 1) / kTN * kTN) return;
   const u32x4 z = {0u, 0u, 0u, 0u};
   const int row = i < n ? a.src[i] : 0;
   const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)row * a.H);
@@ -199,50 +202,55 @@ struct Operand {
 // builtin the compiler waits for every such load before a transposing LDS read, which has a stage wait
 // for the next one's data (dh 2.3 us a stage against 1.8).  m0 needs no saving: the compiler sets it before each
 // use of its own.
-__device__ __forceinline__ void load_lds(const char* base, uint32_t off, const char* dst) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)const_cast<char*>(dst));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
+__device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
 }
 
-template <bool ACROSS>
+// ROWS: rows (plain) or columns (across) of the operand's tile
+template <bool ACROSS, int ROWS>
 struct Loader {
-  const char* base;
-  uint32_t off[4], back[4];  // byte offset of the wave's four pieces of a lane; what takes it back to k = 0
+  static constexpr int N = ROWS * kBK * 2 / 1024 / kWaves;  // loads of a wave and stage
+  static constexpr int SB = 256 / kBK;                 // stages of a block of 256 k
+  const char* at;   // of the next stage
+  uint32_t off[N];  // byte offset of a lane's pieces
   long step;
-  int s0;
-  int kl[4];  // first k of the piece
+  int st;
   __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
-    base = reinterpret_cast<const char*>(o.p);
+    st = o.s0;
+    step = ACROSS ? o.ld * kBK * 2 : o.block - (SB - 1) * kBK * 2;
+    at = reinterpret_cast<const char*>(o.p) + (ACROSS ? 0 : st / SB * o.block + st % SB * (kBK * 2));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < N; ++j) {
       if constexpr (!ACROSS) {
-        const int row = (4 * w + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+        const int row = (N * w + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
         off[j] = (uint32_t)(min(row, o.valid - 1) * o.ld * 2 + c * 16);
-        back[j] = c * 16;
-        kl[j] = c * 8;
       } else {
-        const int row = (4 * w + j) * 2 + (lane >> 5), c = (lane & 31) ^ ((row & 3) << 2);
+        constexpr int P = ROWS / 8;  // pieces of a row
+        const int row = (N * w + j) * (64 / P) + lane / P, c = (lane % P) ^ ((row & 3) << 2);
         off[j] = (uint32_t)(row * o.ld * 2 + min(c * 8, o.valid - 8) * 2);
-        back[j] = (uint32_t)(row * o.ld * 2);
-        kl[j] = row;
       }
     }
-    step = ACROSS ? o.ld * kBK * 2 : o.block;
-    s0 = o.s0;
   }
-  // the wave's share of a stage; left: k that exist from the stage's first on
-  __device__ __forceinline__ void issue(char* dst, int w, int kt, int left) const {
-    const int st = s0 + kt;
-    const char* b = ACROSS ? base + kt * step : base + (st >> 2) * step + (st & 3) * (kBK * 2);
+  // the wave's share of the next stage; left: k that exist from its first on (past them that first again)
+  template <bool WHOLE>
+  __device__ __forceinline__ void issue(uint32_t dst, const Operand& o, int w, int lane, int left) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t o = kl[j] < left ? off[j] : off[j] - back[j];
-      load_lds(b, o, dst + (4 * w + j) * 1024);
+    for (int j = 0; j < N; ++j) {
+      uint32_t x = off[j];
+      if constexpr (!WHOLE) {
+        const int row = ACROSS ? (N * w + j) * (512 / ROWS) + lane / (ROWS / 8) : (N * w + j) * 8 + (lane >> 3);
+        const int c = (lane & 7) ^ ((row >> 1) & 7);
+        if constexpr (ACROSS) x = row < left ? x : x - (uint32_t)(row * o.ld * 2);
+        else x = c * 8 < left ? x : x - c * 16;
+      }
+      load_lds(at, x, dst + j * 1024);
     }
+    if constexpr (ACROSS) at += step;
+    else at += (++st % SB == 0) ? step : kBK * 2;
   }
 };
 
-template <bool ACROSS>
+template <bool ACROSS, int ROWS>
 struct Reader {
   uint32_t off[4];
   // tile0: first 32-row (or 32-column) tile of the wave
@@ -250,20 +258,19 @@ struct Reader {
     const int h = lane >> 5;
     if constexpr (!ACROSS) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        off[ks] = (tile0 * 32 + (lane & 31)) * 128 + (((2 * ks + h) ^ ((lane >> 1) & 7)) << 4);
+      for (int ks = 0; ks < 4; ++ks) off[ks] = (tile0 * 32 + (lane & 31)) * 128 + (((2 * ks + h) ^ ((lane >> 1) & 7)) << 4);
     } else {
       const int i = lane & 15, g = (lane >> 4) & 1, f = i >> 2;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        off[j] = (8 * h + f) * 512 + ((4 * ((tile0 + j) ^ f) + 2 * g + ((i & 3) >> 1)) << 4) + (i & 1) * 8;
+        off[j] = (8 * h + f) * (ROWS * 2) + ((4 * ((tile0 + j) ^ f) + 2 * g + ((i & 3) >> 1)) << 4) + (i & 1) * 8;
     }
   }
   __device__ __forceinline__ u32x4 get(const char* op, int ks, int j) const {
     if constexpr (!ACROSS) return *reinterpret_cast<const u32x4*>(op + off[ks] + j * 4096);
     else {
-      const char* p = op + off[j] + ks * 16 * 512;
-      const u32x2 lo = tr(p), hi = tr(p + 4 * 512);
+      const char* p = op + off[j] + ks * 16 * (ROWS * 2);
+      const u32x2 lo = tr(p), hi = tr(p + 4 * (ROWS * 2));
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
   }
@@ -275,16 +282,16 @@ struct Reader {
 typedef f32x16 Acc[4][2];
 
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
-// something finite.  start(acc) runs while the first stage is on its way.
+// something finite.  start(acc) runs while the first stages are on their way.
 template <bool XA, bool XB, typename F>
 __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc& acc, F&& start) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Loader<XA> la;
-  Loader<XB> lb;
+  Loader<XA, kTM> la;
+  Loader<XB, kTN> lb;
   la.init(oa, w, lane);
   lb.init(ob, w, lane);
-  Reader<XA> ra;
-  Reader<XB> rb;
+  Reader<XA, kTM> ra;
+  Reader<XB, kTN> rb;
   ra.init((w & 1) * 4, lane);
   rb.init((w >> 1) * 2, lane);
 #pragma unroll
@@ -294,31 +301,72 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   const int nk = (K + kBK - 1) / kBK;
-  auto issue = [&](int kt) {
-    char* st = lds + (kt & 1) * 2 * kOpBytes;
-    la.issue(st, w, kt, oa.kend - kt * kBK);
-    lb.issue(st + kOpBytes, w, kt, ob.kend - kt * kBK);
-  };
-  if (nk > 0) issue(0);
-  start(acc);
-  for (int kt = 0; kt < nk; ++kt) {
-    wait_vm_barrier<0>();
-    if (kt + 1 < nk) issue(kt + 1);
-    const char* st = lds + (kt & 1) * 2 * kOpBytes;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      u32x4 fa[4], fb[2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) fa[i] = ra.get(st, ks, i);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) fb[j] = rb.get(st + kOpBytes, ks, j);
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][j] = mfma32(fa[i], fb[j], acc[i][j]);
+  using LA = Loader<XA, kTM>;
+  using LB = Loader<XB, kTN>;
+  constexpr int NL = LA::N + LB::N;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)lds);
+  const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + kABytes + w * LB::N * 1024;
+  int next = 0;  // stage to load
+  // the next stage into the buffer at `buf`; past the last stage nothing
+  auto issue = [&](uint32_t buf) {
+    const int left = min(oa.kend, ob.kend) - next * kBK;
+    if (next < nk) {
+      if (left >= kBK) {
+        la.template issue<true>(da + buf, oa, w, lane, 0);
+        lb.template issue<true>(db + buf, ob, w, lane, 0);
+      } else {
+        la.template issue<false>(da + buf, oa, w, lane, oa.kend - next * kBK);
+        lb.template issue<false>(db + buf, ob, w, lane, ob.kend - next * kBK);
+      }
     }
+    ++next;
+  };
+  struct Frags {
+    u32x4 a[4], b[2];
+  };
+  auto read = [&](Frags& f, uint32_t buf, int ks) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) f.b[j] = rb.get(lds + kABytes + buf, ks, j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.a[i] = ra.get(lds + buf, ks, i);
+  };
+  auto multiply = [&](const Frags& f) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i][j] = mfma32(f.a[i], f.b[j], acc[i][j]);
+  };
+  issue(0);
+  issue(kStageBytes);
+  start(acc);
+  wait_vm_barrier<0>();
+  Frags f0, f1;
+  read(f0, 0, 0);
+  uint32_t buf = 0;
+  for (int kt = 0; kt < nk; ++kt) {
+    // each 16 k are read under the products of the 16 before; when all waves have read the stage's last, its
+    // buffer takes the stage after the next, and the next one is read
+    read(f1, buf, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(f0, buf, 2);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f1);
+    __builtin_amdgcn_sched_barrier(0);
+    read(f1, buf, 3);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f0);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm_barrier<0>();
+    read(f0, buf ^ kStageBytes, 0);
+    issue(buf);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(f1);
+    __builtin_amdgcn_sched_barrier(0);
+    buf ^= kStageBytes;
   }
-  __syncthreads();
+  wait_vm_barrier<0>();
 }
 
 // Output tile t of TA x TB, so that the work-groups that run together on an XCD (ids are dealt to the 8 XCDs
@@ -334,7 +382,7 @@ __device__ __forceinline__ bool tile_of(int id, int TA, int TB, int& ta, int& tb
   return true;
 }
 
-// bf16 tile from LDS to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
+// bf16 tile (256 n x 256 m) from LDS to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
 __device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long ld, int nv, int mv) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll 4
@@ -356,19 +404,18 @@ constexpr float kRise = 80.f;  // how far above its reference (log2) a row's val
 //   kDw     dhead rows of the piece = dz^T h
 template <int MODE>
 __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int piece) {
-  __shared__ __attribute__((aligned(1024))) char lds[4 * kOpBytes];
-  const int n = a.count[0], nb = (n + kTile - 1) / kTile;  // rows with a loss, tiles of them
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
+  const int n = a.count[0], nb = (n + kTN - 1) / kTN;  // rows with a loss, tiles of them
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, wm = w & 1, wn = w >> 1;
   Acc acc;
   int ta, tb;
   if constexpr (MODE <= kExp) {
-    if (!tile_of(blockIdx.x, (nv + kTile - 1) / kTile, nb, ta, tb)) return;
-    const int vt = v0 + ta * kTile, r0 = tb * kTile;
-    product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTile), a.H},
-                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTile, a.ldh}, a.H, lds, acc, [](Acc&) {});
+    if (!tile_of(blockIdx.x, (nv + kTM - 1) / kTM, nb, ta, tb)) return;
+    const int vt = v0 + ta * kTM, r0 = tb * kTN;
+    product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTM), a.H},
+                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTN, INT_MAX}, a.H, lds, acc, [](Acc&) {});
     const int vw = vt + wm * 128;  // the wave's first word
-    float* red = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int rl = wn * 64 + j * 32 + (lane & 31), i = r0 + rl;
@@ -398,14 +445,10 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         }
         float m = -FLT_MAX, s = 0.f;
         each([&](int, int, float& z) { m = fmaxf(m, z); });
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float ml = fmaxf(m * kL2E, -FLT_MAX);  // (finite where the wave has no words: they add 0)
-        each([&](int, int, float& z) { s += ex2(fmaf(z, kL2E, -ml)); });
+        m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) * kL2E, -FLT_MAX);  // (finite where the wave has no words: they add 0)
+        each([&](int, int, float& z) { s += ex2(fmaf(z, kL2E, -m)); });
         s += __shfl_xor(s, 32);
-        if (h == 0) {
-          red[(wm * 256 + rl) * 2] = m;
-          red[(wm * 256 + rl) * 2 + 1] = s;
-        }
+        if (h == 0) a.part[(long)(vw / 128) * a.Mp + i] = make_float2(m, s);
       } else {
         if constexpr (MODE == kDz) {
           const float c = a.c[i], l = a.lse2[i];
@@ -440,29 +483,22 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
           }
       }
     }
-    __syncthreads();
-    if constexpr (MODE == kStats) {
-      if (threadIdx.x < kTile) {
-        const float m0 = red[threadIdx.x * 2], m1 = red[(256 + threadIdx.x) * 2];
-        const float m = fmaxf(m0, m1);
-        const float s = red[threadIdx.x * 2 + 1] * ex2((m0 - m) * kL2E) + red[(256 + threadIdx.x) * 2 + 1] * ex2((m1 - m) * kL2E);
-        a.part[(long)(vt / kTile) * a.Mp + r0 + threadIdx.x] = make_float2(m, s);
-      }
-    } else {
-      store_tile(lds, a.dz + ((long)ta * a.Mp + r0) * kTile, kTile, kTile, kTile);
+    if constexpr (MODE != kStats) {
+      __syncthreads();
+      store_tile(lds, a.dz + ((long)ta * a.Mp + r0) * kTM, kTM, kTN, kTM);
     }
   } else if constexpr (MODE == kDh) {
-    const int na = (a.H + kTile - 1) / kTile, stages = (nv + kBK - 1) / kBK, parts = dh_parts(nb, na, a.stages);
+    const int na = (a.H + kTM - 1) / kTM, stages = (nv + kBK - 1) / kBK, parts = dh_parts(nb, na, a.stages);
     int unit;
     if (!tile_of(blockIdx.x, na * parts, nb, unit, tb)) return;
     ta = unit % na;
-    const int ks = unit / na, m0 = ta * kTile, r0 = tb * kTile;
+    const int ks = unit / na, m0 = ta * kTM, r0 = tb * kTN;
     // this part's words: whole stages
     const int s0 = (int)((long)stages * ks / parts), s1 = (int)((long)stages * (ks + 1) / parts);
     const int words = min(s1 * kBK, nv) - s0 * kBK;
-    product<true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, kTile), words},
-                         Operand{a.dz + (long)r0 * kTile, kTile, kTile, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc, [](Acc&) {});
-    float* out = a.dacc + (long)ks * nb * kTile * a.H;
+    product<true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, kTM), words},
+                         Operand{a.dz + (long)r0 * kTM, kTM, kTN, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc, [](Acc&) {});
+    float* out = a.dacc + (long)ks * nb * kTN * a.H;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float* row = out + (long)(r0 + wn * 64 + j * 32 + (lane & 31)) * a.H;
@@ -478,10 +514,10 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         }
     }
   } else {
-    if (!tile_of(blockIdx.x, (a.H + kTile - 1) / kTile, (nv + kTile - 1) / kTile, ta, tb)) return;
-    const int m0 = ta * kTile, n0 = tb * kTile;
-    product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTile), a.Mp},
-                        Operand{a.dz + (long)tb * a.Mp * kTile, kTile, kTile, a.Mp}, n, lds, acc, [&](Acc& d) {
+    if (!tile_of(blockIdx.x, (a.H + kTM - 1) / kTM, (nv + kTN - 1) / kTN, ta, tb)) return;
+    const int m0 = ta * kTM, n0 = tb * kTN;
+    product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTM), a.Mp},
+                        Operand{a.dz + (long)tb * a.Mp * kTM, kTM, kTN, a.Mp}, n, lds, acc, [&](Acc& d) {
       // the label terms: the rows whose label is one of the wave's 64 words, in order
       const int word0 = v0 + n0 + wn * 64;
       const uint16_t* col = a.hc + m0 + wm * 128 + 4 * h;
@@ -532,7 +568,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         }
     }
     __syncthreads();
-    store_tile(lds, a.dhead + (long)(v0 + n0) * a.H + m0, a.H, min(nv - n0, kTile), min(a.H - m0, kTile));
+    store_tile(lds, a.dhead + (long)(v0 + n0) * a.H + m0, a.H, min(nv - n0, kTN), min(a.H - m0, kTM));
   }
 }
 
@@ -546,7 +582,7 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
   for (int p = g; p < parts; p += 16) {
     const float2 v = a.part[(long)p * a.Mp + i];
     const float mn = fmaxf(m, v.x);
-    s = s * ex2((m - mn) * kL2E) + v.y * ex2((v.x - mn) * kL2E);
+    s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
     m = mn;
   }
   sh[g][l] = make_float2(m, s);
@@ -555,12 +591,12 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
   for (int k = 1; k < 16; ++k) {
     const float2 v = sh[k][l];
     const float mn = fmaxf(m, v.x);
-    s = s * ex2((m - mn) * kL2E) + v.y * ex2((v.x - mn) * kL2E);
+    s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
     m = mn;
   }
-  const float ls = log2f(s);
-  const float ce = (m - a.zlab[i]) + ls * 0.6931471805599453f;
-  a.lse2[i] = m * kL2E + ls;
+  const float lse = m + log2f(s);
+  const float ce = (lse - a.zlab[i] * kL2E) * 0.6931471805599453f;
+  a.lse2[i] = lse;
   a.lab[i] = a.c[i] * -expm1f(-ce);
   a.row_ce[a.src[i]] = ce;
 }
@@ -570,8 +606,8 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
 __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece) {
   __shared__ float red[4];
   if (a.flag[piece] == 0) return;
-  const int n = a.count[0], nb = (n + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
-  const int groups = (nv + kTile - 1) / kTile * 2;
+  const int n = a.count[0], nb = (n + kTN - 1) / kTN, parts = dh_parts(nb, (a.H + kTM - 1) / kTM, a.stages);
+  const int groups = (nv + kTM - 1) / kTM * 2;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const float2* p = a.part + (long)(v0 / 128) * a.Mp + i;
     const float old = a.ref[i];
@@ -587,7 +623,7 @@ __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int p
       const int g = e >> 4;
       const float f = ex2(p[(long)g * a.Mp].x - r);
       if (f == 1.f) continue;
-      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(g >> 1) * a.Mp + i) * kTile + (g & 1) * 128) + (e & 15);
+      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(g >> 1) * a.Mp + i) * kTM + (g & 1) * 128) + (e & 15);
       u32x4 v = *at;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
@@ -595,7 +631,7 @@ __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int p
     }
     if (piece > 0)
       for (int k = 0; k < parts; ++k) {
-        float* d = a.dacc + ((long)k * nb * kTile + i) * a.H;
+        float* d = a.dacc + ((long)k * nb * kTN + i) * a.H;
         for (int m = threadIdx.x; m < a.H; m += 256) d[m] *= ex2(old - r);
       }
     if (threadIdx.x == 0) a.ref[i] = r;
@@ -642,7 +678,7 @@ __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
 
 // dhidden rows: the parts' sum, rounded once; zeros without a loss
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
-  const int nb = (a.count[0] + kTile - 1) / kTile, parts = dh_parts(nb, (a.H + kTile - 1) / kTile, a.stages);
+  const int nb = (a.count[0] + kTN - 1) / kTN, parts = dh_parts(nb, (a.H + kTM - 1) / kTM, a.stages);
   const int i = a.pos[blockIdx.x];
   const float f = a.ref && i >= 0 ? a.fac[i] : 1.f, fl = i >= 0 ? a.lab[i] : 0.f;
   const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (i >= 0 ? (long)a.word[i] * a.H : 0));
@@ -651,7 +687,7 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
     if (i >= 0)
       for (int k = 0; k < parts; ++k) {
-        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * nb * kTile + i) * a.H) + 2 * p;
+        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * nb * kTN + i) * a.H) + 2 * p;
         x += from[0];
         y += from[1];
       }
@@ -679,14 +715,14 @@ struct LceLayout {
 LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   LceLayout L{};
   auto al = [](size_t x) { return (x + 255) / 256 * 256; };
-  const int nb = (rows + kTile - 1) / kTile;
-  L.Mp = nb * kTile;
-  L.ldh = (H + kBK - 1) / kBK * kBK;
-  const int words = (int)((V + (long)kTile - 1) / kTile);  // tiles of the vocabulary
+  const int nb = (rows + kTN - 1) / kTN;
+  L.Mp = nb * kTN;
+  L.ldh = (H + 63) / 64 * 64;
+  const int words = (int)((V + (long)kTM - 1) / kTM);  // tiles of the vocabulary
   // pieces of equal numbers of tiles
-  const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kTile * 2)));
+  const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kTM * 2)));
   const int pieces = (words + most - 1) / most;
-  L.Vp = (words + pieces - 1) / pieces * kTile;
+  L.Vp = (words + pieces - 1) / pieces * kTM;
   size_t o = 0;
   auto take = [&](size_t& at, size_t bytes) {
     at = o;
@@ -706,9 +742,9 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.lab, (size_t)L.Mp * 4);
   take(L.flag, (size_t)words * 4);
   // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
-  const size_t tile = (size_t)kTile * kTile;
-  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kTile * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kTile * 2)));
-  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)16 * L.Mp * H, 512 * tile)) * 4);
+  const size_t tile = (size_t)kTM * kTN;
+  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kTM * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kTM * 2)));
+  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)kMostParts * L.Mp * H, kMostUnits * tile)) * 4);
   L.total = o;
   return L;
 }
@@ -717,7 +753,7 @@ int lce_check(int rows, int V, int H, int B) {
   if (rows < 1 || V < 1 || H < 1 || B < 1 || rows % B) return DFLARE_ERR_INVALID_ARG;
   if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
   // a launch has less than 2^32 threads
-  if ((long)((rows + kTile - 1) / kTile) * ((V + (long)kTile - 1) / kTile) >= (1l << 23) - 8) return DFLARE_ERR_UNSUPPORTED;
+  if ((long)((rows + kTN - 1) / kTN) * ((V + (long)kTM - 1) / kTM) >= (1l << 23) - 8) return DFLARE_ERR_UNSUPPORTED;
   return DFLARE_OK;
 }
 
@@ -781,8 +817,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.ldh = L.ldh;
   a.Vp = L.Vp;
   a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
-  const int nb = L.Mp / kTile, na = (H + kTile - 1) / kTile, words = (int)((V + (long)kTile - 1) / kTile);
-  const int pieces = (words + L.Vp / kTile - 1) / (L.Vp / kTile);
+  const int nb = L.Mp / kTN, na = (H + kTM - 1) / kTM, words = (int)((V + (long)kTM - 1) / kTM);
+  const int pieces = (words + L.Vp / kTM - 1) / (L.Vp / kTM);
   const bool one_pass = dhidden && !dhead;
   if (one_pass) {
     a.ref = (float*)(w + L.ref);
@@ -797,20 +833,20 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
   if (!one_pass) {
     product(mode_c<kStats>{}, (long)words * nb, 0, V, 0);
-    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, words);
+    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, 2 * words);
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
       const int v0 = piece * L.Vp, nv = std::min(V - v0, L.Vp);
-      const long wt = (nv + kTile - 1) / kTile;
+      const long wt = (nv + kTM - 1) / kTM;
       if (one_pass) {
         product(mode_c<kExp>{}, wt * nb, v0, nv, piece);
         hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece);
       } else {
         product(mode_c<kDz>{}, wt * nb, v0, nv, piece);
       }
-      if (dhidden) product(mode_c<kDh>{}, std::max((long)na * nb, std::min(16l * na * nb, 512l)), v0, nv, piece);
-      if (dhead) product(mode_c<kDw>{}, wt * na, v0, nv, piece);
+      if (dhidden) product(mode_c<kDh>{}, std::max((long)na * nb, std::min((long)kMostParts * na * nb, (long)kMostUnits)), v0, nv, piece);
+      if (dhead) product(mode_c<kDw>{}, (nv + kTN - 1) / kTN * (long)na, v0, nv, piece);
     }
   if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(256), 0, st, a, 2 * words);
   hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
