@@ -231,20 +231,23 @@ struct Loader {
       }
     }
   }
-  // the wave's share of the next stage; left: k that exist from its first on (past them that first again)
-  template <bool WHOLE>
-  __device__ __forceinline__ void issue(uint32_t dst, const Operand& o, int w, int lane, int left) {
+  // the next stage has only `left` k: pieces past them take its first again (only before the last stage is loaded)
+  __device__ __forceinline__ void cut(const Operand& o, int w, int lane, int left) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      uint32_t x = off[j];
-      if constexpr (!WHOLE) {
-        const int row = ACROSS ? (N * w + j) * (512 / ROWS) + lane / (ROWS / 8) : (N * w + j) * 8 + (lane >> 3);
-        const int c = (lane & 7) ^ ((row >> 1) & 7);
-        if constexpr (ACROSS) x = row < left ? x : x - (uint32_t)(row * o.ld * 2);
-        else x = c * 8 < left ? x : x - c * 16;
+      if constexpr (!ACROSS) {
+        const int row = (N * w + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+        if (c * 8 >= left) off[j] -= c * 16;
+      } else {
+        const int row = (N * w + j) * (512 / ROWS) + lane / (ROWS / 8);
+        if (row >= left) off[j] -= (uint32_t)(row * o.ld * 2);
       }
-      load_lds(at, x, dst + j * 1024);
     }
+  }
+  // the wave's share of the next stage
+  __device__ __forceinline__ void issue(uint32_t dst) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) load_lds(at, off[j], dst + j * 1024);
     if constexpr (ACROSS) at += step;
     else at += (++st % SB == 0) ? step : kBK * 2;
   }
@@ -303,68 +306,77 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   const int nk = (K + kBK - 1) / kBK;
   using LA = Loader<XA, kTM>;
   using LB = Loader<XB, kTN>;
-  constexpr int NL = LA::N + LB::N;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)lds);
   const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + kABytes + w * LB::N * 1024;
-  int next = 0;  // stage to load
-  // the next stage into the buffer at `buf`; past the last stage nothing
-  auto issue = [&](uint32_t buf) {
-    const int left = min(oa.kend, ob.kend) - next * kBK;
+  int next = 0;  // stage to load; past the last stage nothing is
+  auto issue_a = [&](uint32_t buf) {
+    if (next >= nk) return;
+    if (oa.kend - next * kBK < kBK) la.cut(oa, w, lane, oa.kend - next * kBK);
+    la.issue(da + buf);
+  };
+  auto issue_b = [&](uint32_t buf) {
     if (next < nk) {
-      if (left >= kBK) {
-        la.template issue<true>(da + buf, oa, w, lane, 0);
-        lb.template issue<true>(db + buf, ob, w, lane, 0);
-      } else {
-        la.template issue<false>(da + buf, oa, w, lane, oa.kend - next * kBK);
-        lb.template issue<false>(db + buf, ob, w, lane, ob.kend - next * kBK);
-      }
+      if (ob.kend - next * kBK < kBK) lb.cut(ob, w, lane, ob.kend - next * kBK);
+      lb.issue(db + buf);
     }
     ++next;
   };
   struct Frags {
     u32x4 a[4], b[2];
   };
-  auto read = [&](Frags& f, uint32_t buf, int ks) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) f.b[j] = rb.get(lds + kABytes + buf, ks, j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f.a[i] = ra.get(lds + buf, ks, i);
+  auto read = [&](Frags& f, uint32_t buf, int ks, int n) {  // in the order in which the products take them
+    if (n == 0 || n == 5) f.b[n / 5] = rb.get(lds + kABytes + buf, ks, n / 5);
+    else f.a[n - 1] = ra.get(lds + buf, ks, n - 1);
   };
-  auto multiply = [&](const Frags& f) {
+  auto multiply = [&](const Frags& f, int n) { acc[n & 3][n >> 2] = mfma32(f.a[n & 3], f.b[n >> 2], acc[n & 3][n >> 2]); };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  // 8 products, beside them the reads for the next 8
+  auto step = [&](const Frags& f, Frags& g, uint32_t buf, int ks) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i][j] = mfma32(f.a[i], f.b[j], acc[i][j]);
+    for (int n = 0; n < 8; ++n) {
+      multiply(f, n);
+      if (n < 6) read(g, buf, ks, n);
+      fence();
+    }
   };
-  issue(0);
-  issue(kStageBytes);
+  issue_a(0);
+  issue_b(0);
+  issue_a(kStageBytes);
+  issue_b(kStageBytes);
   start(acc);
   wait_vm_barrier<0>();
   Frags f0, f1;
-  read(f0, 0, 0);
+#pragma unroll
+  for (int n = 0; n < 6; ++n) read(f0, 0, 0, n);
   uint32_t buf = 0;
+  bool late = false;  // the second operand's share of the stage after the next is still to be issued
   for (int kt = 0; kt < nk; ++kt) {
-    // each 16 k are read under the products of the 16 before; when all waves have read the stage's last, its
-    // buffer takes the stage after the next, and the next one is read
-    read(f1, buf, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(f0);
-    __builtin_amdgcn_sched_barrier(0);
-    read(f0, buf, 2);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(f1);
-    __builtin_amdgcn_sched_barrier(0);
-    read(f1, buf, 3);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(f0);
-    __builtin_amdgcn_sched_barrier(0);
-    wait_vm_barrier<0>();
-    read(f0, buf ^ kStageBytes, 0);
-    issue(buf);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(f1);
-    __builtin_amdgcn_sched_barrier(0);
-    buf ^= kStageBytes;
+    const uint32_t other = buf ^ kStageBytes;
+    fence();
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      multiply(f0, n);
+      if (n < 6) read(f1, buf, 1, n);
+      if (n == 1 && late) issue_b(other);
+      fence();
+    }
+    step(f1, f0, buf, 2);
+    step(f0, f1, buf, 3);
+    // in the midst of the stage's last products: the next stage is here, and all waves have read this one, whose
+    // buffer takes the one after the next
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      if (n == 4) wait_vm_barrier<0>();
+      multiply(f1, n);
+      if (n >= 4) {
+        read(f0, other, 0, n - 4);
+        if (n >= 6) read(f0, other, 0, n - 2);
+        if (n == 5) issue_a(buf);
+      }
+      fence();
+    }
+    late = true;
+    buf = other;
   }
   wait_vm_barrier<0>();
 }
