@@ -1,10 +1,12 @@
-"""Build libdflare.so (HIP, gfx950) in-tree: paper_2606_02091_amd/_lib/libdflare.so."""
+"""Build libdflare.so (HIP, gfx950) and the native part of the Python binding (_binding.so) in-tree, in
+paper_2606_02091_amd/_lib/."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -13,6 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libdflare.so")
+BINDING = os.path.join(LIBDIR, "_binding.so")
 SOURCES = ["kernels.hip", "batched.hip", "runtime.hip", "training.hip", "train_ops.hip",
            "linear_ce.hip"]
 ARCH = os.environ.get("DFLARE_OFFLOAD_ARCH", "gfx950")
@@ -36,15 +39,29 @@ def build(verbose: bool = False) -> str:
     cmds = [[hipcc(), *common, "-c", os.path.join(CSRC, src), "-o", obj]
             for src, obj in zip(SOURCES, objs)]
     # the translation units are independent: compile them side by side
+    binding = BINDING + f".tmp{os.getpid()}"
+    cmds.append(_binding_command(binding))
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         for f in [ex.submit(_run, cmd, verbose) for cmd in cmds]:
             f.result()
+    os.replace(binding, BINDING)
     tmp = LIB + f".tmp{os.getpid()}"
     _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     for o in objs:
         os.remove(o)
     return LIB
+
+
+def _binding_command(out: str) -> list[str]:
+    """The host compiler's command for the binding's native part (CPython and PyTorch C++ API, no GPU code)."""
+    import torch
+    from torch.utils import cpp_extension
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return ["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+            *(f"-I{p}" for p in cpp_extension.include_paths()), f"-I{sysconfig.get_paths()['include']}",
+            os.path.join(CSRC, "binding.cpp"), "-o", out, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def _run(cmd, verbose):

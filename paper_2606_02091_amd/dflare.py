@@ -10,12 +10,15 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 
 import numpy as np
 import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "libdflare.so")
+BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib", "_binding.so")
 
 OK, ERR_INVALID_ARG, ERR_OUT_OF_MEMORY, ERR_CONTEXT_FULL, ERR_HIP, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 DBG_FUSED, DBG_KCACHE, DBG_VCACHE, DBG_HIDDEN, DBG_LOGITS, DBG_ALPHA, DBG_TRACE, DBG_BLOGITS = range(8)
@@ -133,8 +136,8 @@ def lib() -> ctypes.CDLL:
         "dflare_linear_ce_workspace": ([i32] * 5, ctypes.c_size_t),
         "dflare_linear_ce": ([vp] * 3 + [i32] * 4 + [ctypes.c_float] + [vp] * 5 + [ctypes.c_size_t, vp], ctypes.c_int),
         "dflare_grad_norm_workspace": ([i32], ctypes.c_size_t),
-        "dflare_grad_norm": ([ctypes.POINTER(dflare_grad_tensor), i32, vp, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
-        "dflare_clip_grads": ([ctypes.POINTER(dflare_grad_tensor), i32, vp, ctypes.c_float, vp], ctypes.c_int),
+        "dflare_grad_norm": ([vp, i32, vp, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_clip_grads": ([vp, i32, vp, ctypes.c_float, vp], ctypes.c_int),
         "dflare_context_len_seq": ([vp, i32, ctypes.POINTER(i32)], ctypes.c_int),
         "dflare_debug_read_seq": ([vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
                                    i64], ctypes.c_int),
@@ -145,6 +148,22 @@ def lib() -> ctypes.CDLL:
         fn.restype = res
     _lib = L
     return L
+
+
+_binding = None
+
+
+def _native():
+    """Load the binding's native part once; raise if it is missing."""
+    global _binding
+    if _binding is None:
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is not built; run __graft_entry__.build() first")
+        loader = importlib.machinery.ExtensionFileLoader("_binding", BINDING_PATH)
+        mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_binding", loader))
+        loader.exec_module(mod)
+        _binding = mod
+    return _binding
 
 
 def _check(rc: int, h=None):
@@ -339,10 +358,13 @@ def _dtype(t: torch.Tensor) -> int:
     raise TypeError(f"expected a bf16 or fp32 tensor, got {t.dtype}")
 
 
-def _like(t, name: str, shape, ref, dtype=None) -> None:
-    """t (or None) is a contiguous tensor of this shape on ref's device, of dtype, or of ref's type."""
+def _like(t, name: str, shape, ref, dtype=None) -> int | None:
+    """Address of t (or None): a contiguous tensor of this shape on ref's device, of dtype, or of ref's type."""
     if t is None:
-        return
+        return None
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.get_device() == ref.get_device() and t.is_contiguous() \
+            and t.dtype is (ref.dtype if dtype is None else dtype):
+        return t.data_ptr()
     _ptr(t)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
@@ -350,19 +372,45 @@ def _like(t, name: str, shape, ref, dtype=None) -> None:
         raise ValueError(f"{name} is on {t.device}, expected {ref.device}")
     if t.dtype != dtype if dtype is not None else _dtype(t) != _dtype(ref):
         raise TypeError(f"{name} is {t.dtype}, expected {dtype or ref.dtype}")
+    return t.data_ptr()
+
+
+# the current stream's handle without a Stream object around it (4 us less a call)
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+class _Here:
+    """A call on the current stream of the current device: nothing to change around it."""
+    __slots__ = ("raw",)
+
+    def __init__(self, raw):
+        self.raw = raw
+
+    def __enter__(self):
+        return self.raw
+
+    def __exit__(self, *exc):
+        return None
 
 
 @contextlib.contextmanager
-def _place(t: torch.Tensor, stream):
-    """Inside, t's device is current and so is the stream of the call (the current one of that device by
-    default), so that what the binding allocates belongs to it.  Gives the raw stream."""
-    with torch.cuda.device(t.device):
+def _elsewhere(device: int, stream):
+    with torch.cuda.device(device):
         raw = _stream(stream)
         if raw == torch.cuda.current_stream().cuda_stream:
             yield raw
         else:
             with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(raw)):
                 yield raw
+
+
+def _place(device: int, stream):
+    """Inside, the tensors' device is current and so is the stream of the call (the current one of that device by
+    default), so that what the binding allocates belongs to it.  Gives the raw stream."""
+    if stream is None and torch.cuda.current_device() == device:
+        return _Here(_current_raw(device))
+    return _elsewhere(device, stream)
 
 
 def rope_frequencies(rotary_dim: int, base: float, method: int = ROPE_PLAIN, factor: float = 1.0,
@@ -391,33 +439,35 @@ def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = RO
             raise TypeError("expected a device tensor")
         if t.dim() != 3 or t.shape[0] != xs[0].shape[0] or t.shape[2] != xs[0].shape[2]:
             raise ValueError("expected [rows, n_heads, head_dim] tensors with the same rows and head_dim")
-    rows, _, hd = xs[0].shape
-    if int(B) < 1:
+    first = xs[0]
+    rows, _, hd = first.shape
+    B = int(B)
+    if B < 1:
         raise ValueError("B must be positive")
     _ptr(inv_freq)
-    _like(inv_freq, "inv_freq", (inv_freq.numel(),), xs[0], torch.float64)
-    _like(positions, "positions", (-(-rows // int(B)),), xs[0], torch.int32)
-    with _place(xs[0], stream) as raw:
+    freq = _like(inv_freq, "inv_freq", (inv_freq.numel(),), first, torch.float64)
+    pos = _like(positions, "positions", (-(-rows // B),), first, torch.int32)
+    dev, dtype = first.get_device(), _dtype(first)
+    with _place(dev, stream) as raw:
         if out is None:
-            outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs)
+            outs = tuple([torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs])
         else:
             outs = out if isinstance(out, (tuple, list)) else (out,)
-        if len(outs) != len(xs):
-            raise ValueError("out and x differ in number")
+            if len(outs) != len(xs):
+                raise ValueError("out and x differ in number")
         tab = (dflare_rope_tensor * len(xs))()
         for e, t, y in zip(tab, xs, outs):
             if not isinstance(y, torch.Tensor) or not y.is_cuda:
                 raise TypeError("expected a device tensor")
-            if y.shape != t.shape or y.dtype != t.dtype or _dtype(t) != _dtype(xs[0]) or \
-                    {t.device, y.device} != {xs[0].device}:
+            if y.shape != t.shape or y.dtype != t.dtype or _dtype(t) != dtype or t.get_device() != dev or y.get_device() != dev:
                 raise ValueError("x and out differ in shape, type or device")
-            if any(v.numel() and v.shape[2] > 1 and v.stride(2) != 1 for v in (t, y)):
+            (xr, xh, xe), (yr, yh, ye) = t.stride(), y.stride()
+            if (xe != 1 or ye != 1) and hd > 1 and t.numel():
                 raise ValueError("the last dimension must be contiguous")
             e.x, e.y, e.n_heads = t.data_ptr(), y.data_ptr(), t.shape[1]
-            e.x_row, e.x_head, e.y_row, e.y_head = t.stride(0), t.stride(1), y.stride(0), y.stride(1)
-        _train_check(lib().dflare_rope(tab, len(xs), _ptr(positions), _ptr(inv_freq), rows, int(B), hd,
-                                       2 * inv_freq.numel(), _dtype(xs[0]), int(layout), float(scale),
-                                       int(bool(inverse)), raw), "rope")
+            e.x_row, e.x_head, e.y_row, e.y_head = xr, xh, yr, yh
+        _train_check(lib().dflare_rope(tab, len(xs), pos, freq, rows, B, hd, 2 * inv_freq.numel(), dtype, int(layout),
+                                       float(scale), int(bool(inverse)), raw), "rope")
     return outs if isinstance(x, (tuple, list)) else outs[0]
 
 
@@ -427,18 +477,18 @@ def norm_fwd(x, gain=None, bias=None, residual=None, kind: int = NORM_RMS, eps: 
     _ptr(x)
     if x.dim() != 2:
         raise ValueError("expected a [rows, H] tensor")
-    rows, H = x.shape
-    _like(residual, "residual", x.shape, x)
-    _like(gain, "gain", (H,), x)
-    _like(bias, "bias", (H,), x)
-    with _place(x, stream) as raw:
+    shape = x.shape
+    rows, H = shape
+    xp, dtype, layer = x.data_ptr(), _dtype(x), kind == NORM_LAYER
+    rp, gp, bp = _like(residual, "residual", shape, x), _like(gain, "gain", (H,), x), _like(bias, "bias", (H,), x)
+    with _place(x.get_device(), stream) as raw:
         h = x if residual is None else torch.empty_like(x)
         y = torch.empty_like(x)
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device) if kind == NORM_LAYER else None
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device) if layer else None
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _train_check(lib().dflare_norm_fwd(_ptr(x), _ptr(residual), _ptr(gain), _ptr(bias), rows, H, _dtype(x), int(kind),
-                                           float(eps), None if residual is None else _ptr(h), _ptr(y), _ptr(mean),
-                                           _ptr(rstd), raw), "norm fwd")
+        _train_check(lib().dflare_norm_fwd(xp, rp, gp, bp, rows, H, dtype, int(kind), float(eps),
+                                           None if residual is None else h.data_ptr(), y.data_ptr(),
+                                           mean.data_ptr() if layer else None, rstd.data_ptr(), raw), "norm fwd")
     return y, h, mean, rstd
 
 
@@ -448,20 +498,19 @@ def norm_bwd(dy, h, gain, mean, rstd, dsum=None, kind: int = NORM_RMS, stream=No
     _ptr(h)
     if h.dim() != 2:
         raise ValueError("expected a [rows, H] tensor")
-    rows, H = h.shape
-    _like(dy, "dy", h.shape, h)
-    _like(dsum, "dsum", h.shape, h)
-    _like(gain, "gain", (H,), h)
-    _like(rstd, "rstd", (rows,), h, torch.float32)
-    _like(mean, "mean", (rows,), h, torch.float32)
-    with _place(h, stream) as raw:
+    shape = h.shape
+    rows, H = shape
+    layer, dtype = kind == NORM_LAYER, _dtype(h)
+    dyp, dsp, gp = _like(dy, "dy", shape, h), _like(dsum, "dsum", shape, h), _like(gain, "gain", (H,), h)
+    rp, mp = _like(rstd, "rstd", (rows,), h, torch.float32), _like(mean, "mean", (rows,), h, torch.float32)
+    with _place(h.get_device(), stream) as raw:
         dx = torch.empty_like(h)
         dgain = torch.empty(H, dtype=torch.float32, device=h.device)
-        dbias = torch.empty(H, dtype=torch.float32, device=h.device) if kind == NORM_LAYER else None
+        dbias = torch.empty(H, dtype=torch.float32, device=h.device) if layer else None
         ws_bytes = lib().dflare_norm_bwd_workspace(rows, H, int(kind))
         ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=h.device)
-        _train_check(lib().dflare_norm_bwd(_ptr(dy), _ptr(h), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dsum), rows, H,
-                                           _dtype(h), int(kind), _ptr(dx), _ptr(dgain), _ptr(dbias), _ptr(ws), ws_bytes,
+        _train_check(lib().dflare_norm_bwd(dyp, h.data_ptr(), gp, mp, rp, dsp, rows, H, dtype, int(kind), dx.data_ptr(),
+                                           dgain.data_ptr(), dbias.data_ptr() if layer else None, ws.data_ptr(), ws_bytes,
                                            raw), "norm bwd")
     return dx, dgain, dbias
 
@@ -477,35 +526,21 @@ def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = T
         raise ValueError("expected bf16 tensors hidden [rows, H] and head [V, H]")
     rows, H = hidden.shape
     V = head.shape[0]
-    _like(head, "head", (V, H), hidden)
-    _like(labels, "labels", (rows,), hidden, torch.int32)
+    wp, yp = _like(head, "head", (V, H), hidden), _like(labels, "labels", (rows,), hidden, torch.int32)
+    _ptr(labels)
     ws_bytes = lib().dflare_linear_ce_workspace(rows, V, H, int(need_dhidden), int(need_dhead))
     if ws_bytes == 0:
         raise DFlareError(ERR_UNSUPPORTED if rows and V and H else ERR_INVALID_ARG, "linear ce: shape")
-    with _place(hidden, stream) as raw:
+    with _place(hidden.get_device(), stream) as raw:
         loss = torch.empty(1, dtype=torch.float32, device=hidden.device)
         ce = torch.empty(rows, dtype=torch.float32, device=hidden.device)
         dhidden = torch.empty_like(hidden) if need_dhidden else None
         dhead = torch.empty_like(head) if need_dhead else None
         ws = torch.empty(ws_bytes, dtype=torch.uint8, device=hidden.device)
-        _train_check(lib().dflare_linear_ce(_ptr(hidden), _ptr(head), _ptr(labels), rows, V, H, int(B), float(gamma),
-                                            _ptr(loss), _ptr(ce), _ptr(dhidden), _ptr(dhead), _ptr(ws), ws_bytes, raw),
+        _train_check(lib().dflare_linear_ce(hidden.data_ptr(), wp, yp, rows, V, H, int(B), float(gamma), loss.data_ptr(),
+                                            ce.data_ptr(), _ptr(dhidden), _ptr(dhead), ws.data_ptr(), ws_bytes, raw),
                      "linear ce")
     return loss, ce, dhidden, dhead
-
-
-def _grad_table(grads, out=None):
-    tab = (dflare_grad_tensor * len(grads))()
-    if out is not None and len(out) != len(grads):
-        raise ValueError("out and grads differ in number")
-    for i, (e, t) in enumerate(zip(tab, grads)):
-        e.data, e.n, e.dtype = _ptr(t), t.numel(), _dtype(t)
-        if t.device != grads[0].device:
-            raise ValueError("the gradients are on different devices")
-        if out is not None:
-            _like(out[i], "out", t.shape, t)
-            e.out = _ptr(out[i])
-    return tab
 
 
 def grad_norm(grads, stream=None):
@@ -513,14 +548,15 @@ def grad_norm(grads, stream=None):
     grads = list(grads)
     if not grads:
         raise ValueError("expected at least one gradient")
-    tab = _grad_table(grads)
-    dev = grads[0].device
-    with _place(grads[0], stream) as raw:
-        sumsq = torch.empty(1, dtype=torch.float64, device=dev)
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    tab, dev = _native().grad_table(grads, None)
+    with _place(dev, stream) as raw:
+        device = grads[0].device
+        sumsq = torch.empty(1, dtype=torch.float64, device=device)
+        norm = torch.empty(1, dtype=torch.float32, device=device)
         ws_bytes = lib().dflare_grad_norm_workspace(len(grads))
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-        _train_check(lib().dflare_grad_norm(tab, len(grads), _ptr(sumsq), _ptr(norm), _ptr(ws), ws_bytes, raw), "grad norm")
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+        _train_check(lib().dflare_grad_norm(tab, len(grads), sumsq.data_ptr(), norm.data_ptr(), ws.data_ptr(), ws_bytes,
+                                            raw), "grad norm")
     return norm, sumsq
 
 
@@ -530,10 +566,11 @@ def clip_grads(grads, sumsq: torch.Tensor, max_norm: float, out=None, stream=Non
     grads = list(grads)
     if not grads:
         return
-    tab = _grad_table(grads, None if out is None else list(out))
-    _like(sumsq, "sumsq", (1,), grads[0], torch.float64)
-    with _place(grads[0], stream) as raw:
-        _train_check(lib().dflare_clip_grads(tab, len(grads), _ptr(sumsq), float(max_norm), raw), "clip grads")
+    tab, dev = _native().grad_table(grads, None if out is None else list(out))
+    _ptr(sumsq)
+    sp = _like(sumsq, "sumsq", (1,), grads[0], torch.float64)
+    with _place(dev, stream) as raw:
+        _train_check(lib().dflare_clip_grads(tab, len(grads), sp, float(max_norm), raw), "clip grads")
 
 
 def dflare_set_sampling(h: int, temperature: float, seed: int = 0) -> None:

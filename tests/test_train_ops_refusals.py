@@ -5,6 +5,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2606_02091_amd import dflare as dfl
 
@@ -31,9 +32,16 @@ def test_linear_ce_refuses(kw, code):
 def test_linear_ce_workspace():
     ws = dfl.lib().dflare_linear_ce_workspace
     assert ws(0, 10, 8, 0, 0) == 0 and ws(8, 10, 12, 0, 0) == 0 and ws(8, 0, 8, 0, 0) == 0
-    # without logits: far below rows x V floats, and more where more is asked for
+    # without logits: below a quarter of rows x V floats, and more where more is asked for
     a, b, c = ws(8192, 151936, 4096, 0, 0), ws(8192, 151936, 4096, 1, 0), ws(8192, 151936, 4096, 1, 1)
-    assert 0 < a < b <= c < 8192 * 151936 * 4 // 8
+    assert 0 < a < b <= c < 8192 * 151936 * 4 // 4
+    # one workspace for the largest call serves the smaller ones
+    last = (0, 0, 0)
+    for rows, V, H in ((32, 500, 64), (300, 500, 64), (300, 40000, 64), (300, 40000, 1000), (2000, 40000, 1000),
+                       (2000, 200000, 1000), (2000, 200000, 4096), (9000, 200000, 4096)):
+        now = tuple(ws(rows, V, H, *k) for k in ((0, 0), (1, 0), (1, 1)))
+        assert all(x <= y for x, y in zip(last, now))
+        last = now
     need = ws(32, 100, 64, 1, 1)
     assert lce(ws=need - 1) == INV
 
@@ -111,6 +119,24 @@ def test_grad_norm_refuses(items, kw, code):
     ([(P, 2 * P, 64, 0), (3 * P, 2 * P, 4, 0)], {}, INV), ([(P, P + 4, 64, 0)], {}, INV), ([(P, 2 * P + 2, 64, 0)], {}, INV)])
 def test_clip_refuses(items, kw, code):
     assert clip(items, **kw) == code
+
+
+def test_binding_refuses_lists_that_are_no_gradients():
+    t = torch.zeros(4)
+    with pytest.raises(TypeError):
+        dfl.grad_norm([t])  # not on a device
+    with pytest.raises(TypeError):
+        dfl.grad_norm([t.double()])
+    with pytest.raises(TypeError):
+        dfl.grad_norm([None])
+    with pytest.raises(ValueError):
+        dfl.grad_norm([])
+    with pytest.raises(ValueError):
+        dfl.clip_grads([t], t, 1.0, out=[])
+    for call in (lambda: dfl.rope(t, t), lambda: dfl.norm_fwd(t), lambda: dfl.norm_bwd(t, t, None, None, t),
+                 lambda: dfl.linear_ce(t, t, t, 1, 1.0)):
+        with pytest.raises(TypeError):
+            call()
 
 
 def freqs(d, base, method=0, factor=1.0, length=0.0):
