@@ -619,7 +619,7 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
  *   workspace  at least dflare_linear_ce_workspace(rows, V, H, dhidden wanted, dhead wanted) bytes; it grows
  *            with rows, V and H, not with rows x V
  * hidden, head, dhidden, dhead and workspace 16-byte aligned.  rows not a multiple of B, gamma <= 0 or not finite:
- * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows or about 2^39 logits: UNSUPPORTED (the
+ * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows, 2^35 values of hidden or about 2^38 logits: UNSUPPORTED (the
  * workspace is then 0 bytes).  Products run on the bf16 matrix cores with fp32 sums; the logits' gradient is
  * rounded to bf16 as their operand, each gradient once more where it is written.  NaN or infinities in a row
  * that takes part, or in head, make results NaN.

@@ -3,11 +3,11 @@
 //   ce_r = lse(z_r) - z_r[y_r],  loss = sum c ce,  dz = c (softmax(z) - onehot(y)),
 //   dh = dz W,  dW = dz^T h.
 // The rows with a loss are gathered first (the others take no part in any product).
-// The loss alone is one product, whose epilogue leaves every row's maximum and sum per 128 words.
+// The loss alone is one product, whose epilogue leaves every row's maximum and sum per wave's words.
 // With dh alone the vocabulary is walked once, in pieces, as one pass of a softmax: a piece's product leaves
 // 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
 // product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
-// fp32, so that R need not be the maximum: only logits more than 2^80 above it (which a piece's 128 words
+// fp32, so that R need not be the maximum: only logits more than 2^80 above it (which a wave's words
 // then take as their own reference, raise a flag and have the row rescaled) move it.
 // With dW, which needs dz of all words of a row at its final scale, the maxima and sums come first, and each
 // piece's logits are formed again: 2 rows V H operations more.
@@ -29,12 +29,17 @@ namespace dflare {
 
 namespace {
 
-constexpr int kT = 512;     // threads of a product's work-group: 8 waves, 2 (m) x 4 (n)
-constexpr int kWaves = kT / 64;
-constexpr int kTM = 256;    // output tile: 256 m x 256 n, a wave 128 x 64
-constexpr int kTN = 256;
 constexpr int kBK = 64;     // k of a stage
-constexpr int kABytes = kTM * kBK * 2, kBBytes = kTN * kBK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kBlock = 256; // words of a block of dz; rows and words are padded to it
+// A product's output tile TM x TN and its WM x WN waves, each with MT x NT products of 32 x 32
+template <int TM_, int TN_, int WM_, int WN_>
+struct Shape {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, W = WM * WN, T = 64 * W;
+  static constexpr int MT = TM / WM / 32, NT = TN / WN / 32;
+  static constexpr int kABytes = TM * kBK * 2, kBBytes = TN * kBK * 2, kStageBytes = kABytes + kBBytes;
+};
+using Large = Shape<256, 256, 2, 4>;  // one work-group per CU
+using Small = Shape<128, 128, 2, 2>;  // two
 constexpr float kL2E = 1.4426950408889634f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -65,7 +70,7 @@ struct Lce {
   int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
-  float2* part;   // [words / 128][Mp] (max log2 e, sum of exp(z - max)); one pass: (R, sum of 2^(z log2 e - R))
+  float2* part;   // [words / a wave's][Mp] (max log2 e, sum of exp(z - max)); one pass: (R, sum of 2^(z log2 e - R))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
   float* lab;     // [Mp] c (1 - p of the label)
@@ -73,21 +78,22 @@ struct Lce {
   float *ref, *fac;
   int* flag;
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
-  float* dacc;    // [parts][tiles of rows x 256][H] dh of the pieces so far
+  float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far
   int Mp, ldh, Vp;
   int stages;     // stages of k of the first (longest) piece
+  int dh_small;   // dh on the small tile
 };
 
-// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for 256 CUs: the
-// number with the least time, a round of work-groups costing its stages of k and about 30
-// more for its start and its sums in memory (measured: 0.9 us a stage, 27 us).  More than one part makes at
-// most 512 work-groups.  The number depends on the rows with a loss, so that it is chosen on the device.
-constexpr int kMostUnits = 512, kMostParts = 16;
-__host__ __device__ inline int dh_parts(int nb, int na, int stages) {
+// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for the `slots` work-groups
+// that 256 CUs hold: the number with the least time, a round of work-groups costing its stages of k and about
+// 12 more for its start and its sums in memory (measured on the large tile: 1.45 us a stage, 17 us).  More than one part
+// makes at most two rounds.  The number depends on the rows with a loss, so that it is chosen on the device.
+constexpr int kMostParts = 32;
+__host__ __device__ inline int dh_parts(int nb, int na, int stages, int slots) {
   int best = 1, cost = 0x7fffffff;
   for (int k = 1; k <= kMostParts; ++k) {
-    if (k > 1 && (nb * na * k > kMostUnits || stages < 8 * k)) break;
-    const int c = (nb * na * k + 255) / 256 * ((stages + k - 1) / k + 30);
+    if (k > 1 && (nb * na * k > 2 * slots || stages < 4 * k)) break;
+    const int c = (nb * na * k + slots - 1) / slots * ((stages + k - 1) / k + 12);
     if (c < cost) {
       best = k;
       cost = c;
@@ -95,6 +101,17 @@ __host__ __device__ inline int dh_parts(int nb, int na, int stages) {
   }
   return best;
 }
+// dh's tiles and parts for n rows with a loss
+struct DhPlan {
+  int tn, nb, na, parts;
+  __device__ __forceinline__ DhPlan(const Lce& a, int n) {
+    tn = a.dh_small ? Small::TN : Large::TN;
+    nb = (n + tn - 1) / tn;
+    na = a.dh_small ? (a.H + Small::TM - 1) / Small::TM : (a.H + Large::TM - 1) / Large::TM;
+    parts = dh_parts(nb, na, a.stages, a.dh_small ? 512 : 256);
+  }
+  __device__ __forceinline__ long part_rows() const { return (long)nb * tn; }
+};
 
 // ---- rows with a loss, in order; their weights; work-group of 1,024 threads ----
 __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
@@ -134,7 +151,7 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
   sum = 0.0;
   for (int k = 0; k < 16; ++k) sum += ws[k];
   const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
-  const int np = min((n + kTN - 1) / kTN * kTN, a.Mp);
+  const int np = min((n + kBlock - 1) / kBlock * kBlock, a.Mp);
   for (int i = tid; i < np; i += 1024) {
     a.c[i] = i < n ? (float)(a.c[i] * inv) : 0.f;
     if (i >= n) a.word[i] = -1;
@@ -148,7 +165,7 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
 __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   __shared__ float red[4];
   const int n = a.count[0], i = blockIdx.x;
-  if (i >= (n + kTN - 1) / kTN * kTN) return;
+  if (i >= (n + kBlock - 1) / kBlock * kBlock) return;
   const u32x4 z = {0u, 0u, 0u, 0u};
   const int row = i < n ? a.src[i] : 0;
   const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)row * a.H);
@@ -180,12 +197,12 @@ __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   }
 }
 
-// ---- products.  D[n][m] = sum over k of A[m, k] B[n, k] for a tile of 256 m x 256 n.  An operand lies in memory
+// ---- products.  D[n][m] = sum over k of A[m, k] B[n, k] for a tile of m x n.  An operand lies in memory
 // either with k along its rows (plain) or with k down its columns (across); both go to LDS as they lie, 16-byte
 // pieces permuted by an xor so that the reads are free of bank conflicts, and the `across` ones are transposed
 // by the LDS read (ds_read_b64_tr_b16):
-//   plain   256 rows x 64 k, 128 bytes a row: piece c of row r at c ^ (r / 2 mod 8)
-//   across  64 k x 256 columns, 512 bytes a row: piece c of row k at c ^ 4 (k mod 4)
+//   plain   rows of 64 k, 128 bytes: piece c of row r at c ^ (r / 2 mod 8)
+//   across  64 rows of as many columns as the tile: piece c of row k at c ^ 4 (k mod 4)
 // m runs along A so that a lane holds, of one n (a token's row), 4 consecutive m at a time: sums over the words
 // of a row stay within a lane. ----
 struct Operand {
@@ -206,10 +223,10 @@ __device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
 }
 
-// ROWS: rows (plain) or columns (across) of the operand's tile
-template <bool ACROSS, int ROWS>
+// ROWS: rows (plain) or columns (across) of the operand's tile; W waves load it
+template <bool ACROSS, int ROWS, int W>
 struct Loader {
-  static constexpr int N = ROWS * kBK * 2 / 1024 / kWaves;  // loads of a wave and stage
+  static constexpr int N = ROWS * kBK * 2 / 1024 / W;  // loads of a wave and stage
   static constexpr int SB = 256 / kBK;                 // stages of a block of 256 k
   const char* at;   // of the next stage
   uint32_t off[N];  // byte offset of a lane's pieces
@@ -282,32 +299,34 @@ struct Reader {
   }
 };
 
-typedef f32x16 Acc[4][2];
+template <typename S>
+using Acc = f32x16[S::MT][S::NT];
 
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
 // something finite.  start(acc) runs while the first stages are on their way.
-template <bool XA, bool XB, typename F>
-__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc& acc, F&& start) {
+template <typename S, bool XA, bool XB, typename F>
+__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc<S>& acc, F&& start) {
+  using LA = Loader<XA, S::TM, S::W>;
+  using LB = Loader<XB, S::TN, S::W>;
+  constexpr int MT = S::MT, NT = S::NT, Q = MT * NT, R = MT + NT, SB = S::kStageBytes;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Loader<XA, kTM> la;
-  Loader<XB, kTN> lb;
+  LA la;
+  LB lb;
   la.init(oa, w, lane);
   lb.init(ob, w, lane);
-  Reader<XA, kTM> ra;
-  Reader<XB, kTN> rb;
-  ra.init((w & 1) * 4, lane);
-  rb.init((w >> 1) * 2, lane);
+  Reader<XA, S::TM> ra;
+  Reader<XB, S::TN> rb;
+  ra.init(w % S::WM * MT, lane);
+  rb.init(w / S::WM * NT, lane);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   const int nk = (K + kBK - 1) / kBK;
-  using LA = Loader<XA, kTM>;
-  using LB = Loader<XB, kTN>;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)lds);
-  const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + kABytes + w * LB::N * 1024;
+  const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + S::kABytes + w * LB::N * 1024;
   int next = 0;  // stage to load; past the last stage nothing is
   auto issue_a = [&](uint32_t buf) {
     if (next >= nk) return;
@@ -322,42 +341,44 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     ++next;
   };
   struct Frags {
-    u32x4 a[4], b[2];
+    u32x4 a[MT], b[NT];
   };
   auto read = [&](Frags& f, uint32_t buf, int ks, int n) {  // in the order in which the products take them
-    if (n == 0 || n == 5) f.b[n / 5] = rb.get(lds + kABytes + buf, ks, n / 5);
+    if (n == 0 || n > MT) f.b[n == 0 ? 0 : n - MT] = rb.get(lds + S::kABytes + buf, ks, n == 0 ? 0 : n - MT);
     else f.a[n - 1] = ra.get(lds + buf, ks, n - 1);
   };
-  auto multiply = [&](const Frags& f, int n) { acc[n & 3][n >> 2] = mfma32(f.a[n & 3], f.b[n >> 2], acc[n & 3][n >> 2]); };
+  auto multiply = [&](const Frags& f, int n) { acc[n % MT][n / MT] = mfma32(f.a[n % MT], f.b[n / MT], acc[n % MT][n / MT]); };
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  // 8 products, beside them the reads for the next 8
+  // Q products, beside them the R reads for the next Q
   auto step = [&](const Frags& f, Frags& g, uint32_t buf, int ks) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
+    for (int n = 0; n < Q; ++n) {
       multiply(f, n);
-      if (n < 6) read(g, buf, ks, n);
+#pragma unroll
+      for (int r = n * R / Q; r < (n + 1) * R / Q; ++r) read(g, buf, ks, r);
       fence();
     }
   };
   issue_a(0);
   issue_b(0);
-  issue_a(kStageBytes);
-  issue_b(kStageBytes);
+  issue_a(SB);
+  issue_b(SB);
   start(acc);
   wait_vm_barrier<0>();
   Frags f0, f1;
 #pragma unroll
-  for (int n = 0; n < 6; ++n) read(f0, 0, 0, n);
+  for (int n = 0; n < R; ++n) read(f0, 0, 0, n);
   uint32_t buf = 0;
   bool late = false;  // the second operand's share of the stage after the next is still to be issued
   for (int kt = 0; kt < nk; ++kt) {
-    const uint32_t other = buf ^ kStageBytes;
+    const uint32_t other = SB - buf;
     fence();
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
+    for (int n = 0; n < Q; ++n) {
       multiply(f0, n);
-      if (n < 6) read(f1, buf, 1, n);
-      if (n == 1 && late) issue_b(other);
+#pragma unroll
+      for (int r = n * R / Q; r < (n + 1) * R / Q; ++r) read(f1, buf, 1, r);
+      if (n == Q / 4 - 1 && late) issue_b(other);
       fence();
     }
     step(f1, f0, buf, 2);
@@ -365,13 +386,13 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     // in the midst of the stage's last products: the next stage is here, and all waves have read this one, whose
     // buffer takes the one after the next
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      if (n == 4) wait_vm_barrier<0>();
+    for (int n = 0; n < Q; ++n) {
+      if (n == Q / 2) wait_vm_barrier<0>();
       multiply(f1, n);
-      if (n >= 4) {
-        read(f0, other, 0, n - 4);
-        if (n >= 6) read(f0, other, 0, n - 2);
-        if (n == 5) issue_a(buf);
+      if (n >= Q / 2) {
+#pragma unroll
+        for (int r = (n - Q / 2) * R / (Q - Q / 2); r < (n + 1 - Q / 2) * R / (Q - Q / 2); ++r) read(f0, other, 0, r);
+        if (n == Q / 2 + (Q > 4)) issue_a(buf);
       }
       fence();
     }
@@ -394,13 +415,29 @@ __device__ __forceinline__ bool tile_of(int id, int TA, int TB, int& ta, int& tb
   return true;
 }
 
-// bf16 tile (256 n x 256 m) from LDS to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
+// The tile as bf16 in LDS, TM m (in 16-byte pieces) by TN n: piece p of row n at p ^ (n mod the pieces)
+template <typename S>
+__device__ __forceinline__ void put_tile(char* lds, const Acc<S>& acc, int j, int n, int m_tile0, int h) {
+  constexpr int P = S::TM / 8;
+#pragma unroll
+  for (int t = 0; t < S::MT; ++t)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x16& z = acc[t][j];
+      const int p = m_tile0 * 4 + t * 4 + q;
+      const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
+      *reinterpret_cast<uint2*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1) & 31)) << 4) + h * 8) = v;
+    }
+}
+// and from there to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
+template <typename S>
 __device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long ld, int nv, int mv) {
+  constexpr int P = S::TM / 8, RW = S::TN / S::W;  // pieces of a row, rows of a wave
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll 4
-  for (int it = 0; it < 16; ++it) {
-    const int n = w * 32 + it * 2 + (lane >> 5), p = lane & 31;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + n * 512 + ((p ^ (n & 31)) << 4));
+  for (int it = 0; it < RW * P / 64; ++it) {
+    const int n = w * RW + it * (64 / P) + lane / P, p = lane % P;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1) & 31)) << 4));
     if (n < nv && p * 8 < mv) *reinterpret_cast<u32x4*>(to + n * ld + p * 8) = v;
   }
 }
@@ -409,35 +446,36 @@ enum { kStats, kDz, kExp, kDh, kDw };
 constexpr float kRise = 80.f;  // how far above its reference (log2) a row's values may lie: 2^80 times 2^24 words fit fp32
 
 // One tile of a product and its epilogue:
-//   kStats  z tile (256 words x 256 rows) -> part, zlab
+//   kStats  z tile (words x rows) -> part, zlab
 //   kDz     z tile of the piece from word v0 on -> dz
 //   kExp    the same -> 2^(z log2 e - R) in the place of dz, part
 //   kDh     dacc (+)= dz W over the piece's words, in parts
 //   kDw     dhead rows of the piece = dz^T h
-template <int MODE>
-__global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, int piece) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
-  const int n = a.count[0], nb = (n + kTN - 1) / kTN;  // rows with a loss, tiles of them
+template <typename S, int MODE>
+__global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, int piece) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+  constexpr int TM = S::TM, TN = S::TN, MT = S::MT, NT = S::NT, WM = MT * 32, WN = NT * 32;  // (a wave's m and n)
+  const int n = a.count[0], nb = (n + TN - 1) / TN;  // rows with a loss, tiles of them
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, wm = w & 1, wn = w >> 1;
-  Acc acc;
+  const int h = lane >> 5, wm = w % S::WM, wn = w / S::WM;
+  Acc<S> acc;
   int ta, tb;
   if constexpr (MODE <= kExp) {
-    if (!tile_of(blockIdx.x, (nv + kTM - 1) / kTM, nb, ta, tb)) return;
-    const int vt = v0 + ta * kTM, r0 = tb * kTN;
-    product<false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, kTM), a.H},
-                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, kTN, INT_MAX}, a.H, lds, acc, [](Acc&) {});
-    const int vw = vt + wm * 128;  // the wave's first word
+    if (!tile_of(blockIdx.x, (nv + TM - 1) / TM, nb, ta, tb)) return;
+    const int vt = v0 + ta * TM, r0 = tb * TN;
+    product<S, false, false>(Operand{a.head + (long)vt * a.H, a.H, min(a.V - vt, TM), a.H},
+                          Operand{a.hc + (long)r0 * a.ldh, a.ldh, TN, INT_MAX}, a.H, lds, acc, [](Acc<S>&) {});
+    const int vw = vt + wm * WM;  // the wave's first word
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int rl = wn * 64 + j * 32 + (lane & 31), i = r0 + rl;
+    for (int j = 0; j < NT; ++j) {
+      const int rl = wn * WN + j * 32 + (lane & 31), i = r0 + rl;
       // the label's place among the wave's words, if it is there
       const int rel = i < n ? a.word[i] - vw : -1;
-      const bool here = rel >= 0 && rel < 128 && ((rel >> 2) & 1) == h;
+      const bool here = rel >= 0 && rel < WM && ((rel >> 2) & 1) == h;
       const int le = here ? (rel >> 5) * 16 + ((rel & 31) >> 3) * 4 + (rel & 3) : -1;  // its (tile, element) of this lane
       auto each = [&](auto f) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float z = acc[t][j][e];
@@ -445,7 +483,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
             acc[t][j][e] = z;
           }
       };
-      if (vw + 128 > a.V)  // words past the last do not take part
+      if (vw + WM > a.V)  // words past the last do not take part
         each([&](int t, int e, float& z) {
           if (vw + t * 32 + 8 * (e >> 2) + 4 * h + (e & 3) >= a.V) z = -INFINITY;
         });
@@ -460,7 +498,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) * kL2E, -FLT_MAX);  // (finite where the wave has no words: they add 0)
         each([&](int, int, float& z) { s += ex2(fmaf(z, kL2E, -m)); });
         s += __shfl_xor(s, 32);
-        if (h == 0) a.part[(long)(vw / 128) * a.Mp + i] = make_float2(m, s);
+        if (h == 0) a.part[(long)(vw / WM) * a.Mp + i] = make_float2(m, s);
       } else {
         if constexpr (MODE == kDz) {
           const float c = a.c[i], l = a.lse2[i];
@@ -481,44 +519,36 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
             s += z;
           });
           s += __shfl_xor(s, 32);
-          if (h == 0) a.part[(long)(vw / 128) * a.Mp + i] = make_float2(r, s);
+          if (h == 0) a.part[(long)(vw / WM) * a.Mp + i] = make_float2(r, s);
         }
-        // columns m of row rl: piece (m / 8) at (m / 8) ^ (rl mod 32)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x16& z = acc[t][j];
-            const int p = wm * 16 + t * 4 + q;
-            const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
-            *reinterpret_cast<uint2*>(lds + rl * 512 + ((p ^ (rl & 31)) << 4) + h * 8) = v;
-          }
+        put_tile<S>(lds, acc, j, rl, wm * MT, h);
       }
     }
     if constexpr (MODE != kStats) {
       __syncthreads();
-      store_tile(lds, a.dz + ((long)ta * a.Mp + r0) * kTM, kTM, kTN, kTM);
+      store_tile<S>(lds, a.dz + ((long)(ta * TM / kBlock) * a.Mp + r0) * kBlock + ta * TM % kBlock, kBlock, TN, TM);
     }
   } else if constexpr (MODE == kDh) {
-    const int na = (a.H + kTM - 1) / kTM, stages = (nv + kBK - 1) / kBK, parts = dh_parts(nb, na, a.stages);
+    const DhPlan plan(a, n);
+    const int na = plan.na, parts = plan.parts, stages = (nv + kBK - 1) / kBK;
     int unit;
     if (!tile_of(blockIdx.x, na * parts, nb, unit, tb)) return;
     ta = unit % na;
-    const int ks = unit / na, m0 = ta * kTM, r0 = tb * kTN;
+    const int ks = unit / na, m0 = ta * TM, r0 = tb * TN;
     // this part's words: whole stages
     const int s0 = (int)((long)stages * ks / parts), s1 = (int)((long)stages * (ks + 1) / parts);
     const int words = min(s1 * kBK, nv) - s0 * kBK;
-    product<true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, kTM), words},
-                         Operand{a.dz + (long)r0 * kTM, kTM, kTN, INT_MAX, (long)a.Mp * 512, s0}, words, lds, acc, [](Acc&) {});
-    float* out = a.dacc + (long)ks * nb * kTN * a.H;
+    product<S, true, false>(Operand{a.head + (long)(v0 + s0 * kBK) * a.H + m0, a.H, min(a.H - m0, TM), words},
+                         Operand{a.dz + (long)r0 * kBlock, kBlock, TN, INT_MAX, (long)a.Mp * kBlock * 2, s0}, words, lds, acc, [](Acc<S>&) {});
+    float* out = a.dacc + ks * plan.part_rows() * a.H;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float* row = out + (long)(r0 + wn * 64 + j * 32 + (lane & 31)) * a.H;
+    for (int j = 0; j < NT; ++j) {
+      float* row = out + (long)(r0 + wn * WN + j * 32 + (lane & 31)) * a.H;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int m = m0 + wm * 128 + t * 32 + q * 8 + 4 * h;
+          const int m = m0 + wm * WM + t * 32 + q * 8 + 4 * h;
           if (m >= a.H) continue;
           f32x4* at = reinterpret_cast<f32x4*>(row + m);
           const f32x4 v = {acc[t][j][4 * q], acc[t][j][4 * q + 1], acc[t][j][4 * q + 2], acc[t][j][4 * q + 3]};
@@ -526,14 +556,14 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         }
     }
   } else {
-    if (!tile_of(blockIdx.x, (a.H + kTM - 1) / kTM, (nv + kTN - 1) / kTN, ta, tb)) return;
-    const int m0 = ta * kTM, n0 = tb * kTN;
-    product<true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, kTM), a.Mp},
-                        Operand{a.dz + (long)tb * a.Mp * kTM, kTM, kTN, a.Mp}, n, lds, acc, [&](Acc& d) {
-      // the label terms: the rows whose label is one of the wave's 64 words, in order
-      const int word0 = v0 + n0 + wn * 64;
-      const uint16_t* col = a.hc + m0 + wm * 128 + 4 * h;
-      const int most = a.ldh - 4 - (m0 + wm * 128 + 4 * h);  // (columns past the last are not kept)
+    if (!tile_of(blockIdx.x, (a.H + TM - 1) / TM, (nv + TN - 1) / TN, ta, tb)) return;
+    const int m0 = ta * TM, n0 = tb * TN;
+    product<S, true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, TM), a.Mp},
+                        Operand{a.dz + (long)(n0 / kBlock) * a.Mp * kBlock + n0 % kBlock, kBlock, TN, a.Mp}, n, lds, acc, [&](Acc<S>& d) {
+      // the label terms: the rows whose label is one of the wave's words, in order
+      const int word0 = v0 + n0 + wn * WN;
+      const uint16_t* col = a.hc + m0 + wm * WM + 4 * h;
+      const int most = a.ldh - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
       for (int i0 = 0; i0 < n; i0 += 256) {
         int y[4];
 #pragma unroll
@@ -543,14 +573,14 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < 64u);
+          uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < (unsigned)WN);
           while (hit) {
             const int b = __builtin_ctzll(hit), i = i0 + 64 * k + b, wl = __builtin_amdgcn_readlane(y[k], b);
             hit &= hit - 1;
             const float f = (lane & 31) == (wl & 31) ? -a.lab[i] : 0.f;
             const uint16_t* row = col + (long)i * a.ldh;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 const u32x2 v = *reinterpret_cast<const u32x2*>(row + min(t * 32 + q * 8, most));
@@ -558,6 +588,7 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
                                  __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                  static_assert(NT == 2, "a wave's words");
                   if (wl < 32) d[t][0][4 * q + e] = fmaf(f, x[e], d[t][0][4 * q + e]);
                   else d[t][1][4 * q + e] = fmaf(f, x[e], d[t][1][4 * q + e]);
                 }
@@ -567,20 +598,9 @@ __global__ __launch_bounds__(kT, 2) void k_lce_product(Lce a, int v0, int nv, in
       }
     });
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int nl = wn * 64 + j * 32 + (lane & 31);
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x16& z = acc[t][j];
-          const int p = wm * 16 + t * 4 + q;
-          const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
-          *reinterpret_cast<uint2*>(lds + nl * 512 + ((p ^ (nl & 31)) << 4) + h * 8) = v;
-        }
-    }
+    for (int j = 0; j < NT; ++j) put_tile<S>(lds, acc, j, wn * WN + j * 32 + (lane & 31), wm * MT, h);
     __syncthreads();
-    store_tile(lds, a.dhead + (long)(v0 + n0) * a.H + m0, a.H, min(nv - n0, kTN), min(a.H - m0, kTM));
+    store_tile<S>(lds, a.dhead + (long)(v0 + n0) * a.H + m0, a.H, min(nv - n0, TN), min(a.H - m0, TM));
   }
 }
 
@@ -615,13 +635,13 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
 
 // A piece in which some words took a reference of their own: the row's reference becomes the highest of them, and
 // what was written under others, dh of the pieces before it included, is scaled to it.
-__global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece) {
+__global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece, int wave) {
   __shared__ float red[4];
   if (a.flag[piece] == 0) return;
-  const int n = a.count[0], nb = (n + kTN - 1) / kTN, parts = dh_parts(nb, (a.H + kTM - 1) / kTM, a.stages);
-  const int groups = (nv + kTM - 1) / kTM * 2;
+  const int n = a.count[0], groups = (nv + wave - 1) / wave;  // groups of a wave's words
+  const DhPlan plan(a, n);
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const float2* p = a.part + (long)(v0 / 128) * a.Mp + i;
+    const float2* p = a.part + (long)(v0 / wave) * a.Mp + i;
     const float old = a.ref[i];
     float r = old;
     for (int g = threadIdx.x; g < groups; g += 256) r = fmaxf(r, p[(long)g * a.Mp].x);
@@ -631,19 +651,19 @@ __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int p
     __syncthreads();
     r = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     if (!(r > old)) continue;
-    for (int e = threadIdx.x; e < groups * 16; e += 256) {  // 8 words each
-      const int g = e >> 4;
+    for (int e = threadIdx.x; e < groups * (wave / 8); e += 256) {  // 8 words each
+      const int g = e / (wave / 8);
       const float f = ex2(p[(long)g * a.Mp].x - r);
       if (f == 1.f) continue;
-      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(g >> 1) * a.Mp + i) * kTM + (g & 1) * 128) + (e & 15);
+      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(e / (kBlock / 8)) * a.Mp + i) * kBlock) + e % (kBlock / 8);
       u32x4 v = *at;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
       *at = v;
     }
     if (piece > 0)
-      for (int k = 0; k < parts; ++k) {
-        float* d = a.dacc + ((long)k * nb * kTN + i) * a.H;
+      for (int k = 0; k < plan.parts; ++k) {
+        float* d = a.dacc + (k * plan.part_rows() + i) * a.H;
         for (int m = threadIdx.x; m < a.H; m += 256) d[m] *= ex2(old - r);
       }
     if (threadIdx.x == 0) a.ref[i] = r;
@@ -688,30 +708,31 @@ __global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
   }
 }
 
-// dhidden rows: the parts' sum, rounded once; zeros without a loss
+// dhidden: the parts' sum, scaled, with the label's term; rounded once; zeros in rows without a loss.  A thread takes
+// 8 values of a row.
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
-  const int nb = (a.count[0] + kTN - 1) / kTN, parts = dh_parts(nb, (a.H + kTM - 1) / kTM, a.stages);
-  const int i = a.pos[blockIdx.x];
-  const float f = a.ref && i >= 0 ? a.fac[i] : 1.f, fl = i >= 0 ? a.lab[i] : 0.f;
-  const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (i >= 0 ? (long)a.word[i] * a.H : 0));
-  u32x4* to = reinterpret_cast<u32x4*>(a.dhidden + (long)blockIdx.x * a.H);
-  for (int p = threadIdx.x; p < a.H / 8; p += 256) {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-    if (i >= 0)
-      for (int k = 0; k < parts; ++k) {
-        const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + ((long)k * nb * kTN + i) * a.H) + 2 * p;
-        x += from[0];
-        y += from[1];
-      }
-    x *= f;
-    y *= f;
-    if (i >= 0) {
-      const u32x4 v = word[p];
-      x -= fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
-      y -= fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
+  const int P = a.H / 8;
+  const long at = blockIdx.x * 256l + threadIdx.x;
+  if (at >= (long)a.rows * P) return;
+  const int row = (int)(at / P), p = (int)(at - (long)row * P), i = a.pos[row];
+  u32x4 out = {0u, 0u, 0u, 0u};
+  if (i >= 0) {
+    const DhPlan plan(a, a.count[0]);
+    const float f = a.ref ? a.fac[i] : 1.f, fl = a.lab[i];
+    const u32x4 v = reinterpret_cast<const u32x4*>(a.head + (long)a.word[i] * a.H)[p];
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + (long)i * a.H) + 2 * p;
+    const long step = plan.part_rows() * a.H / 4;
+    f32x4 x = from[0], y = from[1];
+#pragma unroll 4
+    for (int k = 1; k < plan.parts; ++k) {
+      x += from[k * step];
+      y += from[k * step + 1];
     }
-    to[p] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
+    x = x * f - fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
+    y = y * f - fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
+    out = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
   }
+  reinterpret_cast<u32x4*>(a.dhidden)[at] = out;
 }
 
 // ---- host side ----
@@ -727,14 +748,13 @@ struct LceLayout {
 LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   LceLayout L{};
   auto al = [](size_t x) { return (x + 255) / 256 * 256; };
-  const int nb = (rows + kTN - 1) / kTN;
-  L.Mp = nb * kTN;
+  L.Mp = (rows + kBlock - 1) / kBlock * kBlock;
   L.ldh = (H + 63) / 64 * 64;
-  const int words = (int)((V + (long)kTM - 1) / kTM);  // tiles of the vocabulary
+  const int words = (int)((V + (long)kBlock - 1) / kBlock);  // tiles of the vocabulary
   // pieces of equal numbers of tiles
-  const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kTM * 2)));
+  const int most = (int)std::max<size_t>(1, std::min<size_t>(words, kDzBytes / ((size_t)L.Mp * kBlock * 2)));
   const int pieces = (words + most - 1) / most;
-  L.Vp = (words + pieces - 1) / pieces * kTM;
+  L.Vp = (words + pieces - 1) / pieces * kBlock;
   size_t o = 0;
   auto take = [&](size_t& at, size_t bytes) {
     at = o;
@@ -746,7 +766,7 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.word, (size_t)L.Mp * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
-  take(L.part, (size_t)words * L.Mp * 16);
+  take(L.part, (size_t)words * L.Mp * 32);  // (64 words of a wave of the small tile)
   take(L.zlab, (size_t)L.Mp * 4);
   take(L.lse2, (size_t)L.Mp * 4);
   take(L.ref, (size_t)L.Mp * 4);
@@ -754,9 +774,8 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.lab, (size_t)L.Mp * 4);
   take(L.flag, (size_t)words * 4);
   // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
-  const size_t tile = (size_t)kTM * kTN;
-  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kTM * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kTM * 2)));
-  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)kMostParts * L.Mp * H, kMostUnits * tile)) * 4);
+  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kBlock * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kBlock * 2)));
+  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)kMostParts * L.Mp * H, (size_t)512 * 65536)) * 4);
   L.total = o;
   return L;
 }
@@ -765,7 +784,8 @@ int lce_check(int rows, int V, int H, int B) {
   if (rows < 1 || V < 1 || H < 1 || B < 1 || rows % B) return DFLARE_ERR_INVALID_ARG;
   if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
   // a launch has less than 2^32 threads
-  if ((long)((rows + kTN - 1) / kTN) * ((V + (long)kTM - 1) / kTM) >= (1l << 23) - 8) return DFLARE_ERR_UNSUPPORTED;
+  const long tiles = (long)((rows + kBlock - 1) / kBlock) * ((V + (long)kBlock - 1) / kBlock);
+  if (tiles >= (1l << 22) || (long)rows * H >= (1l << 35)) return DFLARE_ERR_UNSUPPORTED;
   return DFLARE_OK;
 }
 
@@ -829,40 +849,60 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.ldh = L.ldh;
   a.Vp = L.Vp;
   a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
-  const int nb = L.Mp / kTN, na = (H + kTM - 1) / kTM, words = (int)((V + (long)kTM - 1) / kTM);
-  const int pieces = (words + L.Vp / kTM - 1) / (L.Vp / kTM);
+  const int words = (int)((V + (long)kBlock - 1) / kBlock);
+  const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);
   const bool one_pass = dhidden && !dhead;
   if (one_pass) {
     a.ref = (float*)(w + L.ref);
     a.fac = (float*)(w + L.fac);
     a.flag = (int*)(w + L.flag);
   }
+  // The small tile wastes less where rows or tiles are few.  A round of its work-groups takes about 5/8 of a large
+  // one's time (151,936 words x 4,096, logits, large / small: 125 rows 399 / 330 us, 180 403 / 435, 300 614 / 564, 500
+  // 649 / 755; 32,003 x 2,880: 180 85 / 69, 300 85 / 101, 640 169 / 145, 900 185 / 218); for dh, whose words are
+  // split into parts that fill the rounds, the rows' tiles alone count (4,096: 125 rows 327 / 258 us, 180 345 / 414,
+  // 380 586 / 528, 640 901 / 817, 900 1,078 / 1,381).  dW is not faster on it (60 rows 363 / 373, 640 1,063 / 1,274).
+  const int most = std::max(1, rows / B * (B - 1));  // rows with a loss, at most
+  auto tiles = [](auto s, long m, long n) { return ((m + s.TM - 1) / s.TM) * ((n + s.TN - 1) / s.TN); };
+  const long rounds_s = (tiles(Small{}, V, most) + 511) / 512, rounds_l = (tiles(Large{}, V, most) + 255) / 256;
+  const bool z_small = 5 * rounds_s < 8 * rounds_l;
+  a.dh_small = 4 * tiles(Small{}, 1, most) < 7 * tiles(Large{}, 1, most);
+  const int wave = z_small ? Small::MT * 32 : Large::MT * 32;
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
-  auto product = [&](auto mode, long tiles, int v0, int nv, int piece) {
-    hipLaunchKernelGGL((k_lce_product<decltype(mode)::value>), dim3(grid(tiles)), dim3(kT), 0, st, a, v0, nv, piece);
+  auto product = [&](bool small, auto mode, int v0, int nv, int piece) {
+    constexpr int MODE = decltype(mode)::value;
+    auto go = [&](auto s) {
+      using S = decltype(s);
+      long t = MODE <= kExp ? tiles(s, nv, most) : MODE == kDw ? tiles(s, H, nv) : tiles(s, H, most);
+      if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, small ? 1024l : 512l));
+      hipLaunchKernelGGL((k_lce_product<S, MODE>), dim3(grid(t)), dim3(S::T), 0, st, a, v0, nv, piece);
+    };
+    if constexpr (MODE != kDw) {
+      if (small) return go(Small{});
+    }
+    go(Large{});
   };
   hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a, pieces);
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
   if (!one_pass) {
-    product(mode_c<kStats>{}, (long)words * nb, 0, V, 0);
-    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, 2 * words);
+    product(z_small, mode_c<kStats>{}, 0, V, 0);
+    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, (V + wave - 1) / wave);
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
       const int v0 = piece * L.Vp, nv = std::min(V - v0, L.Vp);
-      const long wt = (nv + kTM - 1) / kTM;
       if (one_pass) {
-        product(mode_c<kExp>{}, wt * nb, v0, nv, piece);
-        hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece);
+        product(z_small, mode_c<kExp>{}, v0, nv, piece);
+        hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece, wave);
       } else {
-        product(mode_c<kDz>{}, wt * nb, v0, nv, piece);
+        product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }
-      if (dhidden) product(mode_c<kDh>{}, std::max((long)na * nb, std::min((long)kMostParts * na * nb, (long)kMostUnits)), v0, nv, piece);
-      if (dhead) product(mode_c<kDw>{}, (nv + kTN - 1) / kTN * (long)na, v0, nv, piece);
+      if (dhidden) product(a.dh_small, mode_c<kDh>{}, v0, nv, piece);
+      if (dhead) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
-  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(256), 0, st, a, 2 * words);
+  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(256), 0, st, a, (V + wave - 1) / wave);
   hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
-  if (dhidden) hipLaunchKernelGGL(k_lce_dhidden, dim3(rows), dim3(256), 0, st, a);
+  if (dhidden) hipLaunchKernelGGL(k_lce_dhidden, dim3((unsigned)(((long)rows * (H / 8) + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR_HIP;
 }
 
