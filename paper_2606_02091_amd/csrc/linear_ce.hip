@@ -64,7 +64,7 @@ struct Lce {
   int rows, V, H, B;
   float gamma;
   // workspace; i counts the rows with a loss, Mp = rows rounded up to whole tiles
-  int* count;     // [1] rows with a loss
+  int* count;     // [2] rows with a loss, parts of dh
   int* src;       // [Mp] i -> row
   int* pos;       // [rows] row -> i, -1 without a loss
   int* word;      // [Mp] i -> label, -1 past the last
@@ -84,33 +84,33 @@ struct Lce {
   int dh_small;   // dh on the small tile
 };
 
-// The words of a piece are split into `parts` for dh where there are few tiles (nb x na) for the `slots` work-groups
-// that 256 CUs hold: the number with the least time, a round of work-groups costing its stages of k and about
-// 12 more for its start and its sums in memory (measured on the large tile: 1.45 us a stage, 17 us).  More than one part
-// makes at most two rounds.  The number depends on the rows with a loss, so that it is chosen on the device.
-constexpr int kMostParts = 32;
-__host__ __device__ inline int dh_parts(int nb, int na, int stages, int slots) {
-  int best = 1, cost = 0x7fffffff;
-  for (int k = 1; k <= kMostParts; ++k) {
-    if (k > 1 && (nb * na * k > 2 * slots || stages < 4 * k)) break;
-    const int c = (nb * na * k + slots - 1) / slots * ((stages + k - 1) / k + 12);
-    if (c < cost) {
-      best = k;
-      cost = c;
-    }
-  }
-  return best;
-}
-// dh's tiles and parts for n rows with a loss
+// dh's tiles for n rows with a loss.  The words of a piece are split into `parts` where there are few tiles for the
+// work-groups that 256 CUs hold: the number with the least time, a round of work-groups costing its stages of k
+// and about 8 more for its start and its sums in memory, the sum of the parts n H / 1.45 M each (in stages: 1.45 us
+// measured on the large tile).  More than one part makes at most two rounds.  The number depends on the rows
+// with a loss, so that it is chosen on the device (k_lce_rows).
+constexpr int kMostParts = 128;
 struct DhPlan {
   int tn, nb, na, parts;
   __device__ __forceinline__ DhPlan(const Lce& a, int n) {
     tn = a.dh_small ? Small::TN : Large::TN;
     nb = (n + tn - 1) / tn;
     na = a.dh_small ? (a.H + Small::TM - 1) / Small::TM : (a.H + Large::TM - 1) / Large::TM;
-    parts = dh_parts(nb, na, a.stages, a.dh_small ? 512 : 256);
+    parts = a.count[1];
   }
   __device__ __forceinline__ long part_rows() const { return (long)nb * tn; }
+  // by one wave
+  __device__ __forceinline__ int choose(const Lce& a, int n) const {
+    const int slots = a.dh_small ? 512 : 256;
+    unsigned best = ~0u;  // cost and parts
+    for (int k = 1 + (threadIdx.x & 63); k <= kMostParts; k += 64) {
+      if (k > 1 && (nb * (long)na * k > 2 * slots || a.stages < 4 * k)) continue;
+      const long cost = (nb * (long)na * k + slots - 1) / slots * ((a.stages + k - 1) / k + 8) + (long)n * a.H * k / 1450000;
+      best = min(best, (unsigned)min(cost, (1l << 24) - 2) << 8 | k);
+    }
+    for (int off = 32; off > 0; off >>= 1) best = min(best, (unsigned)__shfl_xor((int)best, off));
+    return best & 255;
+  }
 };
 
 // ---- rows with a loss, in order; their weights; work-group of 1,024 threads ----
@@ -158,7 +158,13 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
   }
   if (a.flag)
     for (int i = tid; i < pieces; i += 1024) a.flag[i] = 0;
-  if (tid == 0) a.count[0] = n;
+  if (wv == 0) {
+    const int parts = DhPlan(a, n).choose(a, n);
+    if (tid == 0) {
+      a.count[0] = n;
+      a.count[1] = parts;
+    }
+  }
 }
 
 // a row of hc; one pass: also the label's logit and the first reference
@@ -604,14 +610,14 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
   }
 }
 
-// log-sum-exp of every row from its parts (16 rows by 16 groups of parts), and its cross-entropy
-__global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
-  __shared__ float2 sh[16][17];
+// log-sum-exp of every row from its parts (16 rows by 64 groups of parts), and its cross-entropy
+__global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
+  __shared__ float2 sh[64][17];
   const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
   if ((int)blockIdx.x * 16 >= n) return;
   float m = -FLT_MAX, s = 0.f;
-#pragma unroll 4
-  for (int p = g; p < parts; p += 16) {
+#pragma unroll 8
+  for (int p = g; p < parts; p += 64) {
     const float2 v = a.part[(long)p * a.Mp + i];
     const float mn = fmaxf(m, v.x);
     s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
@@ -620,7 +626,7 @@ __global__ __launch_bounds__(256) void k_lce_lse(Lce a, int parts) {
   sh[g][l] = make_float2(m, s);
   __syncthreads();
   if (g != 0 || i >= n) return;
-  for (int k = 1; k < 16; ++k) {
+  for (int k = 1; k < 64; ++k) {
     const float2 v = sh[k][l];
     const float mn = fmaxf(m, v.x);
     s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
@@ -671,21 +677,21 @@ __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int p
 }
 
 // one pass: the rows' sums from their parts, their cross-entropy and the factors of dh
-__global__ __launch_bounds__(256) void k_lce_close(Lce a, int parts) {
-  __shared__ float sh[16][17];
+__global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts) {
+  __shared__ float sh[64][17];
   const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
   if ((int)blockIdx.x * 16 >= n) return;
   const float r = a.ref[i];
   float s = 0.f;
-#pragma unroll 4
-  for (int p = g; p < parts; p += 16) {
+#pragma unroll 8
+  for (int p = g; p < parts; p += 64) {
     const float2 v = a.part[(long)p * a.Mp + i];
     s += v.y * ex2(v.x - r);
   }
   sh[g][l] = s;
   __syncthreads();
   if (g != 0 || i >= n) return;
-  for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
+  for (int k = 1; k < 64; ++k) s += sh[k][l];  // all words but the label's
   const float y = a.zlab[i] * kL2E - r, ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey);
   a.fac[i] = c * inv;
   a.lab[i] = c * (s * inv);
@@ -693,26 +699,27 @@ __global__ __launch_bounds__(256) void k_lce_close(Lce a, int parts) {
   a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
 }
 
-// loss = sum of c ce in 64 bits, in a fixed order
-__global__ __launch_bounds__(1024) void k_lce_loss(Lce a) {
-  __shared__ double ws[16];
+// loss = sum of c ce in 64 bits, in a fixed order, by one work-group of 256
+__device__ __forceinline__ void sum_loss(const Lce& a) {
+  __shared__ double ws[4];
   const int n = a.count[0];
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += (double)a.c[i] * a.row_ce[a.src[i]];
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n; i += 256) s += (double)a.c[i] * a.row_ce[a.src[i]];
   for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
   if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int k = 1; k < 16; ++k) s += ws[k];
-    a.loss[0] = (float)s;
-  }
+  if (threadIdx.x == 0) a.loss[0] = (float)((ws[0] + ws[1]) + (ws[2] + ws[3]));
 }
+__global__ __launch_bounds__(256) void k_lce_loss(Lce a) { sum_loss(a); }
 
-// dhidden: the parts' sum, scaled, with the label's term; rounded once; zeros in rows without a loss.  A thread takes
-// 8 values of a row.
+// dhidden: the parts' sum, scaled, with the label's term; rounded once; zeros in rows without a loss.  G threads take
+// 8 values of a row, each every G-th part.  The first work-group forms the loss.
+template <int G>
 __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
-  const int P = a.H / 8;
-  const long at = blockIdx.x * 256l + threadIdx.x;
+  if (blockIdx.x == 0) return sum_loss(a);
+  const int P = a.H / 8, g = threadIdx.x % G;
+  const long at = (blockIdx.x - 1) * (256l / G) + threadIdx.x / G;
   if (at >= (long)a.rows * P) return;
   const int row = (int)(at / P), p = (int)(at - (long)row * P), i = a.pos[row];
   u32x4 out = {0u, 0u, 0u, 0u};
@@ -722,17 +729,24 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
     const u32x4 v = reinterpret_cast<const u32x4*>(a.head + (long)a.word[i] * a.H)[p];
     const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + (long)i * a.H) + 2 * p;
     const long step = plan.part_rows() * a.H / 4;
-    f32x4 x = from[0], y = from[1];
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll 4
-    for (int k = 1; k < plan.parts; ++k) {
+    for (int k = g; k < plan.parts; k += G) {
       x += from[k * step];
       y += from[k * step + 1];
     }
+#pragma unroll
+    for (int off = 1; off < G; off <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] += __shfl_xor(x[e], off);
+        y[e] += __shfl_xor(y[e], off);
+      }
     x = x * f - fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
     y = y * f - fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
     out = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
   }
-  reinterpret_cast<u32x4*>(a.dhidden)[at] = out;
+  if (g == 0) reinterpret_cast<u32x4*>(a.dhidden)[at] = out;
 }
 
 // ---- host side ----
@@ -760,7 +774,7 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
     at = o;
     o = al(o + bytes);
   };
-  take(L.count, 4);
+  take(L.count, 8);
   take(L.src, (size_t)L.Mp * 4);
   take(L.pos, (size_t)rows * 4);
   take(L.word, (size_t)L.Mp * 4);
@@ -866,7 +880,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   auto tiles = [](auto s, long m, long n) { return ((m + s.TM - 1) / s.TM) * ((n + s.TN - 1) / s.TN); };
   const long rounds_s = (tiles(Small{}, V, most) + 511) / 512, rounds_l = (tiles(Large{}, V, most) + 255) / 256;
   const bool z_small = 5 * rounds_s < 8 * rounds_l;
-  a.dh_small = 4 * tiles(Small{}, 1, most) < 7 * tiles(Large{}, 1, most);
+  a.dh_small = 4 * tiles(Small{}, 1, most) < 7 * tiles(Large{}, 1, most) ||
+               tiles(Large{}, H, most) * (a.stages / 4) < 256;  // (too few words for parts on all CUs)
   const int wave = z_small ? Small::MT * 32 : Large::MT * 32;
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
   auto product = [&](bool small, auto mode, int v0, int nv, int piece) {
@@ -874,7 +889,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     auto go = [&](auto s) {
       using S = decltype(s);
       long t = MODE <= kExp ? tiles(s, nv, most) : MODE == kDw ? tiles(s, H, nv) : tiles(s, H, most);
-      if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, small ? 1024l : 512l));
+      if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, small ? 1024l : 512l));  // (the most that the plan makes)
       hipLaunchKernelGGL((k_lce_product<S, MODE>), dim3(grid(t)), dim3(S::T), 0, st, a, v0, nv, piece);
     };
     if constexpr (MODE != kDw) {
@@ -886,7 +901,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
   if (!one_pass) {
     product(z_small, mode_c<kStats>{}, 0, V, 0);
-    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(256), 0, st, a, (V + wave - 1) / wave);
+    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
@@ -900,9 +915,18 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
       if (dhidden) product(a.dh_small, mode_c<kDh>{}, v0, nv, piece);
       if (dhead) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
-  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(256), 0, st, a, (V + wave - 1) / wave);
-  hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(1024), 0, st, a);
-  if (dhidden) hipLaunchKernelGGL(k_lce_dhidden, dim3((unsigned)(((long)rows * (H / 8) + 255) / 256)), dim3(256), 0, st, a);
+  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+  if (dhidden) {
+    // few values have many parts: 16 threads share their sum (207 rows x 264, 64 parts: 18 -> 7 us)
+    const long values = (long)rows * (H / 8);
+    auto go = [&](auto kernel, int g) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((values * g + 255) / 256 + 1)), dim3(256), 0, st, a);
+    };
+    if (values <= 65536) go(k_lce_dhidden<16>, 16);
+    else go(k_lce_dhidden<1>, 1);
+  } else {
+    hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(256), 0, st, a);
+  }
   return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR_HIP;
 }
 

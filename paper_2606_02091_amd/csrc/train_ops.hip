@@ -81,6 +81,20 @@ __device__ __forceinline__ void store_n(T* p, const float (&x)[VE]) {
   }
 }
 
+// VE elements as they lie in memory
+template <typename T, int VE>
+struct Raw {
+  std::conditional_t<VE == kVec<T>, u32x4, T> v;
+  __device__ __forceinline__ void load(const T* p) {
+    static_assert(VE == kVec<T> || VE == 1);
+    v = *reinterpret_cast<const decltype(v)*>(p);
+  }
+  __device__ __forceinline__ void get(float (&x)[VE]) const {
+    if constexpr (VE == 1) x[0] = to_f(v);
+    else unpack(v, x);
+  }
+};
+
 // ---- rotary positions: pair m of a row at position p turns by p f_m.  A work-group takes RW rows: it puts their
 // cosines and sines into LDS (once for all heads) and then walks (row, head, item); an item is the pairs
 // of one 16-byte access (half layout: of the two accesses rot / 2 apart), or VE elements past the rotated
@@ -288,23 +302,40 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
       dg[k][e] = 0.f;
       db[LAYER ? k : 0][e] = 0.f;
     }
-  for (int row = blockIdx.x * RG + sub; row < a.rows; row += gridDim.x * RG) {
-    const long at = (long)row * H;
-    const T *x = (const T*)a.x + at, *dy = (const T*)a.dy + at, *dsum = (const T*)a.dsum + at;
-    T* dx = (T*)a.dx + at;
+  // a row's values as they lie in memory, loaded (where registers allow it) while the row before is worked on
+  constexpr bool AHEAD = WPR <= 4 && S * VE <= 16;
+  const int stride = gridDim.x * RG;
+  Raw<T, VE> nx[S], nd[S], ns[S] = {};
+  auto fetch = [&](int row) {
+    const long at = (long)min(row, a.rows - 1) * H;
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      const unsigned c = min((k * TR + t) * VE, H - VE);
+      nx[k].load((const T*)a.x + at + c);
+      nd[k].load((const T*)a.dy + at + c);
+      if (a.dsum) ns[k].load((const T*)a.dsum + at + c);
+    }
+  };
+  if constexpr (AHEAD) fetch(blockIdx.x * RG + sub);
+  for (int row = blockIdx.x * RG + sub; row < a.rows; row += stride) {
+    if constexpr (!AHEAD) fetch(row);
+    T* dx = (T*)a.dx + (long)row * H;
     const float rstd = a.rstd_in[row], mu = LAYER ? a.mean_in[row] : 0.f;
     float xh[S][VE], d[S][VE];
+    Raw<T, VE> rs[S];
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       const unsigned c = (k * TR + t) * VE;
-      load_n<T, VE>(x + min(c, H - VE), xh[k]);
-      load_n<T, VE>(dy + min(c, H - VE), d[k]);
+      nx[k].get(xh[k]);
+      nd[k].get(d[k]);
+      rs[k] = ns[k];
 #pragma unroll
       for (int e = 0; e < VE; ++e) {  // (past the row no part in the sums)
         xh[k][e] = c < H ? xh[k][e] : mu;
         d[k][e] = c < H ? d[k][e] : 0.f;
       }
     }
+    if constexpr (AHEAD) fetch(row + stride);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
@@ -332,7 +363,7 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
       float r[VE];
 #pragma unroll
       for (int e = 0; e < VE; ++e) r[e] = 0.f;
-      if (a.dsum) load_n<T, VE>(dsum + c, r);
+      if (a.dsum) rs[k].get(r);
 #pragma unroll
       for (int e = 0; e < VE; ++e) r[e] += rstd * ((LAYER ? d[k][e] - s1 : d[k][e]) - xh[k][e] * s2);
       store_n<T, VE>(dx + c, r);
@@ -358,7 +389,7 @@ __global__ __launch_bounds__(kT) void k_norm_cols(const float* part, int parts, 
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
   float v = 0.f;
   if (c < n) {
-#pragma unroll 8
+#pragma unroll 16
     for (int p = g; p < parts; p += 16) v += part[(long)p * n + c];
   }
   s[g][l] = v;

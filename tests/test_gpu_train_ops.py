@@ -81,11 +81,13 @@ def lce_check(h, head, y, B, gamma, got):
 
 
 # (blocks, B, V, H): one word, one row; widths below, at and past a stage of 64; vocabularies around a tile of 256; 255,
-# 256 and 257 rows with a loss at ignored = 0; 4,096 x 70,000: two pieces of the vocabulary
+# 256 and 257 rows with a loss at ignored = 0; 4,096 x 70,000 and 128 x 1,100,000: two pieces of the vocabulary,
+# on either tile
 @pytest.mark.parametrize("n,B,V,H,ignored", [
     (1, 2, 1, 8, 0), (1, 2, 2, 8, 0), (2, 2, 255, 64, 0), (3, 5, 256, 72, 0.1), (7, 3, 257, 56, 0.1),
     (17, 16, 1000, 512, 0), (128, 3, 515, 128, 0), (257, 2, 300, 200, 0), (23, 9, 32003, 264, 0.1),
-    (40, 16, 5000, 2880, 0.5), (1, 700, 2049, 1024, 0.2), (256, 16, 70000, 64, 0.05), (5, 13, 3001, 4096, 0.1)])
+    (40, 16, 5000, 2880, 0.5), (1, 700, 2049, 1024, 0.2), (256, 16, 70000, 64, 0.05), (5, 13, 3001, 4096, 0.1),
+    (1, 128, 1100000, 8, 0.1), (1, 300, 1500, 640, 0)])
 def test_linear_ce(n, B, V, H, ignored):
     print(f"[train ops] linear ce {(n, B, V, H)}", flush=True)
     h, head, y = lce_inputs(n, B, V, H, seed=n + V, ignored=ignored)
