@@ -13,6 +13,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
+import struct
 
 import numpy as np
 import torch
@@ -74,6 +75,9 @@ class dflare_rope_tensor(ctypes.Structure):
                 ("y_row", ctypes.c_int64), ("y_head", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
 
 
+_ROPE_TENSOR = struct.Struct("PPqqqqi4x")  # dflare_rope_tensor
+
+
 class dflare_grad_tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
@@ -128,7 +132,7 @@ def lib() -> ctypes.CDLL:
         "dflare_read_probe": ([vp, i64, vp, vp], ctypes.c_int),
         "dflare_rope_frequencies": ([i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
                                      ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)], ctypes.c_int),
-        "dflare_rope": ([ctypes.POINTER(dflare_rope_tensor), i32, vp, vp] + [i32] * 6 + [ctypes.c_float, i32, vp],
+        "dflare_rope": ([vp, i32, vp, vp] + [i32] * 6 + [ctypes.c_float, i32, vp],
                         ctypes.c_int),
         "dflare_norm_fwd": ([vp] * 4 + [i32] * 4 + [ctypes.c_float] + [vp] * 5, ctypes.c_int),
         "dflare_norm_bwd_workspace": ([i32] * 3, ctypes.c_size_t),
@@ -455,8 +459,8 @@ def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = RO
             outs = out if isinstance(out, (tuple, list)) else (out,)
             if len(outs) != len(xs):
                 raise ValueError("out and x differ in number")
-        tab = (dflare_rope_tensor * len(xs))()
-        for e, t, y in zip(tab, xs, outs):
+        tab = b""
+        for t, y in zip(xs, outs):
             if not isinstance(y, torch.Tensor) or not y.is_cuda:
                 raise TypeError("expected a device tensor")
             if y.shape != t.shape or y.dtype != t.dtype or _dtype(t) != dtype or t.get_device() != dev or y.get_device() != dev:
@@ -464,8 +468,7 @@ def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = RO
             (xr, xh, xe), (yr, yh, ye) = t.stride(), y.stride()
             if (xe != 1 or ye != 1) and hd > 1 and t.numel():
                 raise ValueError("the last dimension must be contiguous")
-            e.x, e.y, e.n_heads = t.data_ptr(), y.data_ptr(), t.shape[1]
-            e.x_row, e.x_head, e.y_row, e.y_head = xr, xh, yr, yh
+            tab += _ROPE_TENSOR.pack(t.data_ptr(), y.data_ptr(), xr, xh, yr, yh, t.shape[1])
         _train_check(lib().dflare_rope(tab, len(xs), pos, freq, rows, B, hd, 2 * inv_freq.numel(), dtype, int(layout),
                                        float(scale), int(bool(inverse)), raw), "rope")
     return outs if isinstance(x, (tuple, list)) else outs[0]
