@@ -618,7 +618,8 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
  *   dhidden  bf16 [rows, H] out, or NULL: not wanted;  dhead  bf16 [V, H] out, or NULL
  *   workspace  at least dflare_linear_ce_workspace(rows, V, H, dhidden wanted, dhead wanted) bytes; it grows
  *            with rows, V and H, not with rows x V
- * hidden, head, dhidden, dhead and workspace 16-byte aligned.  rows not a multiple of B, gamma <= 0 or not finite:
+ * hidden, head, dhidden, dhead and workspace 16-byte aligned; a gradient that overlaps hidden, head or the other one is
+ * INVALID_ARG.  rows not a multiple of B, gamma <= 0 or not finite:
  * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows, 2^35 values of hidden or about 2^38 logits: UNSUPPORTED (the
  * workspace is then 0 bytes).  Products run on the bf16 matrix cores with fp32 sums; the logits' gradient is
  * rounded to bf16 as their operand, each gradient once more where it is written.  NaN or infinities in a row

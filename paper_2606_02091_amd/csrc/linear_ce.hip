@@ -794,6 +794,11 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   return L;
 }
 
+bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && a < b + nq && b < a + np;
+}
+
 int lce_check(int rows, int V, int H, int B) {
   if (rows < 1 || V < 1 || H < 1 || B < 1 || rows % B) return DFLARE_ERR_INVALID_ARG;
   if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
@@ -827,6 +832,11 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     if ((uintptr_t)p & 15) return DFLARE_ERR_INVALID_ARG;
   const LceLayout L = lce_layout(rows, V, H, dhidden != nullptr, dhead != nullptr);
   if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
+  // (the inputs are read until the last launch)
+  const size_t hb = (size_t)rows * H * 2, wb = (size_t)V * H * 2;
+  if (overlap(dhidden, hb, hidden, hb) || overlap(dhidden, hb, head, wb) || overlap(dhead, wb, hidden, hb) ||
+      overlap(dhead, wb, head, wb) || overlap(dhead, wb, dhidden, hb))
+    return DFLARE_ERR_INVALID_ARG;
   hipStream_t st = (hipStream_t)stream;
   if (st) {
     int dev = -1, sdev = -1;

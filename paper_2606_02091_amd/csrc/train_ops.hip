@@ -110,7 +110,7 @@ struct RopeArgs {
   RopeSide t[2];
   const int32_t* positions;
   const double* freq;
-  int rows, B, hd, rot, RW;
+  int rows, B, hd, rot, RW, group0;  // group0: first work-group of the launch
   float scale, sign;
 };
 
@@ -118,7 +118,7 @@ template <typename T, int VE, bool HALF>
 __global__ __launch_bounds__(kT) void k_rope(RopeArgs a) {
   extern __shared__ float tab[];  // [RW][rot / 2] cosines, then sines
   const int half = a.rot / 2;
-  const int row0 = blockIdx.x * a.RW, nr = min(a.RW, a.rows - row0);
+  const int row0 = (a.group0 + (int)blockIdx.x) * a.RW, nr = min(a.RW, a.rows - row0);
   float *tc = tab, *ts = tab + a.RW * half;
   for (int i = threadIdx.x; i < nr * half; i += kT) {
     const int r = i / half, m = i - r * half, row = row0 + r;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kT) void k_rope(RopeArgs a) {
     const int n = nr * t.heads * items;
     for (int i = threadIdx.x; i < n; i += kT) {
       const int s = i / items, it = i - s * items, r = s / t.heads, h = s - r * t.heads;
-      const T* x = (const T*)t.x + (row0 + r) * t.x_row + h * t.x_head;
+      const T* x = (const T*)t.x + (long)(row0 + r) * t.x_row + h * t.x_head;
       T* y = (T*)t.y + (row0 + r) * t.y_row + h * t.y_head;
       if (it >= turn) {
         if (x != y) {
@@ -185,7 +185,7 @@ struct NormArgs {
   void *sum, *y, *dx;
   const float *mean_in, *rstd_in;
   float *mean, *rstd, *part;
-  int rows, H;
+  int rows, H, row0;  // row0: first row of the launch (forward)
   float eps;
 };
 
@@ -214,10 +214,10 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_fwd(NormArgs a) {
   __shared__ float red[16];
   constexpr int TR = 64 * WPR;
   const unsigned t = WPR == 1 ? threadIdx.x % TR : threadIdx.x;
-  const int row = WPR == 1 ? blockIdx.x * 4 + threadIdx.x / TR : blockIdx.x;
+  const long row = a.row0 + (WPR == 1 ? blockIdx.x * 4l + threadIdx.x / TR : (long)blockIdx.x);
   if (WPR == 1 && row >= a.rows) return;  // (WPR > 1: one row per work-group, all of them in range)
   const unsigned H = a.H;
-  const long at = (long)row * H;
+  const long at = row * H;
   const T *x = (const T*)a.x + at, *res = (const T*)a.res + at, *gain = (const T*)a.gain, *bias = (const T*)a.bias;
   T *sum = (T*)a.sum + at, *y = (T*)a.y + at;
   float h[S][VE];
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
   constexpr bool AHEAD = WPR <= 4 && S * VE <= 16;
   const int stride = gridDim.x * RG;
   Raw<T, VE> nx[S], nd[S], ns[S] = {};
-  auto fetch = [&](int row) {
-    const long at = (long)min(row, a.rows - 1) * H;
+  auto fetch = [&](long row) {
+    const long at = min(row, a.rows - 1l) * H;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       const unsigned c = min((k * TR + t) * VE, H - VE);
@@ -317,9 +317,9 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
     }
   };
   if constexpr (AHEAD) fetch(blockIdx.x * RG + sub);
-  for (int row = blockIdx.x * RG + sub; row < a.rows; row += stride) {
+  for (long row = blockIdx.x * RG + sub; row < a.rows; row += stride) {
     if constexpr (!AHEAD) fetch(row);
-    T* dx = (T*)a.dx + (long)row * H;
+    T* dx = (T*)a.dx + row * H;
     const float rstd = a.rstd_in[row], mu = LAYER ? a.mean_in[row] : 0.f;
     float xh[S][VE], d[S][VE];
     Raw<T, VE> rs[S];
@@ -548,6 +548,8 @@ int launched() { return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 int size_of(int dtype) { return dtype == DFLARE_F32 ? 4 : dtype == DFLARE_BF16 ? 2 : 0; }
 
+constexpr int kGroupsOfLaunch = 1 << 21;  // (a launch has less than 2^32 threads)
+
 template <typename F>
 void by_type(int dtype, F&& f) {
   if (dtype == DFLARE_F32) f(float{});
@@ -719,16 +721,20 @@ int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int3
   a.scale = scale;
   a.sign = inverse ? -1.f : 1.f;
   a.RW = std::max(1, std::min(kT / half, rows / 1024));
-  const int grid = (rows + a.RW - 1) / a.RW;
+  const int groups = (int)((rows + a.RW - 1l) / a.RW);
   const size_t lds = (size_t)a.RW * half * 8;
   by_type(dtype, [&](auto z) {
     using T = decltype(z);
     auto go = [&](auto ve_c) {
       constexpr int VE = decltype(ve_c)::value;
-      if (layout == DFLARE_ROPE_HALF)
-        hipLaunchKernelGGL((k_rope<T, VE, true>), dim3(grid), dim3(kT), lds, (hipStream_t)stream, a);
-      else
-        hipLaunchKernelGGL((k_rope<T, VE, false>), dim3(grid), dim3(kT), lds, (hipStream_t)stream, a);
+      for (long g = 0; g < groups; g += kGroupsOfLaunch) {
+        const dim3 grid((unsigned)std::min<long>(groups - g, kGroupsOfLaunch));
+        a.group0 = (int)g;
+        if (layout == DFLARE_ROPE_HALF)
+          hipLaunchKernelGGL((k_rope<T, VE, true>), grid, dim3(kT), lds, (hipStream_t)stream, a);
+        else
+          hipLaunchKernelGGL((k_rope<T, VE, false>), grid, dim3(kT), lds, (hipStream_t)stream, a);
+      }
     };
     if (wide) go(int_c<kVec<T>>{});
     else go(int_c<1>{});
@@ -766,9 +772,12 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
     using T = decltype(z);
     norm_shape<T>(H, wide, [&](auto ve, auto wpr, auto s) {
       constexpr int VE = decltype(ve)::value, WPR = decltype(wpr)::value, S = decltype(s)::value, RG = WPR == 1 ? 4 : 1;
-      const dim3 grid((rows + RG - 1) / RG);
-      if (layer) hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, true>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
-      else hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, false>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+      for (long r = 0; r < rows; r += (long)kGroupsOfLaunch * RG) {
+        const dim3 grid((unsigned)std::min<long>((rows - r + RG - 1) / RG, kGroupsOfLaunch));
+        a.row0 = (int)r;
+        if (layer) hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, true>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, false>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+      }
     });
   });
   return launched();
@@ -811,7 +820,7 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
       using T = decltype(z);
       norm_shape<T>(H, wide, [&](auto ve, auto wpr, auto s) {
         constexpr int VE = decltype(ve)::value, WPR = decltype(wpr)::value, S = decltype(s)::value, RG = WPR == 1 ? 4 : 1;
-        const int grid = std::min((rows + RG - 1) / RG, kNormGroups);
+        const int grid = (int)std::min<long>((rows + RG - 1l) / RG, kNormGroups);
         parts = grid * RG;
         if (layer) hipLaunchKernelGGL((k_norm_bwd<T, VE, WPR, S, true>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
         else hipLaunchKernelGGL((k_norm_bwd<T, VE, WPR, S, false>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);

@@ -400,6 +400,8 @@ class _Here:
 
 @contextlib.contextmanager
 def _elsewhere(device: int, stream):
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError("the stream is not of the tensors' device")
     with torch.cuda.device(device):
         raw = _stream(stream)
         if raw == torch.cuda.current_stream().cuda_stream:

@@ -14,7 +14,8 @@ INV, UNS, OK = dfl.ERR_INVALID_ARG, dfl.ERR_UNSUPPORTED, dfl.OK
 INF, NAN = float("inf"), float("nan")
 
 
-def lce(rows=32, V=100, H=64, B=4, gamma=4.5, ws=1 << 40, hidden=P, head=P, labels=P, loss=P, ce=P, dh=P, dw=P, work=P):
+def lce(rows=32, V=100, H=64, B=4, gamma=4.5, ws=1 << 40, hidden=P, head=16 * P, labels=P, loss=P, ce=P, dh=32 * P,
+        dw=48 * P, work=64 * P):
     return dfl.lib().dflare_linear_ce(hidden, head, labels, rows, V, H, B, gamma, loss, ce, dh, dw, work, ws, None)
 
 
@@ -22,8 +23,9 @@ def lce(rows=32, V=100, H=64, B=4, gamma=4.5, ws=1 << 40, hidden=P, head=P, labe
     (dict(rows=0), INV), (dict(rows=-4), INV), (dict(V=0), INV), (dict(H=0), INV), (dict(B=0), INV), (dict(rows=33), INV),
     (dict(gamma=0.0), INV), (dict(gamma=-1.0), INV), (dict(gamma=NAN), INV), (dict(gamma=INF), INV), (dict(ws=64), INV),
     (dict(hidden=None), INV), (dict(head=None), INV), (dict(labels=None), INV), (dict(loss=None), INV), (dict(ce=None), INV),
-    (dict(work=None), INV), (dict(hidden=P + 8), INV), (dict(head=P + 2), INV), (dict(dh=P + 4), INV), (dict(dw=P + 8), INV),
-    (dict(work=P + 8), INV), (dict(H=60), UNS), (dict(H=16392), UNS), (dict(rows=(1 << 22) + 4), UNS),
+    (dict(work=None), INV), (dict(hidden=P + 8), INV), (dict(head=P + 2), INV), (dict(dh=32 * P + 4), INV), (dict(dw=48 * P + 8), INV),
+    (dict(work=P + 8), INV), (dict(dh=P), INV), (dict(dw=16 * P), INV), (dict(dw=P + 16), INV), (dict(dh=48 * P + 32), INV),
+    (dict(dh=16 * P + 12784), INV), (dict(H=60), UNS), (dict(H=16392), UNS), (dict(rows=(1 << 22) + 4), UNS),
     (dict(rows=1 << 22, V=1 << 20), UNS)])
 def test_linear_ce_refuses(kw, code):
     assert lce(**kw) == code
