@@ -7,13 +7,14 @@
 // With dh alone the vocabulary is walked once, in pieces, as one pass of a softmax: a piece's product leaves
 // 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
 // product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
-// fp32, so that R need not be the maximum: only logits more than 2^80 above it (which a wave's words
+// fp32, so that R need not be the maximum: only values more than 2^40 times it (which a wave's words
 // then take as their own reference, raise a flag and have the row rescaled) move it.
-// With dW, which needs dz of all words of a row at its final scale, the maxima and sums come first, and each
-// piece's logits are formed again: 2 rows V H operations more.
+// dW needs dz of all words of a row at its final scale.  Where the vocabulary is one piece, the rows of h take the
+// scale instead (rounded to bf16: dW's error stays that of its own rounding, which the label's term below dominates);
+// otherwise the maxima and sums come first, and each piece's logits are formed again: 2 rows V H operations more.
 // The label's word is left out of dz: its -c (1 - p), the largest value of its row, goes into dh and dW in fp32
 // (rounded to bf16 with the others it would be 0.7 of the gradients' whole error).
-// Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with dW alone, 8 with both.
+// Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with both from one piece, 8 from more.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -70,6 +71,7 @@ struct Lce {
   int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
+  uint16_t* hs;   // [Mp][ldh] hc times fac, where dW comes from one piece; else null
   float2* part;   // [words / a wave's][Mp] (max log2 e, sum of exp(z - max)); one pass: (R, sum of 2^(z log2 e - R))
   float* zlab;    // [Mp] z at the label
   float* lse2;    // [Mp] log2-domain log-sum-exp
@@ -449,7 +451,7 @@ __device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long l
 }
 
 enum { kStats, kDz, kExp, kDh, kDw };
-constexpr float kRise = 80.f;  // how far above its reference (log2) a row's values may lie: 2^80 times 2^24 words fit fp32
+constexpr float kRise = 40.f;  // how far above its reference (log2) a row's values may lie: their sums and these' inverses stay far inside fp32
 
 // One tile of a product and its epilogue:
 //   kStats  z tile (words x rows) -> part, zlab
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
   } else {
     if (!tile_of(blockIdx.x, (a.H + TM - 1) / TM, (nv + TN - 1) / TN, ta, tb)) return;
     const int m0 = ta * TM, n0 = tb * TN;
-    product<S, true, true>(Operand{a.hc + m0, a.ldh, min(a.ldh - m0, TM), a.Mp},
+    product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + m0, a.ldh, min(a.ldh - m0, TM), a.Mp},
                         Operand{a.dz + (long)(n0 / kBlock) * a.Mp * kBlock + n0 % kBlock, kBlock, TN, a.Mp}, n, lds, acc, [&](Acc<S>& d) {
       // the label terms: the rows whose label is one of the wave's words, in order
       const int word0 = v0 + n0 + wn * WN;
@@ -699,6 +701,21 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts) {
   a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
 }
 
+// hs = hc fac, zeros past the last row
+__global__ __launch_bounds__(256) void k_lce_scale(Lce a) {
+  const int n = a.count[0], i = blockIdx.x;
+  if (i >= (n + kBlock - 1) / kBlock * kBlock) return;
+  const float f = i < n ? a.fac[i] : 0.f;
+  const u32x4* from = reinterpret_cast<const u32x4*>(a.hc + (long)i * a.ldh);
+  u32x4* to = reinterpret_cast<u32x4*>(a.hs + (long)i * a.ldh);
+  for (int p = threadIdx.x; p < a.ldh / 8; p += 256) {
+    u32x4 v = from[p];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pack2(__uint_as_float(v[e] << 16) * f, __uint_as_float(v[e] & 0xFFFF0000u) * f);
+    to[p] = v;
+  }
+}
+
 // loss = sum of c ce in 64 bits, in a fixed order, by one work-group of 256
 __device__ __forceinline__ void sum_loss(const Lce& a) {
   __shared__ double ws[4];
@@ -755,7 +772,7 @@ using mode_c = std::integral_constant<int, N>;
 constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
 
 struct LceLayout {
-  size_t count, src, pos, word, c, hc, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
+  size_t count, src, pos, word, c, hc, hs, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -780,6 +797,7 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.word, (size_t)L.Mp * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
+  if (dhead) take(L.hs, (size_t)L.Mp * L.ldh * 2);
   take(L.part, (size_t)words * L.Mp * 32);  // (64 words of a wave of the small tile)
   take(L.zlab, (size_t)L.Mp * 4);
   take(L.lse2, (size_t)L.Mp * 4);
@@ -875,8 +893,9 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
   const int words = (int)((V + (long)kBlock - 1) / kBlock);
   const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);
-  const bool one_pass = dhidden && !dhead;
+  const bool one_pass = dhead ? pieces == 1 : dhidden != nullptr;
   if (one_pass) {
+    if (dhead) a.hs = (uint16_t*)(w + L.hs);
     a.ref = (float*)(w + L.ref);
     a.fac = (float*)(w + L.fac);
     a.flag = (int*)(w + L.flag);
@@ -923,9 +942,15 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }
       if (dhidden) product(a.dh_small, mode_c<kDh>{}, v0, nv, piece);
-      if (dhead) product(false, mode_c<kDw>{}, v0, nv, piece);
+      if (dhead && !one_pass) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
-  if (one_pass) hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+  if (one_pass) {
+    hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+    if (dhead) {
+      hipLaunchKernelGGL(k_lce_scale, dim3(L.Mp), dim3(256), 0, st, a);
+      product(false, mode_c<kDw>{}, 0, V, 0);
+    }
+  }
   if (dhidden) {
     // few values have many parts: 16 threads share their sum (207 rows x 264, 64 parts: 18 -> 7 us)
     const long values = (long)rows * (H / 8);

@@ -76,8 +76,9 @@ def lce_check(h, head, y, B, gamma, got):
         within(dh, want, 1.01 * ((edz + V * 2 * U * dz.abs()) @ w64.abs() + HALF[BF] * want.abs()) + 1e-37, "dhidden")
         assert not dh[~on].any()
     if dw is not None:
-        want = dz.t() @ h64
-        within(dw, want, 1.01 * ((edz + rows * 2 * U * dz.abs()).t() @ h64.abs() + HALF[BF] * want.abs()) + 1e-37, "dhead")
+        want = dz.t() @ h64  # (from one piece of the vocabulary dz's scale is on the rows of h, rounded as well)
+        edz = edz + (HALF[BF] + rows * 2 * U) * dz.abs()
+        within(dw, want, 1.01 * (edz.t() @ h64.abs() + HALF[BF] * want.abs()) + 1e-37, "dhead")
 
 
 # (blocks, B, V, H): one word, one row; widths below, at and past a stage of 64; vocabularies around a tile of 256; 255,
