@@ -10,8 +10,8 @@
 // fp32, so that R need not be the maximum: only values more than 2^40 times it (which a wave's words
 // then take as their own reference, raise a flag and have the row rescaled) move it.
 // dW needs dz of all words of a row at its final scale.  Where the vocabulary is one piece, the rows of h take the
-// scale instead (rounded to bf16: dW's error stays that of its own rounding, which the label's term below dominates);
-// otherwise the maxima and sums come first, and each piece's logits are formed again: 2 rows V H operations more.
+// scale instead (rounded to bf16; the labels' terms, most of dW, are not taken from them); otherwise the maxima
+// and sums come first, and each piece's logits are formed again: 2 rows V H operations more.
 // The label's word is left out of dz: its -c (1 - p), the largest value of its row, goes into dh and dW in fp32
 // (rounded to bf16 with the others it would be 0.7 of the gradients' whole error).
 // Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with both from one piece, 8 from more.
@@ -54,6 +54,10 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {  // to bf16, nearest even
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_w{a, b}), bf16x2_w));
+}
+__device__ __forceinline__ f32x4 unpack4(uint32_t a, uint32_t b) {
+  return f32x4{__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b << 16),
+               __uint_as_float(b & 0xFFFF0000u)};
 }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -107,7 +111,8 @@ struct DhPlan {
     unsigned best = ~0u;  // cost and parts
     for (int k = 1 + (threadIdx.x & 63); k <= kMostParts; k += 64) {
       if (k > 1 && (nb * (long)na * k > 2 * slots || a.stages < 4 * k)) continue;
-      const long cost = (nb * (long)na * k + slots - 1) / slots * ((a.stages + k - 1) / k + 8) + (long)n * a.H * k / 1450000;
+      const long cost = (nb * (long)na * k + slots - 1) / slots * ((a.stages + k - 1) / k + 8) +
+                        (long)n * a.H * k / 1450000;
       best = min(best, (unsigned)min(cost, (1l << 24) - 2) << 8 | k);
     }
     for (int off = 32; off > 0; off >>= 1) best = min(best, (unsigned)__shfl_xor((int)best, off));
@@ -310,6 +315,12 @@ struct Reader {
 template <typename S>
 using Acc = f32x16[S::MT][S::NT];
 
+// Two stages lie in LDS, one of them on its way; a wave reads the operands of each 16 k between the products of the 16
+// before.  7,296 rows x 30,464 words x 4,096 (1,545 us with the epilogue, 1,178 TFLOP/s; dh of them 1,565): the matrix
+// cores are busy 63% of the clocks, at 1.8 GHz; a library product of that shape takes 1,510 us (dh's 2,070).  The
+// same with 4 waves of 128 x 128 has 13% more clocks at a higher rate of them and the same time, and so have
+// work-groups that stay and load their next tile under the epilogue, 128 x 256 tiles two to a CU are 20% slower, and
+// lines requested into L2 two stages ahead 6%: what is left lies outside the CUs, in the loads that miss L2 (2.3 TB/s).
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
 // something finite.  start(acc) runs while the first stages are on their way.
 template <typename S, bool XA, bool XB, typename F>
@@ -434,7 +445,7 @@ __device__ __forceinline__ void put_tile(char* lds, const Acc<S>& acc, int j, in
       const f32x16& z = acc[t][j];
       const int p = m_tile0 * 4 + t * 4 + q;
       const uint2 v = make_uint2(pack2(z[4 * q], z[4 * q + 1]), pack2(z[4 * q + 2], z[4 * q + 3]));
-      *reinterpret_cast<uint2*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1) & 31)) << 4) + h * 8) = v;
+      *reinterpret_cast<uint2*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1))) << 4) + h * 8) = v;
     }
 }
 // and from there to rows of `to` (of which rows n < nv and columns m < mv exist; mv a multiple of 8)
@@ -445,13 +456,14 @@ __device__ __forceinline__ void store_tile(const char* lds, uint16_t* to, long l
 #pragma unroll 4
   for (int it = 0; it < RW * P / 64; ++it) {
     const int n = w * RW + it * (64 / P) + lane / P, p = lane % P;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1) & 31)) << 4));
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + n * (S::TM * 2) + ((p ^ (n & (P - 1))) << 4));
     if (n < nv && p * 8 < mv) *reinterpret_cast<u32x4*>(to + n * ld + p * 8) = v;
   }
 }
 
 enum { kStats, kDz, kExp, kDh, kDw };
-constexpr float kRise = 40.f;  // how far above its reference (log2) a row's values may lie: their sums and these' inverses stay far inside fp32
+// how far above its reference (log2) a row's values may lie: their sums and these' inverses stay far inside fp32
+constexpr float kRise = 40.f;
 
 // One tile of a product and its epilogue:
 //   kStats  z tile (words x rows) -> part, zlab
@@ -592,8 +604,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 const u32x2 v = *reinterpret_cast<const u32x2*>(row + min(t * 32 + q * 8, most));
-                const f32x4 x = {__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u),
-                                 __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
+                const f32x4 x = unpack4(v[0], v[1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   static_assert(NT == 2, "a wave's words");
@@ -759,8 +770,8 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
         x[e] += __shfl_xor(x[e], off);
         y[e] += __shfl_xor(y[e], off);
       }
-    x = x * f - fl * f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xFFFF0000u)};
-    y = y * f - fl * f32x4{__uint_as_float(v[2] << 16), __uint_as_float(v[2] & 0xFFFF0000u), __uint_as_float(v[3] << 16), __uint_as_float(v[3] & 0xFFFF0000u)};
+    x = x * f - fl * unpack4(v[0], v[1]);
+    y = y * f - fl * unpack4(v[2], v[3]);
     out = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
   }
   if (g == 0) reinterpret_cast<u32x4*>(a.dhidden)[at] = out;
@@ -806,8 +817,9 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.lab, (size_t)L.Mp * 4);
   take(L.flag, (size_t)words * 4);
   // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
-  if (dhidden || dhead) take(L.dz, std::min<size_t>((size_t)L.Mp * words * kBlock * 2, std::max<size_t>(kDzBytes, (size_t)L.Mp * kBlock * 2)));
-  if (dhidden) take(L.dacc, std::max((size_t)L.Mp * H, std::min((size_t)kMostParts * L.Mp * H, (size_t)512 * 65536)) * 4);
+  const size_t tile = (size_t)L.Mp * kBlock * 2, values = (size_t)L.Mp * H;
+  if (dhidden || dhead) take(L.dz, std::min(tile * words, std::max(kDzBytes, tile)));
+  if (dhidden) take(L.dacc, std::max(values, std::min(kMostParts * values, (size_t)512 * 65536)) * 4);
   L.total = o;
   return L;
 }
@@ -822,7 +834,7 @@ int lce_check(int rows, int V, int H, int B) {
   if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
   // a launch has less than 2^32 threads
   const long tiles = (long)((rows + kBlock - 1) / kBlock) * ((V + (long)kBlock - 1) / kBlock);
-  if (tiles >= (1l << 22) || (long)rows * H >= (1l << 35)) return DFLARE_ERR_UNSUPPORTED;
+  if (tiles >= (1l << 22) - 8 || (long)rows * H >= (1l << 35)) return DFLARE_ERR_UNSUPPORTED;
   return DFLARE_OK;
 }
 

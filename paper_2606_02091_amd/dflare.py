@@ -384,6 +384,13 @@ _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+def _i32(n: int, name: str) -> int:
+    """n as an argument of 32 bits (ctypes would cut a larger one)."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} is {n}, beyond 32 bits")
+    return int(n)
+
+
 class _Here:
     """A call on the current stream of the current device: nothing to change around it."""
     __slots__ = ("raw",)
@@ -447,7 +454,8 @@ def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = RO
             raise ValueError("expected [rows, n_heads, head_dim] tensors with the same rows and head_dim")
     first = xs[0]
     rows, _, hd = first.shape
-    B = int(B)
+    B = _i32(B, "B")
+    _i32(rows, "the number of rows")
     if B < 1:
         raise ValueError("B must be positive")
     _ptr(inv_freq)
@@ -484,6 +492,7 @@ def norm_fwd(x, gain=None, bias=None, residual=None, kind: int = NORM_RMS, eps: 
         raise ValueError("expected a [rows, H] tensor")
     shape = x.shape
     rows, H = shape
+    _i32(max(rows, H), "a dimension of x")
     xp, dtype, layer = x.data_ptr(), _dtype(x), kind == NORM_LAYER
     rp, gp, bp = _like(residual, "residual", shape, x), _like(gain, "gain", (H,), x), _like(bias, "bias", (H,), x)
     with _place(x.get_device(), stream) as raw:
@@ -505,6 +514,7 @@ def norm_bwd(dy, h, gain, mean, rstd, dsum=None, kind: int = NORM_RMS, stream=No
         raise ValueError("expected a [rows, H] tensor")
     shape = h.shape
     rows, H = shape
+    _i32(max(rows, H), "a dimension of h")
     layer, dtype = kind == NORM_LAYER, _dtype(h)
     dyp, dsp, gp = _like(dy, "dy", shape, h), _like(dsum, "dsum", shape, h), _like(gain, "gain", (H,), h)
     rp, mp = _like(rstd, "rstd", (rows,), h, torch.float32), _like(mean, "mean", (rows,), h, torch.float32)
@@ -531,6 +541,7 @@ def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = T
         raise ValueError("expected bf16 tensors hidden [rows, H] and head [V, H]")
     rows, H = hidden.shape
     V = head.shape[0]
+    _i32(max(rows, V, H), "a dimension")
     wp, yp = _like(head, "head", (V, H), hidden), _like(labels, "labels", (rows,), hidden, torch.int32)
     _ptr(labels)
     ws_bytes = lib().dflare_linear_ce_workspace(rows, V, H, int(need_dhidden), int(need_dhead))
@@ -542,7 +553,7 @@ def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = T
         dhidden = torch.empty_like(hidden) if need_dhidden else None
         dhead = torch.empty_like(head) if need_dhead else None
         ws = torch.empty(ws_bytes, dtype=torch.uint8, device=hidden.device)
-        _train_check(lib().dflare_linear_ce(hidden.data_ptr(), wp, yp, rows, V, H, int(B), float(gamma), loss.data_ptr(),
+        _train_check(lib().dflare_linear_ce(hidden.data_ptr(), wp, yp, rows, V, H, _i32(B, "B"), float(gamma), loss.data_ptr(),
                                             ce.data_ptr(), _ptr(dhidden), _ptr(dhead), ws.data_ptr(), ws_bytes, raw),
                      "linear ce")
     return loss, ce, dhidden, dhead

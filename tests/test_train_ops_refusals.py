@@ -147,6 +147,13 @@ def test_binding_refuses_lists_that_are_no_gradients():
             call()
 
 
+def test_binding_refuses_numbers_beyond_32_bits():
+    assert dfl._i32(2 ** 31 - 1, "n") == 2 ** 31 - 1
+    for n in (2 ** 31, -2 ** 31 - 1, 2 ** 40):
+        with pytest.raises(ValueError):
+            dfl._i32(n, "n")
+
+
 def freqs(d, base, method=0, factor=1.0, length=0.0):
     f, s = np.zeros(max(d // 2, 1)), ctypes.c_float()
     rc = dfl.lib().dflare_rope_frequencies(d, base, method, factor, length, f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
