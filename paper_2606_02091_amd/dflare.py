@@ -13,7 +13,6 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
-import struct
 
 import numpy as np
 import torch
@@ -73,9 +72,6 @@ class dflare_weights(ctypes.Structure):
 class dflare_rope_tensor(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_row", ctypes.c_int64), ("x_head", ctypes.c_int64),
                 ("y_row", ctypes.c_int64), ("y_head", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
-
-
-_ROPE_TENSOR = struct.Struct("PPqqqqi4x")  # dflare_rope_tensor
 
 
 class dflare_grad_tensor(ctypes.Structure):
@@ -166,8 +162,30 @@ def _native():
         loader = importlib.machinery.ExtensionFileLoader("_binding", BINDING_PATH)
         mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_binding", loader))
         loader.exec_module(mod)
+        mod.bind(*(ctypes.cast(getattr(lib(), "dflare_" + f), ctypes.c_void_p).value for f in (
+            "norm_fwd", "norm_bwd_workspace", "norm_bwd", "rope", "grad_norm_workspace", "grad_norm", "clip_grads")),
+                 _current_raw, torch.OutOfMemoryError)
         _binding = mod
     return _binding
+
+
+def _native_call(what: str, tensor, stream, *args):
+    """A function of the binding's native part, on the given stream or the current one of its tensors' device."""
+    f = getattr(_binding or _native(), what)
+    if stream is None:
+        r = f(*args)
+    else:
+        _ptr_device(tensor)
+        with _elsewhere(tensor.get_device(), stream):
+            r = f(*args)
+    if type(r) is int:
+        _train_check(r, what.replace("_", " "))
+    return r
+
+
+def _ptr_device(t) -> None:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("expected a device tensor")
 
 
 def _check(rc: int, h=None):
@@ -444,90 +462,24 @@ def rope(x, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = RO
     rows (queries and keys).  The last dimension is contiguous, the others may be strided.  Row r sits at
     positions[r // B] + r % B (positions int32 [ceil(rows / B)]), or at r.  inverse: the gradient's rotation.
     out: where the result goes (x itself: in place); by default new tensors.  Returns out."""
-    xs = x if isinstance(x, (tuple, list)) else (x,)
-    if not 1 <= len(xs) <= 2:
-        raise ValueError("expected one tensor or a pair")
-    for t in xs:
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError("expected a device tensor")
-        if t.dim() != 3 or t.shape[0] != xs[0].shape[0] or t.shape[2] != xs[0].shape[2]:
-            raise ValueError("expected [rows, n_heads, head_dim] tensors with the same rows and head_dim")
-    first = xs[0]
-    rows, _, hd = first.shape
-    B = _i32(B, "B")
-    _i32(rows, "the number of rows")
-    if B < 1:
-        raise ValueError("B must be positive")
-    _ptr(inv_freq)
-    freq = _like(inv_freq, "inv_freq", (inv_freq.numel(),), first, torch.float64)
-    pos = _like(positions, "positions", (-(-rows // B),), first, torch.int32)
-    dev, dtype = first.get_device(), _dtype(first)
-    with _place(dev, stream) as raw:
-        if out is None:
-            outs = tuple([torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs])
-        else:
-            outs = out if isinstance(out, (tuple, list)) else (out,)
-            if len(outs) != len(xs):
-                raise ValueError("out and x differ in number")
-        tab = b""
-        for t, y in zip(xs, outs):
-            if not isinstance(y, torch.Tensor) or not y.is_cuda:
-                raise TypeError("expected a device tensor")
-            if y.shape != t.shape or y.dtype != t.dtype or _dtype(t) != dtype or t.get_device() != dev or y.get_device() != dev:
-                raise ValueError("x and out differ in shape, type or device")
-            (xr, xh, xe), (yr, yh, ye) = t.stride(), y.stride()
-            if (xe != 1 or ye != 1) and hd > 1 and t.numel():
-                raise ValueError("the last dimension must be contiguous")
-            tab += _ROPE_TENSOR.pack(t.data_ptr(), y.data_ptr(), xr, xh, yr, yh, t.shape[1])
-        _train_check(lib().dflare_rope(tab, len(xs), pos, freq, rows, B, hd, 2 * inv_freq.numel(), dtype, int(layout),
-                                       float(scale), int(bool(inverse)), raw), "rope")
-    return outs if isinstance(x, (tuple, list)) else outs[0]
+    pair = isinstance(x, (tuple, list))
+    xs = tuple(x) if pair else (x,)
+    if out is not None:
+        out = tuple(out) if isinstance(out, (tuple, list)) else (out,)
+    outs = _native_call("rope", xs[0] if xs else None, stream, xs, inv_freq, positions, B, layout, scale, inverse, out)
+    return outs if pair else outs[0]
 
 
 def norm_fwd(x, gain=None, bias=None, residual=None, kind: int = NORM_RMS, eps: float = 1e-6, stream=None):
     """RMSNorm or LayerNorm of the rows of x [rows, H] (plus residual): returns (y, h, mean, rstd) with h = x, or x +
     residual as stored; mean is None for RMSNorm (include/dflare.h)."""
-    _ptr(x)
-    if x.dim() != 2:
-        raise ValueError("expected a [rows, H] tensor")
-    shape = x.shape
-    rows, H = shape
-    _i32(max(rows, H), "a dimension of x")
-    xp, dtype, layer = x.data_ptr(), _dtype(x), kind == NORM_LAYER
-    rp, gp, bp = _like(residual, "residual", shape, x), _like(gain, "gain", (H,), x), _like(bias, "bias", (H,), x)
-    with _place(x.get_device(), stream) as raw:
-        h = x if residual is None else torch.empty_like(x)
-        y = torch.empty_like(x)
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device) if layer else None
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _train_check(lib().dflare_norm_fwd(xp, rp, gp, bp, rows, H, dtype, int(kind), float(eps),
-                                           None if residual is None else h.data_ptr(), y.data_ptr(),
-                                           mean.data_ptr() if layer else None, rstd.data_ptr(), raw), "norm fwd")
-    return y, h, mean, rstd
+    return _native_call("norm_fwd", x, stream, x, gain, bias, residual, kind, eps)
 
 
 def norm_bwd(dy, h, gain, mean, rstd, dsum=None, kind: int = NORM_RMS, stream=None):
     """Backward of norm_fwd: returns (dx, dgain fp32 [H], dbias fp32 [H], None for RMSNorm); dsum is the gradient
     that reaches h from its other uses."""
-    _ptr(h)
-    if h.dim() != 2:
-        raise ValueError("expected a [rows, H] tensor")
-    shape = h.shape
-    rows, H = shape
-    _i32(max(rows, H), "a dimension of h")
-    layer, dtype = kind == NORM_LAYER, _dtype(h)
-    dyp, dsp, gp = _like(dy, "dy", shape, h), _like(dsum, "dsum", shape, h), _like(gain, "gain", (H,), h)
-    rp, mp = _like(rstd, "rstd", (rows,), h, torch.float32), _like(mean, "mean", (rows,), h, torch.float32)
-    with _place(h.get_device(), stream) as raw:
-        dx = torch.empty_like(h)
-        dgain = torch.empty(H, dtype=torch.float32, device=h.device)
-        dbias = torch.empty(H, dtype=torch.float32, device=h.device) if layer else None
-        ws_bytes = lib().dflare_norm_bwd_workspace(rows, H, int(kind))
-        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=h.device)
-        _train_check(lib().dflare_norm_bwd(dyp, h.data_ptr(), gp, mp, rp, dsp, rows, H, dtype, int(kind), dx.data_ptr(),
-                                           dgain.data_ptr(), dbias.data_ptr() if layer else None, ws.data_ptr(), ws_bytes,
-                                           raw), "norm bwd")
-    return dx, dgain, dbias
+    return _native_call("norm_bwd", h, stream, dy, h, gain, mean, rstd, dsum, kind)
 
 
 def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = True, need_dhead: bool = False,
@@ -562,18 +514,7 @@ def linear_ce(hidden, head, labels, B: int, gamma: float, need_dhidden: bool = T
 def grad_norm(grads, stream=None):
     """Global 2-norm of a list of gradient tensors (bf16 or fp32, contiguous): (norm fp32 [1], sumsq fp64 [1])."""
     grads = list(grads)
-    if not grads:
-        raise ValueError("expected at least one gradient")
-    tab, dev = _native().grad_table(grads, None)
-    with _place(dev, stream) as raw:
-        device = grads[0].device
-        sumsq = torch.empty(1, dtype=torch.float64, device=device)
-        norm = torch.empty(1, dtype=torch.float32, device=device)
-        ws_bytes = lib().dflare_grad_norm_workspace(len(grads))
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
-        _train_check(lib().dflare_grad_norm(tab, len(grads), sumsq.data_ptr(), norm.data_ptr(), ws.data_ptr(), ws_bytes,
-                                            raw), "grad norm")
-    return norm, sumsq
+    return _native_call("grad_norm", grads[0] if grads else None, stream, grads)
 
 
 def clip_grads(grads, sumsq: torch.Tensor, max_norm: float, out=None, stream=None) -> None:
@@ -582,11 +523,7 @@ def clip_grads(grads, sumsq: torch.Tensor, max_norm: float, out=None, stream=Non
     grads = list(grads)
     if not grads:
         return
-    tab, dev = _native().grad_table(grads, None if out is None else list(out))
-    _ptr(sumsq)
-    sp = _like(sumsq, "sumsq", (1,), grads[0], torch.float64)
-    with _place(dev, stream) as raw:
-        _train_check(lib().dflare_clip_grads(tab, len(grads), sp, float(max_norm), raw), "clip grads")
+    _native_call("clip_grads", grads[0], stream, grads, sumsq, max_norm, None if out is None else list(out))
 
 
 def dflare_set_sampling(h: int, temperature: float, seed: int = 0) -> None:

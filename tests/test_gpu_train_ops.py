@@ -629,3 +629,47 @@ def test_training_step_of_a_layer():
     assert abs(float(norm) - total) <= 0.012 * total
     dfl.clip_grads(grads, sumsq, 0.1 * total)
     assert abs(float(dfl.grad_norm(grads)[0]) - 0.1 * total) <= 0.012 * 0.1 * total
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    """Every one is refused on the host, before a launch."""
+    x, gain, f32 = randn((6, 64)), randn((64,)), randn((6, 64), F32)
+    rstd = torch.ones(6, device="cuda")
+    for args, why in (((x[0],), ValueError), ((x.t(),), ValueError), ((x.double(),), TypeError), ((x, gain[:63]), ValueError),
+                      ((x, gain.float()), TypeError), ((x, None, gain[:32]), ValueError), ((x, gain, None, f32), TypeError),
+                      ((x, gain, None, x[:5]), ValueError), ((x, gain.cpu()), TypeError), ((x, gain, None, None, 2 ** 40), ValueError),
+                      ((x, gain, None, None, 7), dfl.DFlareError), ((x, gain, None, None, "rms"), TypeError)):
+        with pytest.raises(why):
+            dfl.norm_fwd(*args)
+    for args, why in (((x[:5], x, gain, None, rstd), ValueError), ((x, x, gain, None, rstd[:5]), ValueError),
+                      ((x, x, gain, None, rstd.double()), TypeError), ((f32, x, gain, None, rstd), TypeError),
+                      ((x, x, gain, None, rstd, x[:, :32].contiguous()), ValueError), ((x, x, gain, None, None), dfl.DFlareError),
+                      ((None, x, gain, None, rstd), dfl.DFlareError), ((x, x, gain, None, rstd, None, dfl.NORM_LAYER), dfl.DFlareError)):
+        with pytest.raises(why):
+            dfl.norm_bwd(*args)
+    q, k, pos = randn((6, 4, 16)), randn((6, 2, 16)), torch.zeros(6, dtype=torch.int32, device="cuda")
+    freq, _ = dfl.rope_frequencies(16, 1e4)
+    wide, _ = dfl.rope_frequencies(32, 1e4)
+    for args, kw, why in (((q[0], freq), {}, ValueError), (((q, k[:5]), freq), {}, ValueError), (((q, k.float()), freq), {}, ValueError),
+                          ((q.transpose(1, 2), freq), {}, ValueError), ((q, freq.float()), {}, TypeError), ((q, None), {}, TypeError),
+                          ((q, wide), {}, dfl.DFlareError), ((q, freq, pos.long()), {}, TypeError), ((q, freq, pos[:5]), {}, ValueError),
+                          ((q, freq, pos, 2), {}, ValueError), ((q, freq, None, 0), {}, ValueError), (((q, k, q), freq), {}, ValueError),
+                          (((), freq), {}, ValueError), ((q, freq), {"out": (q, k)}, ValueError), ((q, freq), {"out": k}, ValueError),
+                          ((q, freq), {"out": q.float()}, ValueError), ((q, freq), {"layout": 5}, dfl.DFlareError)):
+        with pytest.raises(why):
+            dfl.rope(*args, **kw)
+    t = randn((100,), F32)
+    _, sumsq = dfl.grad_norm([t])
+    for args, why in ((([t, t.double()], sumsq, 1.0), TypeError), (([t.view(10, 10).t()], sumsq, 1.0), ValueError),
+                      (([t], sumsq.float(), 1.0), TypeError), (([t], sumsq.expand(2), 1.0), ValueError), (([t], None, 1.0), TypeError),
+                      (([t], sumsq, 1.0, []), ValueError), (([t], sumsq, 1.0, [t[:50]]), ValueError), (([t], sumsq, 1.0, [t.bfloat16()]), ValueError),
+                      (([t], sumsq, "all"), TypeError), (([t.cpu()], sumsq, 1.0), TypeError)):
+        with pytest.raises(why):
+            dfl.clip_grads(*args)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        want = dfl.norm_fwd(x, gain)[0]
+    side.synchronize()
+    got = dfl.norm_fwd(x, gain, stream=side)[0]
+    side.synchronize()
+    assert torch.equal(got, want)  # a refusal leaves nothing behind

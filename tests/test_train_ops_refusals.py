@@ -48,12 +48,6 @@ def test_linear_ce_workspace():
     assert lce(ws=need - 1) == INV
 
 
-def test_packed_rope_tensor_is_the_structure():
-    assert dfl._ROPE_TENSOR.size == ctypes.sizeof(dfl.dflare_rope_tensor)
-    a = dfl.dflare_rope_tensor(1, 2, 3, -4, 5, 6, 7)
-    assert bytes(a)[:52] == dfl._ROPE_TENSOR.pack(1, 2, 3, -4, 5, 6, 7)[:52]
-
-
 def rope(n=1, rows=4, B=1, hd=64, rot=64, dtype=dfl.BF16, layout=0, scale=1.0, pos=P, freq=P, x=P, y=2 * P, heads=2,
          strides=(128, 64, 128, 64), tab=True):
     t = (dfl.dflare_rope_tensor * 2)(*[dfl.dflare_rope_tensor(x, y, *strides, heads)] * 2)
