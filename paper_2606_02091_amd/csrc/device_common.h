@@ -232,4 +232,10 @@ __device__ __forceinline__ void store_frag_pair_wt(uint32_t* hi, uint32_t* lo, i
   st_wt(lo + o, l);
 }
 
+// host: np bytes at p and nq bytes at q share one (NULL shares none)
+inline bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && a < b + nq && b < a + np;
+}
+
 }  // namespace dflare

@@ -824,17 +824,12 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   return L;
 }
 
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  return p && q && a < b + nq && b < a + np;
-}
-
 int lce_check(int rows, int V, int H, int B) {
   if (rows < 1 || V < 1 || H < 1 || B < 1 || rows % B) return DFLARE_ERR_INVALID_ARG;
   if (H % 8 || H > 16384 || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
   // a launch has less than 2^32 threads
   const long tiles = (long)((rows + kBlock - 1) / kBlock) * ((V + (long)kBlock - 1) / kBlock);
-  if (tiles >= (1l << 22) - 8 || (long)rows * H >= (1l << 35)) return DFLARE_ERR_UNSUPPORTED;
+  if (tiles >= (1l << 22) - 8 || (long)rows * H > (1l << 35) - 4096) return DFLARE_ERR_UNSUPPORTED;
   return DFLARE_OK;
 }
 

@@ -599,6 +599,62 @@ int grad_check(const dflare_grad_tensor* t, int n) {
   return DFLARE_OK;
 }
 
+// a and b, of the same size, are one tensor or lie apart (or one is NULL)
+bool same_or_apart(const void* a, const void* b, size_t bytes) { return a == b || !overlap(a, bytes, b, bytes); }
+
+// The bytes of a rotary tensor: runs of `run` bytes at p + i s[0] + j s[1], i < n[0], j < n[1]
+struct Runs {
+  __int128 p, s[2];
+  long n[2], run;
+  Runs(const void* at, long row, long head, int rows, int heads, int hd, int size)
+      : p((uintptr_t)at), s{(__int128)row * size, (__int128)head * size}, n{rows, heads}, run((long)hd * size) {
+    for (int k = 0; k < 2; ++k) {
+      if (n[k] == 1) s[k] = 0;
+      if (s[k] < 0) {  // the same runs from the other end
+        p += s[k] * (n[k] - 1);
+        s[k] = -s[k];
+      }
+    }
+  }
+  bool empty() const { return !n[0] || !n[1]; }
+  // no two runs overlap: one stride clears the runs, the other clears the whole of these
+  bool distinct() const {
+    auto nested = [&](int in, int out) {
+      return (n[in] == 1 || s[in] >= run) && (n[out] == 1 || s[out] >= s[in] * (n[in] - 1) + run);
+    };
+    return nested(0, 1) || nested(1, 0);
+  }
+  // bytes from p to the end of the last run, without the strides that are multiples of m (0: with all)
+  __int128 extent(__int128 m) const {
+    __int128 e = run;
+    for (int k = 0; k < 2; ++k)
+      if (!m || s[k] % m) e += s[k] * (n[k] - 1);
+    return e;
+  }
+};
+// Their strides show that a and b have no byte in common: by their ends, or because they lie in different parts of
+// every period of one of the strides (queries and keys of one buffer).
+bool runs_apart(const Runs& a, const Runs& b) {
+  if (a.empty() || b.empty()) return true;
+  if (a.p + a.extent(0) <= b.p || b.p + b.extent(0) <= a.p) return true;
+  for (const __int128 m : {a.s[0], a.s[1], b.s[0], b.s[1]}) {
+    if (!m) continue;
+    const __int128 to_b = ((b.p - a.p) % m + m) % m;
+    if (a.extent(m) <= to_b && to_b + b.extent(m) <= m) return true;
+  }
+  return false;
+}
+// what a call writes meets nothing else that it writes or reads, a tensor turned in place aside
+bool rope_apart(const dflare_rope_tensor* t, int n, int rows, int hd, int size) {
+  auto x = [&](int k) { return Runs(t[k].x, t[k].x_row, t[k].x_head, rows, t[k].n_heads, hd, size); };
+  auto y = [&](int k) { return Runs(t[k].y, t[k].y_row, t[k].y_head, rows, t[k].n_heads, hd, size); };
+  for (int k = 0; k < n; ++k) {
+    if (!y(k).empty() && !y(k).distinct()) return false;
+    if (t[k].x != t[k].y && !runs_apart(x(k), y(k))) return false;
+  }
+  return n == 1 || (runs_apart(y(0), y(1)) && runs_apart(y(0), x(1)) && runs_apart(y(1), x(0)));
+}
+
 long grad_chunks(const dflare_grad_tensor& t) {
   const int size = size_of(t.dtype);
   const long head = std::min<long>(((0u - (unsigned)(uintptr_t)t.data) & 15u) / size, t.n);
@@ -712,6 +768,7 @@ int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int3
     work += t.n_heads;
   }
   if (rows == 0 || work == 0) return DFLARE_OK;
+  if (!rope_apart(tensors, n_tensors, rows, head_dim, size)) return DFLARE_ERR_INVALID_ARG;
   const int rc = stream_ok(stream);
   if (rc != DFLARE_OK) return rc;
   const int half = rotary_dim / 2;
@@ -756,6 +813,12 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
   if (rows > 0 && (!x || !y || !rstd || (layer && !mean) || (residual && !sum))) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {x, residual, gain, bias, (const void*)sum, (const void*)y})
     if (misplaced(p, size)) return DFLARE_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)rows * H * size;
+  for (const void* p : {x, residual})
+    if (!same_or_apart(y, p, bytes) || (residual && !same_or_apart(sum, p, bytes))) return DFLARE_ERR_INVALID_ARG;
+  for (const void* p : {gain, bias})
+    if (overlap(y, bytes, p, (size_t)H * size) || (residual && overlap(sum, bytes, p, (size_t)H * size))) return DFLARE_ERR_INVALID_ARG;
+  if (residual && overlap(sum, bytes, y, bytes)) return DFLARE_ERR_INVALID_ARG;
   if (rows == 0) return DFLARE_OK;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   bool wide = (long)H * size % 16 == 0;
@@ -804,6 +867,9 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
   if (workspace_bytes < dflare_norm_bwd_workspace(rows, H, kind) || misplaced(workspace, 16)) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {dy, h, gain, dsum, (const void*)dx})
     if (misplaced(p, size)) return DFLARE_ERR_INVALID_ARG;
+  for (const void* p : {dy, h, dsum})
+    if (!same_or_apart(dx, p, (size_t)rows * H * size)) return DFLARE_ERR_INVALID_ARG;
+  if (overlap(dx, (size_t)rows * H * size, gain, (size_t)H * size)) return DFLARE_ERR_INVALID_ARG;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   bool wide = (long)H * size % 16 == 0;
   for (const void* p : {dy, h, gain, dsum, (const void*)dx}) wide = wide && aligned16(p);

@@ -673,3 +673,33 @@ def test_binding_refuses_tensors_that_do_not_fit():
     got = dfl.norm_fwd(x, gain, stream=side)[0]
     side.synchronize()
     assert torch.equal(got, want)  # a refusal leaves nothing behind
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rope_of_views_of_one_buffer(dtype):
+    """In place on queries and keys of one buffer, in three layouts; of broadcast rows and heads; the values beside
+    them stay; outputs that meet are refused."""
+    rows, nq, hd = 37, 6, 32
+    freq, _ = dfl.rope_frequencies(hd, 1e4)
+
+    def views():
+        flat = randn((rows, nq + 4, hd), dtype, seed=3)
+        yield flat, flat[:, :nq], flat[:, nq:nq + 2], flat[:, nq + 2:]
+        first = randn((nq + 4, rows, hd), dtype, seed=4)
+        yield first, first[:nq].transpose(0, 1), first[nq:nq + 2].transpose(0, 1), first[nq + 2:]
+        group = randn((rows, nq, 3, hd), dtype, seed=5)
+        yield group, group[:, :, 0], group[:, :, 1], group[:, :, 2]
+    for buf, q, k, v in views():
+        want = dfl.rope((q.contiguous(), k.contiguous()), freq)
+        kept = v.clone()
+        got = dfl.rope((q, k), freq, out=(q, k))
+        assert got[0] is q and got[1] is k
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, kept)
+        for bad in (((q, q), (q, q)), ((q, k), (q, q[:, :k.shape[1]])), ((k,), (k[:1].expand(rows, -1, -1),))):
+            with pytest.raises((ValueError, dfl.DFlareError)):
+                dfl.rope(bad[0], freq, out=bad[1])
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    one = randn((1, 1, hd), dtype, seed=6).expand(rows, nq, hd)
+    assert torch.equal(dfl.rope(one, freq), dfl.rope(one.contiguous(), freq))
+    with pytest.raises(dfl.DFlareError):
+        dfl.rope(one, freq, out=one)

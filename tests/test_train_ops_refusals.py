@@ -65,6 +65,62 @@ def test_rope_refuses(kw, code):
     assert rope(**kw) == code
 
 
+@pytest.mark.parametrize("kw", [
+    dict(y=P + 2), dict(y=P + 1022), dict(y=P - 1022), dict(strides=(128, 64, 0, 64)), dict(strides=(128, 64, 128, 0)),
+    dict(strides=(128, 64, 128, 63)), dict(strides=(128, 64, 127, 64)), dict(strides=(64, 256, 64, 255)),
+    dict(y=P, strides=(0, 64, 0, 64)), dict(y=P, strides=(128, 0, 128, 0)), dict(n=2), dict(n=2, y=P),
+    dict(x=P, y=P + 128, strides=(192, 64, 192, 64)), dict(strides=(128, 64, -128, 63))])
+def test_rope_refuses_outputs_that_meet(kw):
+    """Rows or heads of y on each other, y beside x itself on a part of it, both tensors the same."""
+    assert rope(**kw) == INV
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="what is not refused is launched")
+def test_rope_refuses_every_overlap():
+    """Against the sets of bytes, over small strides and offsets; and layouts that are not to be refused."""
+    rng = np.random.default_rng(5)
+
+    def call(sides, rows, hd):
+        t = (dfl.dflare_rope_tensor * len(sides))(*[dfl.dflare_rope_tensor(P + 2 * x, P + 2 * y, *st, h) for x, y, st, h in sides])
+        return dfl.lib().dflare_rope(t, len(sides), None, P, rows, 1, hd, 2, dfl.BF16, 0, 1.0, 0, None)
+
+    def places(at, row, head, rows, heads, hd):
+        return (at + row * np.arange(rows)[:, None, None] + head * np.arange(heads)[:, None] + np.arange(hd)).ravel()
+
+    met = refused = 0
+    for _ in range(6000):
+        rows, hd, heads = int(rng.integers(1, 4)), int(rng.integers(2, 5)), rng.integers(1, 4, 2)
+        same = rng.integers(-24, 25, 4)
+        sides = []
+        for k in range(int(rng.integers(1, 3))):
+            st = same if rng.random() < 0.7 else rng.integers(-24, 25, 4)
+            x, y = (int(v) for v in rng.integers(0, 120, 2))
+            if rng.random() < 0.5:
+                st, y = np.concatenate([st[:2], st[:2]]), x
+            sides.append((x, y, [int(v) for v in st], int(heads[k])))
+        bad = False
+        written = [places(y, *st[2:], rows, h, hd) for x, y, st, h in sides]
+        read = [places(x, *st[:2], rows, h, hd) for x, y, st, h in sides]
+        for k, w in enumerate(written):
+            bad |= len(set(w)) < len(w)
+            for j in range(len(sides)):
+                bad |= j != k and bool(set(w) & set(written[j]))
+                bad |= (j != k or sides[k][0] != sides[k][1]) and bool(set(w) & set(read[j]))
+        rc = call(sides, rows, hd)
+        met += bad
+        refused += rc == INV
+        assert rc == INV if bad else rc in (INV, dfl.ERR_HIP)
+    assert met > 1000 and refused < 6000
+    n = 5 * 8
+    fine = [[(0, 0, (n, 8) * 2, 3), (24, 24, (n, 8) * 2, 1)],          # queries and keys of one buffer, in place
+            [(0, 24, (n, 8) * 2, 2)],                                  # from one part of a buffer to another
+            [(0, 0, (8, 64) * 2, 3), (192, 192, (8, 64) * 2, 2)],      # heads first
+            [(0, 0, (48, 24) * 2, 2), (8, 8, (48, 24) * 2, 2)],        # query, key and value of a head side by side
+            [(0, 500, (0, 8, 24, 8), 3)], [(0, 500, (8, 0, 24, 8), 3)]]  # broadcast inputs
+    for sides in fine:
+        assert call(sides, 4, 8) == dfl.ERR_HIP, sides
+
+
 def norm_fwd(rows=4, H=64, dtype=dfl.BF16, kind=0, eps=1e-6, x=P, res=None, gain=P, bias=None, sum_=None, y=P, mean=P, rstd=P):
     return dfl.lib().dflare_norm_fwd(x, res, gain, bias, rows, H, dtype, kind, eps, sum_, y, mean, rstd, None)
 
@@ -78,6 +134,14 @@ def test_norm_fwd_refuses(kw, code):
     assert norm_fwd(**kw) == code
 
 
+@pytest.mark.parametrize("kw", [
+    dict(y=P + 128), dict(y=P - 2), dict(y=64 * P, gain=64 * P + 510), dict(kind=1, y=64 * P, bias=64 * P, gain=None),
+    dict(gain=None, res=2 * P, sum_=P, y=P), dict(gain=None, res=2 * P, sum_=8 * P, y=8 * P + 510), dict(gain=None, res=2 * P, sum_=2 * P + 2),
+    dict(res=2 * P, sum_=8 * P, gain=8 * P, y=4 * P)])
+def test_norm_fwd_refuses_outputs_that_meet(kw):
+    assert norm_fwd(**kw) == INV
+
+
 def norm_bwd(rows=4, H=64, dtype=dfl.BF16, kind=0, dy=P, h=P, gain=P, mean=P, rstd=P, dsum=None, dx=P, dgain=P, dbias=None,
              work=P, ws=1 << 30):
     return dfl.lib().dflare_norm_bwd(dy, h, gain, mean, rstd, dsum, rows, H, dtype, kind, dx, dgain, dbias, work, ws, None)
@@ -89,6 +153,12 @@ def norm_bwd(rows=4, H=64, dtype=dfl.BF16, kind=0, dy=P, h=P, gain=P, mean=P, rs
     (dict(work=None), INV), (dict(work=P + 4), INV), (dict(ws=100), INV), (dict(dsum=P + 1), INV), (dict(H=20000), UNS)])
 def test_norm_bwd_refuses(kw, code):
     assert norm_bwd(**kw) == code
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dx=P + 2, gain=None), dict(dx=9 * P + 510, dy=9 * P, gain=None), dict(dx=9 * P - 510, dsum=9 * P, gain=None), dict(gain=P + 256)])
+def test_norm_bwd_refuses_dx_that_meets_an_input(kw):
+    assert norm_bwd(**kw) == INV
 
 
 def tensors(*items):
