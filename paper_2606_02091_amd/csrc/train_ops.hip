@@ -63,18 +63,23 @@ __device__ __forceinline__ float rounded(float v) {
   return to_f(from_f<T>(v));
 }
 
-// VE elements at p: one 16-byte access where VE is kVec<T>, single ones otherwise
-template <typename T, int VE>
+// 16 bytes at an address that is a multiple of A
+template <int A>
+struct __attribute__((packed, aligned(A))) Piece {
+  u32x4 v;
+};
+// VE elements at p: one 16-byte access where VE is kVec<T> (at any element unless ALIGNED), single ones otherwise
+template <typename T, int VE, bool ALIGNED = true>
 __device__ __forceinline__ void load_n(const T* p, float (&x)[VE]) {
-  if constexpr (VE == kVec<T>) unpack(*reinterpret_cast<const u32x4*>(p), x);
+  if constexpr (VE == kVec<T>) unpack(reinterpret_cast<const Piece<ALIGNED ? 16 : sizeof(T)>*>(p)->v, x);
   else {
 #pragma unroll
     for (int e = 0; e < VE; ++e) x[e] = to_f(p[e]);
   }
 }
-template <typename T, int VE>
+template <typename T, int VE, bool ALIGNED = true>
 __device__ __forceinline__ void store_n(T* p, const float (&x)[VE]) {
-  if constexpr (VE == kVec<T>) *reinterpret_cast<u32x4*>(p) = pack(x);
+  if constexpr (VE == kVec<T>) reinterpret_cast<Piece<ALIGNED ? 16 : sizeof(T)>*>(p)->v = pack(x);
   else {
 #pragma unroll
     for (int e = 0; e < VE; ++e) p[e] = from_f<T>(x[e]);
@@ -82,12 +87,13 @@ __device__ __forceinline__ void store_n(T* p, const float (&x)[VE]) {
 }
 
 // VE elements as they lie in memory
-template <typename T, int VE>
+template <typename T, int VE, bool ALIGNED>
 struct Raw {
   std::conditional_t<VE == kVec<T>, u32x4, T> v;
   __device__ __forceinline__ void load(const T* p) {
     static_assert(VE == kVec<T> || VE == 1);
-    v = *reinterpret_cast<const decltype(v)*>(p);
+    if constexpr (VE == 1) v = *p;
+    else v = reinterpret_cast<const Piece<ALIGNED ? 16 : sizeof(T)>*>(p)->v;
   }
   __device__ __forceinline__ void get(float (&x)[VE]) const {
     if constexpr (VE == 1) x[0] = to_f(v);
@@ -180,7 +186,9 @@ __global__ __launch_bounds__(kT) void k_rope(RopeArgs a) {
 
 // ---- norms.  8,192 x 4,096 bf16 with a residual: forward 45 us (268 MB), backward 53 (268 MB and the partials): memory.
 // Few rows: latency, 4 us a launch.  WPR waves hold a row in registers, S pieces of VE elements per thread (piece k T + t for thread t
-// of the row's T), so that a row is read once and mean and variance are sums over held values. ----
+// of the row's T), so that a row is read once and mean and variance are sums over held values.  Rows that do not start or
+// end on 16-byte boundaries are read and written in 16-byte pieces all the same; a piece that would pass the
+// row's end is the row's last 16 bytes, of which the elements of the piece before take no part. ----
 struct NormArgs {
   const void *x, *res, *gain, *bias, *dy, *dsum;
   void *sum, *y, *dx;
@@ -210,7 +218,22 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
   return v;
 }
 
-template <typename T, int VE, int WPR, int S, bool LAYER>
+// Piece k of thread t: its first element c, where it lies, and which of its elements it stands for
+template <typename T, int VE, bool ALIGNED>
+struct RowPiece {
+  unsigned c, at, H;
+  __device__ __forceinline__ RowPiece(unsigned i, unsigned H_) : c(i * VE), at(min(i * VE, H_ - VE)), H(H_) {}
+  __device__ __forceinline__ bool any() const { return c < H; }
+  __device__ __forceinline__ bool has(int e) const { return ALIGNED ? c < H : at + e >= c; }
+  __device__ __forceinline__ void store(T* row, const float (&x)[VE]) const {
+    if (ALIGNED || c + VE <= H) return store_n<T, VE, ALIGNED>(row + c, x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e)
+      if (has(e)) row[at + e] = from_f<T>(x[e]);
+  }
+};
+
+template <typename T, int VE, bool AL, int WPR, int S, bool LAYER>
 __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_fwd(NormArgs a) {
   __shared__ float red[16];
   constexpr int TR = 64 * WPR;
@@ -221,27 +244,28 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_fwd(NormArgs a) {
   const long at = row * H;
   const T *x = (const T*)a.x + at, *res = (const T*)a.res + at, *gain = (const T*)a.gain, *bias = (const T*)a.bias;
   T *sum = (T*)a.sum + at, *y = (T*)a.y + at;
+  auto piece = [&](int k) { return RowPiece<T, VE, AL>(k * TR + t, H); };
   float h[S][VE];
 #pragma unroll
   for (int k = 0; k < S; ++k) {
-    const unsigned c = (k * TR + t) * VE;
-    load_n<T, VE>(x + min(c, H - VE), h[k]);  // (past the row its last piece again, as zeros)
+    const auto p = piece(k);
+    load_n<T, VE, AL>(x + p.at, h[k]);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) h[k][e] = c < H ? h[k][e] : 0.f;
+    for (int e = 0; e < VE; ++e) h[k][e] = p.has(e) ? h[k][e] : 0.f;
   }
   if (a.res) {
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = (k * TR + t) * VE;
+      const auto p = piece(k);
       float r[VE];
-      load_n<T, VE>(res + min(c, H - VE), r);
+      load_n<T, VE, AL>(res + p.at, r);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) h[k][e] = c < H ? rounded<T>(h[k][e] + r[e]) : 0.f;
+      for (int e = 0; e < VE; ++e) h[k][e] = p.has(e) ? rounded<T>(h[k][e] + r[e]) : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = (k * TR + t) * VE;
-      if (c < H) store_n<T, VE>(sum + c, h[k]);
+      const auto p = piece(k);
+      if (p.any()) p.store(sum, h[k]);
     }
   }
   float mu = 0.f;
@@ -253,9 +277,11 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_fwd(NormArgs a) {
       for (int e = 0; e < VE; ++e) s += h[k][e];
     mu = row_sum<WPR>(s, red) / (float)H;  // (divided, not scaled: exact for constant rows)
 #pragma unroll
-    for (int k = 0; k < S; ++k)
+    for (int k = 0; k < S; ++k) {
+      const auto p = piece(k);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) h[k][e] = (k * TR + t) * VE < H ? h[k][e] - mu : 0.f;
+      for (int e = 0; e < VE; ++e) h[k][e] = p.has(e) ? h[k][e] - mu : 0.f;
+    }
   }
   float q = 0.f;
 #pragma unroll
@@ -269,25 +295,25 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_fwd(NormArgs a) {
   }
 #pragma unroll
   for (int k = 0; k < S; ++k) {
-    const unsigned c = (k * TR + t) * VE;
-    if (c >= H) continue;
+    const auto p = piece(k);
+    if (!p.any()) continue;
     float g[VE], b[VE];
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       g[e] = 1.f;
       b[e] = 0.f;
     }
-    if (a.gain) load_n<T, VE>(gain + c, g);
-    if (LAYER && a.bias) load_n<T, VE>(bias + c, b);
+    if (a.gain) load_n<T, VE, AL>(gain + p.at, g);
+    if (LAYER && a.bias) load_n<T, VE, AL>(bias + p.at, b);
 #pragma unroll
     for (int e = 0; e < VE; ++e) h[k][e] = fmaf(h[k][e] * rstd, g[e], b[e]);
-    store_n<T, VE>(y + c, h[k]);
+    p.store(y, h[k]);
   }
 }
 
 // Backward: dx of every row, and per work-group the sums over its rows of dy xhat and dy (part[work-group][1 or 2][H]),
 // which k_norm_cols adds up in a fixed order.
-template <typename T, int VE, int WPR, int S, bool LAYER>
+template <typename T, int VE, bool AL, int WPR, int S, bool LAYER>
 __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
   __shared__ float red[16];
   constexpr int TR = 64 * WPR, RG = norm_threads<WPR> / TR;
@@ -306,12 +332,13 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
   // a row's values as they lie in memory, loaded (where registers allow it) while the row before is worked on
   constexpr bool AHEAD = WPR <= 4 && S * VE <= 16;
   const int stride = gridDim.x * RG;
-  Raw<T, VE> nx[S], nd[S], ns[S] = {};
+  auto piece = [&](int k) { return RowPiece<T, VE, AL>(k * TR + t, H); };
+  Raw<T, VE, AL> nx[S], nd[S], ns[S] = {};
   auto fetch = [&](long row) {
     const long at = min(row, a.rows - 1l) * H;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = min((k * TR + t) * VE, H - VE);
+      const unsigned c = piece(k).at;
       nx[k].load((const T*)a.x + at + c);
       nd[k].load((const T*)a.dy + at + c);
       if (a.dsum) ns[k].load((const T*)a.dsum + at + c);
@@ -323,28 +350,27 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
     T* dx = (T*)a.dx + row * H;
     const float rstd = a.rstd_in[row], mu = LAYER ? a.mean_in[row] : 0.f;
     float xh[S][VE], d[S][VE];
-    Raw<T, VE> rs[S];
+    Raw<T, VE, AL> rs[S];
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = (k * TR + t) * VE;
+      const auto p = piece(k);
       nx[k].get(xh[k]);
       nd[k].get(d[k]);
       rs[k] = ns[k];
 #pragma unroll
       for (int e = 0; e < VE; ++e) {  // (past the row no part in the sums)
-        xh[k][e] = c < H ? xh[k][e] : mu;
-        d[k][e] = c < H ? d[k][e] : 0.f;
+        xh[k][e] = p.has(e) ? xh[k][e] : mu;
+        d[k][e] = p.has(e) ? d[k][e] : 0.f;
       }
     }
     if constexpr (AHEAD) fetch(row + stride);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = (k * TR + t) * VE;
       float g[VE];
 #pragma unroll
       for (int e = 0; e < VE; ++e) g[e] = 1.f;
-      if (gain) load_n<T, VE>(gain + min(c, H - VE), g);
+      if (gain) load_n<T, VE, AL>(gain + piece(k).at, g);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
         xh[k][e] = (xh[k][e] - mu) * rstd;
@@ -359,27 +385,27 @@ __global__ __launch_bounds__(norm_threads<WPR>) void k_norm_bwd(NormArgs a) {
     s2 = row_sum<WPR>(s2, red) / (float)H;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const unsigned c = (k * TR + t) * VE;
-      if (c >= H) continue;
+      const auto p = piece(k);
+      if (!p.any()) continue;
       float r[VE];
 #pragma unroll
       for (int e = 0; e < VE; ++e) r[e] = 0.f;
       if (a.dsum) rs[k].get(r);
 #pragma unroll
       for (int e = 0; e < VE; ++e) r[e] += rstd * ((LAYER ? d[k][e] - s1 : d[k][e]) - xh[k][e] * s2);
-      store_n<T, VE>(dx + c, r);
+      p.store(dx, r);
     }
   }
-  float* p = a.part + ((long)blockIdx.x * RG + sub) * (LAYER ? 2 : 1) * H;
+  float* part = a.part + ((long)blockIdx.x * RG + sub) * (LAYER ? 2 : 1) * H;
 #pragma unroll
   for (int k = 0; k < S; ++k) {
-    const unsigned c = (k * TR + t) * VE;
-    if (c >= H) continue;
+    const auto p = piece(k);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      p[c + e] = dg[k][e];
-      if constexpr (LAYER) p[H + c + e] = db[k][e];
-    }
+    for (int e = 0; e < VE; ++e)
+      if (p.has(e)) {
+        part[p.at + e] = dg[k][e];
+        if constexpr (LAYER) part[H + p.at + e] = db[k][e];
+      }
   }
 }
 
@@ -561,20 +587,21 @@ template <int N>
 using int_c = std::integral_constant<int, N>;
 
 constexpr int kNormMaxH = 16384;
-// f(VE, WPR, S) of a norm over rows of H: 16-byte accesses where the rows allow them
+// f(VE, aligned, WPR, S) of a norm over rows of H
 template <typename T, typename F>
-void norm_shape(int H, bool wide, F&& f) {
+void norm_shape(int H, bool aligned, F&& f) {
   constexpr int V = kVec<T>;
-  if (!wide) {
-    if (H <= 1024) f(int_c<1>{}, int_c<4>{}, int_c<4>{});
-    else if (H <= 4096) f(int_c<1>{}, int_c<4>{}, int_c<16>{});
-    else f(int_c<1>{}, int_c<16>{}, int_c<16>{});
-  } else if (H <= 64 * V) f(int_c<V>{}, int_c<1>{}, int_c<1>{});
-  else if (H <= 128 * V) f(int_c<V>{}, int_c<1>{}, int_c<2>{});
-  else if (H <= 512 * V) f(int_c<V>{}, int_c<4>{}, int_c<2>{});
-  else if (H <= 1024 * V) f(int_c<V>{}, int_c<4>{}, int_c<4>{});
-  else if (H <= 2048 * V) f(int_c<V>{}, int_c<8>{}, int_c<4>{});
-  else if constexpr (V == 4) f(int_c<V>{}, int_c<16>{}, int_c<4>{});  // (bf16 rows end at 16,384)
+  if (H < V) return f(int_c<1>{}, std::true_type{}, int_c<1>{}, int_c<1>{});
+  auto sized = [&](auto al) {
+    if (H <= 64 * V) f(int_c<V>{}, al, int_c<1>{}, int_c<1>{});
+    else if (H <= 128 * V) f(int_c<V>{}, al, int_c<1>{}, int_c<2>{});
+    else if (H <= 512 * V) f(int_c<V>{}, al, int_c<4>{}, int_c<2>{});
+    else if (H <= 1024 * V) f(int_c<V>{}, al, int_c<4>{}, int_c<4>{});
+    else if (H <= 2048 * V) f(int_c<V>{}, al, int_c<8>{}, int_c<4>{});
+    else if constexpr (V == 4) f(int_c<V>{}, al, int_c<16>{}, int_c<4>{});  // (bf16 rows end at 16,384)
+  };
+  if (aligned) sized(std::true_type{});
+  else sized(std::false_type{});
 }
 // Work-groups of the backward pass, each with a partial of the gain's gradient (8,192 x 4,096 bf16, both passes, 256 / 512 /
 // 1,024 of them: 115 / 100 / 107 us; 777 x 2,881 fp32 27 / 27 / 30)
@@ -837,13 +864,14 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
   a.eps = eps;
   by_type(dtype, [&](auto z) {
     using T = decltype(z);
-    norm_shape<T>(H, wide, [&](auto ve, auto wpr, auto s) {
+    norm_shape<T>(H, wide, [&](auto ve, auto al, auto wpr, auto s) {
       constexpr int VE = decltype(ve)::value, WPR = decltype(wpr)::value, S = decltype(s)::value, RG = WPR == 1 ? 4 : 1;
+      constexpr bool AL = decltype(al)::value;
       for (long r = 0; r < rows; r += (long)kGroupsOfLaunch * RG) {
         const dim3 grid((unsigned)std::min<long>((rows - r + RG - 1) / RG, kGroupsOfLaunch));
         a.row0 = (int)r;
-        if (layer) hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, true>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((k_norm_fwd<T, VE, WPR, S, false>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+        if (layer) hipLaunchKernelGGL((k_norm_fwd<T, VE, AL, WPR, S, true>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((k_norm_fwd<T, VE, AL, WPR, S, false>), grid, dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
       }
     });
   });
@@ -888,12 +916,13 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
   if (rows > 0)
     by_type(dtype, [&](auto z) {
       using T = decltype(z);
-      norm_shape<T>(H, wide, [&](auto ve, auto wpr, auto s) {
+      norm_shape<T>(H, wide, [&](auto ve, auto al, auto wpr, auto s) {
         constexpr int VE = decltype(ve)::value, WPR = decltype(wpr)::value, S = decltype(s)::value, RG = WPR == 1 ? 4 : 1;
+      constexpr bool AL = decltype(al)::value;
         const int grid = (int)std::min<long>((rows + RG - 1l) / RG, kNormGroups);
         parts = grid * RG;
-        if (layer) hipLaunchKernelGGL((k_norm_bwd<T, VE, WPR, S, true>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((k_norm_bwd<T, VE, WPR, S, false>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+        if (layer) hipLaunchKernelGGL((k_norm_bwd<T, VE, AL, WPR, S, true>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((k_norm_bwd<T, VE, AL, WPR, S, false>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
       });
     });
   const int n = layer ? 2 * H : H;

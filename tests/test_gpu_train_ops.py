@@ -703,3 +703,54 @@ def test_rope_of_views_of_one_buffer(dtype):
     assert torch.equal(dfl.rope(one, freq), dfl.rope(one.contiguous(), freq))
     with pytest.raises(dfl.DFlareError):
         dfl.rope(one, freq, out=one)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H", [1, 2, 3, 4, 5, 7, 8, 9, 15, 255, 257, 511, 513, 1023, 1025, 2047, 2049, 4095, 4097, 6047, 8191, 8193, 16381])
+def test_norm_rows_off_the_boundaries(H, dtype):
+    print(f"[train ops] norm off the boundaries {(H, dtype)}", flush=True)
+    for layer in (False, True):
+        x, r, dy, dsum = (randn((37, H), dtype, seed) for seed in range(4))
+        norm_check(x, r, randn((H,), dtype, 4), randn((H,), dtype, 5) if layer else None, dy, dsum, layer)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H", [5, 64, 513, 1030, 2881, 6047])
+def test_norm_in_place_off_the_boundaries(H, dtype):
+    """Tensors that start at any element, y and sum over the inputs and dx over each of its own; what lies around them stays."""
+    rows, code = 41, dfl._dtype(torch.empty(0, dtype=dtype))
+    lib, st = dfl.lib(), torch.cuda.current_stream().cuda_stream
+    x, r, dy, dsum = (randn((rows, H), dtype, seed) for seed in range(4))
+    gain, bias = randn((H,), dtype, 4), randn((H,), dtype, 5)
+    ws = torch.empty(lib.dflare_norm_bwd_workspace(rows, H, 1), dtype=torch.uint8, device="cuda")
+
+    def put(t, lead):
+        buf = torch.full((t.numel() + lead + 9,), 7.0, dtype=dtype, device="cuda")
+        buf[lead:lead + t.numel()] = t.reshape(-1)
+        return buf, buf[lead:lead + t.numel()].view(t.shape)
+
+    for kind in (dfl.NORM_RMS, dfl.NORM_LAYER):
+        layer = kind == dfl.NORM_LAYER
+        # (one operand at an odd place has the same kernel take the others wherever they are: the same bits)
+        odd = [put(t, 1)[1] for t in (x, gain)]
+        y, h, mean, rstd = dfl.norm_fwd(odd[0], odd[1], bias if layer else None, residual=r, kind=kind)
+        dx, dgain, dbias = dfl.norm_bwd(dy, h, odd[1], mean, rstd, dsum=dsum, kind=kind)
+        for lead in (0, 1, 3, 6):
+            (bx, vx), (br, vr), (bg, vg), (bb, vb) = put(x, lead), put(r, lead + 1), put(gain, 1), put(bias, 1)
+            m, s = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+            # sum over x, y over the residual
+            assert lib.dflare_norm_fwd(vx.data_ptr(), vr.data_ptr(), vg.data_ptr(), vb.data_ptr() if layer else None, rows, H, code, kind,
+                                       1e-6, vx.data_ptr(), vr.data_ptr(), m.data_ptr(), s.data_ptr(), st) == dfl.OK
+            torch.cuda.synchronize()
+            assert torch.equal(vx, h) and torch.equal(vr, y) and torch.equal(s, rstd) and (not layer or torch.equal(m, mean))
+            assert bx[:lead].eq(7).all() and br[:lead + 1].eq(7).all() and bx[-9:].eq(7).all() and br[-9:].eq(7).all()
+            for over in range(3):
+                (b0, v0), (b1, v1), (b2, v2) = put(dy, lead), put(h, lead), put(dsum, lead)
+                to, g = (v0, v1, v2)[over], torch.zeros(H, device="cuda")
+                assert lib.dflare_norm_bwd(v0.data_ptr(), v1.data_ptr(), vg.data_ptr(), m.data_ptr() if layer else None, s.data_ptr(),
+                                           v2.data_ptr(), rows, H, code, kind, to.data_ptr(), g.data_ptr(), None, ws.data_ptr(),
+                                           ws.numel(), st) == dfl.OK
+                torch.cuda.synchronize()
+                assert torch.equal(to, dx) and torch.equal(g, dgain)
+                for k, (b, v, t) in enumerate(((b0, v0, dy), (b1, v1, h), (b2, v2, dsum))):
+                    assert b[:lead].eq(7).all() and b[-9:].eq(7).all() and (k == over or torch.equal(v, t))
