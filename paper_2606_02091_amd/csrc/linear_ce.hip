@@ -14,7 +14,7 @@
 // and sums come first, and each piece's logits are formed again: 2 rows V H operations more.
 // The label's word is left out of dz: its -c (1 - p), the largest value of its row, goes into dh and dW in fp32
 // (rounded to bf16 with the others it would be 0.7 of the gradients' whole error).
-// Bound by the matrix cores: 2 rows V H operations for the loss, 4 with dh, 6 with both from one piece, 8 from more.
+// Bound by the matrix cores (up to some 128 rows by reading the head): 2 rows V H operations for the loss, 4 with dh, 6 with both from one piece, 8 from more.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -41,6 +41,7 @@ struct Shape {
 };
 using Large = Shape<256, 256, 2, 4>;  // one work-group per CU
 using Small = Shape<128, 128, 2, 2>;  // two
+using Few = Shape<128, 64, 2, 2>;     // three
 constexpr float kL2E = 1.4426950408889634f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -87,7 +88,7 @@ struct Lce {
   float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far
   int Mp, ldh, Vp;
   int stages;     // stages of k of the first (longest) piece
-  int dh_small;   // dh on the small tile
+  int dh_tile;    // dh on the large tile (0), the small one, or that for few rows
 };
 
 // dh's tiles for n rows with a loss.  The words of a piece are split into `parts` where there are few tiles for the
@@ -96,18 +97,20 @@ struct Lce {
 // measured on the large tile).  More than one part makes at most two rounds.  The number depends on the rows
 // with a loss, so that it is chosen on the device (k_lce_rows).
 constexpr int kMostParts = 128;
+__host__ __device__ constexpr int dh_slots(int tile) { return 256 * (tile + 1); }  // work-groups that the CUs hold
 struct DhPlan {
   int tn, nb, na, parts;
   __device__ __forceinline__ DhPlan(const Lce& a, int n) {
-    tn = a.dh_small ? Small::TN : Large::TN;
+    static_assert(Few::TM == Small::TM);
+    tn = a.dh_tile == 2 ? Few::TN : a.dh_tile ? Small::TN : Large::TN;
     nb = (n + tn - 1) / tn;
-    na = a.dh_small ? (a.H + Small::TM - 1) / Small::TM : (a.H + Large::TM - 1) / Large::TM;
+    na = a.dh_tile ? (a.H + Small::TM - 1) / Small::TM : (a.H + Large::TM - 1) / Large::TM;
     parts = a.count[1];
   }
   __device__ __forceinline__ long part_rows() const { return (long)nb * tn; }
   // by one wave
   __device__ __forceinline__ int choose(const Lce& a, int n) const {
-    const int slots = a.dh_small ? 512 : 256;
+    const int slots = dh_slots(a.dh_tile);
     unsigned best = ~0u;  // cost and parts
     for (int k = 1 + (threadIdx.x & 63); k <= kMostParts; k += 64) {
       if (k > 1 && (nb * (long)na * k > 2 * slots || a.stages < 4 * k)) continue;
@@ -397,7 +400,7 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
       multiply(f0, n);
 #pragma unroll
       for (int r = n * R / Q; r < (n + 1) * R / Q; ++r) read(f1, buf, 1, r);
-      if (n == Q / 4 - 1 && late) issue_b(other);
+      if (n == (Q > 4 ? Q / 4 - 1 : 0) && late) issue_b(other);
       fence();
     }
     step(f1, f0, buf, 2);
@@ -916,19 +919,26 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   auto tiles = [](auto s, long m, long n) { return ((m + s.TM - 1) / s.TM) * ((n + s.TN - 1) / s.TN); };
   const long rounds_s = (tiles(Small{}, V, most) + 511) / 512, rounds_l = (tiles(Large{}, V, most) + 255) / 256;
   const bool z_small = 5 * rounds_s < 8 * rounds_l;
-  a.dh_small = 4 * tiles(Small{}, 1, most) < 7 * tiles(Large{}, 1, most) ||
+  const bool dh_small = 4 * tiles(Small{}, 1, most) < 7 * tiles(Large{}, 1, most) ||
                tiles(Large{}, H, most) * (a.stages / 4) < 256;  // (too few words for parts on all CUs)
-  const int wave = z_small ? Small::MT * 32 : Large::MT * 32;
+  // Up to 64 rows the calls are bound by the head's way from memory, of which three work-groups to a CU keep more
+  // under way (small tile / this: 13 rows of 151,936 x 2,880 with dh 423 / 357 us, 14 of 151,936 x 4,096 loss alone 287 / 232;
+  // two of them for 120 rows lose: of 151,936 x 4,096 with dh 555 / 661).
+  const bool few = most <= Few::TN;
+  a.dh_tile = few ? 2 : dh_small;
+  static_assert(Few::MT == Small::MT, "a wave's words");
+  const int wave = z_small || few ? Small::MT * 32 : Large::MT * 32;
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
   auto product = [&](bool small, auto mode, int v0, int nv, int piece) {
     constexpr int MODE = decltype(mode)::value;
     auto go = [&](auto s) {
       using S = decltype(s);
       long t = MODE <= kExp ? tiles(s, nv, most) : MODE == kDw ? tiles(s, H, nv) : tiles(s, H, most);
-      if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, small ? 1024l : 512l));  // (the most that the plan makes)
+      if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, 2l * dh_slots(a.dh_tile)));  // (the most that the plan makes)
       hipLaunchKernelGGL((k_lce_product<S, MODE>), dim3(grid(t)), dim3(S::T), 0, st, a, v0, nv, piece);
     };
     if constexpr (MODE != kDw) {
+      if (few) return go(Few{});
       if (small) return go(Small{});
     }
     go(Large{});
@@ -948,7 +958,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
       } else {
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }
-      if (dhidden) product(a.dh_small, mode_c<kDh>{}, v0, nv, piece);
+      if (dhidden) product(dh_small, mode_c<kDh>{}, v0, nv, piece);
       if (dhead && !one_pass) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
   if (one_pass) {

@@ -754,3 +754,16 @@ def test_norm_in_place_off_the_boundaries(H, dtype):
                 assert torch.equal(to, dx) and torch.equal(g, dgain)
                 for k, (b, v, t) in enumerate(((b0, v0, dy), (b1, v1, h), (b2, v2, dsum))):
                     assert b[:lead].eq(7).all() and b[-9:].eq(7).all() and (k == over or torch.equal(v, t))
+
+
+# rows with a loss around 64 (n (B - 1) of them at most), on which the products' tile depends; the vocabulary in two pieces
+@pytest.mark.parametrize("n,B,V,H", [(1, 64, 3000, 320), (1, 65, 3000, 320), (1, 66, 3000, 320), (13, 6, 40001, 72), (16, 5, 129, 2880),
+                                     (1, 2, 70001, 1000), (1, 33, 12800, 4096), (1, 50, 1100000, 8), (32, 3, 127, 8)])
+def test_linear_ce_of_few_rows(n, B, V, H):
+    print(f"[train ops] linear ce of few rows {(n, B, V, H)}", flush=True)
+    h, head, y = lce_inputs(n, B, V, H, seed=21, ignored=0.0)
+    for dh, dw in ((False, False), (True, False), (False, True), (True, True)):
+        got = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+        lce_check(h, head, y, B, 4.5, got)
+        again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+        assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))
