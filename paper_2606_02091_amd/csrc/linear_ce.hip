@@ -626,28 +626,30 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
   }
 }
 
-// log-sum-exp of every row from its parts (16 rows by 64 groups of parts), and its cross-entropy
+// A row's values from its parts: work-groups of 1,024 threads take kRowsOf rows, each by 1,024 / kRowsOf groups of parts
+constexpr int kRowsOf = 4;
+
+// log-sum-exp of every row from its parts, and its cross-entropy
 __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
-  __shared__ float2 sh[64][17];
-  const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
-  if ((int)blockIdx.x * 16 >= n) return;
+  __shared__ float2 sh[16][kRowsOf];
+  const int n = a.count[0], l = threadIdx.x % kRowsOf, g = threadIdx.x / kRowsOf, i = blockIdx.x * kRowsOf + l;
+  if ((int)blockIdx.x * kRowsOf >= n) return;
   float m = -FLT_MAX, s = 0.f;
-#pragma unroll 8
-  for (int p = g; p < parts; p += 64) {
-    const float2 v = a.part[(long)p * a.Mp + i];
-    const float mn = fmaxf(m, v.x);
-    s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
+  auto add = [&](float x, float y) {
+    const float mn = fmaxf(m, x);
+    s = s * ex2(m - mn) + y * ex2(x - mn);
     m = mn;
+  };
+#pragma unroll 8
+  for (int p = g; p < parts; p += 1024 / kRowsOf) {
+    const float2 v = a.part[(long)p * a.Mp + i];
+    add(v.x, v.y);
   }
-  sh[g][l] = make_float2(m, s);
+  for (int off = 32; off >= kRowsOf; off >>= 1) add(__shfl_xor(m, off), __shfl_xor(s, off));
+  if ((threadIdx.x & 63) < kRowsOf) sh[threadIdx.x >> 6][l] = make_float2(m, s);
   __syncthreads();
   if (g != 0 || i >= n) return;
-  for (int k = 1; k < 64; ++k) {
-    const float2 v = sh[k][l];
-    const float mn = fmaxf(m, v.x);
-    s = s * ex2(m - mn) + v.y * ex2(v.x - mn);
-    m = mn;
-  }
+  for (int k = 1; k < 16; ++k) add(sh[k][l].x, sh[k][l].y);
   const float lse = m + log2f(s);
   const float ce = (lse - a.zlab[i] * kL2E) * 0.6931471805599453f;
   a.lse2[i] = lse;
@@ -655,78 +657,96 @@ __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
   a.row_ce[a.src[i]] = ce;
 }
 
-// A piece in which some words took a reference of their own: the row's reference becomes the highest of them, and
-// what was written under others, dh of the pieces before it included, is scaled to it.
+// Row i of a piece in which some words took a reference of their own: the row's reference becomes the highest of them
+// (returned), and what was written under others, dh of the pieces before it included, is scaled to it.  By a
+// work-group; red: a float per wave.
+__device__ __forceinline__ float rebase_row(const Lce& a, int i, int v0, int nv, int piece, int wave, float* red) {
+  const int groups = (nv + wave - 1) / wave;  // groups of a wave's words
+  const float2* p = a.part + (long)(v0 / wave) * a.Mp + i;
+  const float old = a.ref[i];
+  float r = old;
+  for (int g = threadIdx.x; g < groups; g += blockDim.x) r = fmaxf(r, p[(long)g * a.Mp].x);
+  for (int off = 32; off > 0; off >>= 1) r = fmaxf(r, __shfl_xor(r, off));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = r;
+  __syncthreads();
+  for (int k = 0; k < (int)blockDim.x / 64; ++k) r = fmaxf(r, red[k]);
+  if (!(r > old)) return old;
+  for (int e = threadIdx.x; e < groups * (wave / 8); e += blockDim.x) {  // 8 words each
+    const int g = e / (wave / 8);
+    const float f = ex2(p[(long)g * a.Mp].x - r);
+    if (f == 1.f) continue;
+    u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(e / (kBlock / 8)) * a.Mp + i) * kBlock) + e % (kBlock / 8);
+    u32x4 v = *at;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
+    *at = v;
+  }
+  if (piece > 0) {
+    const DhPlan plan(a, a.count[0]);
+    for (int k = 0; k < plan.parts; ++k) {
+      float* d = a.dacc + (k * plan.part_rows() + i) * a.H;
+      for (int m = threadIdx.x; m < a.H; m += blockDim.x) d[m] *= ex2(old - r);
+    }
+  }
+  if (threadIdx.x == 0) a.ref[i] = r;
+  return r;
+}
 __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece, int wave) {
   __shared__ float red[4];
   if (a.flag[piece] == 0) return;
-  const int n = a.count[0], groups = (nv + wave - 1) / wave;  // groups of a wave's words
-  const DhPlan plan(a, n);
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const float2* p = a.part + (long)(v0 / wave) * a.Mp + i;
-    const float old = a.ref[i];
-    float r = old;
-    for (int g = threadIdx.x; g < groups; g += 256) r = fmaxf(r, p[(long)g * a.Mp].x);
-    for (int off = 32; off > 0; off >>= 1) r = fmaxf(r, __shfl_xor(r, off));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = r;
-    __syncthreads();
-    r = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    if (!(r > old)) continue;
-    for (int e = threadIdx.x; e < groups * (wave / 8); e += 256) {  // 8 words each
-      const int g = e / (wave / 8);
-      const float f = ex2(p[(long)g * a.Mp].x - r);
-      if (f == 1.f) continue;
-      u32x4* at = reinterpret_cast<u32x4*>(a.dz + ((long)(e / (kBlock / 8)) * a.Mp + i) * kBlock) + e % (kBlock / 8);
-      u32x4 v = *at;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
-      *at = v;
+  const int n = a.count[0];
+  for (int i = blockIdx.x; i < n; i += gridDim.x) rebase_row(a, i, v0, nv, piece, wave, red);
+}
+
+// One pass, after the last piece's logits: its rows rescaled where it needs that, the rows' sums from their parts, their
+// cross-entropy and the factors of dh; with dhead hs = hc fac, zeros past the last row.  (In launches of their own
+// these were 12 us of 67 for 207 rows x 32,003 x 264.)
+__global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, int nv, int piece, int wave) {
+  __shared__ float sh[16][kRowsOf], red[16], ref[kRowsOf], fac[kRowsOf];
+  const int n = a.count[0], row0 = blockIdx.x * kRowsOf;
+  if (row0 >= (a.hs ? (n + kBlock - 1) / kBlock * kBlock : n)) return;
+  const int l = threadIdx.x % kRowsOf, g = threadIdx.x / kRowsOf, i = row0 + l;
+  if (threadIdx.x < kRowsOf) {
+    ref[l] = i < n ? a.ref[i] : 0.f;
+    fac[l] = 0.f;
+  }
+  if (a.flag[piece])
+    for (int k = 0; k < kRowsOf && row0 + k < n; ++k) {
+      const float r = rebase_row(a, row0 + k, v0, nv, piece, wave, red);
+      if (threadIdx.x == 0) ref[k] = r;
     }
-    if (piece > 0)
-      for (int k = 0; k < plan.parts; ++k) {
-        float* d = a.dacc + (k * plan.part_rows() + i) * a.H;
-        for (int m = threadIdx.x; m < a.H; m += 256) d[m] *= ex2(old - r);
-      }
-    if (threadIdx.x == 0) a.ref[i] = r;
-  }
-}
-
-// one pass: the rows' sums from their parts, their cross-entropy and the factors of dh
-__global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts) {
-  __shared__ float sh[64][17];
-  const int n = a.count[0], l = threadIdx.x & 15, g = threadIdx.x >> 4, i = blockIdx.x * 16 + l;
-  if ((int)blockIdx.x * 16 >= n) return;
-  const float r = a.ref[i];
-  float s = 0.f;
-#pragma unroll 8
-  for (int p = g; p < parts; p += 64) {
-    const float2 v = a.part[(long)p * a.Mp + i];
-    s += v.y * ex2(v.x - r);
-  }
-  sh[g][l] = s;
   __syncthreads();
-  if (g != 0 || i >= n) return;
-  for (int k = 1; k < 64; ++k) s += sh[k][l];  // all words but the label's
-  const float y = a.zlab[i] * kL2E - r, ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey);
-  a.fac[i] = c * inv;
-  a.lab[i] = c * (s * inv);
-  // log((s + ey) / ey); far below the reference ey may be 0
-  a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
-}
-
-// hs = hc fac, zeros past the last row
-__global__ __launch_bounds__(256) void k_lce_scale(Lce a) {
-  const int n = a.count[0], i = blockIdx.x;
-  if (i >= (n + kBlock - 1) / kBlock * kBlock) return;
-  const float f = i < n ? a.fac[i] : 0.f;
-  const u32x4* from = reinterpret_cast<const u32x4*>(a.hc + (long)i * a.ldh);
-  u32x4* to = reinterpret_cast<u32x4*>(a.hs + (long)i * a.ldh);
-  for (int p = threadIdx.x; p < a.ldh / 8; p += 256) {
-    u32x4 v = from[p];
+  const float r = ref[l];
+  float s = 0.f;
+  if (i < n) {
+#pragma unroll 8
+    for (int p = g; p < parts; p += 1024 / kRowsOf) {
+      const float2 v = a.part[(long)p * a.Mp + i];
+      s += v.y * ex2(v.x - r);
+    }
+  }
+  for (int off = 32; off >= kRowsOf; off >>= 1) s += __shfl_xor(s, off);
+  if ((threadIdx.x & 63) < kRowsOf) sh[threadIdx.x >> 6][l] = s;
+  __syncthreads();
+  if (g == 0 && i < n) {
+    for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
+    const float y = a.zlab[i] * kL2E - r, ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey);
+    a.fac[i] = fac[l] = c * inv;
+    a.lab[i] = c * (s * inv);
+    // log((s + ey) / ey); far below the reference ey may be 0
+    a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
+  }
+  if (!a.hs) return;
+  __syncthreads();
+  const int P = a.ldh / 8;
+  for (int e = threadIdx.x; e < kRowsOf * P; e += 1024) {
+    const long at = (long)(row0 + e / P) * P + e % P;
+    const float f = fac[e / P];
+    u32x4 v = reinterpret_cast<const u32x4*>(a.hc)[at];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = pack2(__uint_as_float(v[e] << 16) * f, __uint_as_float(v[e] & 0xFFFF0000u) * f);
-    to[p] = v;
+    for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
+    reinterpret_cast<u32x4*>(a.hs)[at] = v;
   }
 }
 
@@ -947,27 +967,23 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
   if (!one_pass) {
     product(z_small, mode_c<kStats>{}, 0, V, 0);
-    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / kRowsOf), dim3(1024), 0, st, a, (V + wave - 1) / wave);
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
       const int v0 = piece * L.Vp, nv = std::min(V - v0, L.Vp);
       if (one_pass) {
         product(z_small, mode_c<kExp>{}, v0, nv, piece);
-        hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece, wave);
+        if (piece < pieces - 1)
+          hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece, wave);
+        else
+          hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / kRowsOf), dim3(1024), 0, st, a, (V + wave - 1) / wave, v0, nv, piece, wave);
       } else {
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }
       if (dhidden) product(dh_small, mode_c<kDh>{}, v0, nv, piece);
-      if (dhead && !one_pass) product(false, mode_c<kDw>{}, v0, nv, piece);
+      if (dhead) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
-  if (one_pass) {
-    hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / 16), dim3(1024), 0, st, a, (V + wave - 1) / wave);
-    if (dhead) {
-      hipLaunchKernelGGL(k_lce_scale, dim3(L.Mp), dim3(256), 0, st, a);
-      product(false, mode_c<kDw>{}, 0, V, 0);
-    }
-  }
   if (dhidden) {
     // few values have many parts: 16 threads share their sum (207 rows x 264, 64 parts: 18 -> 7 us)
     const long values = (long)rows * (H / 8);
