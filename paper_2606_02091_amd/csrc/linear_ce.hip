@@ -626,14 +626,14 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
   }
 }
 
-// A row's values from its parts: work-groups of 1,024 threads take kRowsOf rows, each by 1,024 / kRowsOf groups of parts
-constexpr int kRowsOf = 4;
+// A row's values from its parts: work-groups of 1,024 threads take R rows, each by 1,024 / R groups of parts
 
 // log-sum-exp of every row from its parts, and its cross-entropy
+template <int R>
 __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
-  __shared__ float2 sh[16][kRowsOf];
-  const int n = a.count[0], l = threadIdx.x % kRowsOf, g = threadIdx.x / kRowsOf, i = blockIdx.x * kRowsOf + l;
-  if ((int)blockIdx.x * kRowsOf >= n) return;
+  __shared__ float2 sh[16][R];
+  const int n = a.count[0], l = threadIdx.x % R, g = threadIdx.x / R, i = blockIdx.x * R + l;
+  if ((int)blockIdx.x * R >= n) return;
   float m = -FLT_MAX, s = 0.f;
   auto add = [&](float x, float y) {
     const float mn = fmaxf(m, x);
@@ -641,12 +641,12 @@ __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
     m = mn;
   };
 #pragma unroll 8
-  for (int p = g; p < parts; p += 1024 / kRowsOf) {
+  for (int p = g; p < parts; p += 1024 / R) {
     const float2 v = a.part[(long)p * a.Mp + i];
     add(v.x, v.y);
   }
-  for (int off = 32; off >= kRowsOf; off >>= 1) add(__shfl_xor(m, off), __shfl_xor(s, off));
-  if ((threadIdx.x & 63) < kRowsOf) sh[threadIdx.x >> 6][l] = make_float2(m, s);
+  for (int off = 32; off >= R; off >>= 1) add(__shfl_xor(m, off), __shfl_xor(s, off));
+  if ((threadIdx.x & 63) < R) sh[threadIdx.x >> 6][l] = make_float2(m, s);
   __syncthreads();
   if (g != 0 || i >= n) return;
   for (int k = 1; k < 16; ++k) add(sh[k][l].x, sh[k][l].y);
@@ -701,18 +701,19 @@ __global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int p
 
 // One pass, after the last piece's logits: its rows rescaled where it needs that, the rows' sums from their parts, their
 // cross-entropy and the factors of dh; with dhead hs = hc fac, zeros past the last row.  (In launches of their own
-// these were 12 us of 67 for 207 rows x 32,003 x 264.)
+// these made 207 rows x 32,003 x 264 6 us of 68 longer.)
+template <int R>
 __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, int nv, int piece, int wave) {
-  __shared__ float sh[16][kRowsOf], red[16], ref[kRowsOf], fac[kRowsOf];
-  const int n = a.count[0], row0 = blockIdx.x * kRowsOf;
+  __shared__ float sh[16][R], red[16], ref[R], fac[R];
+  const int n = a.count[0], row0 = blockIdx.x * R;
   if (row0 >= (a.hs ? (n + kBlock - 1) / kBlock * kBlock : n)) return;
-  const int l = threadIdx.x % kRowsOf, g = threadIdx.x / kRowsOf, i = row0 + l;
-  if (threadIdx.x < kRowsOf) {
+  const int l = threadIdx.x % R, g = threadIdx.x / R, i = row0 + l;
+  if (threadIdx.x < R) {
     ref[l] = i < n ? a.ref[i] : 0.f;
     fac[l] = 0.f;
   }
   if (a.flag[piece])
-    for (int k = 0; k < kRowsOf && row0 + k < n; ++k) {
+    for (int k = 0; k < R && row0 + k < n; ++k) {
       const float r = rebase_row(a, row0 + k, v0, nv, piece, wave, red);
       if (threadIdx.x == 0) ref[k] = r;
     }
@@ -721,13 +722,13 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, in
   float s = 0.f;
   if (i < n) {
 #pragma unroll 8
-    for (int p = g; p < parts; p += 1024 / kRowsOf) {
+    for (int p = g; p < parts; p += 1024 / R) {
       const float2 v = a.part[(long)p * a.Mp + i];
       s += v.y * ex2(v.x - r);
     }
   }
-  for (int off = 32; off >= kRowsOf; off >>= 1) s += __shfl_xor(s, off);
-  if ((threadIdx.x & 63) < kRowsOf) sh[threadIdx.x >> 6][l] = s;
+  for (int off = 32; off >= R; off >>= 1) s += __shfl_xor(s, off);
+  if ((threadIdx.x & 63) < R) sh[threadIdx.x >> 6][l] = s;
   __syncthreads();
   if (g == 0 && i < n) {
     for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
@@ -740,7 +741,7 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, in
   if (!a.hs) return;
   __syncthreads();
   const int P = a.ldh / 8;
-  for (int e = threadIdx.x; e < kRowsOf * P; e += 1024) {
+  for (int e = threadIdx.x; e < R * P; e += 1024) {
     const long at = (long)(row0 + e / P) * P + e % P;
     const float f = fac[e / P];
     u32x4 v = reinterpret_cast<const u32x4*>(a.hc)[at];
@@ -963,11 +964,19 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     }
     go(Large{});
   };
+  // four rows a work-group keep more of them busy, 16 use whole lines of the parts (4 / 16: 207 rows of 32,003 x 264 62 / 64 us
+  // the call, 701 of 201,088 the same, 7,296 of 151,936 57 / 25 the launch)
+  auto by_rows = [&](auto go) {
+    if (most <= 1024) go(mode_c<4>{});
+    else go(mode_c<16>{});
+  };
   hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a, pieces);
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
   if (!one_pass) {
     product(z_small, mode_c<kStats>{}, 0, V, 0);
-    hipLaunchKernelGGL(k_lce_lse, dim3(L.Mp / kRowsOf), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+    by_rows([&](auto r) {
+      hipLaunchKernelGGL((k_lce_lse<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, (V + wave - 1) / wave);
+    });
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
@@ -977,7 +986,10 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
         if (piece < pieces - 1)
           hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece, wave);
         else
-          hipLaunchKernelGGL(k_lce_close, dim3(L.Mp / kRowsOf), dim3(1024), 0, st, a, (V + wave - 1) / wave, v0, nv, piece, wave);
+          by_rows([&](auto r) {
+            hipLaunchKernelGGL((k_lce_close<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, (V + wave - 1) / wave, v0, nv, piece,
+                               wave);
+          });
       } else {
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }

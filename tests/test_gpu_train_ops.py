@@ -767,3 +767,16 @@ def test_linear_ce_of_few_rows(n, B, V, H):
         lce_check(h, head, y, B, 4.5, got)
         again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
         assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))
+
+
+@pytest.mark.parametrize("n,B,V,H", [(100, 16, 3001, 264), (64, 17, 1000, 72), (65, 17, 1000, 72)])
+def test_linear_ce_of_one_piece_and_many_rows(n, B, V, H):
+    """Around 1,024 rows with a loss; plain, and with words that take a reference of their own."""
+    h, head, y = lce_inputs(n, B, V, H, seed=31, ignored=0.0)
+    for dh, dw in ((False, False), (True, False), (True, True)):
+        lce_check(h, head, y, B, 4.5, dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw))
+    h, head, y = lce_inputs(n, B, V, H, seed=32, lean=0.0)
+    h[:, 0] = torch.where(torch.arange(n * B, device="cuda") % 3 == 0, 100.0, 0.0).to(BF)
+    head[V // 3, 0], head[V - 1, 0] = 3.0, 5.0
+    for dw in (False, True):
+        lce_check(h, head, y, B, 4.5, dfl.linear_ce(h, head, y, B, 4.5, need_dhead=dw))
