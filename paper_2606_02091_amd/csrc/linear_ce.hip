@@ -85,9 +85,10 @@ struct Lce {
   float *ref, *fac;
   int* flag;
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
-  float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far
+  float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far; then [dw_parts][V][H] dW
   int Mp, ldh, Vp;
   int stages;     // stages of k of the first (longest) piece
+  int dw_parts;   // dW's rows are split into
   int dh_tile;    // dh on the large tile (0), the small one, or that for few rows
 };
 
@@ -579,20 +580,25 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         }
     }
   } else {
-    if (!tile_of(blockIdx.x, (a.H + TM - 1) / TM, (nv + TN - 1) / TN, ta, tb)) return;
-    const int m0 = ta * TM, n0 = tb * TN;
-    product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + m0, a.ldh, min(a.ldh - m0, TM), a.Mp},
-                        Operand{a.dz + (long)(n0 / kBlock) * a.Mp * kBlock + n0 % kBlock, kBlock, TN, a.Mp}, n, lds, acc, [&](Acc<S>& d) {
+    const int na = (a.H + TM - 1) / TM, stages = (n + kBK - 1) / kBK;
+    int unit;
+    if (!tile_of(blockIdx.x, na * a.dw_parts, (nv + TN - 1) / TN, unit, tb)) return;
+    const int ks = unit / na, m0 = unit % na * TM, n0 = tb * TN;
+    // this part's rows: whole stages
+    const int i_first = (int)((long)stages * ks / a.dw_parts) * kBK, i_end = min((int)((long)stages * (ks + 1) / a.dw_parts) * kBK, n);
+    product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
+                        Operand{a.dz + ((long)(n0 / kBlock) * a.Mp + i_first) * kBlock + n0 % kBlock, kBlock, TN, a.Mp - i_first},
+                        max(i_end - i_first, 0), lds, acc, [&](Acc<S>& d) {
       // the label terms: the rows whose label is one of the wave's words, in order
       const int word0 = v0 + n0 + wn * WN;
       const uint16_t* col = a.hc + m0 + wm * WM + 4 * h;
       const int most = a.ldh - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
-      for (int i0 = 0; i0 < n; i0 += 256) {
+      for (int i0 = i_first; i0 < i_end; i0 += 256) {
         int y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int i = i0 + 64 * k + lane;
-          y[k] = i < n ? a.word[i] - word0 : -1;
+          y[k] = i < i_end ? a.word[i] - word0 : -1;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -619,6 +625,23 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         }
       }
     });
+    if (a.dw_parts > 1) {
+      float* out = a.dacc + ((long)ks * nv + n0) * a.H;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int wl = wn * WN + j * 32 + (lane & 31);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int m = m0 + wm * WM + t * 32 + q * 8 + 4 * h;
+            if (n0 + wl < nv && m < a.H)
+              *reinterpret_cast<f32x4*>(out + (long)wl * a.H + m) =
+                  f32x4{acc[t][j][4 * q], acc[t][j][4 * q + 1], acc[t][j][4 * q + 2], acc[t][j][4 * q + 3]};
+          }
+      }
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j) put_tile<S>(lds, acc, j, wn * WN + j * 32 + (lane & 31), wm * MT, h);
     __syncthreads();
@@ -801,6 +824,20 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
   if (g == 0) reinterpret_cast<u32x4*>(a.dhidden)[at] = out;
 }
 
+// dhead from its parts; rounded once
+__global__ __launch_bounds__(256) void k_lce_dhead(Lce a) {
+  const long at = blockIdx.x * 256l + threadIdx.x, n = (long)a.V * a.H / 8;
+  if (at >= n) return;
+  const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc) + 2 * at;
+  f32x4 x = from[0], y = from[1];
+#pragma unroll 4
+  for (int k = 1; k < a.dw_parts; ++k) {
+    x += from[k * 2 * n];
+    y += from[k * 2 * n + 1];
+  }
+  reinterpret_cast<u32x4*>(a.dhead)[at] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
+}
+
 // ---- host side ----
 template <int N>
 using mode_c = std::integral_constant<int, N>;
@@ -843,7 +880,9 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   // (bounds of what is used that grow with every size: a workspace for the largest call serves the smaller ones)
   const size_t tile = (size_t)L.Mp * kBlock * 2, values = (size_t)L.Mp * H;
   if (dhidden || dhead) take(L.dz, std::min(tile * words, std::max(kDzBytes, tile)));
-  if (dhidden) take(L.dacc, std::max(values, std::min(kMostParts * values, (size_t)512 * 65536)) * 4);
+  const size_t dh = std::max(values, std::min(kMostParts * values, (size_t)512 * 65536)),
+               dw = std::min(kMostParts * (size_t)V * H, (size_t)512 * 65536);
+  if (dhidden || dhead) take(L.dacc, std::max(dhidden ? dh : 0, dhead ? dw : 0) * 4);
   L.total = o;
   return L;
 }
@@ -948,13 +987,27 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   const bool few = most <= Few::TN;
   a.dh_tile = few ? 2 : dh_small;
   static_assert(Few::MT == Small::MT, "a wave's words");
+  // dW of few tiles is split over its rows: the least time, in stages of 1.8 us, of rounds of work-groups, each with its
+  // stages, 8 more for its start and its end, and its labels' rows, which a wave adds one by one, and of the parts' sum
+  a.dw_parts = 1;
+  if (dhead && one_pass) {
+    const long t = tiles(Large{}, H, V), stages = (most + kBK - 1) / kBK, labels = (long)most * 64 / V;
+    long best = LONG_MAX;
+    for (long k = 1; k <= kMostParts && (k == 1 || (t * k <= 512 && stages >= 4 * k)); ++k) {
+      const long cost = (t * k + 255) / 256 * ((stages + k - 1) / k + 8 + labels / k) + (k > 1 ? 3 + (long)V * H * k / 1450000 : 0);
+      if (cost < best) {
+        best = cost;
+        a.dw_parts = (int)k;
+      }
+    }
+  }
   const int wave = z_small || few ? Small::MT * 32 : Large::MT * 32;
   auto grid = [](long tiles) { return (unsigned)((tiles + 7) / 8 * 8); };  // whole turns of the XCDs
   auto product = [&](bool small, auto mode, int v0, int nv, int piece) {
     constexpr int MODE = decltype(mode)::value;
     auto go = [&](auto s) {
       using S = decltype(s);
-      long t = MODE <= kExp ? tiles(s, nv, most) : MODE == kDw ? tiles(s, H, nv) : tiles(s, H, most);
+      long t = MODE <= kExp ? tiles(s, nv, most) : MODE == kDw ? tiles(s, H, nv) * a.dw_parts : tiles(s, H, most);
       if (MODE == kDh) t = std::max(t, std::min(kMostParts * t, 2l * dh_slots(a.dh_tile)));  // (the most that the plan makes)
       hipLaunchKernelGGL((k_lce_product<S, MODE>), dim3(grid(t)), dim3(S::T), 0, st, a, v0, nv, piece);
     };
@@ -994,7 +1047,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }
       if (dhidden) product(dh_small, mode_c<kDh>{}, v0, nv, piece);
-      if (dhead) product(false, mode_c<kDw>{}, v0, nv, piece);
+      if (dhead && !one_pass) product(false, mode_c<kDw>{}, v0, nv, piece);
     }
   if (dhidden) {
     // few values have many parts: 16 threads share their sum (207 rows x 264, 64 parts: 18 -> 7 us)
@@ -1006,6 +1059,10 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     else go(k_lce_dhidden<1>, 1);
   } else {
     hipLaunchKernelGGL(k_lce_loss, dim3(1), dim3(256), 0, st, a);
+  }
+  if (dhead && one_pass) {  // (in parts it takes the place of dh's sums)
+    product(false, mode_c<kDw>{}, 0, V, 0);
+    if (a.dw_parts > 1) hipLaunchKernelGGL(k_lce_dhead, dim3((unsigned)(((long)V * H / 8 + 255) / 256)), dim3(256), 0, st, a);
   }
   return hipGetLastError() == hipSuccess ? DFLARE_OK : DFLARE_ERR_HIP;
 }

@@ -780,3 +780,16 @@ def test_linear_ce_of_one_piece_and_many_rows(n, B, V, H):
     head[V // 3, 0], head[V - 1, 0] = 3.0, 5.0
     for dw in (False, True):
         lce_check(h, head, y, B, 4.5, dfl.linear_ce(h, head, y, B, 4.5, need_dhead=dw))
+
+
+@pytest.mark.parametrize("n,B,V,H,ignored", [(200, 16, 300, 264, 0.0), (200, 16, 300, 264, 0.6), (512, 16, 1000, 1024, 0.0), (300, 9, 1, 8, 0.0),
+                                             (64, 33, 777, 520, 0.3), (130, 16, 4000, 72, 0.0)])
+def test_linear_ce_of_few_words_and_many_rows(n, B, V, H, ignored):
+    """Many rows of every label: dhead's rows are split into parts."""
+    print(f"[train ops] linear ce of few words {(n, B, V, H)}", flush=True)
+    h, head, y = lce_inputs(n, B, V, H, seed=41, ignored=ignored)
+    for dh in (False, True):
+        got = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
+        lce_check(h, head, y, B, 4.5, got)
+        again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
+        assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))
