@@ -589,10 +589,35 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
     product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
                         Operand{a.dz + ((long)(n0 / kBlock) * a.Mp + i_first) * kBlock + n0 % kBlock, kBlock, TN, a.Mp - i_first},
                         max(i_end - i_first, 0), lds, acc, [&](Acc<S>& d) {
-      // the label terms: the rows whose label is one of the wave's words, in order
+      // The label terms: the rows whose label is one of the wave's words, in order.  A lane keeps the next row of each of its
+      // two words; when one would have a second, all that are kept are added at once.  (One row at a time, by the wave: 7,300
+      // rows of 1,000 words x 4,096 582 us the call against 378.)
+      static_assert(NT == 2, "a lane's words");
       const int word0 = v0 + n0 + wn * WN;
       const uint16_t* col = a.hc + m0 + wm * WM + 4 * h;
       const int most = a.ldh - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
+      int kept[2] = {-1, -1};
+      uint64_t taken = 0;  // words that have a row
+      auto add_kept = [&] {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (kept[j] >= 0) {
+            const float f = -a.lab[kept[j]];
+            const uint16_t* row = col + (long)kept[j] * a.ldh;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const u32x2 v = *reinterpret_cast<const u32x2*>(row + min(t * 32 + q * 8, most));
+                const f32x4 x = unpack4(v[0], v[1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[t][j][4 * q + e] = fmaf(f, x[e], d[t][j][4 * q + e]);
+              }
+          }
+          kept[j] = -1;
+        }
+        taken = 0;
+      };
       for (int i0 = i_first; i0 < i_end; i0 += 256) {
         int y[4];
 #pragma unroll
@@ -604,26 +629,18 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         for (int k = 0; k < 4; ++k) {
           uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < (unsigned)WN);
           while (hit) {
-            const int b = __builtin_ctzll(hit), i = i0 + 64 * k + b, wl = __builtin_amdgcn_readlane(y[k], b);
+            const int b = __builtin_ctzll(hit), wl = __builtin_amdgcn_readlane(y[k], b);
             hit &= hit - 1;
-            const float f = (lane & 31) == (wl & 31) ? -a.lab[i] : 0.f;
-            const uint16_t* row = col + (long)i * a.ldh;
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const u32x2 v = *reinterpret_cast<const u32x2*>(row + min(t * 32 + q * 8, most));
-                const f32x4 x = unpack4(v[0], v[1]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  static_assert(NT == 2, "a wave's words");
-                  if (wl < 32) d[t][0][4 * q + e] = fmaf(f, x[e], d[t][0][4 * q + e]);
-                  else d[t][1][4 * q + e] = fmaf(f, x[e], d[t][1][4 * q + e]);
-                }
-              }
+            if (taken >> wl & 1) add_kept();
+            taken |= 1ull << wl;
+            if ((lane & 31) == (wl & 31)) {
+              if (wl < 32) kept[0] = i0 + 64 * k + b;
+              else kept[1] = i0 + 64 * k + b;
+            }
           }
         }
       }
+      if (taken) add_kept();
     });
     if (a.dw_parts > 1) {
       float* out = a.dacc + ((long)ks * nv + n0) * a.H;
@@ -988,13 +1005,13 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.dh_tile = few ? 2 : dh_small;
   static_assert(Few::MT == Small::MT, "a wave's words");
   // dW of few tiles is split over its rows: the least time, in stages of 1.8 us, of rounds of work-groups, each with its
-  // stages, 8 more for its start and its end, and its labels' rows, which a wave adds one by one, and of the parts' sum
+  // stages, 8 more for its start and its end, its labels' rows (added some 10 at a time), and of the parts' sum
   a.dw_parts = 1;
   if (dhead && one_pass) {
     const long t = tiles(Large{}, H, V), stages = (most + kBK - 1) / kBK, labels = (long)most * 64 / V;
     long best = LONG_MAX;
     for (long k = 1; k <= kMostParts && (k == 1 || (t * k <= 512 && stages >= 4 * k)); ++k) {
-      const long cost = (t * k + 255) / 256 * ((stages + k - 1) / k + 8 + labels / k) + (k > 1 ? 3 + (long)V * H * k / 1450000 : 0);
+      const long cost = (t * k + 255) / 256 * ((stages + k - 1) / k + 8 + labels / (8 * k)) + (k > 1 ? 3 + (long)V * H * k / 1450000 : 0);
       if (cost < best) {
         best = cost;
         a.dw_parts = (int)k;
