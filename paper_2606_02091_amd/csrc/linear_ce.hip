@@ -77,13 +77,12 @@ struct Lce {
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
   uint16_t* hs;   // [Mp][ldh] hc times fac, where dW comes from one piece; else null
-  float2* part;   // [words / a wave's][Mp] (max log2 e, sum of exp(z - max)); one pass: (R, sum of 2^(z log2 e - R))
+  float2* part;   // [words / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), the label's word left out
   float* zlab;    // [Mp] z at the label
-  float* lse2;    // [Mp] log2-domain log-sum-exp
   float* lab;     // [Mp] c (1 - p of the label)
-  // one pass: the rows' references R (log2 domain) and c / sum at the end; flags of the pieces
-  float *ref, *fac;
-  int* flag;
+  float *ref, *fac;  // [Mp] a row's reference, and c over its sum (the label's word in it)
+  bool one_pass;  // dz is 2^(z log2 e - R); otherwise at its final scale
+  int* flag;      // of the pieces in one pass: a word took a reference of its own
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
   float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far; then [dw_parts][V][H] dW
   int Mp, ldh, Vp;
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   const int row = i < n ? a.src[i] : 0;
   const u32x4* from = reinterpret_cast<const u32x4*>(a.hidden + (long)row * a.H);
   u32x4* to = reinterpret_cast<u32x4*>(a.hc + (long)i * a.ldh);
-  const bool dot = a.ref && i < n;
+  const bool dot = a.one_pass && i < n;
   const u32x4* word = reinterpret_cast<const u32x4*>(a.head + (dot ? (long)a.word[i] * a.H : 0));
   float s = 0.f;
   for (int p = threadIdx.x; p < a.ldh / 8; p += 256) {
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
       }
     }
   }
-  if (!a.ref) return;
+  if (!a.one_pass) return;
   for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -512,9 +511,13 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
           if (vw + t * 32 + 8 * (e >> 2) + 4 * h + (e & 3) >= a.V) z = -INFINITY;
         });
       if constexpr (MODE == kStats) {
-        if (__builtin_amdgcn_ballot_w64(here)) {
+        if (__builtin_amdgcn_ballot_w64(here)) {  // (left out of the sum: 1 - p would be lost in it where p is nearly 1)
           float zl = 0.f;
-          each([&](int t, int e, float& z) { zl = t * 16 + e == le ? z : zl; });
+          each([&](int t, int e, float& z) {
+            const bool l = t * 16 + e == le;
+            zl = l ? z : zl;
+            z = l ? -INFINITY : z;
+          });
           if (here) a.zlab[i] = zl;
         }
         float m = -FLT_MAX, s = 0.f;
@@ -525,9 +528,9 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         if (h == 0) a.part[(long)(vw / WM) * a.Mp + i] = make_float2(m, s);
       } else {
         if constexpr (MODE == kDz) {
-          const float c = a.c[i], l = a.lse2[i];
+          const float c = a.c[i], f = a.fac[i], r = a.ref[i];
           each([&](int t, int e, float& z) {
-            z = c * ex2(fmaf(z, kL2E, -l));
+            z = f * ex2(fmaf(z, kL2E, -r));
             if (t * 16 + e == le || c == 0.f) z = 0.f;
           });
         } else {
@@ -669,7 +672,17 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
 
 // A row's values from its parts: work-groups of 1,024 threads take R rows, each by 1,024 / R groups of parts
 
-// log-sum-exp of every row from its parts, and its cross-entropy
+// The cross-entropy of row i, log(1 + s / 2^y), s and the label's 2^y (y = z log2 e - r) on the reference r; what the gradients take
+__device__ __forceinline__ float close_row(const Lce& a, int i, float s, float r) {
+  const float y = fmaf(a.zlab[i], kL2E, -r), ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey), f = c * inv;
+  a.fac[i] = f;
+  a.lab[i] = c * (s * inv);
+  // far below the reference 2^y may be 0
+  a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
+  return f;
+}
+
+// a row's sum from its parts, and its cross-entropy
 template <int R>
 __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
   __shared__ float2 sh[16][R];
@@ -691,11 +704,9 @@ __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
   __syncthreads();
   if (g != 0 || i >= n) return;
   for (int k = 1; k < 16; ++k) add(sh[k][l].x, sh[k][l].y);
-  const float lse = m + log2f(s);
-  const float ce = (lse - a.zlab[i] * kL2E) * 0.6931471805599453f;
-  a.lse2[i] = lse;
-  a.lab[i] = a.c[i] * -expm1f(-ce);
-  a.row_ce[a.src[i]] = ce;
+  const float r = fmaxf(m, a.zlab[i] * kL2E);  // of all words: 2^y is 1 at most
+  a.ref[i] = r;
+  close_row(a, i, s * ex2(m - r), r);
 }
 
 // Row i of a piece in which some words took a reference of their own: the row's reference becomes the highest of them
@@ -773,11 +784,7 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, in
   __syncthreads();
   if (g == 0 && i < n) {
     for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
-    const float y = a.zlab[i] * kL2E - r, ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey);
-    a.fac[i] = fac[l] = c * inv;
-    a.lab[i] = c * (s * inv);
-    // log((s + ey) / ey); far below the reference ey may be 0
-    a.row_ce[a.src[i]] = y > -60.f ? log1pf(s / ey) : (log2f(s + ey) - y) * 0.6931471805599453f;
+    fac[l] = close_row(a, i, s, r);
   }
   if (!a.hs) return;
   __syncthreads();
@@ -818,7 +825,7 @@ __global__ __launch_bounds__(256) void k_lce_dhidden(Lce a) {
   u32x4 out = {0u, 0u, 0u, 0u};
   if (i >= 0) {
     const DhPlan plan(a, a.count[0]);
-    const float f = a.ref ? a.fac[i] : 1.f, fl = a.lab[i];
+    const float f = a.one_pass ? a.fac[i] : 1.f, fl = a.lab[i];
     const u32x4 v = reinterpret_cast<const u32x4*>(a.head + (long)a.word[i] * a.H)[p];
     const f32x4* from = reinterpret_cast<const f32x4*>(a.dacc + (long)i * a.H) + 2 * p;
     const long step = plan.part_rows() * a.H / 4;
@@ -862,7 +869,7 @@ using mode_c = std::integral_constant<int, N>;
 constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
 
 struct LceLayout {
-  size_t count, src, pos, word, c, hc, hs, part, zlab, lse2, ref, fac, lab, flag, dz, dacc, total;
+  size_t count, src, pos, word, c, hc, hs, part, zlab, ref, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -890,7 +897,6 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   if (dhead) take(L.hs, (size_t)L.Mp * L.ldh * 2);
   take(L.part, (size_t)words * L.Mp * 32);  // (64 words of a wave of the small tile)
   take(L.zlab, (size_t)L.Mp * 4);
-  take(L.lse2, (size_t)L.Mp * 4);
   take(L.ref, (size_t)L.Mp * 4);
   take(L.fac, (size_t)L.Mp * 4);
   take(L.lab, (size_t)L.Mp * 4);
@@ -972,7 +978,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.hc = (uint16_t*)(w + L.hc);
   a.part = (float2*)(w + L.part);
   a.zlab = (float*)(w + L.zlab);
-  a.lse2 = (float*)(w + L.lse2);
+  a.ref = (float*)(w + L.ref);
+  a.fac = (float*)(w + L.fac);
   a.dz = (uint16_t*)(w + L.dz);
   a.dacc = (float*)(w + L.dacc);
   a.Mp = L.Mp;
@@ -982,10 +989,9 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   const int words = (int)((V + (long)kBlock - 1) / kBlock);
   const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);
   const bool one_pass = dhead ? pieces == 1 : dhidden != nullptr;
+  a.one_pass = one_pass;
   if (one_pass) {
     if (dhead) a.hs = (uint16_t*)(w + L.hs);
-    a.ref = (float*)(w + L.ref);
-    a.fac = (float*)(w + L.fac);
     a.flag = (int*)(w + L.flag);
   }
   // The small tile wastes less where rows or tiles are few.  A round of its work-groups takes about 5/8 of a large

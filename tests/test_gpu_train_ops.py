@@ -793,3 +793,61 @@ def test_linear_ce_of_few_words_and_many_rows(n, B, V, H, ignored):
         lce_check(h, head, y, B, 4.5, got)
         again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
         assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))
+
+
+# ---- rows whose label takes all ----
+
+def peaked_inputs(n, B, V, H, low, high, seed):
+    """Label logits of low to high, those of the other words around zero."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    head = randn((V, H), seed=seed, std=0.02)
+    y = torch.randint(0, V, (n * B,), generator=g, device="cuda", dtype=torch.int32)
+    size = torch.empty((n * B, 1), device="cuda").uniform_(low, high, generator=g)
+    word = head[y.long()].float()
+    return (word * size / (word * word).sum(1, keepdim=True)).to(BF), head, y
+
+
+def peaked_check(h, head, y, B, gamma, got):
+    """As lce_check, but the error of 1 - p is relative to 1 - p and not to 1: cross-entropies and gradients far below 2^-24
+    have correct digits too."""
+    loss, ce, dh, dw = got
+    rows, H = h.shape
+    V = head.shape[0]
+    b = torch.arange(rows, device="cuda") % B
+    w = torch.where(b > 0, torch.exp(-(b - 1).double() / gamma), 0.0)
+    c = (w / w.sum())[:, None]
+    h64, w64, lab = torch.where(b[:, None] > 0, h.double(), 0.0), head.double(), y.long()[:, None]
+    z = h64 @ w64.t()
+    tz = float(2 * H * U * (h64.abs() @ w64.abs().t()).max() + 8 * U * z.abs().max())  # as in lce_check
+    d = (z - z.gather(1, lab)).scatter_(1, lab, float("-inf"))
+    del z
+    rest = torch.logsumexp(d, 1, keepdim=True)  # log of (1 - p) / p
+    total = torch.nn.functional.softplus(rest, threshold=700.0)
+    want_ce = torch.where(b > 0, torch.log1p(rest.exp())[:, 0], 0.0)
+    # sums of exponentials and their logarithm: a few units each, of values whose exponents are off by 2 tz
+    rel = math.expm1(2 * tz) + 64 * U
+    assert bool((ce >= 0).all())
+    within(ce, want_ce, rel * want_ce + 1e-44, "row_ce")
+    assert abs(float(loss) - float((c[:, 0] * want_ce).sum())) <= (rel + 2 * U) * float((c[:, 0] * want_ce).sum())
+    dz = (d - total).exp_()
+    del d
+    dz.scatter_(1, lab, -(rest - total).exp())
+    dz *= c
+    edz = dz.abs() * (rel + HALF[BF]) + (V * 2 * U) * dz.abs()
+    if dh is not None:
+        want = dz @ w64
+        within(dh, want, 1.01 * (edz @ w64.abs() + HALF[BF] * want.abs()) + 1e-37, "dhidden")
+    if dw is not None:
+        want = dz.t() @ h64
+        edz += (HALF[BF] + rows * 2 * U) * dz.abs()
+        within(dw, want, 1.01 * (edz.t() @ h64.abs() + HALF[BF] * want.abs()) + 1e-37, "dhead")
+
+
+# one piece of the vocabulary, and two
+@pytest.mark.parametrize("n,B,V,H,low,high", [(30, 11, 3333, 192, 25.0, 60.0), (5, 9, 700, 64, 30.0, 80.0), (256, 16, 70000, 64, 60.0, 75.0),
+                                              (8, 5, 1, 64, 20.0, 40.0)])
+def test_linear_ce_of_rows_whose_label_takes_all(n, B, V, H, low, high):
+    print(f"[train ops] linear ce of peaked rows {(n, B, V, H)}", flush=True)
+    h, head, y = peaked_inputs(n, B, V, H, low, high, seed=V)
+    for dh, dw in ((False, False), (True, False), (False, True), (True, True)):
+        peaked_check(h, head, y, B, 4.5, dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw))
