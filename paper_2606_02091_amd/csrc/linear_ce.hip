@@ -5,16 +5,18 @@
 // The rows with a loss are gathered first (the others take no part in any product).
 // The loss alone is one product, whose epilogue leaves every row's maximum and sum per wave's words.
 // With dh alone the vocabulary is walked once, in pieces, as one pass of a softmax: a piece's product leaves
-// 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit; a second
-// product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has the range of
-// fp32, so that R need not be the maximum: only values more than 2^40 times it (which a wave's words
-// then take as their own reference, raise a flag and have the row rescaled) move it.
+// 2^(z log2 e - R) in bf16 and the sums of these, R being a reference of the row, at first its label's logit to the
+// next whole number; a second product adds (these) W to dh, which is divided by the whole sum at the end.  bf16 has
+// the range of fp32, so that R need not be the maximum: only values more than 2^40 times it (which a wave's words
+// then take as their own reference, raise a flag and have the row rescaled) move it.  References are whole numbers,
+// so that what is rescaled is not rounded again.
 // dW needs dz of all words of a row at its final scale.  Where the vocabulary is one piece, the rows of h take the
 // scale instead (rounded to bf16; the labels' terms, most of dW, are not taken from them); otherwise the maxima
 // and sums come first, and each piece's logits are formed again: 2 rows V H operations more.
 // The label's word is left out of dz: its -c (1 - p), the largest value of its row, goes into dh and dW in fp32
 // (rounded to bf16 with the others it would be 0.7 of the gradients' whole error).
-// Bound by the matrix cores (up to some 128 rows by reading the head): 2 rows V H operations for the loss, 4 with dh, 6 with both from one piece, 8 from more.
+// Bound by the matrix cores (up to some 128 rows by reading the head): 2 rows V H operations for the loss, 4 with dh,
+// 6 with both from one piece, 8 from more.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256) void k_lce_gather(Lce a) {
   if (threadIdx.x == 0) {
     s = (red[0] + red[1]) + (red[2] + red[3]);
     a.zlab[i] = s;
-    a.ref[i] = s * kL2E;
+    a.ref[i] = rintf(s * kL2E);
   }
 }
 
@@ -540,7 +542,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
           m = fmaxf(m, __shfl_xor(m, 32)) * kL2E;
           const bool over = m > r + kRise;
           if (__builtin_amdgcn_ballot_w64(over) && lane == 0) a.flag[piece] = 1;
-          r = over ? m : r;
+          r = over ? rintf(m) : r;
           each([&](int, int, float& z) {
             z = ex2(fmaf(z, kL2E, -r));
             s += z;

@@ -851,3 +851,25 @@ def test_linear_ce_of_rows_whose_label_takes_all(n, B, V, H, low, high):
     h, head, y = peaked_inputs(n, B, V, H, low, high, seed=V)
     for dh, dw in ((False, False), (True, False), (False, True), (True, True)):
         peaked_check(h, head, y, B, 4.5, dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw))
+
+
+@pytest.mark.parametrize("n,B,V,H", [(12, 16, 4099, 64), (256, 16, 70000, 64)])
+def test_linear_ce_moved_references_round_nothing_again(n, B, V, H):
+    """The label 20 or 60 powers of two below all other words: the others' gradients are the same sums, which in the second
+    case are written against references that move.  Both differ by the rounding of exponents of about 20 (2^-20 of a
+    value, which turns one value in 4,000 to the next bf16, so 2^-13.5 of a sum, and one output in 60 to its next one: 2^-10.8
+    of the 2-norm at most); a second rounding of every value would add 2^-9.3 to each sum, 2^-9 with the outputs'."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    head = randn((V, H), seed=1, std=0.05)
+    y = torch.randint(0, 40, (n * B,), generator=g, device="cuda", dtype=torch.int32)  # the first 40 words are the labels
+    h = randn((n * B, H), seed=2, std=1.0 if V < 10000 else 0.05)  # (a sum of many words is mostly their common part otherwise)
+    h[:, 0] = 16.0
+    head[:, 0] = 0.0
+    head[:40, 1:] = 0.0
+    outs = []
+    for below in (20.0, 60.0):
+        head[:40, 0] = -below * math.log(2.0) / 16.0
+        outs.append(dfl.linear_ce(h, head, y, B, 4.5)[2][:, 1:].double())
+    on = torch.arange(n * B, device="cuda") % B > 0
+    assert outs[0][on].abs().max() > 0
+    assert float((outs[0] - outs[1]).norm()) <= 2.0 ** -10 * float(outs[0].norm())
