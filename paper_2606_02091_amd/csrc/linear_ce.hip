@@ -77,12 +77,12 @@ struct Lce {
   int* pos;       // [rows] row -> i, -1 without a loss
   int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
-  uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
-  uint16_t* hs;   // [Mp][ldh] hc times fac, where dW comes from one piece; else null
-  float2* part;   // [words / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), the label's word left out
+  uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile; times fac for dW from one piece
+  float2* part;   // [words of a piece / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), the label's word left out
   float* zlab;    // [Mp] z at the label
   float* lab;     // [Mp] c (1 - p of the label)
-  float *ref, *fac;  // [Mp] a row's reference, and c over its sum (the label's word in it)
+  float *ref, *sum;  // [Mp] a row's reference and its sum over the pieces so far
+  float* fac;     // [Mp] c over the whole sum (the label's word in it)
   bool one_pass;  // dz is 2^(z log2 e - R); otherwise at its final scale
   int* flag;      // of the pieces in one pass: a word took a reference of its own
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         m = fmaxf(fmaxf(m, __shfl_xor(m, 32)) * kL2E, -FLT_MAX);  // (finite where the wave has no words: they add 0)
         each([&](int, int, float& z) { s += ex2(fmaf(z, kL2E, -m)); });
         s += __shfl_xor(s, 32);
-        if (h == 0) a.part[(long)(vw / WM) * a.Mp + i] = make_float2(m, s);
+        if (h == 0) a.part[(long)((vw - v0) / WM) * a.Mp + i] = make_float2(m, s);
       } else {
         if constexpr (MODE == kDz) {
           const float c = a.c[i], f = a.fac[i], r = a.ref[i];
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
             s += z;
           });
           s += __shfl_xor(s, 32);
-          if (h == 0) a.part[(long)(vw / WM) * a.Mp + i] = make_float2(r, s);
+          if (h == 0) a.part[(long)((vw - v0) / WM) * a.Mp + i] = make_float2(r, s);
         }
         put_tile<S>(lds, acc, j, rl, wm * MT, h);
       }
@@ -591,7 +591,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
     const int ks = unit / na, m0 = unit % na * TM, n0 = tb * TN;
     // this part's rows: whole stages
     const int i_first = (int)((long)stages * ks / a.dw_parts) * kBK, i_end = min((int)((long)stages * (ks + 1) / a.dw_parts) * kBK, n);
-    product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
+    product<S, true, true>(Operand{a.hc + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
                         Operand{a.dz + ((long)(n0 / kBlock) * a.Mp + i_first) * kBlock + n0 % kBlock, kBlock, TN, a.Mp - i_first},
                         max(i_end - i_first, 0), lds, acc, [&](Acc<S>& d) {
       // The label terms: the rows whose label is one of the wave's words, in order.  A lane keeps the next row of each of its
@@ -600,16 +600,16 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
       // rows of 32,003 words x 2,560 4.1 ms where no label stands out, 4.1 with one in 5% of them, 11 where all are the same.
       static_assert(NT == 2, "a lane's words");
       const int word0 = v0 + n0 + wn * WN;
-      const uint16_t* col = a.hc + m0 + wm * WM + 4 * h;
-      const int most = a.ldh - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
-      int kept[2] = {-1, -1};
+      const uint16_t* col = a.hidden + m0 + wm * WM + 4 * h;
+      const int most = a.H - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
+      int kept[2] = {-1, -1}, from[2] = {0, 0};  // the rows' places among those with a loss, and in hidden
       uint64_t taken = 0;  // words that have a row
       auto add_kept = [&] {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (kept[j] >= 0) {
             const float f = -a.lab[kept[j]];
-            const uint16_t* row = col + (long)kept[j] * a.ldh;
+            const uint16_t* row = col + (long)from[j] * a.H;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -625,23 +625,25 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         taken = 0;
       };
       for (int i0 = i_first; i0 < i_end; i0 += 256) {
-        int y[4];
+        int y[4], src[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int i = i0 + 64 * k + lane;
           y[k] = i < i_end ? a.word[i] - word0 : -1;
+          src[k] = i < i_end ? a.src[i] : 0;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < (unsigned)WN);
           while (hit) {
-            const int b = __builtin_ctzll(hit), wl = __builtin_amdgcn_readlane(y[k], b);
+            const int b = __builtin_ctzll(hit), wl = __builtin_amdgcn_readlane(y[k], b), row = __builtin_amdgcn_readlane(src[k], b);
             hit &= hit - 1;
             if (taken >> wl & 1) add_kept();
             taken |= 1ull << wl;
             if ((lane & 31) == (wl & 31)) {
-              if (wl < 32) kept[0] = i0 + 64 * k + b;
-              else kept[1] = i0 + 64 * k + b;
+              const int j = wl >> 5;
+              if (j == 0) kept[0] = i0 + 64 * k + b, from[0] = row;
+              else kept[1] = i0 + 64 * k + b, from[1] = row;
             }
           }
         }
@@ -684,9 +686,9 @@ __device__ __forceinline__ float close_row(const Lce& a, int i, float s, float r
   return f;
 }
 
-// a row's sum from its parts, and its cross-entropy
+// After a piece of the first pass over the maxima: a row's sum so far from its parts; after the last, its cross-entropy
 template <int R>
-__global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
+__global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts, bool first, bool last) {
   __shared__ float2 sh[16][R];
   const int n = a.count[0], l = threadIdx.x % R, g = threadIdx.x / R, i = blockIdx.x * R + l;
   if ((int)blockIdx.x * R >= n) return;
@@ -706,6 +708,12 @@ __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
   __syncthreads();
   if (g != 0 || i >= n) return;
   for (int k = 1; k < 16; ++k) add(sh[k][l].x, sh[k][l].y);
+  if (!first) add(a.ref[i], a.sum[i]);
+  if (!last) {
+    a.ref[i] = m;
+    a.sum[i] = s;
+    return;
+  }
   const float r = fmaxf(m, a.zlab[i] * kL2E);  // of all words: 2^y is 1 at most
   a.ref[i] = r;
   close_row(a, i, s * ex2(m - r), r);
@@ -714,9 +722,9 @@ __global__ __launch_bounds__(1024) void k_lce_lse(Lce a, int parts) {
 // Row i of a piece in which some words took a reference of their own: the row's reference becomes the highest of them
 // (returned), and what was written under others, dh of the pieces before it included, is scaled to it.  By a
 // work-group; red: a float per wave.
-__device__ __forceinline__ float rebase_row(const Lce& a, int i, int v0, int nv, int piece, int wave, float* red) {
+__device__ __forceinline__ float rebase_row(const Lce& a, int i, int nv, int piece, int wave, float* red) {
   const int groups = (nv + wave - 1) / wave;  // groups of a wave's words
-  const float2* p = a.part + (long)(v0 / wave) * a.Mp + i;
+  const float2* p = a.part + i;
   const float old = a.ref[i];
   float r = old;
   for (int g = threadIdx.x; g < groups; g += blockDim.x) r = fmaxf(r, p[(long)g * a.Mp].x);
@@ -746,29 +754,24 @@ __device__ __forceinline__ float rebase_row(const Lce& a, int i, int v0, int nv,
   if (threadIdx.x == 0) a.ref[i] = r;
   return r;
 }
-__global__ __launch_bounds__(256) void k_lce_rebase(Lce a, int v0, int nv, int piece, int wave) {
-  __shared__ float red[4];
-  if (a.flag[piece] == 0) return;
-  const int n = a.count[0];
-  for (int i = blockIdx.x; i < n; i += gridDim.x) rebase_row(a, i, v0, nv, piece, wave, red);
-}
 
-// One pass, after the last piece's logits: its rows rescaled where it needs that, the rows' sums from their parts, their
-// cross-entropy and the factors of dh; with dhead hs = hc fac, zeros past the last row.  (In launches of their own
-// these made 207 rows x 32,003 x 264 6 us of 68 longer.)
+// One pass, after a piece's logits: its rows rescaled where it needs that, and the rows' sums so far from their parts; after the
+// last piece their cross-entropy and the factors of dh, and with dhead hc times these.  (In launches of their own these
+// made 207 rows x 32,003 x 264 6 us of 68 longer.)
 template <int R>
-__global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, int nv, int piece, int wave) {
+__global__ __launch_bounds__(1024) void k_lce_close(Lce a, int nv, int piece, bool last, int wave) {
   __shared__ float sh[16][R], red[16], ref[R], fac[R];
-  const int n = a.count[0], row0 = blockIdx.x * R;
-  if (row0 >= (a.hs ? (n + kBlock - 1) / kBlock * kBlock : n)) return;
+  const int n = a.count[0], row0 = blockIdx.x * R, parts = (nv + wave - 1) / wave;
+  if (row0 >= n) return;
   const int l = threadIdx.x % R, g = threadIdx.x / R, i = row0 + l;
+  const float old = i < n ? a.ref[i] : 0.f;
   if (threadIdx.x < R) {
-    ref[l] = i < n ? a.ref[i] : 0.f;
+    ref[l] = old;
     fac[l] = 0.f;
   }
   if (a.flag[piece])
     for (int k = 0; k < R && row0 + k < n; ++k) {
-      const float r = rebase_row(a, row0 + k, v0, nv, piece, wave, red);
+      const float r = rebase_row(a, row0 + k, nv, piece, wave, red);
       if (threadIdx.x == 0) ref[k] = r;
     }
   __syncthreads();
@@ -786,18 +789,20 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int parts, int v0, in
   __syncthreads();
   if (g == 0 && i < n) {
     for (int k = 1; k < 16; ++k) s += sh[k][l];  // all words but the label's
-    fac[l] = close_row(a, i, s, r);
+    if (piece > 0) s += a.sum[i] * ex2(old - r);
+    if (last) fac[l] = close_row(a, i, s, r);
+    else a.sum[i] = s;
   }
-  if (!a.hs) return;
+  if (!last || !a.dhead) return;
   __syncthreads();
   const int P = a.ldh / 8;
   for (int e = threadIdx.x; e < R * P; e += 1024) {
     const long at = (long)(row0 + e / P) * P + e % P;
     const float f = fac[e / P];
-    u32x4 v = reinterpret_cast<const u32x4*>(a.hc)[at];
+    u32x4 v = reinterpret_cast<u32x4*>(a.hc)[at];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
-    reinterpret_cast<u32x4*>(a.hs)[at] = v;
+    reinterpret_cast<u32x4*>(a.hc)[at] = v;
   }
 }
 
@@ -868,10 +873,11 @@ __global__ __launch_bounds__(256) void k_lce_dhead(Lce a) {
 // ---- host side ----
 template <int N>
 using mode_c = std::integral_constant<int, N>;
-constexpr size_t kDzBytes = 512u << 20;  // room for dz of a piece of the vocabulary
+constexpr size_t kDzBytes = 512u << 20;    // room for dz of a piece of the vocabulary
+constexpr size_t kPartBytes = 128u << 20;  // and for the parts of one (8,192 rows x 201,088 words, the loss alone: one piece)
 
 struct LceLayout {
-  size_t count, src, pos, word, c, hc, hs, part, zlab, ref, fac, lab, flag, dz, dacc, total;
+  size_t part_bytes, count, src, pos, word, c, hc, part, zlab, ref, sum, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -896,10 +902,12 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.word, (size_t)L.Mp * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
-  if (dhead) take(L.hs, (size_t)L.Mp * L.ldh * 2);
-  take(L.part, (size_t)words * L.Mp * 32);  // (64 words of a wave of the small tile)
+  // (a wave of the small tile has 64 words, so a piece with dz, of 2^28 logits or one block of words, has 32 MB or a block's)
+  L.part_bytes = std::min((size_t)words * L.Mp * 32, std::max(kPartBytes, (size_t)L.Mp * 32));
+  take(L.part, L.part_bytes);
   take(L.zlab, (size_t)L.Mp * 4);
   take(L.ref, (size_t)L.Mp * 4);
+  take(L.sum, (size_t)L.Mp * 4);
   take(L.fac, (size_t)L.Mp * 4);
   take(L.lab, (size_t)L.Mp * 4);
   take(L.flag, (size_t)words * 4);
@@ -981,6 +989,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.part = (float2*)(w + L.part);
   a.zlab = (float*)(w + L.zlab);
   a.ref = (float*)(w + L.ref);
+  a.sum = (float*)(w + L.sum);
   a.fac = (float*)(w + L.fac);
   a.dz = (uint16_t*)(w + L.dz);
   a.dacc = (float*)(w + L.dacc);
@@ -992,10 +1001,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);
   const bool one_pass = dhead ? pieces == 1 : dhidden != nullptr;
   a.one_pass = one_pass;
-  if (one_pass) {
-    if (dhead) a.hs = (uint16_t*)(w + L.hs);
-    a.flag = (int*)(w + L.flag);
-  }
+  if (one_pass) a.flag = (int*)(w + L.flag);
   // The small tile wastes less where rows or tiles are few.  A round of its work-groups takes about 5/8 of a large
   // one's time (151,936 words x 4,096, logits, large / small: 125 rows 399 / 330 us, 180 403 / 435, 300 614 / 564, 500
   // 649 / 755; 32,003 x 2,880: 180 85 / 69, 300 85 / 101, 640 169 / 145, 900 185 / 218); for dh, whose words are
@@ -1051,24 +1057,25 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   };
   hipLaunchKernelGGL(k_lce_rows, dim3(1), dim3(1024), 0, st, a, pieces);
   hipLaunchKernelGGL(k_lce_gather, dim3(L.Mp), dim3(256), 0, st, a);
-  if (!one_pass) {
-    product(z_small, mode_c<kStats>{}, 0, V, 0);
-    by_rows([&](auto r) {
-      hipLaunchKernelGGL((k_lce_lse<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, (V + wave - 1) / wave);
-    });
+  if (!one_pass) {  // in pieces whose parts have room
+    const int most_words = (int)std::min<size_t>(words, L.part_bytes / ((size_t)L.Mp * 8) * wave / kBlock);
+    const int turns = (words + most_words - 1) / most_words, step = (words + turns - 1) / turns * kBlock;
+    for (int v0 = 0; v0 < V; v0 += step) {
+      const int nv = std::min(V - v0, step);
+      product(z_small, mode_c<kStats>{}, v0, nv, 0);
+      by_rows([&](auto r) {
+        hipLaunchKernelGGL((k_lce_lse<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, (nv + wave - 1) / wave, v0 == 0, nv == V - v0);
+      });
+    }
   }
   if (dhidden || dhead)
     for (int piece = 0; piece < pieces; ++piece) {
       const int v0 = piece * L.Vp, nv = std::min(V - v0, L.Vp);
       if (one_pass) {
         product(z_small, mode_c<kExp>{}, v0, nv, piece);
-        if (piece < pieces - 1)
-          hipLaunchKernelGGL(k_lce_rebase, dim3(std::min(L.Mp, 1024)), dim3(256), 0, st, a, v0, nv, piece, wave);
-        else
-          by_rows([&](auto r) {
-            hipLaunchKernelGGL((k_lce_close<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, (V + wave - 1) / wave, v0, nv, piece,
-                               wave);
-          });
+        by_rows([&](auto r) {
+          hipLaunchKernelGGL((k_lce_close<r.value>), dim3(L.Mp / r.value), dim3(1024), 0, st, a, nv, piece, piece == pieces - 1, wave);
+        });
       } else {
         product(z_small, mode_c<kDz>{}, v0, nv, piece);
       }

@@ -873,3 +873,21 @@ def test_linear_ce_moved_references_round_nothing_again(n, B, V, H):
     on = torch.arange(n * B, device="cuda") % B > 0
     assert outs[0][on].abs().max() > 0
     assert float((outs[0] - outs[1]).norm()) <= 2.0 ** -10 * float(outs[0].norm())
+
+
+@pytest.mark.parametrize("lean", [1.0, 40.0])
+def test_linear_ce_of_many_pieces(lean):
+    """Many rows of which few carry a loss, a vocabulary in 17 pieces (and, without gradients, in pieces of its parts' room): as the
+    rows with a loss by themselves.  Then with words that move the references in some of the pieces."""
+    B, V, H, m = 16, 1100000, 8, 128
+    h, head, y = lce_inputs(256, B, V, H, seed=61, lean=lean)
+    y[m:] = -1
+    for words in ((), (7,), (40000, 300000, 1099999)):
+        w = head.clone()
+        for k, v in enumerate(words):
+            w[v, 0] = 4.0 + 3.0 * k
+            h[::3, 0] = 100.0
+        for dh, dw in ((False, False), (True, False), (True, True)):
+            loss, ce, gh, gw = dfl.linear_ce(h, w, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+            assert not ce[m:].any() and (gh is None or not gh[m:].any())
+            lce_check(h[:m], w, y[:m], B, 4.5, (loss, ce[:m], None if gh is None else gh[:m], gw))

@@ -48,6 +48,27 @@ def test_linear_ce_workspace():
     assert lce(ws=need - 1) == INV
 
 
+def test_linear_ce_workspace_does_not_grow_with_rows_times_words():
+    """Past the sizes at which a piece has its full room, twice the rows and twice the words need twice as much at most, and the words
+    alone some bytes each (the flags of pieces); one call's workspace serves every smaller call."""
+    ws = dfl.lib().dflare_linear_ce_workspace
+    for k in ((0, 0), (1, 0), (0, 1), (1, 1)):
+        for rows, V, H in ((8192, 151936, 4096), (65536, 100000, 64), (1 << 18, 50000, 1024), (1 << 19, 100000, 64), (1 << 20, 40000, 8)):
+            one, words, both = ws(rows, V, H, *k), ws(rows, 2 * V, H, *k), ws(2 * rows, 2 * V, H, *k)
+            assert 0 < one <= words <= both
+            assert both <= 2 * one + (1 << 16), (rows, V, H, k)
+            assert words - one <= V, (rows, V, H, k)
+        # the rows themselves once (dhidden: and their sums), dz and the parts up to their room
+        assert ws(1 << 20, 200000, 64, *k) <= (1 << 20) * 64 * (2 + 4 * k[0]) + (1 << 20) * 64 + (512 + 128 + 128 << 20) + (1 << 20)
+    rng = np.random.default_rng(3)
+    for _ in range(3000):
+        big = [int(2 ** rng.uniform(0, m)) for m in (22, 20)] + [8 * int(2 ** rng.uniform(0, 10))]
+        small = [int(rng.integers(1, v + 1)) for v in big[:2]] + [8 * int(rng.integers(1, big[2] // 8 + 1))]
+        for k in ((0, 0), (1, 0), (0, 1), (1, 1)):
+            if ws(*big, *k):
+                assert ws(*small, *k) <= ws(*big, *k), (small, big, k)
+
+
 def rope(n=1, rows=4, B=1, hd=64, rot=64, dtype=dfl.BF16, layout=0, scale=1.0, pos=P, freq=P, x=P, y=2 * P, heads=2,
          strides=(128, 64, 128, 64), tab=True):
     t = (dfl.dflare_rope_tensor * 2)(*[dfl.dflare_rope_tensor(x, y, *strides, heads)] * 2)
