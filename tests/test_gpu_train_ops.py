@@ -891,3 +891,65 @@ def test_linear_ce_of_many_pieces(lean):
             loss, ce, gh, gw = dfl.linear_ce(h, w, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
             assert not ce[m:].any() and (gh is None or not gh[m:].any())
             lce_check(h[:m], w, y[:m], B, 4.5, (loss, ce[:m], None if gh is None else gh[:m], gw))
+
+
+# ---- no word and no row of a product is lost ----
+
+def near_in_norm(got, want, err, what):
+    """Roundings that are independent of one another: the 2-norm of the difference against that of the values' errors `err`
+    (elementwise, root mean square)."""
+    off, most = float((got.double() - want).norm()), float(err.norm())
+    assert off <= 1.1 * most, (what, off, most)
+
+
+def sparse_inputs(rows, B, targets, V, H, seed):
+    """Row r's probability is all on word targets[k] for the k-th row with a loss, its label another word; the last word of
+    a stage, a part or a piece that is lost then changes dhidden of its row and dhead of its word by all of them."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    head = torch.where(torch.rand((V, H), generator=g, device="cuda") < 0.5, 0.5, -0.5).to(BF)
+    b = torch.arange(rows, device="cuda") % B
+    on = torch.nonzero(b > 0)[:, 0]
+    t = torch.full((rows,), -1, device="cuda")
+    t[on] = targets[torch.arange(on.numel(), device="cuda") % targets.numel()]
+    y = torch.where(b > 0, (t + V // 2) % V, 0).to(torch.int32)
+    h = torch.where(t[:, None] >= 0, head[t.clamp_min(0)].float(), 0.0) * (600.0 / H)
+    return h.to(BF), head, y
+
+
+# targets: the first and the last word of every stage of 64 words, as many as there are rows, from a start that moves; on each of
+# the tiles, with one piece of the vocabulary and two
+@pytest.mark.parametrize("n,B,V,H,calls", [(23, 9, 32003, 264, 6), (5, 13, 3001, 512, 2), (40, 16, 5000, 328, 1), (256, 16, 70000, 256, 1),
+                                           (1, 128, 1100000, 64, 3), (9, 8, 12801, 1024, 4), (200, 16, 300, 264, 1), (260, 16, 20011, 520, 1)])
+def test_linear_ce_keeps_every_word_and_row(n, B, V, H, calls):
+    ends = torch.arange(V, device="cuda")
+    ends = ends[(ends % 64 == 0) | (ends % 64 == 63) | (ends == V - 1)]
+    rows, m = n * B, n * (B - 1)
+    for k in range(calls):
+        print(f"[train ops] linear ce keeps words and rows {(n, B, V, H, k)}", flush=True)
+        # the last words in every call, the others in turn (where they are too many: evenly spread)
+        mine = torch.cat([ends[-4:], ends[(torch.arange(max(m - 4, 1), device="cuda") * max(1, ends.numel() // (m * calls)) + k * (m - 4)) % ends.numel()]])
+        h, head, y = sparse_inputs(rows, B, mine, V, H, seed=k)
+        for dw in (False, True):
+            lce_check(h, head, y, B, 9.0, dfl.linear_ce(h, head, y, B, 9.0, need_dhead=dw))
+
+
+@pytest.mark.parametrize("n,B,V,H,ignored", [(23, 9, 32003, 264, 0.1), (5, 13, 3001, 4096, 0.1), (256, 16, 70000, 64, 0.05), (17, 16, 1000, 512, 0.0),
+                                             (512, 16, 1000, 1024, 0.0), (13, 6, 40001, 72, 0.0)])
+def test_linear_ce_gradients_in_the_norm(n, B, V, H, ignored):
+    """A rounding to bf16 is off by 2^-8 / sqrt(3) of the value in the root mean square, at most.  dhidden: those of dz and of the result;
+    dhead: those of dz, of the scaled rows and of the result; the labels' terms are not rounded on the way."""
+    h, head, y = lce_inputs(n, B, V, H, seed=51, ignored=ignored, lean=100.0 / H)
+    _, _, dh, dw = dfl.linear_ce(h, head, y, B, 4.5, need_dhead=True)
+    only = dfl.linear_ce(h, head, y, B, 4.5)[2]
+    b = torch.arange(n * B, device="cuda") % B
+    on = (b > 0) & (y >= 0) & (y < V)
+    w = torch.where(on, torch.exp(-(b - 1).double() / 4.5), 0.0)
+    h64, w64, lab = torch.where(on[:, None], h.double(), 0.0), head.double(), torch.where(on, y, 0).long()[:, None]
+    dz = torch.softmax(h64 @ w64.t(), 1) * (w / w.sum())[:, None]
+    square = (dz * dz).scatter_(1, lab, 0.0)
+    dz.scatter_add_(1, lab, -(w / w.sum())[:, None])
+    want, want_w = dz @ w64, dz.t() @ h64
+    half = HALF[BF] / math.sqrt(3.0)
+    for got in (dh, only):
+        near_in_norm(got, want, half * (want * want + square @ (w64 * w64)).sqrt(), "dhidden")
+    near_in_norm(dw, want_w, half * (want_w * want_w + 2 * (square.t() @ (h64 * h64))).sqrt(), "dhead")
