@@ -77,7 +77,8 @@ struct Lce {
   int* pos;       // [rows] row -> i, -1 without a loss
   int* word;      // [Mp] i -> label, -1 past the last
   float* c;       // [Mp] w / sum w, 0 past the last
-  uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile; times fac for dW from one piece
+  uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
+  uint16_t* hs;   // [Mp][ldh] hc times fac, for dW from one piece: a place of its own, or hc's; else null
   float2* part;   // [words of a piece / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), the label's word left out
   float* zlab;    // [Mp] z at the label
   float* lab;     // [Mp] c (1 - p of the label)
@@ -591,7 +592,7 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
     const int ks = unit / na, m0 = unit % na * TM, n0 = tb * TN;
     // this part's rows: whole stages
     const int i_first = (int)((long)stages * ks / a.dw_parts) * kBK, i_end = min((int)((long)stages * (ks + 1) / a.dw_parts) * kBK, n);
-    product<S, true, true>(Operand{a.hc + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
+    product<S, true, true>(Operand{(a.hs ? a.hs : a.hc) + (long)i_first * a.ldh + m0, a.ldh, min(a.ldh - m0, TM), a.Mp - i_first},
                         Operand{a.dz + ((long)(n0 / kBlock) * a.Mp + i_first) * kBlock + n0 % kBlock, kBlock, TN, a.Mp - i_first},
                         max(i_end - i_first, 0), lds, acc, [&](Acc<S>& d) {
       // The label terms: the rows whose label is one of the wave's words, in order.  A lane keeps the next row of each of its
@@ -600,16 +601,18 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
       // rows of 32,003 words x 2,560 4.1 ms where no label stands out, 4.1 with one in 5% of them, 11 where all are the same.
       static_assert(NT == 2, "a lane's words");
       const int word0 = v0 + n0 + wn * WN;
-      const uint16_t* col = a.hidden + m0 + wm * WM + 4 * h;
-      const int most = a.H - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
-      int kept[2] = {-1, -1}, from[2] = {0, 0};  // the rows' places among those with a loss, and in hidden
+      const bool scaled = a.hs == a.hc;  // hc holds hs: the rows themselves are read where they came from
+      const long ld = scaled ? a.H : a.ldh;
+      const uint16_t* col = (scaled ? a.hidden : a.hc) + m0 + wm * WM + 4 * h;
+      const int most = (int)ld - 4 - (m0 + wm * WM + 4 * h);  // (columns past the last are not kept)
+      int kept[2] = {-1, -1};
       uint64_t taken = 0;  // words that have a row
       auto add_kept = [&] {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (kept[j] >= 0) {
             const float f = -a.lab[kept[j]];
-            const uint16_t* row = col + (long)from[j] * a.H;
+            const uint16_t* row = col + (scaled ? a.src[kept[j]] : kept[j]) * ld;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -625,25 +628,23 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
         taken = 0;
       };
       for (int i0 = i_first; i0 < i_end; i0 += 256) {
-        int y[4], src[4];
+        int y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int i = i0 + 64 * k + lane;
           y[k] = i < i_end ? a.word[i] - word0 : -1;
-          src[k] = i < i_end ? a.src[i] : 0;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint64_t hit = __builtin_amdgcn_ballot_w64((unsigned)y[k] < (unsigned)WN);
           while (hit) {
-            const int b = __builtin_ctzll(hit), wl = __builtin_amdgcn_readlane(y[k], b), row = __builtin_amdgcn_readlane(src[k], b);
+            const int b = __builtin_ctzll(hit), wl = __builtin_amdgcn_readlane(y[k], b);
             hit &= hit - 1;
             if (taken >> wl & 1) add_kept();
             taken |= 1ull << wl;
             if ((lane & 31) == (wl & 31)) {
-              const int j = wl >> 5;
-              if (j == 0) kept[0] = i0 + 64 * k + b, from[0] = row;
-              else kept[1] = i0 + 64 * k + b, from[1] = row;
+              if (wl < 32) kept[0] = i0 + 64 * k + b;
+              else kept[1] = i0 + 64 * k + b;
             }
           }
         }
@@ -756,13 +757,13 @@ __device__ __forceinline__ float rebase_row(const Lce& a, int i, int nv, int pie
 }
 
 // One pass, after a piece's logits: its rows rescaled where it needs that, and the rows' sums so far from their parts; after the
-// last piece their cross-entropy and the factors of dh, and with dhead hc times these.  (In launches of their own these
+// last piece their cross-entropy and the factors of dh, and with dhead hs.  (In launches of their own these
 // made 207 rows x 32,003 x 264 6 us of 68 longer.)
 template <int R>
 __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int nv, int piece, bool last, int wave) {
   __shared__ float sh[16][R], red[16], ref[R], fac[R];
   const int n = a.count[0], row0 = blockIdx.x * R, parts = (nv + wave - 1) / wave;
-  if (row0 >= n) return;
+  if (row0 >= (a.hs ? (n + kBlock - 1) / kBlock * kBlock : n)) return;
   const int l = threadIdx.x % R, g = threadIdx.x / R, i = row0 + l;
   const float old = i < n ? a.ref[i] : 0.f;
   if (threadIdx.x < R) {
@@ -793,16 +794,16 @@ __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int nv, int piece, bo
     if (last) fac[l] = close_row(a, i, s, r);
     else a.sum[i] = s;
   }
-  if (!last || !a.dhead) return;
+  if (!a.hs) return;
   __syncthreads();
   const int P = a.ldh / 8;
   for (int e = threadIdx.x; e < R * P; e += 1024) {
     const long at = (long)(row0 + e / P) * P + e % P;
     const float f = fac[e / P];
-    u32x4 v = reinterpret_cast<u32x4*>(a.hc)[at];
+    u32x4 v = reinterpret_cast<const u32x4*>(a.hc)[at];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
-    reinterpret_cast<u32x4*>(a.hc)[at] = v;
+    reinterpret_cast<u32x4*>(a.hs)[at] = v;
   }
 }
 
@@ -875,9 +876,12 @@ template <int N>
 using mode_c = std::integral_constant<int, N>;
 constexpr size_t kDzBytes = 512u << 20;    // room for dz of a piece of the vocabulary
 constexpr size_t kPartBytes = 128u << 20;  // and for the parts of one (8,192 rows x 201,088 words, the loss alone: one piece)
+// hs has a place of its own up to this size: 8,192 rows x 1,024 are scaled in 9.7 us there and in 13.7 in hc's place (of 156
+// the call with 1,000 words), x 4,096 in 24.0 and 24.5
+constexpr size_t kScaledBytes = 32u << 20;
 
 struct LceLayout {
-  size_t part_bytes, count, src, pos, word, c, hc, part, zlab, ref, sum, fac, lab, flag, dz, dacc, total;
+  size_t part_bytes, count, src, pos, word, c, hc, hs, part, zlab, ref, sum, fac, lab, flag, dz, dacc, total;
   int Mp, ldh, Vp;
 };
 
@@ -902,6 +906,7 @@ LceLayout lce_layout(int rows, int V, int H, bool dhidden, bool dhead) {
   take(L.word, (size_t)L.Mp * 4);
   take(L.c, (size_t)L.Mp * 4);
   take(L.hc, (size_t)L.Mp * L.ldh * 2);
+  if (dhead) take(L.hs, std::min((size_t)L.Mp * L.ldh * 2, kScaledBytes));
   // (a wave of the small tile has 64 words, so a piece with dz, of 2^28 logits or one block of words, has 32 MB or a block's)
   L.part_bytes = std::min((size_t)words * L.Mp * 32, std::max(kPartBytes, (size_t)L.Mp * 32));
   take(L.part, L.part_bytes);
@@ -1001,7 +1006,10 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);
   const bool one_pass = dhead ? pieces == 1 : dhidden != nullptr;
   a.one_pass = one_pass;
-  if (one_pass) a.flag = (int*)(w + L.flag);
+  if (one_pass) {
+    a.flag = (int*)(w + L.flag);
+    if (dhead) a.hs = (size_t)L.Mp * L.ldh * 2 <= kScaledBytes ? (uint16_t*)(w + L.hs) : a.hc;
+  }
   // The small tile wastes less where rows or tiles are few.  A round of its work-groups takes about 5/8 of a large
   // one's time (151,936 words x 4,096, logits, large / small: 125 rows 399 / 330 us, 180 403 / 435, 300 614 / 564, 500
   // 649 / 755; 32,003 x 2,880: 180 85 / 69, 300 85 / 101, 640 169 / 145, 900 185 / 218); for dh, whose words are

@@ -953,3 +953,16 @@ def test_linear_ce_gradients_in_the_norm(n, B, V, H, ignored):
     for got in (dh, only):
         near_in_norm(got, want, half * (want * want + square @ (w64 * w64)).sqrt(), "dhidden")
     near_in_norm(dw, want_w, half * (want_w * want_w + 2 * (square.t() @ (h64 * h64))).sqrt(), "dhead")
+
+
+@pytest.mark.parametrize("V,ignored", [(300, 0.3), (5000, 0.0)])
+def test_linear_ce_of_large_rows_and_one_piece(V, ignored):
+    """Gathered rows of more than 32 MB take dhead's scale where they lie."""
+    n, B, H = 512, 16, 2568
+    print(f"[train ops] linear ce of large rows {(n, B, V, H)}", flush=True)
+    h, head, y = lce_inputs(n, B, V, H, seed=71, ignored=ignored)
+    for dh in (False, True):
+        got = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
+        lce_check(h, head, y, B, 4.5, got)
+        again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
+        assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))

@@ -59,7 +59,7 @@ def test_linear_ce_workspace_does_not_grow_with_rows_times_words():
             assert both <= 2 * one + (1 << 16), (rows, V, H, k)
             assert words - one <= V, (rows, V, H, k)
         # the rows themselves once (dhidden: and their sums), dz and the parts up to their room
-        assert ws(1 << 20, 200000, 64, *k) <= (1 << 20) * 64 * (2 + 4 * k[0]) + (1 << 20) * 64 + (512 + 128 + 128 << 20) + (1 << 20)
+        assert ws(1 << 20, 200000, 64, *k) <= (1 << 20) * 64 * (2 + 4 * k[0]) + (1 << 20) * 64 + (512 + 128 + 128 + 32 << 20) + (1 << 20)
     rng = np.random.default_rng(3)
     for _ in range(3000):
         big = [int(2 ** rng.uniform(0, m)) for m in (22, 20)] + [8 * int(2 ** rng.uniform(0, 10))]
