@@ -29,7 +29,9 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source of the library for gfx950 and link the shared object."""
+    """Compile every HIP source of the library for gfx950 and link the shared object; beside it the binding's native part.
+    The library needs neither PyTorch nor Python's headers: it is in its place before a binding that cannot be built
+    raises BindingError (and takes an older binding with it)."""
     os.makedirs(LIBDIR, exist_ok=True)
     common = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
               # keep the compiler away from packed fp32 instructions
@@ -39,18 +41,29 @@ def build(verbose: bool = False) -> str:
     cmds = [[hipcc(), *common, "-c", os.path.join(CSRC, src), "-o", obj]
             for src, obj in zip(SOURCES, objs)]
     # the translation units are independent: compile them side by side
-    binding = BINDING + f".tmp{os.getpid()}"
-    cmds.append(_binding_command(binding))
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
-        for f in [ex.submit(_run, cmd, verbose) for cmd in cmds]:
+    with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
+        units = [ex.submit(_run, cmd, verbose) for cmd in cmds]
+        binding = BINDING + f".tmp{os.getpid()}"
+        part = ex.submit(lambda: _run(_binding_command(binding), verbose))
+        for f in units:
             f.result()
-    os.replace(binding, BINDING)
-    tmp = LIB + f".tmp{os.getpid()}"
-    _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
-    os.replace(tmp, LIB)
-    for o in objs:
-        os.remove(o)
+        tmp = LIB + f".tmp{os.getpid()}"
+        _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
+        os.replace(tmp, LIB)
+        for o in objs:
+            os.remove(o)
+        try:
+            part.result()
+            os.replace(binding, BINDING)
+        except Exception as e:
+            if os.path.exists(BINDING):
+                os.remove(BINDING)  # (it may call the new library with an older one's arguments)
+            raise BindingError(f"{LIB} is built without {os.path.basename(BINDING)}: {e}") from e
     return LIB
+
+
+class BindingError(RuntimeError):
+    """The library is built; the native part of the Python binding is not."""
 
 
 def _binding_command(out: str) -> list[str]:
