@@ -957,6 +957,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {hidden, head, (const void*)dhidden, (const void*)dhead, (const void*)workspace})
     if ((uintptr_t)p & 15) return DFLARE_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)labels, (const void*)loss, (const void*)row_ce})
+    if ((uintptr_t)p & 3) return DFLARE_ERR_INVALID_ARG;
   const LceLayout L = lce_layout(rows, V, H, dhidden != nullptr, dhead != nullptr);
   if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
   // (the inputs are read until the last launch)

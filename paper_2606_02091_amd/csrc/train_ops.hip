@@ -841,6 +841,7 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
   if (rows > 0 && (!x || !y || !rstd || (layer && !mean) || (residual && !sum))) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {x, residual, gain, bias, (const void*)sum, (const void*)y})
     if (misplaced(p, size)) return DFLARE_ERR_INVALID_ARG;
+  if (misplaced(rstd, 4) || (layer && misplaced(mean, 4))) return DFLARE_ERR_INVALID_ARG;
   const size_t bytes = (size_t)rows * H * size;
   for (const void* p : {x, residual})
     if (!same_or_apart(y, p, bytes) || (residual && !same_or_apart(sum, p, bytes))) return DFLARE_ERR_INVALID_ARG;
@@ -896,6 +897,8 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
   if (workspace_bytes < dflare_norm_bwd_workspace(rows, H, kind) || misplaced(workspace, 16)) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {dy, h, gain, dsum, (const void*)dx})
     if (misplaced(p, size)) return DFLARE_ERR_INVALID_ARG;
+  for (const float* p : {rstd, (const float*)dgain, (const float*)dbias, layer ? mean : nullptr})
+    if (misplaced(p, 4)) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {dy, h, dsum})
     if (!same_or_apart(dx, p, (size_t)rows * H * size)) return DFLARE_ERR_INVALID_ARG;
   if (overlap(dx, (size_t)rows * H * size, gain, (size_t)H * size)) return DFLARE_ERR_INVALID_ARG;
@@ -939,7 +942,7 @@ int dflare_grad_norm(const dflare_grad_tensor* tensors, int32_t n, double* sumsq
                      size_t workspace_bytes, void* stream) {
   int rc = grad_check(tensors, n);
   if (rc != DFLARE_OK) return rc;
-  if (!sumsq || !workspace || misplaced(sumsq, 8) || misplaced(workspace, 8) ||
+  if (!sumsq || !workspace || misplaced(sumsq, 8) || misplaced(norm, 4) || misplaced(workspace, 8) ||
       workspace_bytes < dflare_grad_norm_workspace(n))
     return DFLARE_ERR_INVALID_ARG;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;

@@ -270,3 +270,22 @@ def test_frequencies(d, base):
     assert np.allclose(f[turns <= 1], plain[turns <= 1] / 8, rtol=1e-14)
     mid = (turns > 1) & (turns < 32)
     assert np.all((f[mid] < plain[mid]) & (f[mid] > plain[mid] / 8))
+
+
+FAR = {k: (i + 1) << 32 for i, k in enumerate("abcdefghijkl")}  # addresses far from one another
+
+
+@pytest.mark.parametrize("lead", [1, 2, 3])
+def test_numbers_off_their_alignment_are_refused(lead):
+    """Labels, losses, statistics and gradients of gains, in fp32 and int32, at addresses that are no multiple of 4."""
+    a = FAR
+    kw = dict(hidden=a["a"], head=a["b"], labels=a["c"], loss=a["d"], ce=a["e"], dh=a["f"], dw=a["g"], work=a["h"])
+    for k in ("labels", "loss", "ce"):
+        assert lce(**{**kw, k: kw[k] + lead}) == INV, k
+    kw = dict(x=a["a"], gain=a["b"], y=a["c"], mean=a["d"], rstd=a["e"], kind=dfl.NORM_LAYER)
+    for k in ("mean", "rstd"):
+        assert norm_fwd(**{**kw, k: kw[k] + lead}) == INV, k
+    kw = dict(dy=a["a"], h=a["b"], gain=a["c"], mean=a["d"], rstd=a["e"], dx=a["f"], dgain=a["g"], dbias=a["h"], work=a["i"], kind=dfl.NORM_LAYER)
+    for k in ("mean", "rstd", "dgain", "dbias"):
+        assert norm_bwd(**{**kw, k: kw[k] + lead}) == INV, k
+    assert dfl.lib().dflare_grad_norm(tensors((a["a"], None, 64, dfl.F32)), 1, a["b"], a["c"] + lead, a["d"], 1 << 30, None) == INV
