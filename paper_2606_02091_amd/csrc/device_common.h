@@ -3,6 +3,8 @@
 // write-through stores and coherent loads, and the MFMA A-fragment layout of activations.
 #pragma once
 
+#include <initializer_list>
+
 #include "dflare_impl.h"
 
 namespace dflare {
@@ -235,7 +237,22 @@ __device__ __forceinline__ void store_frag_pair_wt(uint32_t* hi, uint32_t* lo, i
 // host: np bytes at p and nq bytes at q share one (NULL shares none)
 inline bool overlap(const void* p, size_t np, const void* q, size_t nq) {
   const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  return p && q && a < b + nq && b < a + np;
+  return p && q && np && nq && a < b + nq && b < a + np;
+}
+
+struct Bytes {
+  const void* p;  // or NULL
+  size_t n;
+};
+// host: what a call writes meets nothing else that it writes or reads
+inline bool apart(std::initializer_list<Bytes> written, std::initializer_list<Bytes> read) {
+  for (const Bytes* w = written.begin(); w != written.end(); ++w) {
+    for (const Bytes* o = w + 1; o != written.end(); ++o)
+      if (overlap(w->p, w->n, o->p, o->n)) return false;
+    for (const Bytes& o : read)
+      if (overlap(w->p, w->n, o.p, o.n)) return false;
+  }
+  return true;
 }
 
 }  // namespace dflare

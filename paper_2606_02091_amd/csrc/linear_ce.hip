@@ -961,10 +961,9 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
     if ((uintptr_t)p & 3) return DFLARE_ERR_INVALID_ARG;
   const LceLayout L = lce_layout(rows, V, H, dhidden != nullptr, dhead != nullptr);
   if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
-  // (the inputs are read until the last launch)
-  const size_t hb = (size_t)rows * H * 2, wb = (size_t)V * H * 2;
-  if (overlap(dhidden, hb, hidden, hb) || overlap(dhidden, hb, head, wb) || overlap(dhead, wb, hidden, hb) ||
-      overlap(dhead, wb, head, wb) || overlap(dhead, wb, dhidden, hb))
+  // (the inputs are read until the last launch, row_ce is written by the first)
+  const size_t hb = (size_t)rows * H * 2, wb = (size_t)V * H * 2, rb = (size_t)rows * 4;
+  if (!apart({{loss, 4}, {row_ce, rb}, {dhidden, hb}, {dhead, wb}, {workspace, L.total}}, {{hidden, hb}, {head, wb}, {labels, rb}}))
     return DFLARE_ERR_INVALID_ARG;
   hipStream_t st = (hipStream_t)stream;
   if (st) {

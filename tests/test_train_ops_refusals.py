@@ -289,3 +289,18 @@ def test_numbers_off_their_alignment_are_refused(lead):
     for k in ("mean", "rstd", "dgain", "dbias"):
         assert norm_bwd(**{**kw, k: kw[k] + lead}) == INV, k
     assert dfl.lib().dflare_grad_norm(tensors((a["a"], None, 64, dfl.F32)), 1, a["b"], a["c"] + lead, a["d"], 1 << 30, None) == INV
+
+
+def refused(call, kw, pairs):
+    """Every pair (written, other, bytes of the other): the first bytes of what is written lie on the other's last ones."""
+    for w, o, n in pairs:
+        assert call(**{**kw, w: kw[o] + n - 16 if n >= 16 else kw[o]}) == INV, (w, o)
+
+
+def test_linear_ce_refuses_every_output_on_another_tensor():
+    a = FAR
+    kw = dict(hidden=a["a"], head=a["b"], labels=a["c"], loss=a["d"], ce=a["e"], dh=a["f"], dw=a["g"], work=a["h"])
+    size = dict(hidden=32 * 128, head=100 * 128, labels=128, loss=4, ce=128, dh=32 * 128, dw=100 * 128,
+                work=dfl.lib().dflare_linear_ce_workspace(32, 100, 64, 1, 1) // 16 * 16)
+    for w in ("loss", "ce", "dh", "dw", "work"):
+        refused(lce, kw, [(w, o, size[o]) for o in size if o != w])
