@@ -588,8 +588,7 @@ int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int3
  *   kind     DFLARE_NORM_RMS: mean = 0, rstd = 1 / sqrt(mean of h^2 + eps), no bias (must be NULL);
  *            DFLARE_NORM_LAYER: rstd = 1 / sqrt(mean of (h - mean)^2 + eps).
  *   x, residual (or NULL), gain (or NULL: ones), bias (or NULL: zeros), sum (read only with a residual), y: of
- *            type dtype, [rows, H] or [H].  sum and y may be x or residual; where they overlap
- *            these otherwise, gain, bias or each other: INVALID_ARG.
+ *            type dtype, [rows, H] or [H].  sum and y may each be x or residual.
  *   mean     fp32 [rows] out (LAYER; not written for RMS);  rstd  fp32 [rows] out.
  * Statistics and products in fp32.  rows = 0 does nothing; H > 16,384: UNSUPPORTED.
  */
@@ -601,9 +600,9 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
  * dflare_norm_bwd -- gradients of the above for the output gradient dy:
  *   h        the normalised rows (x, or sum where there was a residual);  mean, rstd  of the forward pass
  *   dsum     gradient of sum from its other uses, added to dx, or NULL
- *   dx       [rows, H] of type dtype out: the gradient of h (of x and of residual alike); may be dy, h or dsum;
- *            where it overlaps these otherwise or gain: INVALID_ARG
- *   dgain    fp32 [H] out;  dbias  fp32 [H] out (LAYER) or NULL: summed over the rows in a fixed order in fp32
+ *   dx       [rows, H] of type dtype out: the gradient of h (of x and of residual alike); may be dy, h or dsum
+ *   dgain    fp32 [H] out;  dbias  fp32 [H] out (LAYER) or NULL: summed over the rows in a fixed order in fp32; written last,
+ *            so that they may lie in an input
  *   workspace  16-byte aligned, at least dflare_norm_bwd_workspace(rows, H, kind) bytes
  * rows = 0 writes zeros to dgain and dbias.
  */

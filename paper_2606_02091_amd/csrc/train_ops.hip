@@ -851,6 +851,11 @@ int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const
   if (rows == 0) return DFLARE_OK;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   bool wide = (long)H * size % 16 == 0;
+  // a row's statistics are written while other rows are read
+  const size_t rb = (size_t)rows * 4, hb = (size_t)H * size;
+  if (!apart({{rstd, rb}, {layer ? mean : nullptr, rb}},
+             {{x, bytes}, {residual, bytes}, {gain, hb}, {bias, hb}, {residual ? sum : nullptr, bytes}, {y, bytes}}))
+    return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {x, residual, gain, bias, (const void*)sum, (const void*)y}) wide = wide && aligned16(p);
   NormArgs a{};
   a.x = x;
@@ -901,7 +906,14 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
     if (misplaced(p, 4)) return DFLARE_ERR_INVALID_ARG;
   for (const void* p : {dy, h, dsum})
     if (!same_or_apart(dx, p, (size_t)rows * H * size)) return DFLARE_ERR_INVALID_ARG;
-  if (overlap(dx, (size_t)rows * H * size, gain, (size_t)H * size)) return DFLARE_ERR_INVALID_ARG;
+  // the inputs are read until the last row; dgain and dbias are written after that
+  const size_t bytes = (size_t)rows * H * size, rb = (size_t)rows * 4, hb = (size_t)H * 4, gb = (size_t)H * size;
+  const size_t wb = dflare_norm_bwd_workspace(rows, H, kind);
+  const float* mu = layer ? mean : nullptr;
+  if (!apart({{dx, bytes}}, {{gain, gb}, {mu, rb}, {rstd, rb}}) ||
+      !apart({{workspace, wb}}, {{dy, bytes}, {h, bytes}, {dsum, bytes}, {gain, gb}, {mu, rb}, {rstd, rb}}) ||
+      !apart({{dx, bytes}, {dgain, hb}, {dbias, hb}, {workspace, wb}}, {}))
+    return DFLARE_ERR_INVALID_ARG;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   bool wide = (long)H * size % 16 == 0;
   for (const void* p : {dy, h, gain, dsum, (const void*)dx}) wide = wide && aligned16(p);

@@ -304,3 +304,19 @@ def test_linear_ce_refuses_every_output_on_another_tensor():
                 work=dfl.lib().dflare_linear_ce_workspace(32, 100, 64, 1, 1) // 16 * 16)
     for w in ("loss", "ce", "dh", "dw", "work"):
         refused(lce, kw, [(w, o, size[o]) for o in size if o != w])
+
+
+def test_norms_refuse_statistics_on_another_tensor():
+    a = FAR
+    kw = dict(x=a["a"], res=a["b"], gain=a["c"], bias=a["d"], sum_=a["e"], y=a["f"], mean=a["g"], rstd=a["h"], kind=dfl.NORM_LAYER)
+    size = dict(x=512, res=512, gain=128, bias=128, sum_=512, y=512, mean=16, rstd=16)
+    for w in ("mean", "rstd"):
+        refused(norm_fwd, kw, [(w, o, size[o]) for o in size if o != w])
+    kw = dict(dy=a["a"], h=a["b"], gain=a["c"], mean=a["d"], rstd=a["e"], dsum=a["f"], dx=a["g"], dgain=a["h"], dbias=a["i"],
+              work=a["j"], kind=dfl.NORM_LAYER)
+    size = dict(dy=512, h=512, gain=128, mean=16, rstd=16, dsum=512, dx=512, dgain=256, dbias=256,
+                work=dfl.lib().dflare_norm_bwd_workspace(4, 64, dfl.NORM_LAYER))
+    refused(norm_bwd, kw, [("work", o, size[o]) for o in size if o != "work"])
+    refused(norm_bwd, kw, [("dx", o, size[o]) for o in ("mean", "rstd", "gain", "dgain", "dbias", "work")])
+    refused(norm_bwd, kw, [("dgain", o, size[o]) for o in ("dx", "dbias", "work")])
+    refused(norm_bwd, kw, [("dbias", o, size[o]) for o in ("dx", "dgain", "work")])
