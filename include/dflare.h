@@ -563,7 +563,7 @@ int dflare_rope_frequencies(int32_t rotary_dim, double base, int32_t method, dou
  *               elements from row to row and from head to head (a head's elements are contiguous).  y may
  *               be x with the same strides (in place); otherwise nothing written may overlap anything else:
  *               INVALID_ARG unless the ends or a stride show that it does not (views of one buffer of queries and
- *               keys do).
+ *               keys do).  That inv_freq lies apart is left to the caller.
  *   positions   DEVICE int32 [ceil(rows / B)] or NULL: row r sits at positions[r / B] + r % B (B = 1: a position
  *               per row; blocks anchored at positions: B rows each); NULL: at r.
  *   inv_freq    DEVICE double [rotary_dim / 2], as dflare_rope_frequencies gives them.

@@ -673,11 +673,12 @@ bool runs_apart(const Runs& a, const Runs& b) {
   return false;
 }
 // what a call writes meets nothing else that it writes or reads, a tensor turned in place aside
-bool rope_apart(const dflare_rope_tensor* t, int n, int rows, int hd, int size) {
+bool rope_apart(const dflare_rope_tensor* t, int n, const int32_t* positions, int n_positions, int rows, int hd, int size) {
   auto x = [&](int k) { return Runs(t[k].x, t[k].x_row, t[k].x_head, rows, t[k].n_heads, hd, size); };
   auto y = [&](int k) { return Runs(t[k].y, t[k].y_row, t[k].y_head, rows, t[k].n_heads, hd, size); };
   for (int k = 0; k < n; ++k) {
     if (!y(k).empty() && !y(k).distinct()) return false;
+    if (positions && !runs_apart(y(k), Runs(positions, 0, 0, 1, 1, n_positions, 4))) return false;
     if (t[k].x != t[k].y && !runs_apart(x(k), y(k))) return false;
   }
   return n == 1 || (runs_apart(y(0), y(1)) && runs_apart(y(0), x(1)) && runs_apart(y(1), x(0)));
@@ -796,7 +797,8 @@ int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int3
     work += t.n_heads;
   }
   if (rows == 0 || work == 0) return DFLARE_OK;
-  if (!rope_apart(tensors, n_tensors, rows, head_dim, size)) return DFLARE_ERR_INVALID_ARG;
+  const int n_positions = (int)((rows + B - 1l) / B);
+  if (!rope_apart(tensors, n_tensors, positions, n_positions, rows, head_dim, size)) return DFLARE_ERR_INVALID_ARG;
   const int rc = stream_ok(stream);
   if (rc != DFLARE_OK) return rc;
   const int half = rotary_dim / 2;

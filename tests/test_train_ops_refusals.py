@@ -320,3 +320,10 @@ def test_norms_refuse_statistics_on_another_tensor():
     refused(norm_bwd, kw, [("dx", o, size[o]) for o in ("mean", "rstd", "gain", "dgain", "dbias", "work")])
     refused(norm_bwd, kw, [("dgain", o, size[o]) for o in ("dx", "dbias", "work")])
     refused(norm_bwd, kw, [("dbias", o, size[o]) for o in ("dx", "dgain", "work")])
+
+
+def test_rope_refuses_outputs_on_the_positions():
+    y = FAR["b"]  # 4 rows of 128 elements, 2 bytes each
+    for pos in (y, y + 4, y + 1020, y - 12):
+        assert rope(x=FAR["a"], y=y, pos=pos, freq=FAR["c"]) == INV
+        assert rope(x=FAR["a"], y=y, pos=pos, freq=FAR["c"], n=1, B=4 if pos != y - 12 else 1) == INV
