@@ -532,7 +532,8 @@ int dflare_weighted_ce_noalloc(const float* logits, const int32_t* labels, int32
  * aligned to their elements (to 16 bytes where said); DFLARE_F32 and DFLARE_BF16 name their types.
  * Every call is asynchronous on `stream` (hipStream_t, NULL = default), which must belong to the current device
  * (else INVALID_ARG), allocates nothing, can be captured into a graph, and gives the same bits when it
- * is repeated.  A workspace belongs to one call at a time; its contents need not be kept.
+ * is repeated.  A workspace belongs to one call at a time; its contents need not be kept.  Nothing that a call writes
+ * may overlap anything else that it writes or reads, where no exception is named: INVALID_ARG.
  */
 enum { DFLARE_F32 = 0, DFLARE_BF16 = 1 };
 
@@ -621,8 +622,7 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
  *   dhidden  bf16 [rows, H] out, or NULL: not wanted;  dhead  bf16 [V, H] out, or NULL
  *   workspace  at least dflare_linear_ce_workspace(rows, V, H, dhidden wanted, dhead wanted) bytes; it grows
  *            with rows, V and H, not with rows x V
- * hidden, head, dhidden, dhead and workspace 16-byte aligned; a gradient that overlaps hidden, head or the other one is
- * INVALID_ARG.  rows not a multiple of B, gamma <= 0 or not finite:
+ * hidden, head, dhidden, dhead and workspace 16-byte aligned.  rows not a multiple of B, gamma <= 0 or not finite:
  * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows, 2^35 values of hidden or about 2^38 logits: UNSUPPORTED (the
  * workspace is then 0 bytes).  Products run on the bf16 matrix cores with fp32 sums; the logits' gradient is
  * rounded to bf16 as their operand, each gradient once more where it is written.  NaN or infinities in a row
@@ -642,8 +642,7 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
  *   workspace  8-byte aligned, at least dflare_grad_norm_workspace(n) bytes
  * dflare_clip_grads -- out = data max_norm / norm where norm = sqrt(*sumsq) is above max_norm, out = data
  * otherwise; also where *sumsq is NaN or infinite (the caller sees it there and drops the step).
- *   out        of each tensor: where the clipped values go, NULL: data itself.  No tensor that is written may
- *              overlap another one (INVALID_ARG).
+ *   out        of each tensor: where the clipped values go, NULL or data: in place.
  *   max_norm   >= 0; infinite: nothing is clipped.
  * More than 2^36 elements in one tensor: UNSUPPORTED.
  */

@@ -715,14 +715,15 @@ void grad_launches(const dflare_grad_tensor* t, int n, F&& f) {
   flush();
 }
 
-// INVALID_ARG where a tensor written by a clip overlaps another one that it reads or writes
-int grad_apart(const dflare_grad_tensor* t, int n) try {
+// INVALID_ARG where a tensor written by a clip overlaps another one that it reads or writes, or sumsq
+int grad_apart(const dflare_grad_tensor* t, int n, const double* sumsq) try {
   struct Span {
     uintptr_t a, b;
     bool out;
   };
   std::vector<Span> s;
-  s.reserve(2 * (size_t)n);
+  s.reserve(2 * (size_t)n + 1);
+  s.push_back({(uintptr_t)sumsq, (uintptr_t)sumsq + sizeof(double), false});
   for (int i = 0; i < n; ++i) {
     if (!t[i].n) continue;
     const size_t bytes = (size_t)t[i].n * size_of(t[i].dtype);
@@ -959,6 +960,11 @@ int dflare_grad_norm(const dflare_grad_tensor* tensors, int32_t n, double* sumsq
   if (!sumsq || !workspace || misplaced(sumsq, 8) || misplaced(norm, 4) || misplaced(workspace, 8) ||
       workspace_bytes < dflare_grad_norm_workspace(n))
     return DFLARE_ERR_INVALID_ARG;
+  // the partial sums are written while the gradients are read, the results while the partial sums are
+  const Bytes work{workspace, dflare_grad_norm_workspace(n)};
+  if (!apart({work, {sumsq, 8}, {norm, 4}}, {})) return DFLARE_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i)
+    if (!apart({work, {sumsq, 8}, {norm, 4}}, {{tensors[i].data, (size_t)tensors[i].n * size_of(tensors[i].dtype)}})) return DFLARE_ERR_INVALID_ARG;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   double* part = (double*)workspace;
   int used = 0;
@@ -974,7 +980,7 @@ int dflare_clip_grads(const dflare_grad_tensor* tensors, int32_t n, const double
   int rc = grad_check(tensors, n);
   if (rc != DFLARE_OK) return rc;
   if (!sumsq || misplaced(sumsq, 8) || !(max_norm >= 0.f)) return DFLARE_ERR_INVALID_ARG;
-  if ((rc = grad_apart(tensors, n)) != DFLARE_OK) return rc;
+  if ((rc = grad_apart(tensors, n, sumsq)) != DFLARE_OK) return rc;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
   bool out = false;
   for (int i = 0; i < n; ++i) out |= tensors[i].out && tensors[i].out != tensors[i].data;

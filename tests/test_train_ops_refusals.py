@@ -327,3 +327,38 @@ def test_rope_refuses_outputs_on_the_positions():
     for pos in (y, y + 4, y + 1020, y - 12):
         assert rope(x=FAR["a"], y=y, pos=pos, freq=FAR["c"]) == INV
         assert rope(x=FAR["a"], y=y, pos=pos, freq=FAR["c"], n=1, B=4 if pos != y - 12 else 1) == INV
+
+
+def test_gradients_refuse_results_on_another_tensor():
+    t, lib = tensors((FAR["a"], None, 64, dfl.F32), (FAR["b"], None, 64, dfl.F32)), dfl.lib()
+    ws = lib.dflare_grad_norm_workspace(2)
+
+    def norm(sumsq=FAR["c"], out=FAR["d"], work=FAR["e"]):
+        return lib.dflare_grad_norm(t, 2, sumsq, out, work, ws, None)
+    for at in (FAR["a"] + 248, FAR["b"]):
+        assert norm(sumsq=at) == INV and norm(out=at) == INV and norm(work=at) == INV
+    assert norm(sumsq=FAR["e"] + ws - 8) == INV and norm(out=FAR["e"]) == INV and norm(out=FAR["c"] + 4) == INV
+    assert clip([(FAR["a"], None, 64, dfl.F32)], sumsq=FAR["a"] + 248) == INV
+    assert clip([(FAR["a"], FAR["b"], 64, dfl.F32)], sumsq=FAR["b"]) == INV
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="what is not refused is launched")
+def test_tensors_that_lie_apart_are_not_refused():
+    """Calls in place, and tensors that follow each other without a byte between them, reach the launch."""
+    a, launched = FAR, dfl.ERR_HIP
+    at, ptr = a["a"], {}
+    sizes = dict(hidden=32 * 128, head=100 * 128, work=dfl.lib().dflare_linear_ce_workspace(32, 100, 64, 1, 1), dh=32 * 128, dw=100 * 128,
+                 labels=128, ce=128, loss=4)
+    for k, n in sizes.items():
+        ptr[k], at = at, at + n
+    assert lce(**ptr) == launched
+    assert norm_fwd(x=a["a"], res=a["b"], gain=a["c"], sum_=a["a"], y=a["b"], rstd=a["a"] + 512, mean=a["a"]) == launched  # (no mean is written)
+    assert norm_fwd(x=a["a"], gain=a["c"], y=a["a"], mean=a["b"], rstd=a["b"] + 16, kind=dfl.NORM_LAYER) == launched
+    for over in ("a", "b", "f"):
+        assert norm_bwd(dy=a["a"], h=a["b"], dsum=a["f"], gain=a["c"], mean=a["d"], rstd=a["e"], dx=a[over], dgain=a["h"], dbias=a["h"] + 256,
+                        work=a["h"] + 512, kind=dfl.NORM_LAYER) == launched
+    assert rope(x=a["a"], y=a["a"], pos=a["a"] + 1024, freq=a["c"]) == launched
+    ws = dfl.lib().dflare_grad_norm_workspace(1)
+    assert dfl.lib().dflare_grad_norm(tensors((a["a"], None, 64, dfl.F32)), 1, a["a"] + 256, a["a"] + 264, a["b"], ws, None) == launched
+    assert clip([(a["a"], None, 64, dfl.F32)], sumsq=a["a"] + 256) == launched
+    assert clip([(None, None, 0, dfl.F32), (a["a"], a["b"], 64, dfl.F32)], sumsq=a["b"] + 256) == launched
