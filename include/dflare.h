@@ -591,7 +591,8 @@ int dflare_rope(const dflare_rope_tensor* tensors, int32_t n_tensors, const int3
  *   x, residual (or NULL), gain (or NULL: ones), bias (or NULL: zeros), sum (read only with a residual), y: of
  *            type dtype, [rows, H] or [H].  sum and y may each be x or residual.
  *   mean     fp32 [rows] out (LAYER; not written for RMS);  rstd  fp32 [rows] out.
- * Statistics and products in fp32.  rows = 0 does nothing; H > 16,384: UNSUPPORTED.
+ * Statistics and products in fp32.  A row with NaN or infinities is what the formula gives; other rows are not touched.
+ * rows = 0 does nothing; H > 16,384: UNSUPPORTED.
  */
 enum { DFLARE_NORM_RMS = 0, DFLARE_NORM_LAYER = 1 };
 int dflare_norm_fwd(const void* x, const void* residual, const void* gain, const void* bias, int32_t rows, int32_t H,
@@ -623,10 +624,15 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
  *   workspace  at least dflare_linear_ce_workspace(rows, V, H, dhidden wanted, dhead wanted) bytes; it grows
  *            with rows, V and H, not with rows x V
  * hidden, head, dhidden, dhead and workspace 16-byte aligned.  rows not a multiple of B, gamma <= 0 or not finite:
- * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows, 2^35 values of hidden or about 2^38 logits: UNSUPPORTED (the
- * workspace is then 0 bytes).  Products run on the bf16 matrix cores with fp32 sums; the logits' gradient is
- * rounded to bf16 as their operand, each gradient once more where it is written.  NaN or infinities in a row
- * that takes part, or in head, make results NaN.
+ * INVALID_ARG; H not a multiple of 8 or above 16,384, more than 2^22 rows, 2^35 values of hidden or about 2^38 logits:
+ * UNSUPPORTED (the workspace is then 0 bytes).
+ * Products run on the bf16 matrix cores with fp32 sums.  Rounded to bf16 on the way: the logits' gradient, as their operand
+ * (the label's own is kept in fp32); where dhead comes from up to 2^28 logits (rows and V as multiples of 256) or 256 words also
+ * hidden times its row's scale, so that the gradient of a word that is no row's label carries one such rounding more there.
+ * Each gradient is rounded once more where it is written.
+ * NaN and infinities: in a row that takes part they make its cross-entropy, the loss, its row of dhidden and what it adds to dhead
+ * NaN or infinite, and leave the other rows' cross-entropies and dhidden alone; in head they do so for every row whose
+ * logit they make NaN or +infinite, and their column of dhidden is NaN in all rows that take part.
  */
 size_t dflare_linear_ce_workspace(int32_t rows, int32_t V, int32_t H, int32_t dhidden, int32_t dhead);
 int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels, int32_t rows, int32_t V, int32_t H,

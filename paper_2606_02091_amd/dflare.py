@@ -364,6 +364,8 @@ def weighted_ce_noalloc(logits, labels, B: int, gamma: float, loss, row_ce, dlog
 
 
 # ---- the rest of a draft layer's training step (no handle) ----
+# As with the other training-side calls, autograd records none of these: results are plain tensors also where inputs require
+# gradients, and what is written in place does not raise a tensor's version.
 
 F32, BF16 = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = range(4)

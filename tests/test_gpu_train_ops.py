@@ -966,3 +966,59 @@ def test_linear_ce_of_large_rows_and_one_piece(V, ignored):
         lce_check(h, head, y, B, 4.5, got)
         again = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=True)
         assert all(u is v or torch.equal(u, v) for u, v in zip(got, again))
+
+
+# ---- values that are not finite ----
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_linear_ce_of_values_that_are_not_finite(bad):
+    """NaN and infinities, in a row that takes part or in a word, on both forms of the call: the loss and the rows that they
+    reach are NaN or infinite; the other rows' cross-entropies are as without them where a row holds them."""
+    B = 8
+    h, head, y = lce_inputs(40, B, 700, 128, seed=8, ignored=0.3)
+    on = (torch.arange(h.shape[0], device="cuda") % B > 0) & (y >= 0) & (y < 700)
+    row = int(torch.nonzero(on)[5])
+    for dh, dw in ((False, False), (True, False), (False, True), (True, True)):
+        clean = dfl.linear_ce(h, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+        x = h.clone()
+        x[row, 17] = bad
+        loss, ce, gh, gw = dfl.linear_ce(x, head, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+        rest = torch.arange(h.shape[0], device="cuda") != row
+        assert not math.isfinite(float(loss)) and not math.isfinite(float(ce[row])) and torch.equal(ce[rest], clean[1][rest])
+        if dh:
+            assert gh[row].isnan().all() and torch.equal(gh[rest], clean[2][rest])
+        if dw:  # every word has a share of the row
+            assert not gw[:, 17].isfinite().any()
+        w = head.clone()
+        w[333, 5] = bad
+        loss, ce, gh, gw = dfl.linear_ce(h, w, y, B, 4.5, need_dhidden=dh, need_dhead=dw)
+        # the word's logit is NaN, or infinite with the sign of bad h: +inf and NaN reach the row's sum
+        z = h[:, 5].float() * bad
+        hit = on & ~(z == -float("inf"))
+        assert not math.isfinite(float(loss)) and not ce[hit].isfinite().any() and torch.equal(ce[~on], torch.zeros_like(ce[~on]))
+        if dh:
+            assert not gh[on][:, 5].isfinite().any()
+            assert not gh[hit].isfinite().any()
+
+
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_norm_of_values_that_are_not_finite(layer, dtype):
+    """A row with NaN is NaN, one with an infinity what the formula gives (RMSNorm: zeros beside the infinity); the other rows
+    and their gradients are as without them, dgain and dbias are NaN where such a row reaches them."""
+    kind = dfl.NORM_LAYER if layer else dfl.NORM_RMS
+    x, dy = randn((12, 1000), dtype, 1), randn((12, 1000), dtype, 2)
+    clean = dfl.norm_fwd(x, kind=kind)
+    back = dfl.norm_bwd(dy, clean[1], None, clean[2], clean[3], kind=kind)
+    bad = x.clone()
+    bad[3, 7], bad[8, 999] = float("nan"), float("inf")
+    y, h, mean, rstd = dfl.norm_fwd(bad, kind=kind)
+    dx, dgain, _ = dfl.norm_bwd(dy, h, None, mean, rstd, kind=kind)
+    rest = torch.tensor([k for k in range(12) if k not in (3, 8)], device="cuda")
+    assert torch.equal(y[rest], clean[0][rest]) and torch.equal(rstd[rest], clean[3][rest]) and torch.equal(dx[rest], back[0][rest])
+    assert y[3].isnan().all() and rstd[3].isnan() and dx[3].isnan().all() and y[8, 999].isnan()
+    if layer:
+        assert y[8].isnan().all() and dx[8].isnan().all()
+    else:
+        assert not y[8, :999].any() and rstd[8] == 0
+    assert dgain.isnan().all()
