@@ -405,9 +405,11 @@ _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 
 def _i32(n: int, name: str) -> int:
-    """n as an argument of 32 bits (ctypes would cut a larger one)."""
+    """n as an argument of 32 bits (ctypes would cut a larger one, int() a broken one)."""
     if not -2 ** 31 <= n < 2 ** 31:
         raise ValueError(f"{name} is {n}, beyond 32 bits")
+    if n != int(n):
+        raise ValueError(f"{name} is {n}, not a whole number")
     return int(n)
 
 
@@ -450,9 +452,10 @@ def rope_frequencies(rotary_dim: int, base: float, method: int = ROPE_PLAIN, fac
                      original_len: float = 0.0, device="cuda"):
     """Inverse frequencies of a rotary embedding (include/dflare.h): (fp64 tensor [rotary_dim / 2] on the device,
     the factor on cosines and sines)."""
-    f = np.empty(max(int(rotary_dim) // 2, 1), dtype=np.float64)
+    d = _i32(rotary_dim, "rotary_dim")
+    f = np.empty(max(d // 2, 1), dtype=np.float64)
     scale = ctypes.c_float()
-    _train_check(lib().dflare_rope_frequencies(int(rotary_dim), float(base), int(method), float(factor),
+    _train_check(lib().dflare_rope_frequencies(d, float(base), _i32(method, "method"), float(factor),
                                                float(original_len), f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
                                                ctypes.byref(scale)), "rope frequencies")
     return torch.from_numpy(f).to(device), scale.value

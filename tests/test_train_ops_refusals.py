@@ -362,3 +362,15 @@ def test_tensors_that_lie_apart_are_not_refused():
     assert dfl.lib().dflare_grad_norm(tensors((a["a"], None, 64, dfl.F32)), 1, a["a"] + 256, a["a"] + 264, a["b"], ws, None) == launched
     assert clip([(a["a"], None, 64, dfl.F32)], sumsq=a["a"] + 256) == launched
     assert clip([(None, None, 0, dfl.F32), (a["a"], a["b"], 64, dfl.F32)], sumsq=a["b"] + 256) == launched
+
+
+def test_binding_refuses_numbers_that_are_cut():
+    """A dimension beyond 32 bits would reach the library as another one, with room for the first; a broken number as a whole one."""
+    for d in (2 ** 31, 2 ** 32 + 64, -2 ** 32 + 64, 64.5):
+        with pytest.raises(ValueError):
+            dfl.rope_frequencies(d, 1e4, device="cpu")
+    with pytest.raises(ValueError):
+        dfl.rope_frequencies(64, 1e4, 2 ** 32, device="cpu")
+    with pytest.raises(ValueError):
+        dfl._i32(4.5, "B")
+    assert dfl._i32(16.0, "B") == 16 and dfl.rope_frequencies(64, 1e4, device="cpu")[0].shape == (32,)
