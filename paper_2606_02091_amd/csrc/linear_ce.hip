@@ -79,7 +79,8 @@ struct Lce {
   float* c;       // [Mp] w / sum w, 0 past the last
   uint16_t* hc;   // [Mp][ldh] gathered rows, zeros past H and past the last row of the last tile
   uint16_t* hs;   // [Mp][ldh] hc times fac, for dW from one piece: a place of its own, or hc's; else null
-  float2* part;   // [words of a piece / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), the label's word left out
+  float2* part;   // [words of a piece / a wave's][Mp] a reference R (log2 domain) and the sum of 2^(z log2 e - R), without the
+                  // label's word
   float* zlab;    // [Mp] z at the label
   float* lab;     // [Mp] c (1 - p of the label)
   float *ref, *sum;  // [Mp] a row's reference and its sum over the pieces so far
@@ -88,7 +89,7 @@ struct Lce {
   int* flag;      // of the pieces in one pass: a word took a reference of its own
   uint16_t* dz;   // [words of a piece / 256][Mp][256] dz of a piece of the vocabulary
   float* dacc;    // [parts][rows of whole tiles][H] dh of the pieces so far; then [dw_parts][V][H] dW
-  int Mp, ldh, Vp;
+  int Mp, ldh;
   int stages;     // stages of k of the first (longest) piece
   int dw_parts;   // dW's rows are split into
   int dh_tile;    // dh on the large tile (0), the small one, or that for few rows
@@ -677,7 +678,8 @@ __global__ __launch_bounds__(S::T, 2) void k_lce_product(Lce a, int v0, int nv, 
 
 // A row's values from its parts: work-groups of 1,024 threads take R rows, each by 1,024 / R groups of parts
 
-// The cross-entropy of row i, log(1 + s / 2^y), s and the label's 2^y (y = z log2 e - r) on the reference r; what the gradients take
+// The cross-entropy log(1 + s / 2^y) of row i, s and the label's 2^y (y = z log2 e - r) on the reference r, and what the
+// gradients take
 __device__ __forceinline__ float close_row(const Lce& a, int i, float s, float r) {
   const float y = fmaf(a.zlab[i], kL2E, -r), ey = ex2(y), c = a.c[i], inv = 1.f / (s + ey), f = c * inv;
   a.fac[i] = f;
@@ -1001,7 +1003,6 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
   a.dacc = (float*)(w + L.dacc);
   a.Mp = L.Mp;
   a.ldh = L.ldh;
-  a.Vp = L.Vp;
   a.stages = (std::min(V, L.Vp) + kBK - 1) / kBK;
   const int words = (int)((V + (long)kBlock - 1) / kBlock);
   const int pieces = (words + L.Vp / kBlock - 1) / (L.Vp / kBlock);

@@ -937,7 +937,7 @@ int dflare_norm_bwd(const void* dy, const void* h, const void* gain, const float
       using T = decltype(z);
       norm_shape<T>(H, wide, [&](auto ve, auto al, auto wpr, auto s) {
         constexpr int VE = decltype(ve)::value, WPR = decltype(wpr)::value, S = decltype(s)::value, RG = WPR == 1 ? 4 : 1;
-      constexpr bool AL = decltype(al)::value;
+        constexpr bool AL = decltype(al)::value;
         const int grid = (int)std::min<long>((rows + RG - 1l) / RG, kNormGroups);
         parts = grid * RG;
         if (layer) hipLaunchKernelGGL((k_norm_bwd<T, VE, AL, WPR, S, true>), dim3(grid), dim3(norm_threads<WPR>), 0, (hipStream_t)stream, a);
