@@ -98,7 +98,8 @@ struct Lce {
 // dh's tiles for n rows with a loss.  The words of a piece are split into `parts` where there are few tiles for the
 // work-groups that 256 CUs hold: the number with the least time, a round of work-groups costing its stages of k
 // and about 8 more for its start and its sums in memory, the sum of the parts n H / 1.45 M each (in stages: 1.45 us
-// measured on the large tile).  More than one part makes at most two rounds.  The number depends on the rows
+// measured on the large tile).  More than one part makes at most two rounds, which is what dacc is sized by (more was not
+// measured; 290 tiles, as of 7,296 rows x 2,560, stay whole and fill 57% of two rounds).  The number depends on the rows
 // with a loss, so that it is chosen on the device (k_lce_rows).
 constexpr int kMostParts = 128;
 __host__ __device__ constexpr int dh_slots(int tile) { return 256 * (tile + 1); }  // work-groups that the CUs hold
@@ -323,7 +324,7 @@ template <typename S>
 using Acc = f32x16[S::MT][S::NT];
 
 // Two stages lie in LDS, one of them on its way; a wave reads the operands of each 16 k between the products of the 16
-// before.  7,296 rows x 30,464 words x 4,096 (1,545 us with the epilogue, 1,178 TFLOP/s; dh of them 1,565): the matrix
+// before.  7,296 rows x 30,464 words x 4,096 (1,545 to 1,570 us with the epilogue, 1,170 TFLOP/s; dh of them 1,615 to 1,680): the matrix
 // cores are busy 63% of the clocks, at 1.8 GHz; a library product of that shape takes 1,510 us (dh's 2,070).  The
 // same with 4 waves of 128 x 128 has 13% more clocks at a higher rate of them and the same time, and so have
 // work-groups that stay and load their next tile under the epilogue, 128 x 256 tiles two to a CU are 20% slower, and
@@ -760,7 +761,7 @@ __device__ __forceinline__ float rebase_row(const Lce& a, int i, int nv, int pie
 
 // One pass, after a piece's logits: its rows rescaled where it needs that, and the rows' sums so far from their parts; after the
 // last piece their cross-entropy and the factors of dh, and with dhead hs.  (In launches of their own these
-// made 207 rows x 32,003 x 264 6 us of 68 longer.)
+// made 207 rows x 32,003 x 264 6 us of 68 longer.)  7,296 rows x 30,464 words: 9.4 us.
 template <int R>
 __global__ __launch_bounds__(1024) void k_lce_close(Lce a, int nv, int piece, bool last, int wave) {
   __shared__ float sh[16][R], red[16], ref[R], fac[R];

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kT) void k_rope(RopeArgs a) {
   }
 }
 
-// ---- norms.  8,192 x 4,096 bf16 with a residual: forward 45 us (268 MB), backward 53 (268 MB and the partials): memory.
+// ---- norms.  8,192 x 4,096 bf16 with a residual: forward 45 us (268 MB), backward 52 (268 MB and the partials): memory.
 // Few rows: latency, 4 us a launch.  WPR waves hold a row in registers, S pieces of VE elements per thread (piece k T + t for thread t
 // of the row's T), so that a row is read once and mean and variance are sums over held values.  Rows that do not start or
 // end on 16-byte boundaries are read and written in 16-byte pieces all the same; a piece that would pass the
@@ -527,6 +527,8 @@ __global__ __launch_bounds__(kT) void k_grad_norm(const double* part, int n, dou
   }
 }
 
+// (Streamed stores: 2% faster than others into tensors of their own at 3.2 GB; in place the same within 2% from 4 MB to 3.2 GB, and so
+// is a pass that reads the values afterwards.)
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T* p, T* o, long n, int c, float f) {
   constexpr int VE = kVec<T>;
@@ -542,7 +544,7 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* o, long n, int c, flo
       load_n<T, VE>(p + head + e * VE, x);
 #pragma unroll
       for (int k = 0; k < VE; ++k) x[k] *= f;
-      __builtin_nontemporal_store(pack(x), reinterpret_cast<u32x4*>(o + head + e * VE));  // (2% faster at 3.2 GB)
+      __builtin_nontemporal_store(pack(x), reinterpret_cast<u32x4*>(o + head + e * VE));
     }
   } else {
     for (long e = head + e0 * VE + threadIdx.x; e < head + e1 * VE; e += kT) o[e] = from_f<T>(to_f(p[e]) * f);
@@ -605,7 +607,7 @@ void norm_shape(int H, bool aligned, F&& f) {
   else sized(std::false_type{});
 }
 // Work-groups of the backward pass, each with a partial of the gain's gradient (8,192 x 4,096 bf16, both passes, 256 / 512 /
-// 1,024 of them: 115 / 100 / 107 us)
+// 1,024 of them: 115 / 100 / 107 us; not measured at fewer rows, where 777 x 2,881 has two rows a group at most)
 constexpr int kNormGroups = 512;
 int norm_parts(int rows) { return std::min(std::max(rows, 0), kNormGroups) * 4; }
 
