@@ -641,8 +641,8 @@ int dflare_linear_ce(const void* hidden, const void* head, const int32_t* labels
 
 /*
  * dflare_grad_norm -- the global 2-norm of n gradient tensors: *sumsq = sum of all squares, formed and added
- * in double in a fixed order; *norm = its root in fp32.  Ranks that hold parts of the gradients add their
- * sumsq before they clip.
+ * in double in a fixed order; *norm = its root in fp32 (infinite beyond its range; clipping goes by
+ * sumsq).  Ranks that hold parts of the gradients add their sumsq before they clip.
  *   tensors    HOST [n], read before the call returns; `out` is not read.  Empty tensors (n = 0) and n = 0 are allowed.
  *   sumsq      DEVICE double [1] out;  norm  DEVICE fp32 [1] out or NULL
  *   workspace  8-byte aligned, at least dflare_grad_norm_workspace(n) bytes

@@ -1022,3 +1022,21 @@ def test_norm_of_values_that_are_not_finite(layer, dtype):
     else:
         assert not y[8, :999].any() and rstd[8] == 0
     assert dgain.isnan().all()
+
+
+@pytest.mark.parametrize("std,max_norm", [(1e37, 1.0), (5e36, 1e-20), (1e-20, 1e-42)])
+def test_grad_clip_by_factors_below_the_normal_range(std, max_norm):
+    """Finite gradients whose norm is beyond fp32 (the fp32 norm is infinite, the sum of squares is not), and bounds so small that
+    max_norm / norm is below its normal range: the clipped values keep their digits."""
+    grads = grads_of([5000, 6001, 77], std=std)
+    _, sumsq = dfl.grad_norm(grads)
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    assert abs(math.sqrt(float(sumsq)) - want) <= 1e-12 * want
+    coef = float(np.float32(max_norm)) / want
+    out = [torch.empty_like(g) for g in grads]
+    dfl.clip_grads(grads, sumsq, max_norm, out=out)
+    for g, o in zip(grads, out):  # (bounds as in clip_check)
+        least = 2.0 ** -126 * HALF[g.dtype]
+        within(o, g.double() * coef, (HALF[g.dtype] + 3 * U) * g.double().abs() * coef + least, "clip")
+    dfl.clip_grads(grads, sumsq, max_norm)
+    assert all(torch.equal(g, o) for g, o in zip(grads, out))
