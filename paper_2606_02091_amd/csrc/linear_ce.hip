@@ -160,11 +160,31 @@ __global__ __launch_bounds__(1024) void k_lce_rows(Lce a, int pieces) {
       if (!on) a.row_ce[r] = 0.f;
     }
   }
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-  if (lane == 0) ws[wv] = sum;
-  __syncthreads();
-  sum = 0.0;
-  for (int k = 0; k < 16; ++k) sum += ws[k];
+  auto total = [&](double v) {  // over the work-group
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    __syncthreads();
+    if (lane == 0) ws[wv] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int k = 0; k < 16; ++k) v += ws[k];
+    return v;
+  };
+  sum = total(sum);
+  if (n > 0 && sum < 1e-30) {  // the first rows with a loss lie so late in their blocks that the weights leave fp32: from there
+    int lo = INT_MAX;
+    for (int i = tid; i < n; i += 1024) lo = min(lo, a.src[i] % a.B);
+    for (int off = 32; off > 0; off >>= 1) lo = min(lo, __shfl_xor(lo, off));
+    if (lane == 0) wc[wv] = lo;
+    __syncthreads();
+    for (int k = 0; k < 16; ++k) lo = min(lo, wc[k]);
+    sum = 0.0;
+    for (int i = tid; i < n; i += 1024) {
+      const float w = expf(-(float)(a.src[i] % a.B - lo) / a.gamma);
+      sum += w;
+      a.c[i] = w;
+    }
+    sum = total(sum);
+  }
   const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
   const int np = min((n + kBlock - 1) / kBlock * kBlock, a.Mp);
   for (int i = tid; i < np; i += 1024) {

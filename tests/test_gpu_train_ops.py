@@ -1040,3 +1040,12 @@ def test_grad_clip_by_factors_below_the_normal_range(std, max_norm):
         within(o, g.double() * coef, (HALF[g.dtype] + 3 * U) * g.double().abs() * coef + least, "clip")
     dfl.clip_grads(grads, sumsq, max_norm)
     assert all(torch.equal(g, o) for g, o in zip(grads, out))
+
+
+@pytest.mark.parametrize("n,B,first,gamma", [(3, 700, 400, 2.0), (40, 4, 2, 0.01), (2, 1024, 900, 4.5), (300, 8, 7, 0.06), (40, 4, 1, 0.01)])
+def test_linear_ce_of_late_positions(n, B, first, gamma):
+    """The first positions of every block have no target, so that all weights lie below fp32: only their ratios count."""
+    h, head, y = lce_inputs(n, B, 300, 64, seed=81, ignored=0.1)
+    y[torch.arange(n * B, device="cuda") % B < first] = -1
+    for dh, dw in ((False, False), (True, False), (True, True)):
+        lce_check(h, head, y, B, gamma, dfl.linear_ce(h, head, y, B, gamma, need_dhidden=dh, need_dhead=dw))
