@@ -1,0 +1,501 @@
+"""Operators that complete a draft layer's training step, and its projections for single blocks: cases, inputs,
+plain forms and 64-bit results.
+
+* ``qk``: the norm of each query and key head with its rotary position, forward and backward;
+* ``gated``: the gated feed-forward block (both projections, activation, product), forward and backward;
+* ``linear``: a projection with bias, activation and residual, forward and backward;
+* ``adamw``: the AdamW step over many tensors, with states in fp32 or in 8 bits.
+
+The plain forms compute in 32 bits (angles, long sums and clipping factors in 64) with elementary tensor operations.
+A backward pass is taken at the values that its forward pass stored (the pre-activations, in bf16).
+"""
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+BLOCK = 256  # values that share a scale of an 8-bit state
+E4M3_MOST, E4M3_LEAST = 448.0, 2.0 ** -9
+
+
+def listed():
+    return [
+        # queries and block keys of 512 anchored blocks of 16 positions, with their gradients
+        dict(name="qk_blocks", kind="qk", rows=8192, block=16, n_q=32, n_kv=8, hd=128, rot=128, layout="half",
+             dtype="bf16", scale=1.0, far=4096, backward=True),
+        # one token of each of 32 sequences, 64-wide heads: latency
+        dict(name="qk_token", kind="qk", rows=32, block=1, n_q=64, n_kv=8, hd=64, rot=64, layout="half",
+             dtype="bf16", scale=1.0, far=8192, backward=False),
+        # fp32, a part of each head turned in interleaved pairs whose number fits no wide access, far positions
+        dict(name="qk_odd", kind="qk", rows=4001, block=4001, n_q=16, n_kv=3, hd=80, rot=36, layout="interleaved",
+             dtype="f32", scale=1.25, far=1000000, backward=True),
+        # the feed-forward block of a draft layer over 512 blocks of 16 positions, with all gradients
+        dict(name="gated_train", kind="gated", rows=8192, hidden=4096, ffn=12288, act="silu", backward=True),
+        # the same for one drafted block: the weights are read once
+        dict(name="gated_block", kind="gated", rows=16, hidden=4096, ffn=12288, act="silu", backward=False),
+        # square weights that end inside a tile, odd rows
+        dict(name="gated_odd", kind="gated", rows=1003, hidden=2880, ffn=2880, act="gelu_tanh", backward=True),
+        # the down projection with the residual stream, with its gradients
+        dict(name="linear_down", kind="linear", rows=8192, n=4096, k=12288, act="none", bias=False, residual=True,
+             backward=True),
+        # the joint query, key and value projection of one drafted block, with a bias
+        dict(name="linear_block", kind="linear", rows=16, n=6144, k=2560, act="none", bias=True, residual=False,
+             backward=False),
+        # odd rows through an activation with a bias, with all gradients
+        dict(name="linear_odd", kind="linear", rows=777, n=5120, k=2880, act="gelu", bias=True, residual=False,
+             backward=True),
+        # two draft layers (Qwen3-8B shape): matrices in bf16 with fp32 masters, gains in fp32, states in fp32
+        dict(name="adamw_layers", kind="adamw", tensors=26, small=4096, large=50331648, bits=32, masters=True,
+             max_norm=1.0),
+        # the same layers without masters, states in 8 bits
+        dict(name="adamw_8bit", kind="adamw", tensors=26, small=4096, large=50331648, bits=8, masters=False,
+             max_norm=1.0),
+        # many small ragged tensors, states in 8 bits: tables and latency
+        dict(name="adamw_ragged", kind="adamw", tensors=301, small=1, large=70001, bits=8, masters=True,
+             max_norm=0.5),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    """Uniform over the logarithm of [lo, hi]."""
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(["qk", "gated", "gated", "linear", "linear", "adamw"])
+    if kind == "qk":
+        hd = rng.choice([64, 128, 128, 96, 256, 80])
+        return dict(kind=kind, rows=_log_int(rng, 1, 8192), block=rng.choice([1, 16, rng.randint(2, 300)]),
+                    n_q=rng.choice([8, 16, 32, rng.randint(1, 32)]), n_kv=rng.choice([0, 8, rng.randint(1, 8)]),
+                    hd=hd, rot=rng.choice([hd, hd, hd // 2]), layout=rng.choice(["half", "interleaved"]),
+                    dtype=rng.choice(["bf16", "bf16", "f32"]), scale=rng.choice([1.0, 1.0, 1.25]),
+                    far=_log_int(rng, 10, 1000000), backward=rng.random() < 0.5)
+    if kind == "gated":
+        return dict(kind=kind, rows=_log_int(rng, 1, 8192), hidden=rng.choice([4096, 2880, 2560, 8 * _log_int(rng, 4, 512)]),
+                    ffn=rng.choice([12288, 9728, 2880, 8 * _log_int(rng, 4, 1536)]),
+                    act=rng.choice(["silu", "silu", "gelu", "gelu_tanh", "relu", "none"]), backward=rng.random() < 0.5)
+    if kind == "linear":
+        return dict(kind=kind, rows=_log_int(rng, 1, 8192), n=rng.choice([4096, 6144, 5120, 8 * _log_int(rng, 4, 1536)]),
+                    k=rng.choice([4096, 2880, 2560, 12288, 8 * _log_int(rng, 4, 1536)]),
+                    act=rng.choice(["none", "none", "silu", "gelu", "gelu_tanh", "relu"]), bias=rng.random() < 0.5,
+                    residual=rng.random() < 0.5, backward=rng.random() < 0.5)
+    large = _log_int(rng, 1000, 50000000)
+    return dict(kind=kind, tensors=_log_int(rng, 1, max(2, min(400, int(1.5e9 / large)))), small=_log_int(rng, 1, 999),
+                large=large, bits=rng.choice([8, 32]), masters=rng.random() < 0.5,
+                max_norm=round(math.exp(rng.uniform(-2.0, 2.0)), 3))
+
+
+# ---- inputs ---------------------------------------------------------------------------------
+
+def _gen(seed, salt):
+    return torch.Generator(device="cuda").manual_seed(1000 * seed + salt)
+
+
+_TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _normal(shape, dtype, g, std=1.0, mean=0.0):
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(mean, std, generator=g)
+
+
+def _qk_inputs(case, seed):
+    """Queries and keys as projections give them, gains around one, positions of blocks, output gradients."""
+    g = _gen(seed, 1)
+    rows, hd, t = case["rows"], case["hd"], _TYPES[case["dtype"]]
+    heads = [n for n in (case["n_q"], case["n_kv"]) if n > 0]
+    xs = [_normal((rows, n, hd), t, g, 1.5) for n in heads]
+    gains = [_normal((hd,), t, g, 0.1, 1.0) for _ in heads]
+    dys = [_normal((rows, n, hd), t, g) for n in heads] if case["backward"] else None
+    n_blocks = -(-rows // case["block"])
+    pos = torch.randint(0, max(case["far"] - case["block"], 0) + 1, (n_blocks,), generator=g, device="cuda",
+                        dtype=torch.int32)
+    m = torch.arange(case["rot"] // 2, dtype=torch.float64, device="cuda")
+    return xs, gains, pos, 1e6 ** (-2.0 * m / case["rot"]), dys
+
+
+def _gated_inputs(case, seed):
+    """Rows N(0, 1) as a norm gives them; weights that keep the pre-activations near that."""
+    g = _gen(seed, 2)
+    rows, H, F, t = case["rows"], case["hidden"], case["ffn"], torch.bfloat16
+    x = _normal((rows, H), t, g)
+    wg, wu = (_normal((F, H), t, g, H ** -0.5) for _ in range(2))
+    return x, wg, wu, _normal((rows, F), t, g) if case["backward"] else None
+
+
+def _linear_inputs(case, seed):
+    g = _gen(seed, 3)
+    rows, N, K, t = case["rows"], case["n"], case["k"], torch.bfloat16
+    x, w = _normal((rows, K), t, g), _normal((N, K), t, g, K ** -0.5)
+    bias = _normal((N,), t, g, 0.5) if case["bias"] else None
+    res = _normal((rows, N), t, g, 2.0) if case["residual"] else None
+    return x, w, bias, res, _normal((rows, N), t, g) if case["backward"] else None
+
+
+def _adamw_sizes(case):
+    """Sizes spread over the logarithm of [small, large], none of them at random: (bf16 ones, fp32 ones)."""
+    n, lo, hi = case["tensors"], math.log(case["small"]), math.log(case["large"])
+    if case["small"] == 4096:  # layers: 13 tensors each, matrices of the draft layer, then its gains
+        layer = [4096 * 4096] * 2 + [1024 * 4096] * 4 + [12288 * 4096] * 3
+        return layer * (n // 13), [4096] * (4 * (n // 13))
+    sizes = [int(round(math.exp(lo + (hi - lo) * (((7 * i + 3) % n) + 0.5) / n))) for i in range(n)]
+    return sizes[0::2], sizes[1::2]
+
+
+HYPER = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
+STEP = 1000
+
+
+class _Group:
+    """Tensors of one type as a program keeps them, side by side in one buffer of each kind: parameters, gradients,
+    masters, moments; the 8-bit moments with a scale for every 256 values of a tensor."""
+
+    def __init__(self, sizes, dtype, case, g, std):
+        self.sizes, self.n = sizes, sum(sizes)
+        self.bits, self.max_norm = case["bits"], case["max_norm"]
+        self.master = _normal((self.n,), torch.float32, g, 0.02)
+        self.param = self.master.to(dtype)
+        if dtype == torch.float32 or not case["masters"]:
+            self.master = None
+        self.grad = _normal((self.n,), dtype, g, std)
+        self.m = _normal((self.n,), torch.float32, g, 0.3 * std)
+        self.v = _normal((self.n,), torch.float32, g, std).square_()
+        blocks = [-(-s // BLOCK) for s in sizes]
+        self.blocks = sum(blocks)
+        self.at = None  # places of the values in whole blocks, where a tensor does not end with one
+        if any(s % BLOCK for s in sizes):
+            skipped = torch.tensor([b * BLOCK - s for b, s in zip(blocks, sizes)], device="cuda").cumsum(0).roll(1)
+            skipped[:1] = 0
+            self.at = torch.arange(self.n, device="cuda") + skipped.repeat_interleave(torch.tensor(sizes, device="cuda"))
+        self.m_scale = self.v_scale = None
+        if self.bits == 8:
+            self.m, self.m_scale = self.quantise(self.m)
+            self.v, self.v_scale = self.quantise(self.v.sqrt_(), True)
+        # what the calls take: the tensors and their states
+        cut = lambda t: None if t is None else list(t.split(sizes))  # noqa: E731
+        self.params, self.grads, self.masters, self.ms, self.vs = map(
+            cut, (self.param, self.grad, self.master, self.m, self.v))
+        cut = lambda t: None if t is None else list(t.split(blocks))  # noqa: E731
+        self.m_scales, self.v_scales = cut(self.m_scale), cut(self.v_scale)
+
+    def padded(self, x):
+        if self.at is not None:
+            x = torch.zeros(self.blocks * BLOCK, dtype=x.dtype, device=x.device).index_copy_(0, self.at, x)
+        return x.view(self.blocks, BLOCK)
+
+    def flat(self, x):
+        return x.reshape(-1) if self.at is None else x.reshape(-1)[self.at]
+
+    def quantise(self, x, up=False):
+        """(e4m3 values, scales of the blocks); up: what is above zero stays above it."""
+        b = self.padded(x)
+        scale = (b.abs().amax(1) / E4M3_MOST).clamp_min(2.0 ** -96)
+        q = b / scale[:, None]
+        if up:
+            q = torch.where(b > 0, q.clamp_min(E4M3_LEAST), q)
+        return self.flat(q).to(torch.float8_e4m3fn), scale
+
+    def value(self, q, scale):
+        return self.flat(self.padded(q.float()) * scale[:, None])
+
+    def outputs(self):
+        return [t for t in (self.param, self.master, self.m, self.v, self.m_scale, self.v_scale) if t is not None]
+
+
+def _adamw_inputs(case, seed):
+    """Two groups of tensors in the midst of a training, gradients of three times the norm that they are clipped to."""
+    g = _gen(seed, 4)
+    sizes = _adamw_sizes(case)
+    std = 3.0 * case["max_norm"] / math.sqrt(sum(map(sum, sizes)))
+    groups = [_Group(s, t, case, g, std) for s, t in zip(sizes, (torch.bfloat16, torch.float32)) if s]
+    # the gradients' sum of squares, from the call that gives their norm
+    sumsq = torch.stack([(x.grad.double() if x.n < 1 << 26 else x.grad.float()).square().sum(dtype=torch.float64)
+                         for x in groups]).sum().view(1)
+    return groups, sumsq
+
+
+class _Lists:
+    """The two groups' tensors as the lists that a program passes."""
+
+    def __init__(self, groups, sumsq):
+        self.groups, self.sumsq = groups, sumsq
+        both = lambda f: [t for x in groups for t in (getattr(x, f) or [None] * len(x.sizes))]  # noqa: E731
+        self.params, self.grads, self.m, self.v, self.masters = map(both, ("params", "grads", "ms", "vs", "masters"))
+        self.m_scales, self.v_scales = both("m_scales"), both("v_scales")
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    if kind == "qk":
+        return kind, case, _qk_inputs(case, seed)
+    if kind == "gated":
+        return kind, case, _gated_inputs(case, seed)
+    if kind == "linear":
+        return kind, case, _linear_inputs(case, seed)
+    return kind, case, _Lists(*_adamw_inputs(case, seed))
+
+
+# ---- one pass ---------------------------------------------------------------------------------
+
+def run(state):
+    kind, case, x = state
+    return {"qk": _qk, "gated": _gated, "linear": _linear, "adamw": _adamw}[kind](case, x)
+
+
+def _turn(u, c, s, rot, half):
+    """The first rot values of each head, turned."""
+    v = u[..., :rot]
+    a, b = (v[..., :rot // 2], v[..., rot // 2:]) if half else (v[..., 0::2], v[..., 1::2])
+    pair = (a * c - b * s, b * c + a * s)
+    return torch.cat([torch.cat(pair, -1) if half else torch.stack(pair, -1).flatten(-2), u[..., rot:]], -1)
+
+
+def _qk(case, x):
+    xs, gains, pos, freq, dys = x
+    B, scale = case["block"], case["scale"]
+    if own:
+        from paper_2606_02091_amd import dflare as dfl
+        layout = dfl.ROPE_HALF if case["layout"] == "half" else dfl.ROPE_INTERLEAVED
+        outs = list(dfl.qk_norm_rope_fwd(tuple(xs), tuple(gains), freq, pos, B=B, layout=layout, scale=scale, eps=EPS))
+        if dys is not None:
+            dxs, dgains = dfl.qk_norm_rope_bwd(tuple(dys), tuple(xs), tuple(gains), freq, pos, B=B, layout=layout,
+                                               scale=scale, eps=EPS)
+            outs += [*dxs, *dgains]
+        return outs
+    rot, half = case["rot"], case["layout"] == "half"
+    r = torch.arange(case["rows"], device=pos.device)
+    th = (pos[r // B].double() + r % B)[:, None] * freq
+    c, s = (torch.cos(th) * scale).float()[:, None], (torch.sin(th) * scale).float()[:, None]
+    ys, dxs, dgains = [], [], []
+    for i, (t, gain) in enumerate(zip(xs, gains)):
+        u, w = t.float(), gain.float()
+        rstd = torch.rsqrt((u * u).mean(-1, keepdim=True) + EPS)
+        n = u * rstd
+        ys.append(_turn(n * w, c, s, rot, half).to(t.dtype))
+        if dys is not None:
+            d = _turn(dys[i].float(), c, -s, rot, half)
+            e = d * w
+            dxs.append((rstd * (e - n * (e * n).mean(-1, keepdim=True))).to(t.dtype))
+            dgains.append((d * n).double().sum((0, 1)).float())
+    return ys + dxs + dgains
+
+
+def _act(name, z):
+    """The activation and its derivative."""
+    if name == "relu":
+        on = (z > 0).to(z.dtype)
+        return z * on, on
+    if name == "silu":
+        s = 1.0 / (1.0 + torch.exp(-z))
+        return z * s, s * (1.0 + z * (1.0 - s))
+    if name == "gelu":
+        phi = 0.5 * (1.0 + torch.erf(z * math.sqrt(0.5)))
+        return z * phi, phi + z * torch.exp(-0.5 * z * z) * (1.0 / math.sqrt(2.0 * math.pi))
+    if name == "gelu_tanh":
+        a = math.sqrt(2.0 / math.pi)
+        t = torch.tanh(a * (z + 0.044715 * z * z * z))
+        return 0.5 * z * (1.0 + t), 0.5 * (1.0 + t) + 0.5 * z * (1.0 - t * t) * a * (1.0 + 3.0 * 0.044715 * z * z)
+    return z, torch.ones_like(z)
+
+
+def _gated(case, x):
+    x, wg, wu, dh = x
+    if own:
+        from paper_2606_02091_amd import dflare as dfl
+        act = getattr(dfl, "ACT_" + case["act"].upper())
+        h, gate, up = dfl.gated_fwd(x, wg, wu, act=act, save=dh is not None)
+        if dh is None:
+            return [h]
+        return [h, gate, up, *dfl.gated_bwd(dh, x, gate, up, wg, wu, act=act)]
+    xf, g32, u32 = x.float(), wg.float(), wu.float()
+    gate, up = xf @ g32.t(), xf @ u32.t()
+    h = (_act(case["act"], gate)[0] * up).to(x.dtype)
+    if dh is None:
+        return [h]
+    gate, up = gate.to(x.dtype), up.to(x.dtype)
+    d = dh.float()
+    a, da = _act(case["act"], gate.float())
+    dg, du = d * up.float() * da, d * a
+    dx = (dg @ g32).add_(du @ u32)
+    return [h, gate, up, dx.to(x.dtype), (dg.t() @ xf).to(x.dtype), (du.t() @ xf).to(x.dtype)]
+
+
+def _linear(case, x):
+    x, w, bias, res, dy = x
+    named = case["act"] != "none"
+    if own:
+        from paper_2606_02091_amd import dflare as dfl
+        act = getattr(dfl, "ACT_" + case["act"].upper())
+        y, z = dfl.linear_fwd(x, w, bias, residual=res, act=act, save=named and dy is not None)
+        outs = [y] + ([z] if z is not None else [])
+        if dy is not None:
+            outs += [t for t in dfl.linear_bwd(dy, x, w, z, act=act, need_dbias=bias is not None) if t is not None]
+        return outs
+    xf, wf = x.float(), w.float()
+    z = xf @ wf.t()
+    if bias is not None:
+        z += bias.float()
+    y = _act(case["act"], z)[0]
+    if res is not None:
+        y = y + res.float()
+    outs = [y.to(x.dtype)]
+    if dy is not None:
+        dz = dy.float()
+        if named:
+            z = z.to(x.dtype)
+            outs.append(z)
+            dz = dz * _act(case["act"], z.float())[1]
+        outs += [(dz @ wf).to(x.dtype), (dz.t() @ xf).to(x.dtype)]
+        if bias is not None:
+            outs.append(dz.double().sum(0).to(x.dtype))
+    return outs
+
+
+def _adamw(case, x):
+    if own:
+        from paper_2606_02091_amd import dflare as dfl
+        dfl.adamw(x.params, x.grads, x.m, x.v, STEP, masters=x.masters, m_scales=x.m_scales, v_scales=x.v_scales,
+                  sumsq=x.sumsq, max_norm=case["max_norm"], **HYPER)
+        return [t for g in x.groups for t in g.outputs()]
+    lr, b1, b2, eps, wd = (HYPER[k] for k in ("lr", "beta1", "beta2", "eps", "weight_decay"))
+    norm = torch.sqrt(x.sumsq)
+    factor = torch.where(norm > case["max_norm"], case["max_norm"] / norm, 1.0).float()
+    for g in x.groups:
+        d = g.grad.float() * factor
+        m, v = (g.m, g.v) if g.bits == 32 else (g.value(g.m, g.m_scale), g.value(g.v, g.v_scale).square_())
+        m = b1 * m + (1.0 - b1) * d
+        v = b2 * v + (1.0 - b2) * (d * d)
+        p = (g.param if g.master is None else g.master).float()
+        p = p * (1.0 - lr * wd) - lr / (1.0 - b1 ** STEP) * m / (torch.sqrt(v) / math.sqrt(1.0 - b2 ** STEP) + eps)
+        g.param.copy_(p)
+        if g.master is not None:
+            g.master.copy_(p)
+        if g.bits == 8:
+            m, s = g.quantise(m)
+            g.m_scale.copy_(s)
+            v, s = g.quantise(v.sqrt_(), True)
+            g.v_scale.copy_(s)
+        g.m.copy_(m)
+        g.v.copy_(v)
+    return [t for g in x.groups for t in g.outputs()]
+
+
+# ---- work -----------------------------------------------------------------------------------
+
+def work(case):
+    kind = case["kind"]
+    if kind == "qk":
+        n, size = case["rows"] * (case["n_q"] + case["n_kv"]) * case["hd"], 2 if case["dtype"] == "bf16" else 4
+        return {"bytes": (4 if case["backward"] else 2) * n * size + 4 * -(-case["rows"] // case["block"]) + 8 * case["hd"],
+                "flops": (24 if case["backward"] else 8) * n}
+    if kind == "gated":
+        rows, H, F, b = case["rows"], case["hidden"], case["ffn"], case["backward"]
+        moved = rows * H + 2 * F * H + rows * F + b * (2 * rows * F + rows * F + rows * H + 2 * F * H)
+        return {"bytes": 2 * moved, "flops": 4 * rows * H * F * (3 if b else 1)}
+    if kind == "linear":
+        rows, N, K, b = case["rows"], case["n"], case["k"], case["backward"]
+        moved = rows * K + N * K + rows * N * (1 + case["residual"]) + N * case["bias"]
+        moved += b * (rows * N * (1 + (case["act"] != "none")) + rows * K + N * K + N * case["bias"])
+        return {"bytes": 2 * moved, "flops": 2 * rows * N * K * (3 if b else 1)}
+    a, b = map(sum, _adamw_sizes(case))
+    state = 16 if case["bits"] == 32 else 4 * (1 + 4 / BLOCK)  # both moments, read and written
+    low = 2 + 2 + 8 if case["masters"] else 2 + 2 + 2  # gradient, parameter (written only beside a master), master
+    return {"bytes": int(a * (low + state) + b * (4 + 8 + state)), "flops": 16 * (a + b)}
+
+
+# ---- 64-bit results ---------------------------------------------------------------------------
+
+def _exact_qk(case, seed):
+    xs, gains, pos, freq, dys = _qk_inputs(case, seed)
+    rows, rot, B, hd = case["rows"], case["rot"], case["block"], case["hd"]
+    at = torch.tensor([k % B for k in range(rows)], device="cuda") + pos.long().repeat_interleave(B)[:rows]
+    turn = torch.polar(torch.full_like(freq, case["scale"]).expand(rows, -1), at.double()[:, None] * freq)[:, None]
+    ys, dxs, dgains = [], [], []
+    for i, (t, gain) in enumerate(zip(xs, gains)):
+        u, w = t.double().requires_grad_(dys is not None), gain.double().requires_grad_(dys is not None)
+        n = u / torch.sqrt(u.square().sum(-1, keepdim=True) / hd + EPS) * w
+        half = case["layout"] == "half"
+        pairs = n[..., :rot].unflatten(-1, (2, rot // 2)).transpose(-1, -2) if half else n[..., :rot].unflatten(-1, (rot // 2, 2))
+        z = torch.view_as_real(torch.view_as_complex(pairs.contiguous()) * turn)
+        y = torch.cat([(z.transpose(-1, -2) if half else z).flatten(-2), n[..., rot:]], -1)
+        ys.append(y.detach())
+        if dys is not None:
+            du, dw = torch.autograd.grad(y, (u, w), dys[i].double())
+            dxs.append(du)
+            dgains.append(dw)
+    return ys + dxs + dgains
+
+
+def _exact_act(name, z):
+    if name == "silu":
+        return z * torch.sigmoid(z)
+    if name == "gelu":
+        return 0.5 * z * torch.erfc(-z / math.sqrt(2.0))
+    if name == "gelu_tanh":
+        return z * torch.sigmoid(2.0 * math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3))
+    return z.clamp_min(0.0) if name == "relu" else z
+
+
+def _exact_gated(case, seed):
+    x, wg, wu, dh = _gated_inputs(case, seed)
+    x64, g64, u64 = x.double(), wg.double(), wu.double()
+    gate, up = x64.mm(g64.t()), x64.mm(u64.t())
+    outs = [_exact_act(case["act"], gate).mul_(up).detach()]
+    if dh is None:
+        return outs
+    outs += [gate, up]
+    # the gradients at the stored pre-activations
+    gate, up = (t.to(x.dtype).double().requires_grad_() for t in (gate, up))
+    dgate, dup = torch.autograd.grad(_exact_act(case["act"], gate) * up, (gate, up), dh.double())
+    return outs + [dgate.mm(g64) + dup.mm(u64), dgate.t().mm(x64), dup.t().mm(x64)]
+
+
+def _exact_linear(case, seed):
+    x, w, bias, res, dy = _linear_inputs(case, seed)
+    x64, w64 = x.double(), w.double()
+    z = x64.mm(w64.t()) + (0.0 if bias is None else bias.double())
+    y = _exact_act(case["act"], z) + (0.0 if res is None else res.double())
+    outs = [y]
+    if dy is None:
+        return outs
+    dz = dy.double()
+    if case["act"] != "none":
+        outs.append(z)
+        z = z.to(x.dtype).double().requires_grad_()
+        dz, = torch.autograd.grad(_exact_act(case["act"], z), z, dz)
+    outs += [dz.mm(w64), dz.t().mm(x64)]
+    return outs + ([dz.sum(0)] if bias is not None else [])
+
+
+def _exact_adamw(case, seed):
+    groups, sumsq = _adamw_inputs(case, seed)
+    factor = min(1.0, case["max_norm"] / float(sumsq.sqrt()))
+    lr, b1, b2, eps, wd = (HYPER[k] for k in ("lr", "beta1", "beta2", "eps", "weight_decay"))
+    outs = []
+    for x in groups:
+        m, v = x.m.double(), x.v.double()
+        if x.bits == 8:
+            m, v = x.flat(x.padded(m) * x.m_scale.double()[:, None]), x.flat(x.padded(v) * x.v_scale.double()[:, None]) ** 2
+        d = x.grad.double().mul_(factor)
+        m.mul_(b1).add_(d, alpha=1 - b1)
+        v.mul_(b2).addcmul_(d, d, value=1 - b2)
+        p = (x.param if x.master is None else x.master).double()
+        p = p - lr * (m / (1 - b1 ** STEP) / ((v / (1 - b2 ** STEP)).sqrt() + eps) + wd * p)
+        outs += [p] + ([p] if x.master is not None else [])
+        if x.bits == 32:
+            outs += [m, v]
+            continue
+        scales, parts = [], []
+        for t in (m, v.sqrt()):
+            b = x.padded(t)
+            scales.append(b.abs().amax(1) / E4M3_MOST)
+            parts.append(x.flat(b / scales[-1].clamp_min(1e-300)[:, None]))
+        outs += parts + scales
+    return outs
+
+
+def exact(case, seed):
+    kinds = {"qk": _exact_qk, "gated": _exact_gated, "linear": _exact_linear, "adamw": _exact_adamw}
+    with torch.set_grad_enabled(True):
+        return [t.detach() for t in kinds[case["kind"]](case, seed)]
