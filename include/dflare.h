@@ -663,6 +663,133 @@ int dflare_grad_norm(const dflare_grad_tensor* tensors, int32_t n, double* sumsq
                      size_t workspace_bytes, void* stream);
 int dflare_clip_grads(const dflare_grad_tensor* tensors, int32_t n, const double* sumsq, float max_norm, void* stream);
 
+/*
+ * dflare_qk_norm_rope_fwd -- the RMSNorm of each query and key head and its rotary position, in one pass:
+ *   y = scale R(p) (x / sqrt(mean of x^2 + eps) gain), the mean over the head's head_dim values,
+ * with the turn R(p), positions, inv_freq, B, layout, scale and rotary_dim of dflare_rope.  Nothing between is rounded: dflare_norm_fwd
+ * followed by dflare_rope rounds the norm's result once more.
+ *   tensors  HOST [n_tensors], 1 or 2 (queries and keys, of the same rows): x and y as in dflare_rope; gain [head_dim] of type
+ *            dtype, for all heads of the tensor, or NULL: ones.  y may be x with the same strides.
+ * dflare_qk_norm_rope_bwd -- the gradients for the output gradients dy, from x itself (nothing is kept by the forward pass):
+ *   dx       of type dtype; may be x or dy, with the same strides
+ *   dgain    fp32 [head_dim] out, or NULL: summed over rows and heads in a fixed order in fp32 (zeros without any)
+ *   workspace  16-byte aligned, at least dflare_qk_norm_rope_bwd_workspace(rows, head_dim, n_tensors) bytes
+ * A head with NaN or infinities is what the formula gives; other heads' results are not touched, dgain aside.
+ * rows = 0 does nothing, but for dgain.  head_dim > 512 or n_heads head_dim > 2^20: UNSUPPORTED.  Any alignment and strides, as in dflare_rope.
+ */
+typedef struct {
+  const void* x;
+  void* y;
+  const void* gain;
+  int64_t x_row, x_head, y_row, y_head; /* strides, in elements */
+  int32_t n_heads;
+} dflare_qk_tensor;
+typedef struct {
+  const void* x;
+  const void* dy;
+  void* dx;
+  const void* gain;
+  float* dgain;
+  int64_t x_row, x_head, dy_row, dy_head, dx_row, dx_head;
+  int32_t n_heads;
+} dflare_qk_grad;
+int dflare_qk_norm_rope_fwd(const dflare_qk_tensor* tensors, int32_t n_tensors, const int32_t* positions, const double* inv_freq,
+                            int32_t rows, int32_t B, int32_t head_dim, int32_t rotary_dim, int32_t dtype, int32_t layout, float scale,
+                            float eps, void* stream);
+size_t dflare_qk_norm_rope_bwd_workspace(int32_t rows, int32_t head_dim, int32_t n_tensors);
+int dflare_qk_norm_rope_bwd(const dflare_qk_grad* tensors, int32_t n_tensors, const int32_t* positions, const double* inv_freq,
+                            int32_t rows, int32_t B, int32_t head_dim, int32_t rotary_dim, int32_t dtype, int32_t layout, float scale,
+                            float eps, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Activations of the projections and the gated block: z, max(z, 0), z / (1 + e^-z), z Phi(z), and
+ * z / (1 + e^-2t) with t = sqrt(2 / pi) (z + 0.044715 z^3), which is 0.5 z (1 + tanh t).  Value and derivative have their limits at the
+ * infinities (the derivative of RELU at 0 is 0); NaN stays NaN.
+ */
+enum { DFLARE_ACT_NONE = 0, DFLARE_ACT_RELU = 1, DFLARE_ACT_SILU = 2, DFLARE_ACT_GELU = 3, DFLARE_ACT_GELU_TANH = 4 };
+
+/*
+ * dflare_linear_fwd -- a projection with its epilogue: z = x w^T + bias, y = act(z) + residual.
+ *   x  bf16 [rows, K];  w  bf16 [N, K];  bias  bf16 [N] or NULL;  residual  bf16 [rows, N] or NULL
+ *   y  bf16 [rows, N] out; may be residual;  z  bf16 [rows, N] out, what the backward pass through an activation takes, or NULL: not wanted
+ *   workspace  at least dflare_linear_fwd_workspace(rows, N, K) bytes
+ * dflare_linear_bwd -- its gradients for the output gradient dy (which is also residual's), dz = dy act'(z):
+ *   z      of the forward pass; not read without an activation
+ *   dx     bf16 [rows, K] out: dz w;  dw  bf16 [N, K] out: dz^T x;  dbias  bf16 [N] out: dz added over the rows; each may be NULL: not
+ *          wanted (x is read for dw alone, w for dx alone)
+ *   workspace  at least dflare_linear_bwd_workspace(rows, N, K, act, dx wanted, dw wanted, dbias wanted) bytes
+ * Products run on the bf16 matrix cores with fp32 sums; everything up to y is formed in fp32 and rounded once.  The gradients are those at
+ * the stored z; dz is rounded to bf16 as an operand of dx and dw (dbias adds it unrounded).  All tensors 16-byte aligned.
+ * rows = 0 writes zeros to dw and dbias.  N or K not a multiple of 8 or above 2^18, more than 2^22 rows, or about 2^35 values of y or
+ * of w: UNSUPPORTED (a workspace is then 0 bytes).  Each workspace grows with rows, N and K.
+ * NaN and infinities stay in the rows of y and dx, and the rows and columns of dw, whose sums they belong to.
+ */
+size_t dflare_linear_fwd_workspace(int32_t rows, int32_t N, int32_t K);
+int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, int32_t rows, int32_t N, int32_t K,
+                      int32_t act, void* y, void* z, void* workspace, size_t workspace_bytes, void* stream);
+size_t dflare_linear_bwd_workspace(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias);
+int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* z, int32_t rows, int32_t N, int32_t K, int32_t act,
+                      void* dx, void* dw, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dflare_gated_fwd -- the gated feed-forward block up to its down projection, in one product: gate = x w_gate^T, up = x w_up^T,
+ * h = act(gate) up.
+ *   x  bf16 [rows, H];  w_gate, w_up  bf16 [F, H];  h  bf16 [rows, F] out
+ *   gate, up  bf16 [rows, F] out, what the backward pass takes, or both NULL: not wanted
+ *   workspace  at least dflare_gated_fwd_workspace(rows, H, F) bytes
+ * dflare_gated_bwd -- its gradients for dh, dgate = dh up act'(gate), dup = dh act(gate):
+ *   dx  bf16 [rows, H] out: dgate w_gate + dup w_up, or NULL;  dw_gate, dw_up  bf16 [F, H] out: dgate^T x, dup^T x, or both NULL
+ *   workspace  at least dflare_gated_bwd_workspace(rows, H, F, dx wanted, dw wanted) bytes
+ * Roundings, alignment, sizes, rows = 0, NaN and infinities as for the projections (N = F, K = H): gate and up are used unrounded in h, and as
+ * stored in the gradients; dgate and dup are rounded to bf16 as operands.
+ */
+size_t dflare_gated_fwd_workspace(int32_t rows, int32_t H, int32_t F);
+int dflare_gated_fwd(const void* x, const void* w_gate, const void* w_up, int32_t rows, int32_t H, int32_t F, int32_t act, void* h,
+                     void* gate, void* up, void* workspace, size_t workspace_bytes, void* stream);
+size_t dflare_gated_bwd_workspace(int32_t rows, int32_t H, int32_t F, int32_t dx, int32_t dw);
+int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void* up, const void* w_gate, const void* w_up, int32_t rows,
+                     int32_t H, int32_t F, int32_t act, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/*
+ * dflare_adamw -- one AdamW step over n tensors, in place.  With the clipped gradient g:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * formed in fp32 (the factors in double) and rounded once where stored.
+ *   param    of type param_dtype;  grad  of type grad_dtype
+ *   master   fp32 parameter in whose place param (bf16) is only written, rounded; or NULL: param is the parameter
+ *   m, v     the moments, zeros before the first step.  state_bits 32: fp32.  8: e4m3 (OCP, no infinities) numbers times a scale
+ *            for each 256 values of a tensor, m_scale and v_scale fp32 [ceil(n / 256)], the scale being the largest of them / 448 (2^-96 at
+ *            least); v holds the root of the second moment, of which what is above zero is at least the smallest number above
+ *            zero.  Numbers are rounded to nearest even; param and master are formed before that.
+ *   options  HOST: lr, beta1, beta2, eps, weight_decay; step, from 1; lr_device, step_device: DEVICE double and int64, read in their
+ *            place by the kernels (a captured step goes on counting), or NULL
+ *   sumsq    DEVICE double [1], dflare_grad_norm's, or NULL.  g = grad max_norm / norm where norm = sqrt(*sumsq) is above max_norm,
+ *            as dflare_clip_grads gives it, but for its rounding; where *sumsq is not finite the step is left out: nothing is written.
+ * Without sumsq a gradient that is not finite makes its value, and with 8 bits its 256 values of the states, what the formulas give.
+ * beta outside [0, 1), eps not above 0 in fp32, lr or weight_decay negative or not finite, step < 1, max_norm < 0 beside a sumsq,
+ * state_bits neither 8 nor 32: INVALID_ARG; more than 2^36 values in one tensor: UNSUPPORTED.  Tensors need the alignment of their elements alone.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  float* master;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  int64_t n; /* values */
+  int32_t param_dtype, grad_dtype;
+} dflare_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;
+  const double* lr_device;
+  const int64_t* step_device;
+  const double* sumsq;
+  float max_norm;
+  int32_t state_bits;
+} dflare_adamw_options;
+int dflare_adamw(const dflare_adamw_tensor* tensors, int32_t n, const dflare_adamw_options* options, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,7 +17,7 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libdflare.so")
 BINDING = os.path.join(LIBDIR, "_binding.so")
 SOURCES = ["kernels.hip", "batched.hip", "runtime.hip", "training.hip", "train_ops.hip",
-           "linear_ce.hip"]
+           "linear_ce.hip", "linear.hip", "qk_norm.hip", "adamw.hip"]
 ARCH = os.environ.get("DFLARE_OFFLOAD_ARCH", "gfx950")
 
 

@@ -1,0 +1,398 @@
+// The AdamW step over many tensors (Loshchilov and Hutter, "Decoupled weight decay regularization", 2019) and its C-ABI entry
+// point.  With the clipped gradient g, decoupled decay w and step t:
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+//   p = p (1 - lr w) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+// Clipping takes place here, by the gradients' sum of squares, so that no pass of its own reads and writes them.
+// States in 8 bits: m and sqrt(v) as e4m3 numbers times a scale for each 256 values of a tensor, its largest over 448.  The
+// root, because e4m3 then covers 2^36 of v instead of 2^18; what is above zero stays above zero, so that no step divides a
+// remembered m by eps alone.  Bound by memory: 28 bytes a value (bf16 with an fp32 master and fp32 states), 10 (bf16, 8 bits).
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+#include <vector>
+
+#include "dflare.h"
+#include "elements.h"
+
+namespace dflare {
+
+namespace {
+
+constexpr int kValues = 8;             // of a thread: a lane's share of a block of 256 is 1/32
+constexpr int kChunk = kT * kValues;   // values of a work-group's turn
+constexpr int kScaled = 256;           // values that share a scale
+constexpr int kGroups = 2048;          // work-groups of a launch, at most
+constexpr float kMost = 448.f, kLeast = 0.001953125f;  // of e4m3: largest, smallest above zero (2^-9)
+constexpr float kLeastScale = 1.2621774483536189e-29f;  // 2^-96: scales and their inverses stay inside fp32
+
+struct Hyper {
+  float decay, alpha, root;  // 1 - lr w, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float b1, c1, b2, c2, eps; // c: 1 - b
+};
+struct Options {
+  double lr, weight_decay, ln1, ln2;  // logarithms of b1, b2
+  const double* lr_device;
+  const int64_t* step_device;
+  const double* sumsq;
+  int64_t step;
+  float max_norm;
+  Hyper h;
+};
+__host__ __device__ inline void set_step(Hyper& h, double lr, double weight_decay, double ln1, double ln2, double t) {
+  h.decay = (float)(1.0 - lr * weight_decay);
+  h.alpha = (float)(lr / (1.0 - exp(t * ln1)));
+  h.root = (float)(1.0 / sqrt(1.0 - exp(t * ln2)));
+}
+
+// The tensors of a launch, as many as its arguments (4 KB) hold beside the options
+template <bool MASTER, bool BYTE>
+struct Tab {
+  static constexpr int N = 3850 / ((4 + MASTER + 2 * BYTE) * 8 + 9);
+  void* p[N];
+  const void* g[N];
+  void *m[N], *v[N];
+  float* w[MASTER ? N : 1];
+  float *ms[BYTE ? N : 1], *vs[BYTE ? N : 1];
+  uint32_t n[N];     // values, the low 32 bits
+  int first[N + 1];  // chunks before the tensor
+  uint8_t tag[N];    // 1: fp32 parameter; 2: fp32 gradient; 4: a master; the high bits of n above
+  int count;
+  __device__ __forceinline__ long size(int i) const { return (long)n[i] | (long)(tag[i] >> 3) << 32; }
+};
+static_assert(sizeof(Tab<true, true>) + sizeof(Options) <= 4048 && sizeof(Tab<false, false>) + sizeof(Options) <= 4048, "kernel arguments");
+
+// 8 values at any element
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  float a[4], b[4];
+  load_n<float, 4, false>(p, a);
+  load_n<float, 4, false>(p + 4, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = a[e];
+    x[4 + e] = b[e];
+  }
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) { load_n<bf16_t, 8, false>(p, x); }
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  const float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[4], x[5], x[6], x[7]};
+  store_n<float, 4, false>(p, a);
+  store_n<float, 4, false>(p + 4, b);
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) { store_n<bf16_t, 8, false>(p, x); }
+struct e4m3_t {
+  uint8_t b;
+};
+struct __attribute__((packed, aligned(1))) Bytes8 {
+  u32x2 v;
+};
+__device__ __forceinline__ void unpack8(u32x2 w, float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+    x[4 * k] = lo[0];
+    x[4 * k + 1] = lo[1];
+    x[4 * k + 2] = hi[0];
+    x[4 * k + 3] = hi[1];
+  }
+}
+__device__ __forceinline__ u32x2 pack8(const float (&x)[8]) {  // nearest even
+  u32x2 w;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k], x[4 * k + 1], 0, false);
+    w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2], x[4 * k + 3], r, true);
+  }
+  return w;
+}
+__device__ __forceinline__ void load8(const e4m3_t* p, float (&x)[8]) { unpack8(reinterpret_cast<const Bytes8*>(p)->v, x); }
+__device__ __forceinline__ void store8(e4m3_t* p, const float (&x)[8]) { reinterpret_cast<Bytes8*>(p)->v = pack8(x); }
+
+// `left` values at p, 0 to 8; zeros past them
+template <typename T>
+__device__ __forceinline__ void load_some(const T* p, int left, float (&x)[8]) {
+  if (left >= 8) return load8(p, x);
+  if constexpr (std::is_same_v<T, e4m3_t>) {
+    u32x2 w = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) w[e / 4] |= (uint32_t)p[e].b << (e % 4 * 8);
+    unpack8(w, x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < left ? to_f(p[e]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T* p, int left, const float (&x)[8]) {
+  if (left >= 8) return store8(p, x);
+  if constexpr (std::is_same_v<T, e4m3_t>) {
+    const u32x2 w = pack8(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e].b = (uint8_t)(w[e / 4] >> (e % 4 * 8));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = from_f<T>(x[e]);
+  }
+}
+
+// x over the scale of its 256 values, which 32 lanes hold, and the scale
+__device__ __forceinline__ float to_scale(float (&x)[8]) {
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
+  const float scale = fmaxf(most / kMost, kLeastScale), inv = 1.f / scale;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  return scale;
+}
+
+template <bool MASTER, bool BYTE, typename P, typename G>
+__device__ __forceinline__ void chunk(const Tab<MASTER, BYTE>& tab, int i, int c, const Hyper& h, Factor f) {
+  using S = std::conditional_t<BYTE, e4m3_t, float>;
+  const long at = (long)c * kChunk + threadIdx.x * kValues;
+  const int left = (int)max(min(tab.size(i) - at, 8l), 0l);
+  if (!BYTE && left == 0) return;
+  float p[8], g[8], m[8], v[8];
+  P* param = (P*)tab.p[i] + at;
+  S *pm = (S*)tab.m[i] + at, *pv = (S*)tab.v[i] + at;
+  float* master = MASTER && (tab.tag[i] & 4) ? tab.w[i] + at : nullptr;
+  load_some((const G*)tab.g[i] + at, left, g);
+  load_some(pm, left, m);
+  load_some(pv, left, v);
+  if (master) load_some((const float*)master, left, p);
+  else load_some((const P*)param, left, p);
+  float *sm = nullptr, *sv = nullptr;
+  if constexpr (BYTE) {
+    if (left > 0) {
+      sm = tab.ms[i] + at / kScaled;
+      sv = tab.vs[i] + at / kScaled;
+      const float a = *sm, b = *sv;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        m[e] *= a;
+        v[e] *= b;
+        v[e] *= v[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = f.of(g[e]);
+    m[e] = fmaf(h.c1, x, h.b1 * m[e]);
+    v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
+    const float r = sqrtf(v[e]);
+    p[e] = fmaf(-h.alpha, m[e] / fmaf(r, h.root, h.eps), p[e] * h.decay);
+    if constexpr (BYTE) v[e] = r;
+  }
+  if constexpr (BYTE) {
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[e];
+    const float a = to_scale(m), b = to_scale(v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (r[e] > 0.f) v[e] = v[e] < kLeast ? kLeast : v[e];
+    if (left > 0 && threadIdx.x % 32 == 0) {
+      *sm = a;
+      *sv = b;
+    }
+  }
+  store_some(pm, left, m);
+  store_some(pv, left, v);
+  store_some(param, left, p);
+  if (master) store_some(master, left, p);
+}
+
+template <bool MASTER, bool BYTE>
+__global__ __launch_bounds__(kT) void k_adamw(Tab<MASTER, BYTE> tab, Options o) {
+  Hyper h = o.h;
+  if (o.lr_device || o.step_device)
+    set_step(h, o.lr_device ? *o.lr_device : o.lr, o.weight_decay, o.ln1, o.ln2, (double)(o.step_device ? *o.step_device : o.step));
+  Factor f{1.f, 0};
+  if (o.sumsq) {
+    const double norm = sqrt(o.sumsq[0]);
+    if (!(norm < (double)INFINITY)) return;  // not finite: the step is left out
+    if (norm > (double)o.max_norm) f.m = (float)frexp((double)o.max_norm / norm, &f.e);
+  }
+  const long total = tab.first[tab.count];
+  int c = (int)(total * blockIdx.x / gridDim.x);
+  const int end = (int)(total * (blockIdx.x + 1) / gridDim.x);
+  if (c >= end) return;
+  int lo = 0, hi = tab.count - 1;  // the last tensor whose first chunk is not after c
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (tab.first[mid] <= c) lo = mid;
+    else hi = mid - 1;
+  }
+  for (; c < end; ++c) {
+    while (tab.first[lo + 1] <= c) ++lo;
+    const int at = c - tab.first[lo];
+    switch (tab.tag[lo] & 3) {
+      case 0: chunk<MASTER, BYTE, bf16_t, bf16_t>(tab, lo, at, h, f); break;
+      case 1: chunk<MASTER, BYTE, float, bf16_t>(tab, lo, at, h, f); break;
+      case 2: chunk<MASTER, BYTE, bf16_t, float>(tab, lo, at, h, f); break;
+      default: chunk<MASTER, BYTE, float, float>(tab, lo, at, h, f);
+    }
+  }
+}
+
+// ---- host side ----
+
+int check(const dflare_adamw_tensor* t, int n, const dflare_adamw_options& o) {
+  if (n < 0 || (n > 0 && !t)) return DFLARE_ERR_INVALID_ARG;
+  if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return DFLARE_ERR_INVALID_ARG;
+  if (!((float)o.eps > 0.f) || !isfinite((float)o.eps) || !(o.weight_decay >= 0.0) || !isfinite(o.weight_decay)) return DFLARE_ERR_INVALID_ARG;
+  if (!o.lr_device && (!(o.lr >= 0.0) || !isfinite(o.lr))) return DFLARE_ERR_INVALID_ARG;
+  if (!o.step_device && o.step < 1) return DFLARE_ERR_INVALID_ARG;
+  if (misplaced(o.lr_device, 8) || misplaced(o.step_device, 8) || misplaced(o.sumsq, 8)) return DFLARE_ERR_INVALID_ARG;
+  if (o.sumsq && !(o.max_norm >= 0.f)) return DFLARE_ERR_INVALID_ARG;
+  if (o.state_bits != 8 && o.state_bits != 32) return DFLARE_ERR_INVALID_ARG;
+  const bool byte = o.state_bits == 8;
+  for (int i = 0; i < n; ++i) {
+    const dflare_adamw_tensor& x = t[i];
+    const int ps = size_of(x.param_dtype), gs = size_of(x.grad_dtype);
+    if (!ps || !gs || x.n < 0 || (x.master && x.param_dtype != DFLARE_BF16)) return DFLARE_ERR_INVALID_ARG;
+    if (x.n > 0 && (!x.param || !x.grad || !x.m || !x.v || (byte && (!x.m_scale || !x.v_scale)))) return DFLARE_ERR_INVALID_ARG;
+    if (misplaced(x.param, ps) || misplaced(x.grad, gs) || misplaced(x.master, 4)) return DFLARE_ERR_INVALID_ARG;
+    if (byte ? misplaced(x.m_scale, 4) || misplaced(x.v_scale, 4) : misplaced(x.m, 4) || misplaced(x.v, 4)) return DFLARE_ERR_INVALID_ARG;
+    if (x.n > (1ll << 36)) return DFLARE_ERR_UNSUPPORTED;
+  }
+  return DFLARE_OK;
+}
+
+// INVALID_ARG where what is written (parameters, masters, states) overlaps anything else.  The lists of a call are
+// mostly in the order of their addresses: each is sorted only if it is not, then they are merged.
+int all_apart(const dflare_adamw_tensor* t, int n, const dflare_adamw_options& o) try {
+  struct Span {
+    uintptr_t a, b;
+    bool out;
+  };
+  const auto before = [](const Span& x, const Span& y) { return x.a < y.a; };
+  std::vector<Span> all, list, both;
+  all.reserve(7 * (size_t)n + 3);
+  both.reserve(7 * (size_t)n + 3);
+  list.reserve((size_t)n + 3);
+  auto add = [&](const void* p, size_t bytes, bool out) {
+    if (p && bytes) list.push_back({(uintptr_t)p, (uintptr_t)p + bytes, out});
+  };
+  auto merge = [&] {
+    if (!std::is_sorted(list.begin(), list.end(), before)) std::sort(list.begin(), list.end(), before);
+    both.clear();
+    std::merge(all.begin(), all.end(), list.begin(), list.end(), std::back_inserter(both), before);
+    all.swap(both);
+    list.clear();
+  };
+  add(o.lr_device, 8, false);
+  add(o.step_device, 8, false);
+  add(o.sumsq, 8, false);
+  merge();
+  const bool byte = o.state_bits == 8;
+  const size_t state = byte ? 1 : 4;
+  auto each = [&](auto f) {
+    for (int i = 0; i < n; ++i)
+      if (t[i].n > 0) f(t[i], (size_t)t[i].n);
+    merge();
+  };
+  each([&](const auto& x, size_t k) { add(x.param, k * size_of(x.param_dtype), true); });
+  each([&](const auto& x, size_t k) { add(x.grad, k * size_of(x.grad_dtype), false); });
+  each([&](const auto& x, size_t k) { add(x.master, k * 4, true); });
+  each([&](const auto& x, size_t k) { add(x.m, k * state, true); });
+  each([&](const auto& x, size_t k) { add(x.v, k * state, true); });
+  if (byte) {
+    each([&](const auto& x, size_t k) { add(x.m_scale, (k + kScaled - 1) / kScaled * 4, true); });
+    each([&](const auto& x, size_t k) { add(x.v_scale, (k + kScaled - 1) / kScaled * 4, true); });
+  }
+  uintptr_t end_out = 0, end_any = 0;
+  for (const Span& x : all) {
+    if (x.a < end_out || (x.out && x.a < end_any)) return DFLARE_ERR_INVALID_ARG;
+    end_any = std::max(end_any, x.b);
+    if (x.out) end_out = std::max(end_out, x.b);
+  }
+  return DFLARE_OK;
+} catch (const std::bad_alloc&) {
+  return DFLARE_ERR_OUT_OF_MEMORY;
+}
+
+template <bool MASTER, bool BYTE>
+void launch(const dflare_adamw_tensor* t, int n, const Options& o, hipStream_t st) {
+  Tab<MASTER, BYTE> tab;
+  tab.count = 0;
+  tab.first[0] = 0;
+  auto flush = [&] {
+    if (tab.count) hipLaunchKernelGGL((k_adamw<MASTER, BYTE>), dim3(std::min(tab.first[tab.count], kGroups)), dim3(kT), 0, st, tab, o);
+    tab.count = 0;
+  };
+  for (int i = 0; i < n; ++i) {
+    const dflare_adamw_tensor& x = t[i];
+    if (!x.n) continue;
+    const long chunks = (x.n + kChunk - 1) / kChunk;
+    if (tab.count == tab.N || (tab.count && tab.first[tab.count] + chunks > (1l << 30))) flush();
+    const int k = tab.count++;
+    tab.p[k] = x.param;
+    tab.g[k] = x.grad;
+    tab.m[k] = x.m;
+    tab.v[k] = x.v;
+    if (MASTER) tab.w[k] = x.master;
+    if (BYTE) {
+      tab.ms[k] = x.m_scale;
+      tab.vs[k] = x.v_scale;
+    }
+    tab.n[k] = (uint32_t)x.n;
+    tab.tag[k] = (uint8_t)((x.param_dtype == DFLARE_F32) | (x.grad_dtype == DFLARE_F32) << 1 | (x.master != nullptr) << 2 | (x.n >> 32) << 3);
+    tab.first[k + 1] = tab.first[k] + (int)chunks;
+  }
+  flush();
+}
+
+}  // namespace
+
+}  // namespace dflare
+
+using namespace dflare;
+
+extern "C" {
+
+int dflare_adamw(const dflare_adamw_tensor* tensors, int32_t n, const dflare_adamw_options* options, void* stream) {
+  if (!options) return DFLARE_ERR_INVALID_ARG;
+  const dflare_adamw_options& o = *options;
+  int rc = check(tensors, n, o);
+  if (rc != DFLARE_OK) return rc;
+  if ((rc = all_apart(tensors, n, o)) != DFLARE_OK) return rc;
+  if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
+  Options k{};
+  k.lr = o.lr;
+  k.weight_decay = o.weight_decay;
+  k.ln1 = log(o.beta1);
+  k.ln2 = log(o.beta2);
+  k.lr_device = o.lr_device;
+  k.step_device = o.step_device;
+  k.sumsq = o.sumsq;
+  k.step = o.step;
+  k.max_norm = o.max_norm;
+  k.h.b1 = (float)o.beta1;
+  k.h.c1 = (float)(1.0 - o.beta1);
+  k.h.b2 = (float)o.beta2;
+  k.h.c2 = (float)(1.0 - o.beta2);
+  k.h.eps = (float)o.eps;
+  if (!o.lr_device && !o.step_device) set_step(k.h, o.lr, o.weight_decay, k.ln1, k.ln2, (double)o.step);
+  bool master = false;
+  for (int i = 0; i < n; ++i) master |= tensors[i].master && tensors[i].n > 0;
+  const hipStream_t st = (hipStream_t)stream;
+  if (o.state_bits == 8) {
+    if (master) launch<true, true>(tensors, n, k, st);
+    else launch<false, true>(tensors, n, k, st);
+  } else {
+    if (master) launch<true, false>(tensors, n, k, st);
+    else launch<false, false>(tensors, n, k, st);
+  }
+  return launched();
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
 // Native part of the Python binding: the calls of the training step that are small enough for Python's own time to
-// count (norms, rotary positions, gradient norm and clipping).  Each checks its tensors, makes its outputs on the current stream
+// count (norms, rotary positions, projections of few rows, gradient norm and clipping, AdamW).  Each checks its tensors, makes its outputs on the current stream
 // of their device and calls the C entry point (include/dflare.h), whose address dflare.py hands over once.
 // In Python the same work made a norm of 16 rows 11 us long instead of 7.0 (its kernel takes 3.7), rotary positions of 32 rows
 // 16 instead of 6.3 (3.8), and a list of 301 gradients 0.8 ms instead of 38 us.
@@ -23,6 +23,18 @@ decltype(&dflare_rope) p_rope;
 decltype(&dflare_grad_norm_workspace) p_grad_norm_workspace;
 decltype(&dflare_grad_norm) p_grad_norm;
 decltype(&dflare_clip_grads) p_clip_grads;
+decltype(&dflare_qk_norm_rope_fwd) p_qk_norm_rope_fwd;
+decltype(&dflare_qk_norm_rope_bwd_workspace) p_qk_norm_rope_bwd_workspace;
+decltype(&dflare_qk_norm_rope_bwd) p_qk_norm_rope_bwd;
+decltype(&dflare_linear_fwd_workspace) p_linear_fwd_workspace;
+decltype(&dflare_linear_fwd) p_linear_fwd;
+decltype(&dflare_linear_bwd_workspace) p_linear_bwd_workspace;
+decltype(&dflare_linear_bwd) p_linear_bwd;
+decltype(&dflare_gated_fwd_workspace) p_gated_fwd_workspace;
+decltype(&dflare_gated_fwd) p_gated_fwd;
+decltype(&dflare_gated_bwd_workspace) p_gated_bwd_workspace;
+decltype(&dflare_gated_bwd) p_gated_bwd;
+decltype(&dflare_adamw) p_adamw;
 PyObject* p_raw_stream;     // device index -> address of its current stream
 PyObject* p_out_of_memory;  // torch's exception
 
@@ -227,6 +239,260 @@ PyObject* clip_grads(PyObject* const* a) {
   }));
 }
 
+// one or two [rows, n_heads, head_dim] tensors with the positions, gains and numbers of a call on them
+struct Heads {
+  int n = 0;
+  const at::Tensor* x[2];
+  PyObject* x_items[2];
+  void* gain[2];
+  int32_t rows, hd, rot, B, layout;
+  int dtype;
+  double scale, eps;
+  void *positions, *freq;
+  // (x tuple, gain tuple, inv_freq, positions, B, layout, scale, eps)
+  explicit Heads(PyObject* const* a) {
+    if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) < 1 || PyTuple_GET_SIZE(a[0]) > 2) value_error("expected one tensor or a pair");
+    n = (int)PyTuple_GET_SIZE(a[0]);
+    if (!PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != n) value_error("gain and x differ in number");
+    B = to32(PyLong_AsLongLong(a[4]), "B");
+    layout = to32(PyLong_AsLongLong(a[5]), "layout");
+    scale = PyFloat_AsDouble(a[6]);
+    eps = PyFloat_AsDouble(a[7]);
+    if (PyErr_Occurred()) throw Refused{nullptr, ""};
+    if (B < 1) value_error("B must be positive");
+    const at::Tensor& first = tensor(PyTuple_GET_ITEM(a[0], 0));
+    dtype = type_code(first);
+    if (first.dim() != 3) value_error("expected [rows, n_heads, head_dim] tensors");
+    rows = to32(first.size(0), "rows");
+    hd = to32(first.size(2), "head_dim");
+    const at::Tensor& f = dense(a[2]);
+    freq = like(a[2], "inv_freq", {f.numel()}, first, at::kDouble);
+    rot = to32(2 * f.numel(), "rotary_dim");
+    positions = like(a[3], "positions", {((int64_t)rows + B - 1) / B}, first, at::kInt);
+    for (int k = 0; k < n; ++k) {
+      x_items[k] = PyTuple_GET_ITEM(a[0], k);
+      x[k] = &tensor(x_items[k]);
+      if (x[k]->dim() != 3 || x[k]->size(0) != rows || x[k]->size(2) != hd)
+        value_error("expected [rows, n_heads, head_dim] tensors with the same rows and head_dim");
+      if (type_code(*x[k]) != dtype || x[k]->device() != first.device()) value_error("the tensors differ in type or device");
+      contiguous_heads(*x[k]);
+      gain[k] = like(PyTuple_GET_ITEM(a[1], k), "gain", {hd}, first);
+      to32(x[k]->size(1), "n_heads");
+    }
+  }
+  void contiguous_heads(const at::Tensor& t) const {
+    if (hd > 1 && t.numel() && t.stride(2) != 1) value_error("the last dimension must be contiguous");
+  }
+  // a tensor beside x[k]
+  const at::Tensor& beside(PyObject* o, int k, const char* name) const {
+    const at::Tensor& t = tensor(o);
+    if (t.sizes() != x[k]->sizes() || t.device() != x[k]->device()) value_error(std::string(name) + " and x differ in shape or device");
+    if (type_code(t) != dtype) type_error(std::string(name) + " and x differ in type");
+    contiguous_heads(t);
+    return t;
+  }
+};
+PyObject* pair_of(const at::Tensor (&t)[2], int n) { return n == 1 ? Py_BuildValue("(N)", wrapped(t[0])) : Py_BuildValue("NN", wrapped(t[0]), wrapped(t[1])); }
+
+// qk_norm_rope_fwd(x, gain, inv_freq, positions, B, layout, scale, eps, None or tuple of outputs) -> tuple of outputs
+PyObject* qk_norm_rope_fwd(PyObject* const* a) {
+  const Heads h(a);
+  const bool given = a[8] != Py_None;
+  if (given && (!PyTuple_Check(a[8]) || PyTuple_GET_SIZE(a[8]) != h.n)) value_error("out and x differ in number");
+  const Here here(h.x[0]->device());
+  dflare_qk_tensor tab[2] = {};
+  at::Tensor outs[2];
+  for (int k = 0; k < h.n; ++k) {
+    const at::Tensor& x = *h.x[k];
+    outs[k] = given ? h.beside(PyTuple_GET_ITEM(a[8], k), k, "out") : fresh(x.sizes(), x, x.scalar_type());
+    const at::Tensor& y = outs[k];
+    tab[k] = {x.data_ptr(), y.data_ptr(), h.gain[k], x.stride(0), x.stride(1), y.stride(0), y.stride(1), (int32_t)x.size(1)};
+  }
+  const int rc = unlocked([&] {
+    return p_qk_norm_rope_fwd(tab, h.n, (const int32_t*)h.positions, (const double*)h.freq, h.rows, h.B, h.hd, h.rot, h.dtype, h.layout,
+                              (float)h.scale, (float)h.eps, here.stream);
+  });
+  if (rc != DFLARE_OK) return PyLong_FromLong(rc);
+  return given ? Py_NewRef(a[8]) : pair_of(outs, h.n);
+}
+
+// qk_norm_rope_bwd(x, gain, inv_freq, positions, B, layout, scale, eps, dy) -> (tuple of dx, tuple of dgain)
+PyObject* qk_norm_rope_bwd(PyObject* const* a) {
+  const Heads h(a);
+  if (!PyTuple_Check(a[8]) || PyTuple_GET_SIZE(a[8]) != h.n) value_error("dy and x differ in number");
+  const Here here(h.x[0]->device());
+  dflare_qk_grad tab[2] = {};
+  at::Tensor dx[2], dgain[2];
+  for (int k = 0; k < h.n; ++k) {
+    const at::Tensor &x = *h.x[k], &dy = h.beside(PyTuple_GET_ITEM(a[8], k), k, "dy");
+    dx[k] = fresh(x.sizes(), x, x.scalar_type());
+    if (h.gain[k]) dgain[k] = fresh({h.hd}, x, at::kFloat);
+    tab[k] = {x.data_ptr(), dy.data_ptr(), dx[k].data_ptr(), h.gain[k], (float*)address(dgain[k]), x.stride(0), x.stride(1),
+              dy.stride(0), dy.stride(1), dx[k].stride(0), dx[k].stride(1), (int32_t)x.size(1)};
+  }
+  const size_t bytes = p_qk_norm_rope_bwd_workspace(h.rows, h.hd, h.n);
+  const at::Tensor ws = fresh({(int64_t)std::max<size_t>(bytes, 16)}, *h.x[0], at::kByte);
+  const int rc = unlocked([&] {
+    return p_qk_norm_rope_bwd(tab, h.n, (const int32_t*)h.positions, (const double*)h.freq, h.rows, h.B, h.hd, h.rot, h.dtype, h.layout,
+                              (float)h.scale, (float)h.eps, ws.data_ptr(), bytes, here.stream);
+  });
+  if (rc != DFLARE_OK) return PyLong_FromLong(rc);
+  return Py_BuildValue("NN", pair_of(dx, h.n), pair_of(dgain, h.n));
+}
+
+// rows and weights of a projection: x [rows, K] and w [N, K], both bf16
+struct Projection {
+  const at::Tensor &x, &w;
+  int32_t rows, N, K;
+  Projection(PyObject* px, PyObject* pw, const char* name) : x(dense(px)), w(dense(pw)) {
+    if (x.dim() != 2 || w.dim() != 2) value_error("expected bf16 tensors x [rows, K] and weights [N, K]");
+    if (type_code(x) != DFLARE_BF16) type_error("expected bf16 tensors");
+    rows = to32(x.size(0), "rows");
+    K = to32(x.size(1), "K");
+    N = to32(w.size(0), "N");
+    like(pw, name, {N, K}, x);
+  }
+};
+at::Tensor scratch(size_t bytes, const at::Tensor& ref) { return fresh({(int64_t)std::max<size_t>(bytes, 16)}, ref, at::kByte); }
+int truth(PyObject* o) {
+  const int r = PyObject_IsTrue(o);
+  if (r < 0) throw Refused{nullptr, ""};
+  return r;
+}
+
+// linear_fwd(x, w, bias, residual, act, save) -> (y, z)
+PyObject* linear_fwd(PyObject* const* a) {
+  const Projection p(a[0], a[1], "w");
+  void *bias = like(a[2], "bias", {p.N}, p.x), *res = like(a[3], "residual", {p.rows, p.N}, p.x);
+  const int32_t act = to32(PyLong_AsLongLong(a[4]), "act");
+  if (PyErr_Occurred()) return nullptr;
+  const bool save = truth(a[5]);
+  const Here here(p.x.device());
+  const size_t bytes = p_linear_fwd_workspace(p.rows, p.N, p.K);
+  const at::Tensor ws = scratch(bytes, p.x), y = fresh({p.rows, p.N}, p.x, p.x.scalar_type());
+  const at::Tensor z = save ? fresh({p.rows, p.N}, p.x, p.x.scalar_type()) : at::Tensor();
+  const int rc = unlocked([&] {
+    return p_linear_fwd(p.x.data_ptr(), p.w.data_ptr(), bias, res, p.rows, p.N, p.K, act, y.data_ptr(), address(z), ws.data_ptr(), bytes,
+                        here.stream);
+  });
+  return rc != DFLARE_OK ? PyLong_FromLong(rc) : Py_BuildValue("NN", wrapped(y), wrapped(z));
+}
+
+// linear_bwd(dy, x, w, z, act, need_dx, need_dw, need_dbias) -> (dx, dw, dbias)
+PyObject* linear_bwd(PyObject* const* a) {
+  const Projection p(a[1], a[2], "w");
+  void *dy = like(a[0], "dy", {p.rows, p.N}, p.x), *z = like(a[3], "z", {p.rows, p.N}, p.x);
+  const int32_t act = to32(PyLong_AsLongLong(a[4]), "act");
+  if (PyErr_Occurred()) return nullptr;
+  tensor(a[0]);
+  const int need_dx = truth(a[5]), need_dw = truth(a[6]), need_dbias = truth(a[7]);
+  const Here here(p.x.device());
+  const size_t bytes = p_linear_bwd_workspace(p.rows, p.N, p.K, act, need_dx, need_dw, need_dbias);
+  const auto type = p.x.scalar_type();
+  const at::Tensor ws = scratch(bytes, p.x), dx = need_dx ? fresh(p.x.sizes(), p.x, type) : at::Tensor();
+  const at::Tensor dw = need_dw ? fresh(p.w.sizes(), p.x, type) : at::Tensor(), dbias = need_dbias ? fresh({p.N}, p.x, type) : at::Tensor();
+  const int rc = unlocked([&] {
+    return p_linear_bwd(dy, p.x.data_ptr(), p.w.data_ptr(), z, p.rows, p.N, p.K, act, address(dx), address(dw), address(dbias), ws.data_ptr(),
+                        bytes, here.stream);
+  });
+  return rc != DFLARE_OK ? PyLong_FromLong(rc) : Py_BuildValue("NNN", wrapped(dx), wrapped(dw), wrapped(dbias));
+}
+
+// gated_fwd(x, w_gate, w_up, act, save) -> (h, gate, up)
+PyObject* gated_fwd(PyObject* const* a) {
+  const Projection p(a[0], a[1], "w_gate");
+  void* up_w = dense(a[2]).data_ptr();
+  like(a[2], "w_up", p.w.sizes(), p.x);
+  const int32_t act = to32(PyLong_AsLongLong(a[3]), "act");
+  if (PyErr_Occurred()) return nullptr;
+  const bool save = truth(a[4]);
+  const Here here(p.x.device());
+  const size_t bytes = p_gated_fwd_workspace(p.rows, p.K, p.N);
+  auto rows_of = [&] { return fresh({p.rows, p.N}, p.x, p.x.scalar_type()); };
+  const at::Tensor ws = scratch(bytes, p.x), h = rows_of(), gate = save ? rows_of() : at::Tensor(), up = save ? rows_of() : at::Tensor();
+  const int rc = unlocked([&] {
+    return p_gated_fwd(p.x.data_ptr(), p.w.data_ptr(), up_w, p.rows, p.K, p.N, act, h.data_ptr(), address(gate), address(up), ws.data_ptr(), bytes,
+                       here.stream);
+  });
+  return rc != DFLARE_OK ? PyLong_FromLong(rc) : Py_BuildValue("NNN", wrapped(h), wrapped(gate), wrapped(up));
+}
+
+// gated_bwd(dh, x, gate, up, w_gate, w_up, act, need_dx, need_dw) -> (dx, dw_gate, dw_up)
+PyObject* gated_bwd(PyObject* const* a) {
+  const Projection p(a[1], a[4], "w_gate");
+  void *dh = like(a[0], "dh", {p.rows, p.N}, p.x), *gate = like(a[2], "gate", {p.rows, p.N}, p.x), *up = like(a[3], "up", {p.rows, p.N}, p.x);
+  void* up_w = like(a[5], "w_up", p.w.sizes(), p.x);
+  const int32_t act = to32(PyLong_AsLongLong(a[6]), "act");
+  if (PyErr_Occurred()) return nullptr;
+  for (int k : {0, 2, 3, 5}) tensor(a[k]);
+  const int need_dx = truth(a[7]), need_dw = truth(a[8]);
+  const Here here(p.x.device());
+  const size_t bytes = p_gated_bwd_workspace(p.rows, p.K, p.N, need_dx, need_dw);
+  const auto type = p.x.scalar_type();
+  auto weights = [&] { return need_dw ? fresh(p.w.sizes(), p.x, type) : at::Tensor(); };
+  const at::Tensor ws = scratch(bytes, p.x), dx = need_dx ? fresh(p.x.sizes(), p.x, type) : at::Tensor(), dg = weights(), du = weights();
+  const int rc = unlocked([&] {
+    return p_gated_bwd(dh, p.x.data_ptr(), gate, up, p.w.data_ptr(), up_w, p.rows, p.K, p.N, act, address(dx), address(dg), address(du),
+                       ws.data_ptr(), bytes, here.stream);
+  });
+  return rc != DFLARE_OK ? PyLong_FromLong(rc) : Py_BuildValue("NNN", wrapped(dx), wrapped(dg), wrapped(du));
+}
+
+// adamw(params, grads, m, v, masters, m_scales, v_scales, step, lr, beta1, beta2, eps, weight_decay, sumsq, max_norm) -> status;
+// lists of tensors; masters and scales: lists, in which tensors may be None, or None; step and lr: numbers, or tensors of one
+PyObject* adamw(PyObject* const* a) {
+  for (int k = 0; k < 7; ++k)
+    if (!PyList_Check(a[k]) && (k < 4 || a[k] != Py_None)) type_error("expected a list");
+  const Py_ssize_t n = PyList_GET_SIZE(a[0]);
+  if (n < 1) value_error("expected at least one parameter");
+  to32(n, "the number of parameters");
+  for (int k = 1; k < 7; ++k)
+    if (a[k] != Py_None && PyList_GET_SIZE(a[k]) != n) value_error("the lists differ in length");
+  const at::Tensor& first = dense(PyList_GET_ITEM(a[0], 0));
+  std::vector<dflare_adamw_tensor> table(n);
+  const at::ScalarType state = tensor(PyList_GET_ITEM(a[2], 0)).scalar_type();
+  if (state != at::kFloat && state != at::kFloat8_e4m3fn) type_error("the moments are fp32 or float8_e4m3fn tensors");
+  const bool byte = state == at::kFloat8_e4m3fn;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const at::Tensor &p = dense(PyList_GET_ITEM(a[0], i)), &g = dense(PyList_GET_ITEM(a[1], i));
+    if (p.device() != first.device() || g.device() != first.device()) value_error("the tensors are on different devices");
+    if (g.sizes() != p.sizes()) value_error("a gradient has another shape than its parameter");
+    auto item = [&](int k) { return a[k] == Py_None ? Py_None : PyList_GET_ITEM(a[k], i); };
+    auto moment = [&](int k, const char* name) {
+      const at::Tensor& t = dense(item(k));
+      if (t.sizes() != p.sizes()) value_error(std::string(name) + " has another shape than its parameter");
+      if (t.device() != p.device() || t.scalar_type() != state) type_error("the moments differ in type or device");
+      return t.data_ptr();
+    };
+    dflare_adamw_tensor& t = table[i];
+    t = {p.data_ptr(), g.data_ptr(), nullptr, moment(2, "m"), moment(3, "v"), nullptr, nullptr, p.numel(), type_code(p), type_code(g)};
+    t.master = (float*)like(item(4), "master", p.sizes(), p, at::kFloat);
+    const int64_t scales = (p.numel() + 255) / 256;
+    if (byte) {
+      t.m_scale = (float*)like(item(5), "m_scale", {scales}, p, at::kFloat);
+      t.v_scale = (float*)like(item(6), "v_scale", {scales}, p, at::kFloat);
+    } else if (item(5) != Py_None || item(6) != Py_None) {
+      value_error("scales beside fp32 moments");
+    }
+  }
+  dflare_adamw_options o{};
+  if (THPVariable_Check(a[7])) o.step_device = (const int64_t*)like(a[7], "step", {1}, first, at::kLong);
+  else o.step = PyLong_AsLongLong(a[7]);
+  if (THPVariable_Check(a[8])) o.lr_device = (const double*)like(a[8], "lr", {1}, first, at::kDouble);
+  else o.lr = PyFloat_AsDouble(a[8]);
+  o.beta1 = PyFloat_AsDouble(a[9]);
+  o.beta2 = PyFloat_AsDouble(a[10]);
+  o.eps = PyFloat_AsDouble(a[11]);
+  o.weight_decay = PyFloat_AsDouble(a[12]);
+  const double max_norm = PyFloat_AsDouble(a[14]);
+  if (PyErr_Occurred()) return nullptr;
+  o.sumsq = (const double*)like(a[13], "sumsq", {1}, first, at::kDouble);
+  o.max_norm = (float)max_norm;
+  o.state_bits = byte ? 8 : 32;
+  const Here here(first.device());
+  return PyLong_FromLong(unlocked([&] { return p_adamw(table.data(), (int32_t)n, &o, here.stream); }));
+}
+
 // F with exactly N arguments, its refusals and C++ exceptions as Python's
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -237,6 +503,7 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   try {
     return F(args);
   } catch (const Refused& r) {
+    if (!r.type) return nullptr;  // (Python's own error stands)
     PyErr_Clear();
     PyErr_SetString(r.type, r.why.c_str());
   } catch (const c10::OutOfMemoryError& e) {
@@ -247,21 +514,28 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
+constexpr int kBound = 21;
 // bind(addresses of the entry points in the order below, function from a device index to its current stream's address,
 // torch's out-of-memory exception)
 PyObject* bind(PyObject* const* a) {
   void** to[] = {(void**)&p_norm_fwd, (void**)&p_norm_bwd_workspace, (void**)&p_norm_bwd, (void**)&p_rope,
-                 (void**)&p_grad_norm_workspace, (void**)&p_grad_norm, (void**)&p_clip_grads};
-  for (int k = 0; k < 7; ++k) *to[k] = PyLong_AsVoidPtr(a[k]);
+                 (void**)&p_grad_norm_workspace, (void**)&p_grad_norm, (void**)&p_clip_grads,
+                 (void**)&p_qk_norm_rope_fwd, (void**)&p_qk_norm_rope_bwd_workspace, (void**)&p_qk_norm_rope_bwd,
+                 (void**)&p_linear_fwd_workspace, (void**)&p_linear_fwd, (void**)&p_linear_bwd_workspace, (void**)&p_linear_bwd,
+                 (void**)&p_gated_fwd_workspace, (void**)&p_gated_fwd, (void**)&p_gated_bwd_workspace, (void**)&p_gated_bwd, (void**)&p_adamw};
+  constexpr int n = sizeof(to) / sizeof(to[0]);
+  static_assert(n + 2 == kBound);
+  for (int k = 0; k < n; ++k) *to[k] = PyLong_AsVoidPtr(a[k]);
   if (PyErr_Occurred()) return nullptr;
-  p_raw_stream = Py_NewRef(a[7]);
-  p_out_of_memory = Py_NewRef(a[8]);
+  p_raw_stream = Py_NewRef(a[n]);
+  p_out_of_memory = Py_NewRef(a[n + 1]);
   return Py_NewRef(Py_None);
 }
 
 #define FUNCTION(f, n) {#f, (PyCFunction)(void*)guarded<f, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FUNCTION(bind, 9), FUNCTION(norm_fwd, 6), FUNCTION(norm_bwd, 7), FUNCTION(rope, 8), FUNCTION(grad_norm, 1),
-                         FUNCTION(clip_grads, 4), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FUNCTION(bind, kBound), FUNCTION(norm_fwd, 6), FUNCTION(norm_bwd, 7), FUNCTION(rope, 8), FUNCTION(grad_norm, 1),
+                         FUNCTION(clip_grads, 4), FUNCTION(qk_norm_rope_fwd, 9), FUNCTION(qk_norm_rope_bwd, 9), FUNCTION(linear_fwd, 6),
+                         FUNCTION(linear_bwd, 8), FUNCTION(gated_fwd, 5), FUNCTION(gated_bwd, 9), FUNCTION(adamw, 15), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,754 @@
+// Projections and the gated feed-forward block of a draft layer's training step, forward and backward, and their
+// C-ABI entry points.  Over rows of x, with weights W [N, K] as nn.Linear keeps them:
+//   projection   z = x W^T + b, y = act(z) + residual;  dz = dy act'(z), dx = dz W, dW = dz^T x, db = sum dz
+//   gated block  g = x Wg^T, u = x Wu^T, h = act(g) u;  dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu,
+//                dWg = dg^T x, dWu = du^T x
+// Both are the same three products (of one matrix or of two); the gated block's forward product takes its tiles' rows of W
+// from both matrices in turn, so that a lane holds g and u of the same element and h is formed in registers.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "dflare.h"
+#include "product.h"
+
+namespace dflare {
+
+namespace {
+
+// ---- activations: value and derivative in fp32.  Arguments are clamped where both have reached their limits (0, z, 1), so that
+// infinities give these and no 0 x infinity; NaN stays. ----
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_(float x) { return __builtin_amdgcn_rcpf(x); }
+constexpr float kLog2E = 1.4426950408889634f;
+__device__ __forceinline__ float from_below(float z, float least) { return z < least ? least : z; }
+__device__ __forceinline__ float within(float z, float most) { return z < -most ? -most : z > most ? most : z; }
+
+// Phi(z), and exp(-z^2 / 2).  Phi(-a) = exp(-a^2 / 2) t P(t), t = 1 / (1 + 0.31 a), for a >= 0: P is a least-maximum fit of degree 7
+// to t^-1 erfcx(a / sqrt 2) / 2 on [0, 20], off by 4e-7 of it in fp32 (and by less than 1e-6 past it)
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float a = fabsf(z), t = rcp_(fmaf(0.31f, a, 1.f));
+  float p = 0.03591751679778099f;
+  p = fmaf(p, t, -0.14193730056285858f);
+  p = fmaf(p, t, 0.15567456185817719f);
+  p = fmaf(p, t, -0.0154969971626997f);
+  p = fmaf(p, t, 0.11044538021087646f);
+  p = fmaf(p, t, 0.10766226798295975f);
+  p = fmaf(p, t, 0.12407905608415604f);
+  p = fmaf(p, t, 0.12365560233592987f);
+  e = exp2_(-0.5f * kLog2E * a * a);
+  const float q = e * t * p;
+  return z < 0.f ? q : 1.f - q;
+}
+
+template <int ACT>
+struct Activation {
+  static __device__ __forceinline__ float value(float z) {
+    float d;
+    if constexpr (ACT == DFLARE_ACT_RELU) return z <= 0.f ? 0.f : z;
+    if constexpr (ACT == DFLARE_ACT_SILU) {
+      z = from_below(z, -128.f);
+      return z * rcp_(1.f + exp2_(-kLog2E * z));
+    }
+    if constexpr (ACT == DFLARE_ACT_GELU) {
+      z = from_below(z, -64.f);
+      return z * normal_cdf(z, d);
+    }
+    if constexpr (ACT == DFLARE_ACT_GELU_TANH) {
+      z = from_below(z, -64.f);
+      return z * rcp_(1.f + exp2_(-kLog2E * inner(z)));
+    }
+    return z;
+  }
+  // 2 sqrt(2 / pi) (z + 0.044715 z^3): 0.5 z (1 + tanh of half of it) = z / (1 + exp(-it))
+  static __device__ __forceinline__ float inner(float z) { return 1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.f); }
+  // the value, and its derivative in d
+  static __device__ __forceinline__ float both(float z, float& d) {
+    if constexpr (ACT == DFLARE_ACT_RELU) {
+      d = z <= 0.f ? 0.f : z > 0.f ? 1.f : z;
+      return value(z);
+    }
+    if constexpr (ACT == DFLARE_ACT_SILU) {
+      const float c = within(z, 128.f), s = rcp_(1.f + exp2_(-kLog2E * c));
+      d = fmaf(c * s, 1.f - s, s);
+      return from_below(z, -128.f) * s;
+    }
+    if constexpr (ACT == DFLARE_ACT_GELU) {
+      float e;
+      const float c = within(z, 64.f), p = normal_cdf(c, e);
+      d = fmaf(0.3989422804014327f * c, e, p);
+      return from_below(z, -64.f) * p;
+    }
+    if constexpr (ACT == DFLARE_ACT_GELU_TANH) {
+      const float c = within(z, 64.f), s = rcp_(1.f + exp2_(-kLog2E * inner(c)));
+      d = fmaf(c * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f), s);
+      return from_below(z, -64.f) * s;
+    }
+    d = 1.f;
+    return z;
+  }
+};
+template <typename F>
+__host__ __device__ __forceinline__ void with_act(int act, F&& f) {
+  switch (act) {
+    case DFLARE_ACT_RELU: return f(int_c<DFLARE_ACT_RELU>{});
+    case DFLARE_ACT_SILU: return f(int_c<DFLARE_ACT_SILU>{});
+    case DFLARE_ACT_GELU: return f(int_c<DFLARE_ACT_GELU>{});
+    case DFLARE_ACT_GELU_TANH: return f(int_c<DFLARE_ACT_GELU_TANH>{});
+    default: return f(int_c<DFLARE_ACT_NONE>{});
+  }
+}
+
+// The products of a call.  n2: matrices (2: the gated block)
+struct Call {
+  const uint16_t *x, *w[2], *bias, *res;  // [rows, K], [N, K], [N], [rows, N]
+  const uint16_t* d[2];                   // [rows, N] gradients of z, or of g and u
+  uint16_t *y, *z[2];                     // [rows, N] outputs: y or h; z, or g and u, or null
+  uint16_t *dx, *dw[2];                   // [rows, K], [N, K]
+  float* part;                            // sums of a product's parts
+  int rows, N, K, n2, act, parts;
+};
+
+// a part's stages of k: [first, past the last) of `stages`
+__device__ __forceinline__ void part_of(int stages, int parts, int ks, int& s0, int& s1) {
+  s0 = (int)((long)stages * ks / parts);
+  s1 = (int)((long)stages * (ks + 1) / parts);
+}
+
+// 4 values as bf16 into LDS rows of TMO values; piece p of row n at p ^ (n mod the pieces)
+template <int TMO>
+__device__ __forceinline__ void put4(char* lds, int n, int p, int h, f32x4 v) {
+  *reinterpret_cast<uint2*>(lds + n * (TMO * 2) + ((p ^ (n & (TMO / 8 - 1))) << 4) + h * 8) =
+      make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+}
+// and from there, 16 bytes at a time, to to(row, piece) where that is not null
+template <typename S, int TMO, typename F>
+__device__ __forceinline__ void take(const char* lds, F&& to) {
+  constexpr int P = TMO / 8, RW = S::TN / S::W;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll 4
+  for (int it = 0; it < RW * P / 64; ++it) {
+    const int n = w * RW + it * (64 / P) + lane / P, p = lane % P;
+    if (uint16_t* at = to(n, p))
+      *reinterpret_cast<u32x4*>(at) = *reinterpret_cast<const u32x4*>(lds + n * (TMO * 2) + ((p ^ (n & (P - 1))) << 4));
+  }
+}
+__device__ __forceinline__ f32x4 four(const f32x16& v, int q) { return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]}; }
+__device__ __forceinline__ f32x4 bf4(const uint16_t* p) {
+  const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+  return unpack4(v[0], v[1]);
+}
+
+// ---- z = x W^T, a tile of rows x TM rows of W, and its epilogue; or a part's sums ----
+template <typename S, bool GATED>
+__global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+  constexpr int MT = S::MT, NT = S::NT, HT = GATED ? MT / 2 : MT;  // HT: a wave's 32-row tiles of one matrix
+  constexpr int PART = GATED ? HT * 32 : 0, TMO = GATED ? S::TM / 2 : S::TM;
+  const int nb = (a.rows + S::TN - 1) / S::TN, na = (a.N + TMO - 1) / TMO;
+  int unit, tb;
+  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
+  const int ks = unit / na, m0 = unit % na * TMO, r0 = tb * S::TN;
+  int s0, s1;
+  part_of((a.K + kBK - 1) / kBK, a.parts, ks, s0, s1);
+  const int k0 = s0 * kBK, kn = min(s1 * kBK, a.K) - k0, nv = min(a.rows - r0, S::TN), mv = min(a.N - m0, TMO);
+  const long wo = (long)m0 * a.K + k0;
+  Operand ow{a.w[0] + wo, a.K, mv, kn}, ox{a.x + (long)r0 * a.K + k0, a.K, nv, kn};
+  if constexpr (GATED) ow.other = a.w[1] + wo;
+  Acc<S> acc;
+  clear<S>(acc);
+  product<S, false, false, true, PART>(ow, ox, kn, lds, acc, [](Acc<S>&) {});
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int wm = w % S::WM, n_wave = w / S::WM * (NT * 32) + (lane & 31);
+  // f(32-row tile t of one matrix, j, q, row of the tile, first of four columns of the tile)
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) f(t, j, q, n_wave + j * 32, (wm * HT + t) * 32 + 8 * q + 4 * h);
+  };
+  if (a.parts > 1) {
+    const long ld = (GATED ? 2l : 1l) * a.N;
+    float* out = a.part + ((long)ks * a.rows + r0) * ld + m0;
+    each([&](int t, int j, int q, int n, int m) {
+      if (n >= nv || m >= mv) return;
+      *reinterpret_cast<f32x4*>(out + n * ld + m) = four(acc[t][j], q);
+      if constexpr (GATED) *reinterpret_cast<f32x4*>(out + n * ld + a.N + m) = four(acc[HT + t][j], q);
+    });
+    return;
+  }
+  const long at0 = (long)r0 * a.N + m0;
+  auto out_at = [&](uint16_t* to) {
+    return [=](int n, int p) { return n < nv && p * 8 < mv ? to + at0 + (long)n * a.N + p * 8 : nullptr; };
+  };
+  if constexpr (GATED) {
+    if (a.z[0]) {
+      each([&](int t, int j, int q, int n, int m) {
+        const int p = (wm * MT + t) * 4 + q;  // rows of the tile as they lie in LDS: HT tiles of g, then of u
+        put4<S::TM>(lds, n, p, h, four(acc[t][j], q));
+        put4<S::TM>(lds, n, p + HT * 4, h, four(acc[HT + t][j], q));
+      });
+      __syncthreads();
+      take<S, S::TM>(lds, [&](int n, int p) -> uint16_t* {
+        const int c = p * 8, m = c / (2 * PART) * PART + c % PART;
+        return n < nv && m < mv ? a.z[c / PART & 1] + at0 + (long)n * a.N + m : nullptr;
+      });
+      __syncthreads();
+    }
+    with_act(a.act, [&](auto act) {
+      each([&](int t, int j, int q, int n, int m) {
+        f32x4 v = four(acc[t][j], q);
+        const f32x4 u = four(acc[HT + t][j], q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = Activation<act.value>::value(v[e]) * u[e];
+        put4<TMO>(lds, n, m / 8, h, v);
+      });
+    });
+  } else {
+    if (a.bias)
+      each([&](int t, int j, int q, int n, int m) {
+        const f32x4 b = bf4(a.bias + m0 + min(m, mv - 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][j][4 * q + e] += b[e];
+      });
+    if (a.z[0]) {
+      each([&](int t, int j, int q, int n, int m) { put4<TMO>(lds, n, m / 8, h, four(acc[t][j], q)); });
+      __syncthreads();
+      take<S, TMO>(lds, out_at(a.z[0]));
+      __syncthreads();
+    }
+    with_act(a.act, [&](auto act) {
+      each([&](int t, int j, int q, int n, int m) {
+        f32x4 v = four(acc[t][j], q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = Activation<act.value>::value(v[e]);
+        if (a.res) v += bf4(a.res + at0 + (long)min(n, nv - 1) * a.N + min(m, mv - 4));
+        put4<TMO>(lds, n, m / 8, h, v);
+      });
+    });
+  }
+  __syncthreads();  // (y may lie on the residual: a tile of it has been read when any of it is written)
+  take<S, TMO>(lds, out_at(a.y));
+}
+
+// a forward product's parts, added in order, and its epilogue; a thread takes 8 columns of a row
+template <bool GATED>
+__global__ __launch_bounds__(kT) void k_finish(Call a) {
+  const int P = a.N / 8;
+  const long i = blockIdx.x * (long)kT + threadIdx.x;
+  if (i >= (long)a.rows * P) return;
+  const long row = i / P, m = (i - row * P) * 8, at = row * a.N + m, ld = (GATED ? 2l : 1l) * a.N;
+  float v[8], u[8];
+  auto sum = [&](float(&s)[8], const float* from) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.parts; ++k) {
+      const f32x4* p = reinterpret_cast<const f32x4*>(from + k * a.rows * ld);
+      const f32x4 x = p[0], y = p[1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] += x[e];
+        s[4 + e] += y[e];
+      }
+    }
+  };
+  const float* from = a.part + row * ld + m;
+  auto put = [&](uint16_t* to, const float(&s)[8]) { *reinterpret_cast<u32x4*>(to + at) = pack(s); };
+  sum(v, from);
+  if constexpr (GATED) {
+    sum(u, from + a.N);
+    if (a.z[0]) {
+      put(a.z[0], v);
+      put(a.z[1], u);
+    }
+  } else {
+    if (a.bias) {
+      unpack(*reinterpret_cast<const u32x4*>(a.bias + m), u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += u[e];
+    }
+    if (a.z[0]) put(a.z[0], v);
+  }
+  with_act(a.act, [&](auto act) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = Activation<act.value>::value(v[e]);
+  });
+  if constexpr (GATED) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= u[e];
+  } else if (a.res) {
+    unpack(*reinterpret_cast<const u32x4*>(a.res + at), u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += u[e];
+  }
+  put(a.y, v);
+}
+
+// the tile's sums, as a part or as they are stored
+template <typename S>
+__device__ __forceinline__ void put_sums(char* lds, const Acc<S>& acc, float* part, uint16_t* out, long ld, int nv, int mv) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int wm = w % S::WM, n_wave = w / S::WM * (S::NT * 32) + (lane & 31);
+#pragma unroll
+  for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+    for (int t = 0; t < S::MT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = n_wave + j * 32, m = (wm * S::MT + t) * 32 + 8 * q + 4 * h;
+        if (!part) put4<S::TM>(lds, n, m / 8, h, four(acc[t][j], q));
+        else if (n < nv && m < mv) *reinterpret_cast<f32x4*>(part + n * ld + m) = four(acc[t][j], q);
+      }
+  if (part) return;
+  __syncthreads();
+  take<S, S::TM>(lds, [&](int n, int p) { return n < nv && p * 8 < mv ? out + n * ld + p * 8 : nullptr; });
+}
+
+// ---- dx = d W over the rows of W (of both matrices, one after the other) ----
+template <typename S>
+__global__ __launch_bounds__(S::T, 2) void k_dx(Call a) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+  const int nb = (a.rows + S::TN - 1) / S::TN, na = (a.K + S::TM - 1) / S::TM;
+  int unit, tb;
+  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
+  const int ks = unit / na, m0 = unit % na * S::TM, r0 = tb * S::TN, one = (a.N + kBK - 1) / kBK;
+  int s0, s1;
+  part_of(a.n2 * one, a.parts, ks, s0, s1);
+  const int nv = min(a.rows - r0, S::TN), mv = min(a.K - m0, S::TM);
+  Acc<S> acc;
+  clear<S>(acc);
+#pragma unroll 1
+  for (int p = 0; p < a.n2; ++p) {
+    const int k0 = max(s0 - p * one, 0) * kBK, kn = min((s1 - p * one) * kBK, a.N) - k0;
+    if (kn <= 0) continue;
+    product<S, true, false, true>(Operand{a.w[p] + (long)k0 * a.K + m0, a.K, mv, kn}, Operand{a.d[p] + (long)r0 * a.N + k0, a.N, nv, kn}, kn,
+                                  lds, acc, [](Acc<S>&) {});
+  }
+  const long at = (long)r0 * a.K + m0;
+  put_sums<S>(lds, acc, a.parts > 1 ? a.part + (long)ks * a.rows * a.K + at : nullptr, a.dx + at, a.K, nv, mv);
+}
+
+// ---- dW = d^T x over the rows, for each matrix ----
+template <typename S>
+__global__ __launch_bounds__(S::T, 2) void k_dw(Call a) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+  const int one = (a.N + S::TN - 1) / S::TN, nb = a.n2 * one, na = (a.K + S::TM - 1) / S::TM;
+  int unit, tb;
+  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
+  const int ks = unit / na, m0 = unit % na * S::TM, p = tb / one, n0 = tb % one * S::TN;
+  int s0, s1;
+  part_of((a.rows + kBK - 1) / kBK, a.parts, ks, s0, s1);
+  const int k0 = s0 * kBK, kn = min(s1 * kBK, a.rows) - k0;
+  const int nv = min(a.N - n0, S::TN), mv = min(a.K - m0, S::TM);
+  Acc<S> acc;
+  clear<S>(acc);
+  product<S, true, true, true>(Operand{a.x + (long)k0 * a.K + m0, a.K, mv, kn}, Operand{a.d[p] + (long)k0 * a.N + n0, a.N, nv, kn}, kn, lds, acc,
+                               [](Acc<S>&) {});
+  const long at = (long)n0 * a.K + m0;
+  put_sums<S>(lds, acc, a.parts > 1 ? a.part + ((long)ks * a.n2 + p) * a.N * a.K + at : nullptr, a.dw[p] + at, a.K, nv, mv);
+}
+
+// the parts of `values` fp32 sums, added in order; the first `n0` of them go to out0, the others to out1
+__global__ __launch_bounds__(kT) void k_add_parts(const float* part, int parts, long values, long n0, uint16_t* out0, uint16_t* out1) {
+  const long i = (blockIdx.x * (long)kT + threadIdx.x) * 8;
+  if (i >= values) return;
+  float s[8] = {};
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(part + k * values + i);
+    const f32x4 x = p[0], y = p[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[e] += x[e];
+      s[4 + e] += y[e];
+    }
+  }
+  *reinterpret_cast<u32x4*>(i < n0 ? out0 + i : out1 + (i - n0)) = pack(s);
+}
+
+// ---- gradients of the pre-activations.  A thread takes 8 columns of the rows of a chunk; with a bias it adds them up. ----
+struct Pre {
+  const uint16_t *dy, *z[2];  // [rows, N]; z, or g and u, or null (no activation: d is dy, and only the sums are wanted)
+  uint16_t* d[2];
+  float* sums;                // [chunks][N], or null
+  int rows, N, act, chunks;
+};
+template <bool GATED>
+__global__ __launch_bounds__(kT) void k_pre(Pre a) {
+  const int P = a.N / 8, groups = (P + kT - 1) / kT;
+  const int c = blockIdx.x / groups, p = (blockIdx.x - c * groups) * kT + threadIdx.x;
+  if (p >= P) return;
+  const int first = (int)((long)a.rows * c / a.chunks), last = (int)((long)a.rows * (c + 1) / a.chunks);
+  float s[8] = {};
+  with_act(a.act, [&](auto act) {
+#pragma unroll 2
+    for (int r = first; r < last; ++r) {
+      const long at = (long)r * a.N + p * 8;
+      float dy[8], z[8], u[8], d[8];
+      unpack(*reinterpret_cast<const u32x4*>(a.dy + at), dy);
+      if (GATED || act.value != DFLARE_ACT_NONE) {
+        unpack(*reinterpret_cast<const u32x4*>(a.z[0] + at), z);
+        if constexpr (GATED) unpack(*reinterpret_cast<const u32x4*>(a.z[1] + at), u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = Activation<act.value>::both(z[e], d[e]);
+          if constexpr (GATED) {
+            z[e] = dy[e] * v;
+            dy[e] *= u[e];
+          }
+          dy[e] *= d[e];
+        }
+        *reinterpret_cast<u32x4*>(a.d[0] + at) = pack(dy);
+        if constexpr (GATED) *reinterpret_cast<u32x4*>(a.d[1] + at) = pack(z);
+      }
+      if constexpr (!GATED) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += dy[e];
+      }
+    }
+  });
+  if (GATED || !a.sums) return;
+  f32x4* to = reinterpret_cast<f32x4*>(a.sums + (long)c * a.N + p * 8);
+  to[0] = f32x4{s[0], s[1], s[2], s[3]};
+  to[1] = f32x4{s[4], s[5], s[6], s[7]};
+}
+
+// the bias' gradient from the chunks' sums (16 groups of them, then these in order)
+__global__ __launch_bounds__(kT) void k_dbias(const float* sums, int chunks, int N, uint16_t* out) {
+  __shared__ float s[16][17];
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
+  float v = 0.f;
+  if (c < N) {
+#pragma unroll 8
+    for (int k = g; k < chunks; k += 16) v += sums[(long)k * N + c];
+  }
+  s[g][l] = v;
+  __syncthreads();
+  if (g == 0 && c < N) {
+    for (int k = 1; k < 16; ++k) v += s[k][l];
+    out[c] = (uint16_t)pack2(v, 0.f);
+  }
+}
+
+// ---- host side ----
+constexpr int kMostParts = 128;         // of a product
+constexpr long kPartValues = 1l << 25;  // and most sums of these together
+constexpr int kPreGroups = 2048;        // work-groups of k_pre, about
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+// bytes of the parts of a product of `values` sums, at most (grows with them)
+size_t part_bytes(long values) { return up((size_t)std::min(kPartValues, kMostParts * values) * 4); }
+
+// How a product of m x n over `stages` of k is cut: the tile, and the parts of k.
+struct Plan {
+  int tile, parts;  // 0 large, 1 small, 2 for few rows
+  long groups;
+};
+Plan plan_of(long m_large, long m_small, long n, int stages, long values, bool few) {
+  auto over = [](long a, long b) { return (a + b - 1) / b; };
+  Plan best{};
+  double least = 1e300;
+  for (int t = 0; t < 3; ++t) {
+    if ((t == 2) != (few && n <= Few::TN)) continue;
+    const long tn = t == 0 ? Large::TN : t == 1 ? Small::TN : Few::TN;
+    const long tiles = (t == 0 ? over(m_large, Large::TM) : over(m_small, Small::TM)) * over(n, tn), slots = 256l * (t + 1);
+    const double stage = t == 0 ? 1.8 : 1.15;
+    for (int k = 1; k <= kMostParts; ++k) {
+      if (k > 1 && (tiles * k > 2 * slots || stages < 4 * k || values * k > kPartValues)) break;
+      const double cost = over(tiles * k, slots) * (over(stages, k) + 8) * stage + (k > 1 ? 4.0 + (double)values * k * 4 / 4e6 : 0.0);
+      if (cost < least) {
+        least = cost;
+        best = Plan{t, k, tiles * k};
+      }
+    }
+  }
+  return best;
+}
+
+int check(int rows, int N, int K, int act) {
+  if (rows < 0 || N < 1 || K < 1 || act < DFLARE_ACT_NONE || act > DFLARE_ACT_GELU_TANH) return DFLARE_ERR_INVALID_ARG;
+  if (N % 8 || K % 8 || N > (1 << 18) || K > (1 << 18) || rows > (1 << 22)) return DFLARE_ERR_UNSUPPORTED;
+  // a launch has less than 2^32 threads: of 256 over tiles of 128 x 64, and over 8 values each
+  const long tiles = std::max({(rows + 63l) / 64 * ((std::max(N, K) + 63l) / 64), (N + 63l) / 64 * 2 * ((K + 127l) / 128)});
+  return tiles >= (1l << 23) ? DFLARE_ERR_UNSUPPORTED : DFLARE_OK;
+}
+
+template <typename F>
+void by_tile(int tile, F&& f) {
+  if (tile == 0) f(Large{});
+  else if (tile == 1) f(Small{});
+  else f(Few{});
+}
+unsigned whole_turns(long groups) { return (unsigned)((groups + 7) / 8 * 8); }  // of the XCDs
+int stages_of(long k) { return (int)((k + kBK - 1) / kBK); }
+
+template <bool GATED>
+void forward(Call a, hipStream_t st) {
+  const long values = (long)a.rows * a.N * a.n2;
+  const Plan p = plan_of(GATED ? (a.N + 127l) / 128 * 256 : a.N, GATED ? (a.N + 63l) / 64 * 128 : a.N, a.rows, stages_of(a.K), values, true);
+  a.parts = p.parts;
+  by_tile(p.tile, [&](auto s) {
+    using S = decltype(s);
+    hipLaunchKernelGGL((k_forward<S, GATED>), dim3(whole_turns(p.groups)), dim3(S::T), 0, st, a);
+  });
+  if (p.parts > 1) {
+    const long threads = (long)a.rows * (a.N / 8);
+    hipLaunchKernelGGL((k_finish<GATED>), dim3((unsigned)((threads + kT - 1) / kT)), dim3(kT), 0, st, a);
+  }
+}
+void add_parts(const Call& a, long values, long n0, uint16_t* out0, uint16_t* out1, hipStream_t st) {
+  if (a.parts == 1) return;
+  hipLaunchKernelGGL(k_add_parts, dim3((unsigned)((values / 8 + kT - 1) / kT)), dim3(kT), 0, st, a.part, a.parts, values, n0, out0, out1);
+}
+void gradient_of_x(Call a, hipStream_t st) {
+  const long values = (long)a.rows * a.K;
+  const Plan p = plan_of(a.K, a.K, a.rows, a.n2 * stages_of(a.N), values, true);
+  a.parts = p.parts;
+  by_tile(p.tile, [&](auto s) {
+    using S = decltype(s);
+    hipLaunchKernelGGL((k_dx<S>), dim3(whole_turns(p.groups)), dim3(S::T), 0, st, a);
+  });
+  add_parts(a, values, values, a.dx, nullptr, st);
+}
+void gradient_of_w(Call a, hipStream_t st) {
+  const long one = (long)a.N * a.K;
+  const Plan p = plan_of(a.K, a.K, (long)a.n2 * a.N, stages_of(a.rows), a.n2 * one, false);
+  a.parts = p.parts;
+  auto go = [&](auto s) {  // (operands across have no tiles of 64)
+    using S = decltype(s);
+    const long tiles = (a.K + S::TM - 1l) / S::TM * ((a.N + S::TN - 1l) / S::TN) * a.n2;
+    hipLaunchKernelGGL((k_dw<S>), dim3(whole_turns(tiles * a.parts)), dim3(S::T), 0, st, a);
+  };
+  if (p.tile == 0) go(Large{});
+  else go(Small{});
+  add_parts(a, a.n2 * one, one, a.dw[0], a.dw[1], st);
+}
+// work-groups over 2,048 columns each, and chunks of rows
+int pre_chunks(int rows, int N) { return (int)std::max(1l, std::min<long>(rows, kPreGroups / ((N / 8 + kT - 1) / kT))); }
+template <bool GATED>
+void pre_gradients(const Pre& a, hipStream_t st) {
+  const long groups = (long)(a.N / 8 + kT - 1) / kT * a.chunks;
+  hipLaunchKernelGGL((k_pre<GATED>), dim3((unsigned)groups), dim3(kT), 0, st, a);
+}
+
+bool off16(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (misplaced(p, 16)) return true;
+  return false;
+}
+
+struct BwdLayout {
+  size_t d, sums, part, total;
+};
+// d: n_d gradients of [rows, N]; sums of a bias' gradient; the parts of the larger product
+BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx, bool dw) {
+  BwdLayout L{};
+  size_t o = 0;
+  L.d = o;
+  o += n_d * up((size_t)rows * N * 2);
+  L.sums = o;
+  if (sums) o += up((size_t)std::min(std::max(rows, 1), kPreGroups) * N * 4);
+  L.part = o;
+  o += std::max(dx ? part_bytes((long)rows * K) : 0, dw ? part_bytes((long)n2 * N * K) : 0);
+  L.total = std::max<size_t>(o, 256);
+  return L;
+}
+// zeros by a kernel (a memset node of a captured graph is not relied upon)
+__global__ __launch_bounds__(kT) void k_zero(u32x4* p, long n) {
+  const long i = blockIdx.x * (long)kT + threadIdx.x;
+  if (i < n) p[i] = u32x4{0u, 0u, 0u, 0u};
+}
+void zero(void* p, size_t bytes, hipStream_t st) {
+  if (p) hipLaunchKernelGGL(k_zero, dim3((unsigned)((bytes / 16 + kT - 1) / kT)), dim3(kT), 0, st, (u32x4*)p, (long)(bytes / 16));
+}
+
+}  // namespace
+
+}  // namespace dflare
+
+using namespace dflare;
+
+extern "C" {
+
+size_t dflare_linear_fwd_workspace(int32_t rows, int32_t N, int32_t K) {
+  return check(rows, N, K, 0) == DFLARE_OK ? std::max<size_t>(part_bytes((long)rows * N), 256) : 0;
+}
+
+int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, int32_t rows, int32_t N, int32_t K, int32_t act,
+                      void* y, void* z, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check(rows, N, K, act);
+  if (rc != DFLARE_OK) return rc;
+  if (!w || !workspace || (rows > 0 && (!x || !y))) return DFLARE_ERR_INVALID_ARG;
+  if (off16({x, w, bias, residual, y, z, workspace}) || workspace_bytes < dflare_linear_fwd_workspace(rows, N, K)) return DFLARE_ERR_INVALID_ARG;
+  const size_t xb = (size_t)rows * K * 2, wb = (size_t)N * K * 2, yb = (size_t)rows * N * 2, ws = dflare_linear_fwd_workspace(rows, N, K);
+  if (!apart({{y, yb}, {z, yb}, {workspace, ws}}, {{x, xb}, {w, wb}, {bias, (size_t)N * 2}}) ||
+      !apart({{z, yb}, {workspace, ws}}, {{residual, yb}}) || !same_or_apart(y, residual, yb))
+    return DFLARE_ERR_INVALID_ARG;
+  if (rows == 0) return DFLARE_OK;
+  if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
+  Call a{};
+  a.x = (const uint16_t*)x;
+  a.w[0] = (const uint16_t*)w;
+  a.bias = (const uint16_t*)bias;
+  a.res = (const uint16_t*)residual;
+  a.y = (uint16_t*)y;
+  a.z[0] = (uint16_t*)z;
+  a.part = (float*)workspace;
+  a.rows = rows;
+  a.N = N;
+  a.K = K;
+  a.n2 = 1;
+  a.act = act;
+  forward<false>(a, (hipStream_t)stream);
+  return launched();
+}
+
+size_t dflare_linear_bwd_workspace(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias) {
+  if (check(rows, N, K, act) != DFLARE_OK) return 0;
+  return bwd_layout(rows, N, K, 1, act != DFLARE_ACT_NONE, dbias != 0, dx != 0, dw != 0).total;
+}
+
+int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* z, int32_t rows, int32_t N, int32_t K, int32_t act, void* dx,
+                      void* dw, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check(rows, N, K, act);
+  if (rc != DFLARE_OK) return rc;
+  const bool named = act != DFLARE_ACT_NONE;
+  if (!workspace || (rows > 0 && (!dy || (named && !z) || (dx && !w) || (dw && !x)))) return DFLARE_ERR_INVALID_ARG;
+  if (off16({dy, x, w, z, dx, dw, dbias, workspace})) return DFLARE_ERR_INVALID_ARG;
+  const BwdLayout L = bwd_layout(rows, N, K, 1, named, dbias != nullptr, dx != nullptr, dw != nullptr);
+  if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
+  const size_t xb = (size_t)rows * K * 2, wb = (size_t)N * K * 2, yb = (size_t)rows * N * 2;
+  if (!apart({{dx, xb}, {dw, wb}, {dbias, (size_t)N * 2}, {workspace, L.total}},
+             {{dy, yb}, {dw ? x : nullptr, xb}, {dx ? w : nullptr, wb}, {named ? z : nullptr, yb}}))
+    return DFLARE_ERR_INVALID_ARG;
+  if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  if (rows == 0) {
+    zero(dw, wb, st);
+    zero(dbias, (size_t)N * 2, st);
+    return launched();
+  }
+  char* ws = (char*)workspace;
+  Call a{};
+  a.x = (const uint16_t*)x;
+  a.w[0] = (const uint16_t*)w;
+  a.dx = (uint16_t*)dx;
+  a.dw[0] = (uint16_t*)dw;
+  a.part = (float*)(ws + L.part);
+  a.rows = rows;
+  a.N = N;
+  a.K = K;
+  a.n2 = 1;
+  a.d[0] = named ? (const uint16_t*)(ws + L.d) : (const uint16_t*)dy;
+  if (dbias || (named && (dx || dw))) {
+    Pre p{};
+    p.dy = (const uint16_t*)dy;
+    p.z[0] = (const uint16_t*)z;
+    p.d[0] = (uint16_t*)(ws + L.d);
+    p.sums = dbias ? (float*)(ws + L.sums) : nullptr;
+    p.rows = rows;
+    p.N = N;
+    p.act = act;
+    p.chunks = pre_chunks(rows, N);
+    pre_gradients<false>(p, st);
+    if (dbias) hipLaunchKernelGGL(k_dbias, dim3((N + 15) / 16), dim3(kT), 0, st, p.sums, p.chunks, N, (uint16_t*)dbias);
+  }
+  if (dx) gradient_of_x(a, st);
+  if (dw) gradient_of_w(a, st);
+  return launched();
+}
+
+size_t dflare_gated_fwd_workspace(int32_t rows, int32_t H, int32_t F) {
+  return check(rows, F, H, 0) == DFLARE_OK ? std::max<size_t>(part_bytes(2l * rows * F), 256) : 0;
+}
+
+int dflare_gated_fwd(const void* x, const void* w_gate, const void* w_up, int32_t rows, int32_t H, int32_t F, int32_t act, void* h, void* gate,
+                     void* up, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check(rows, F, H, act);
+  if (rc != DFLARE_OK) return rc;
+  if (!w_gate || !w_up || !workspace || (rows > 0 && (!x || !h)) || !gate != !up) return DFLARE_ERR_INVALID_ARG;
+  if (off16({x, w_gate, w_up, h, gate, up, workspace}) || workspace_bytes < dflare_gated_fwd_workspace(rows, H, F)) return DFLARE_ERR_INVALID_ARG;
+  const size_t xb = (size_t)rows * H * 2, wb = (size_t)F * H * 2, yb = (size_t)rows * F * 2;
+  if (!apart({{h, yb}, {gate, yb}, {up, yb}, {workspace, dflare_gated_fwd_workspace(rows, H, F)}}, {{x, xb}, {w_gate, wb}, {w_up, wb}}))
+    return DFLARE_ERR_INVALID_ARG;
+  if (rows == 0) return DFLARE_OK;
+  if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
+  Call a{};
+  a.x = (const uint16_t*)x;
+  a.w[0] = (const uint16_t*)w_gate;
+  a.w[1] = (const uint16_t*)w_up;
+  a.y = (uint16_t*)h;
+  a.z[0] = (uint16_t*)gate;
+  a.z[1] = (uint16_t*)up;
+  a.part = (float*)workspace;
+  a.rows = rows;
+  a.N = F;
+  a.K = H;
+  a.n2 = 2;
+  a.act = act;
+  forward<true>(a, (hipStream_t)stream);
+  return launched();
+}
+
+size_t dflare_gated_bwd_workspace(int32_t rows, int32_t H, int32_t F, int32_t dx, int32_t dw) {
+  return check(rows, F, H, 0) == DFLARE_OK ? bwd_layout(rows, F, H, 2, 2, false, dx != 0, dw != 0).total : 0;
+}
+
+int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void* up_, const void* w_gate, const void* w_up, int32_t rows,
+                     int32_t H, int32_t F, int32_t act, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  int rc = check(rows, F, H, act);
+  if (rc != DFLARE_OK) return rc;
+  if (!workspace || !dw_gate != !dw_up) return DFLARE_ERR_INVALID_ARG;
+  if (rows > 0 && (!dh || !gate || !up_ || (dx && (!w_gate || !w_up)) || (dw_gate && !x))) return DFLARE_ERR_INVALID_ARG;
+  if (off16({dh, x, gate, up_, w_gate, w_up, dx, dw_gate, dw_up, workspace})) return DFLARE_ERR_INVALID_ARG;
+  const BwdLayout L = bwd_layout(rows, F, H, 2, 2, false, dx != nullptr, dw_gate != nullptr);
+  if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
+  const size_t xb = (size_t)rows * H * 2, wb = (size_t)F * H * 2, yb = (size_t)rows * F * 2;
+  if (!apart({{dx, xb}, {dw_gate, wb}, {dw_up, wb}, {workspace, L.total}},
+             {{dh, yb}, {gate, yb}, {up_, yb}, {dw_gate ? x : nullptr, xb}, {dx ? w_gate : nullptr, wb}, {dx ? w_up : nullptr, wb}}))
+    return DFLARE_ERR_INVALID_ARG;
+  if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  if (rows == 0) {
+    zero(dw_gate, wb, st);
+    zero(dw_up, wb, st);
+    return launched();
+  }
+  char* ws = (char*)workspace;
+  Call a{};
+  a.x = (const uint16_t*)x;
+  a.w[0] = (const uint16_t*)w_gate;
+  a.w[1] = (const uint16_t*)w_up;
+  a.dx = (uint16_t*)dx;
+  a.dw[0] = (uint16_t*)dw_gate;
+  a.dw[1] = (uint16_t*)dw_up;
+  a.part = (float*)(ws + L.part);
+  a.rows = rows;
+  a.N = F;
+  a.K = H;
+  a.n2 = 2;
+  Pre p{};
+  p.dy = (const uint16_t*)dh;
+  p.z[0] = (const uint16_t*)gate;
+  p.z[1] = (const uint16_t*)up_;
+  p.d[0] = (uint16_t*)(ws + L.d);
+  p.d[1] = (uint16_t*)(ws + L.d + up((size_t)rows * F * 2));
+  p.rows = rows;
+  p.N = F;
+  p.act = act;
+  p.chunks = pre_chunks(rows, F);
+  a.d[0] = p.d[0];
+  a.d[1] = p.d[1];
+  if (dx || dw_gate) pre_gradients<true>(p, st);
+  if (dx) gradient_of_x(a, st);
+  if (dw_gate) gradient_of_w(a, st);
+  return launched();
+}
+
+}  // extern "C"

@@ -50,6 +50,8 @@ struct Operand {
   // plain: 256 k lie side by side, the next 256 `block` bytes on (512: rows of any length); first stage
   long block = 512;
   int s0 = 0;
+  // plain, in two parts: the rows of a tile are PART of p, then PART of `other` (of the same ld and valid), and so on in turn
+  const uint16_t* other = nullptr;
 };
 
 // 1 KB from base + off (16 bytes per lane) to LDS, asynchronously.  In asm, and waited for by wait_vm_barrier: with the
@@ -60,9 +62,10 @@ __device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
 }
 
-// ROWS: rows (plain) or columns (across) of the operand's tile; W waves load it
-template <bool ACROSS, int ROWS, int W>
+// ROWS: rows (plain) or columns (across) of the operand's tile; W waves load it.  PART: rows of an operand's part, 0: whole
+template <bool ACROSS, int ROWS, int W, int PART = 0>
 struct Loader {
+  static_assert(!ACROSS || ROWS % 128 == 0, "the pieces' permutation");
   static constexpr int N = ROWS * kBK * 2 / 1024 / W;  // loads of a wave and stage
   static constexpr int SB = 256 / kBK;                 // stages of a block of 256 k
   const char* at;   // of the next stage
@@ -72,12 +75,19 @@ struct Loader {
   __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
     st = o.s0;
     step = ACROSS ? o.ld * kBK * 2 : o.block - (SB - 1) * kBK * 2;
-    at = reinterpret_cast<const char*>(o.p) + (ACROSS ? 0 : st / SB * o.block + st % SB * (kBK * 2));
+    const uint16_t* p = o.p;
+    if constexpr (PART > 0) {
+      static_assert(!ACROSS && PART % (8 * N) == 0, "a wave loads rows of one part");
+      if (N * w * 8 / PART & 1) p = o.other;
+    }
+    at = reinterpret_cast<const char*>(p) + (ACROSS ? 0 : st / SB * o.block + st % SB * (kBK * 2));
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if constexpr (!ACROSS) {
         const int row = (N * w + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
-        off[j] = (uint32_t)(min(row, o.valid - 1) * o.ld * 2 + c * 16);
+        int from = row;
+        if constexpr (PART > 0) from = row / (2 * PART) * PART + row % PART;
+        off[j] = (uint32_t)(min(from, o.valid - 1) * o.ld * 2 + c * 16);
       } else {
         constexpr int P = ROWS / 8;  // pieces of a row
         const int row = (N * w + j) * (64 / P) + lane / P, c = (lane % P) ^ ((row & 3) << 2);
@@ -131,6 +141,11 @@ struct Reader {
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
   }
+  // the same for a ks that the compiler does not know
+  __device__ __forceinline__ u32x4 at(const char* op, int ks, int j) const {
+    if constexpr (!ACROSS) return *reinterpret_cast<const u32x4*>(op + (ks == 0 ? off[0] : ks == 1 ? off[1] : ks == 2 ? off[2] : off[3]) + j * 4096);
+    else return get(op, ks, j);
+  }
   static __device__ __forceinline__ u32x2 tr(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDSP s16x4*)(LDSP char*)const_cast<char*>(p)));
   }
@@ -138,6 +153,15 @@ struct Reader {
 
 template <typename S>
 using Acc = f32x16[S::MT][S::NT];
+template <typename S>
+__device__ __forceinline__ void clear(Acc<S>& acc) {
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+}
 
 // Two stages lie in LDS, one of them on its way; a wave reads the operands of each 16 k between the products of the 16
 // before.  7,296 rows x 30,464 words x 4,096 (1,545 to 1,570 us with the epilogue, 1,170 TFLOP/s; dh of them 1,615 to 1,680): the matrix
@@ -147,9 +171,11 @@ using Acc = f32x16[S::MT][S::NT];
 // lines requested into L2 two stages ahead 6%: what is left lies outside the CUs, in the loads that miss L2 (2.3 TB/s).
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
 // something finite.  start(acc) runs while the first stages are on their way.
-template <typename S, bool XA, bool XB, typename F>
+// MASK: acc += A B^T over k in [0, K) alone, kend of both operands being K; what lies past it takes no part (a stage that K
+// ends in comes last, by itself, with both operands' k past the end set to zero).
+template <typename S, bool XA, bool XB, bool MASK = false, int PART = 0, typename F>
 __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc<S>& acc, F&& start) {
-  using LA = Loader<XA, S::TM, S::W>;
+  using LA = Loader<XA, S::TM, S::W, PART>;
   using LB = Loader<XB, S::TN, S::W>;
   constexpr int MT = S::MT, NT = S::NT, Q = MT * NT, R = MT + NT, SB = S::kStageBytes;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -161,13 +187,8 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   Reader<XB, S::TN> rb;
   ra.init(w % S::WM * MT, lane);
   rb.init(w / S::WM * NT, lane);
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  const int nk = (K + kBK - 1) / kBK;
+  if constexpr (!MASK) clear<S>(acc);
+  const int nk = (K + kBK - 1) / kBK, whole = MASK ? K / kBK : nk;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)lds);
   const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + S::kABytes + w * LB::N * 1024;
   int next = 0;  // stage to load; past the last stage nothing is
@@ -213,7 +234,7 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   for (int n = 0; n < R; ++n) read(f0, 0, 0, n);
   uint32_t buf = 0;
   bool late = false;  // the second operand's share of the stage after the next is still to be issued
-  for (int kt = 0; kt < nk; ++kt) {
+  for (int kt = 0; kt < whole; ++kt) {
     const uint32_t other = SB - buf;
     fence();
 #pragma unroll
@@ -241,6 +262,27 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     }
     late = true;
     buf = other;
+  }
+  if constexpr (MASK) {
+    if (whole < nk) {
+      const int left = K - whole * kBK, h = lane >> 5;
+#pragma unroll 1
+      for (int ks = 0; ks * 16 < left; ++ks) {
+        const int n = left - ks * 16 - 8 * h;  // of a lane's 8 k those below n are there
+        u32x4 keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[e] = 2 * e + 1 < n ? ~0u : 2 * e < n ? 0xFFFFu : 0u;
+        u32x4 a[MT], b[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) a[i] = ra.at(lds + buf, ks, i) & keep;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = rb.at(lds + S::kABytes + buf, ks, j) & keep;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma32(a[i], b[j], acc[i][j]);
+      }
+    }
   }
   wait_vm_barrier<0>();
 }

@@ -35,7 +35,9 @@ EXPORTED = (
     "dflare_weighted_ce_workspace", "dflare_weighted_ce", "dflare_weighted_ce_noalloc", "dflare_read_probe",
     "dflare_rope_frequencies", "dflare_rope", "dflare_norm_fwd", "dflare_norm_bwd_workspace", "dflare_norm_bwd",
     "dflare_linear_ce_workspace", "dflare_linear_ce", "dflare_grad_norm_workspace", "dflare_grad_norm",
-    "dflare_clip_grads",
+    "dflare_clip_grads", "dflare_qk_norm_rope_fwd", "dflare_qk_norm_rope_bwd_workspace", "dflare_qk_norm_rope_bwd",
+    "dflare_linear_fwd_workspace", "dflare_linear_fwd", "dflare_linear_bwd_workspace", "dflare_linear_bwd",
+    "dflare_gated_fwd_workspace", "dflare_gated_fwd", "dflare_gated_bwd_workspace", "dflare_gated_bwd", "dflare_adamw",
 )
 K_QKV, K_ATTN, K_O, K_GATE_UP, K_DOWN, K_LM_HEAD, K_FUSE, K_KV_T, K_DRAFT = range(1, 10)
 (K_B_QKV, K_B_ATTN, K_B_O, K_B_GATE_UP, K_B_DOWN, K_B_LM_HEAD, K_B_KV_T, K_B_EPI, K_B_FUSE, K_B_DRAFT,
@@ -76,6 +78,28 @@ class dflare_rope_tensor(ctypes.Structure):
 
 class dflare_grad_tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class dflare_qk_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "y", "gain")] + [
+        (n, ctypes.c_int64) for n in ("x_row", "x_head", "y_row", "y_head")] + [("n_heads", ctypes.c_int32)]
+
+
+class dflare_qk_grad(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dy", "dx", "gain", "dgain")] + [
+        (n, ctypes.c_int64) for n in ("x_row", "x_head", "dy_row", "dy_head", "dx_row", "dx_head")] + [
+        ("n_heads", ctypes.c_int32)]
+
+
+class dflare_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")] + [
+        ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class dflare_adamw_options(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("step", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("lr_device", "step_device", "sumsq")] + [
+        ("max_norm", ctypes.c_float), ("state_bits", ctypes.c_int32)]
 
 
 _lib = None
@@ -138,6 +162,18 @@ def lib() -> ctypes.CDLL:
         "dflare_grad_norm_workspace": ([i32], ctypes.c_size_t),
         "dflare_grad_norm": ([vp, i32, vp, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
         "dflare_clip_grads": ([vp, i32, vp, ctypes.c_float, vp], ctypes.c_int),
+        "dflare_qk_norm_rope_fwd": ([vp, i32, vp, vp] + [i32] * 6 + [ctypes.c_float] * 2 + [vp], ctypes.c_int),
+        "dflare_qk_norm_rope_bwd_workspace": ([i32] * 3, ctypes.c_size_t),
+        "dflare_qk_norm_rope_bwd": ([vp, i32, vp, vp] + [i32] * 6 + [ctypes.c_float] * 2 + [vp, ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_linear_fwd_workspace": ([i32] * 3, ctypes.c_size_t),
+        "dflare_linear_fwd": ([vp] * 4 + [i32] * 4 + [vp] * 3 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_linear_bwd_workspace": ([i32] * 7, ctypes.c_size_t),
+        "dflare_linear_bwd": ([vp] * 4 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_gated_fwd_workspace": ([i32] * 3, ctypes.c_size_t),
+        "dflare_gated_fwd": ([vp] * 3 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_gated_bwd_workspace": ([i32] * 5, ctypes.c_size_t),
+        "dflare_gated_bwd": ([vp] * 6 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_adamw": ([vp, i32, vp, vp], ctypes.c_int),
         "dflare_context_len_seq": ([vp, i32, ctypes.POINTER(i32)], ctypes.c_int),
         "dflare_debug_read_seq": ([vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
                                    i64], ctypes.c_int),
@@ -163,7 +199,9 @@ def _native():
         mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_binding", loader))
         loader.exec_module(mod)
         mod.bind(*(ctypes.cast(getattr(lib(), "dflare_" + f), ctypes.c_void_p).value for f in (
-            "norm_fwd", "norm_bwd_workspace", "norm_bwd", "rope", "grad_norm_workspace", "grad_norm", "clip_grads")),
+            "norm_fwd", "norm_bwd_workspace", "norm_bwd", "rope", "grad_norm_workspace", "grad_norm", "clip_grads",
+            "qk_norm_rope_fwd", "qk_norm_rope_bwd_workspace", "qk_norm_rope_bwd", "linear_fwd_workspace", "linear_fwd",
+            "linear_bwd_workspace", "linear_bwd", "gated_fwd_workspace", "gated_fwd", "gated_bwd_workspace", "gated_bwd", "adamw")),
                  _current_raw, torch.OutOfMemoryError)
         _binding = mod
     return _binding
@@ -529,6 +567,85 @@ def clip_grads(grads, sumsq: torch.Tensor, max_norm: float, out=None, stream=Non
     if not grads:
         return
     _native_call("clip_grads", grads[0], stream, grads, sumsq, max_norm, None if out is None else list(out))
+
+
+def _pair(x) -> tuple:
+    return tuple(x) if isinstance(x, (tuple, list)) else (x,)
+
+
+def qk_norm_rope_fwd(x, gain, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = ROPE_HALF, scale: float = 1.0,
+                     eps: float = 1e-6, out=None, stream=None):
+    """RMSNorm of each head of x [rows, n_heads, head_dim] by its gain [head_dim] (or None: ones), and its rotary position as
+    rope gives it, in one pass (include/dflare.h); or of a pair of such tensors with a pair of gains (queries and keys).  The
+    last dimension is contiguous, the others may be strided.  out: where the result goes (x itself: in place); by default new
+    tensors.  Returns out."""
+    xs = _pair(x)
+    outs = _native_call("qk_norm_rope_fwd", xs[0] if xs else None, stream, xs, _pair(gain), inv_freq, positions, B, layout, scale, eps,
+                        None if out is None else _pair(out))
+    return outs if isinstance(x, (tuple, list)) else outs[0]
+
+
+def qk_norm_rope_bwd(dy, x, gain, inv_freq: torch.Tensor, positions=None, B: int = 1, layout: int = ROPE_HALF, scale: float = 1.0,
+                     eps: float = 1e-6, stream=None):
+    """Backward of qk_norm_rope_fwd, from its x: returns (dx, dgain fp32 [head_dim], None beside a gain of None), or
+    pairs of them."""
+    xs = _pair(x)
+    dx, dgain = _native_call("qk_norm_rope_bwd", xs[0] if xs else None, stream, xs, _pair(gain), inv_freq, positions, B, layout, scale,
+                             eps, _pair(dy))
+    return (dx, dgain) if isinstance(x, (tuple, list)) else (dx[0], dgain[0])
+
+
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
+
+
+def linear_fwd(x, w, bias=None, residual=None, act: int = ACT_NONE, save: bool = False, stream=None):
+    """act(x w^T + bias) + residual (include/dflare.h): x bf16 [rows, K], w bf16 [N, K], bias bf16 [N], residual bf16
+    [rows, N].  Returns (y, z), z the pre-activation that linear_bwd takes, None unless it is to be saved."""
+    return _native_call("linear_fwd", x, stream, x, w, bias, residual, act, save)
+
+
+def linear_bwd(dy, x, w, z=None, act: int = ACT_NONE, need_dx: bool = True, need_dw: bool = True, need_dbias: bool = False,
+               stream=None):
+    """Backward of linear_fwd: returns (dx, dw, dbias) in bf16, None where not wanted.  dy is the residual's gradient."""
+    return _native_call("linear_bwd", x, stream, dy, x, w, z, act, need_dx, need_dw, need_dbias)
+
+
+def gated_fwd(x, w_gate, w_up, act: int = ACT_SILU, save: bool = False, stream=None):
+    """act(x w_gate^T) * (x w_up^T), in one product (include/dflare.h): x bf16 [rows, H], weights bf16 [F, H].  Returns
+    (h, gate, up) of [rows, F], the last two for gated_bwd, None unless they are to be saved."""
+    return _native_call("gated_fwd", x, stream, x, w_gate, w_up, act, save)
+
+
+def gated_bwd(dh, x, gate, up, w_gate, w_up, act: int = ACT_SILU, need_dx: bool = True, need_dw: bool = True, stream=None):
+    """Backward of gated_fwd: returns (dx, dw_gate, dw_up) in bf16, None where not wanted."""
+    return _native_call("gated_bwd", x, stream, dh, x, gate, up, w_gate, w_up, act, need_dx, need_dw)
+
+
+def adamw_state(params, bits: int = 32):
+    """The moments of parameters before the first step, as adamw takes them: (m, v, m_scales, v_scales), lists; the scales
+    are None for 32 bits."""
+    if bits not in (8, 32):
+        raise ValueError("states have 8 or 32 bits")
+    params = list(params)
+    m, v = ([torch.zeros(p.shape, dtype=torch.float8_e4m3fn if bits == 8 else torch.float32, device=p.device) for p in params]
+            for _ in range(2))
+    if bits == 32:
+        return m, v, None, None
+    ms, vs = ([torch.zeros(-(-p.numel() // 256), dtype=torch.float32, device=p.device) for p in params] for _ in range(2))
+    return m, v, ms, vs
+
+
+def adamw(params, grads, m, v, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+          masters=None, m_scales=None, v_scales=None, sumsq=None, max_norm: float = float("inf"), stream=None) -> None:
+    """One AdamW step over lists of parameters (bf16 or fp32), in place (include/dflare.h).  m, v: fp32, or float8_e4m3fn
+    with the scales of adamw_state; masters: fp32 parameters of the bf16 ones, or None; step (from 1) and lr: numbers, or device
+    tensors of one int64 and one fp64, which the kernels read; sumsq: grad_norm's, by which gradients are clipped to max_norm
+    (a step whose sumsq is not finite is left out)."""
+    params = list(params)
+    if not params:
+        return
+    lists = [params, *(None if t is None else list(t) for t in (grads, m, v, masters, m_scales, v_scales))]
+    _native_call("adamw", params[0], stream, *lists, step, lr, beta1, beta2, eps, weight_decay, sumsq, max_norm)
 
 
 def dflare_set_sampling(h: int, temperature: float, seed: int = 0) -> None:
