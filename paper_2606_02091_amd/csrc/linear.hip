@@ -117,6 +117,9 @@ __device__ __forceinline__ void part_of(int stages, int parts, int ks, int& s0, 
   s1 = (int)((long)stages * (ks + 1) / parts);
 }
 
+// the stage of k that a work-group begins with: another one on each XCD
+__device__ __forceinline__ int first_stage(int kn) { return (int)(blockIdx.x % 8) * (kn / kBK) / 8; }
+
 // 4 values as bf16 into LDS rows of TMO values; piece p of row n at p ^ (n mod the pieces)
 template <int TMO>
 __device__ __forceinline__ void put4(char* lds, int n, int p, int h, f32x4 v) {
@@ -141,6 +144,54 @@ __device__ __forceinline__ f32x4 bf4(const uint16_t* p) {
   return unpack4(v[0], v[1]);
 }
 
+// y = act(sums) + residual of a tile (y may lie on the residual).  The sums go through LDS in fp32, a 32-row tile of every wave at a
+// time, so that they wait there for their activation (with all of a wave's 128 in its lanes' registers these spill), and the
+// residual is read as wide as y is written.
+template <typename S>
+__device__ __forceinline__ void finish_tile(char* lds, const Acc<S>& acc, int act, const uint16_t* res, uint16_t* y, int ld, int nv, int mv) {
+  constexpr int TMO = S::TM, P = TMO / 8, ROWS = S::TN / S::NT, N = ROWS * P / S::T;  // rows of a turn, a thread's pieces of 8 columns
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int wm = w % S::WM, wn = w / S::WM, p = threadIdx.x % P, m = min(p * 8, mv - 8);
+  static_assert(ROWS * TMO * 4 <= 2 * S::kStageBytes && ROWS * P % S::T == 0 && S::T % P == 0);
+#pragma unroll
+  for (int j = 0; j < S::NT; ++j) {
+    auto row_of = [&](int i) { return (int)threadIdx.x / P + i * (S::T / P); };  // of the turn
+    auto n_of = [&](int row) { return row / 32 * (S::NT * 32) + j * 32 + row % 32; };
+    u32x4 r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      r[i] = res ? *reinterpret_cast<const u32x4*>(res + (uint32_t)(min(n_of(row_of(i)), nv - 1) * ld + m)) : u32x4{0u, 0u, 0u, 0u};
+    const int row = wn * 32 + (lane & 31);
+#pragma unroll
+    for (int t = 0; t < S::MT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(lds + row * (TMO * 4) + ((((wm * S::MT + t) * 8 + 2 * q + h) ^ (row & 31)) << 4)) = four(acc[t][j], q);
+    __syncthreads();
+    with_act(act, [&](auto a) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = row_of(i), n = n_of(row);
+        const char* from = lds + row * (TMO * 4);
+        f32x4 u = *reinterpret_cast<const f32x4*>(from + (((2 * p) ^ (row & 31)) << 4));
+        f32x4 v = *reinterpret_cast<const f32x4*>(from + (((2 * p + 1) ^ (row & 31)) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          u[e] = Activation<a.value>::value(u[e]);
+          v[e] = Activation<a.value>::value(v[e]);
+        }
+        if (res) {
+          u += unpack4(r[i][0], r[i][1]);
+          v += unpack4(r[i][2], r[i][3]);
+        }
+        if (n < nv && p * 8 < mv)
+          *reinterpret_cast<u32x4*>(y + (uint32_t)(n * ld + p * 8)) = u32x4{pack2(u[0], u[1]), pack2(u[2], u[3]), pack2(v[0], v[1]), pack2(v[2], v[3])};
+      }
+    });
+    __syncthreads();
+  }
+}
+
 // ---- z = x W^T, a tile of rows x TM rows of W, and its epilogue; or a part's sums ----
 template <typename S, bool GATED>
 __global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
@@ -157,11 +208,24 @@ __global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
   const long wo = (long)m0 * a.K + k0;
   Operand ow{a.w[0] + wo, a.K, mv, kn}, ox{a.x + (long)r0 * a.K + k0, a.K, nv, kn};
   if constexpr (GATED) ow.other = a.w[1] + wo;
-  Acc<S> acc;
-  clear<S>(acc);
-  product<S, false, false, true, PART>(ow, ox, kn, lds, acc, [](Acc<S>&) {});
+  ow.s0 = ox.s0 = first_stage(kn);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int wm = w % S::WM, n_wave = w / S::WM * (NT * 32) + (lane & 31);
+  Acc<S> acc;
+  clear<S>(acc);
+  product<S, false, false, true, PART>(ow, ox, kn, lds, acc, [&](Acc<S>& z) {  // (the bias is the sums' first term)
+    if (GATED || a.parts > 1 || !a.bias) return;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 b = bf4(a.bias + m0 + min((wm * MT + t) * 32 + 8 * q + 4 * h, mv - 4));
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[t][j][4 * q + e] = b[e];
+      }
+  });
   // f(32-row tile t of one matrix, j, q, row of the tile, first of four columns of the tile)
   auto each = [&](auto f) {
 #pragma unroll
@@ -209,30 +273,163 @@ __global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
       });
     });
   } else {
-    if (a.bias)
-      each([&](int t, int j, int q, int n, int m) {
-        const f32x4 b = bf4(a.bias + m0 + min(m, mv - 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[t][j][4 * q + e] += b[e];
-      });
     if (a.z[0]) {
       each([&](int t, int j, int q, int n, int m) { put4<TMO>(lds, n, m / 8, h, four(acc[t][j], q)); });
       __syncthreads();
       take<S, TMO>(lds, out_at(a.z[0]));
       __syncthreads();
     }
-    with_act(a.act, [&](auto act) {
-      each([&](int t, int j, int q, int n, int m) {
-        f32x4 v = four(acc[t][j], q);
+    if (a.res || a.act != DFLARE_ACT_NONE) return finish_tile<S>(lds, acc, a.act, a.res ? a.res + at0 : nullptr, a.y + at0, a.N, nv, mv);
+    each([&](int t, int j, int q, int n, int m) { put4<TMO>(lds, n, m / 8, h, four(acc[t][j], q)); });
+  }
+  __syncthreads();
+  take<S, TMO>(lds, out_at(a.y));
+}
+
+// ---- the same for up to 32 rows, bound by the way of W from memory.  A work-group per CU walks tiles of 16 T rows of each matrix.
+// Its eight waves take a part of k each, all of it through rings of NS stages of 64 k in LDS that are a wave's own, so that none
+// waits for another while a tile lasts and the stages of the next tile are on their way at the end of one.  There the waves' sums
+// meet in LDS, in order. ----
+template <bool GATED, int RT, int T>
+struct FewRows {
+  static constexpr int W = 8, TW = GATED ? 2 * T : T;       // waves, tiles of W
+  static constexpr int kStage = (TW + RT) * 2048;           // bytes of a wave's stage: 16 rows of 128 bytes a tile
+  static constexpr int kSums = W * TW * RT * 1024;
+  static constexpr int NS = (kLdsBytes - kSums) / (W * kStage) > 4 ? 4 : (kLdsBytes - kSums) / (W * kStage);
+  static constexpr int kLds = W * NS * kStage + kSums;
+  static_assert(NS >= 2);
+};
+template <bool GATED, int RT, int T>
+__global__ __launch_bounds__(512, 2) void k_few(Call a) {
+  using F = FewRows<GATED, RT, T>;
+  constexpr int W = F::W, TW = F::TW, NS = F::NS, L = (TW + RT) * 2;  // L: loads of a stage
+  __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
+  char* sums = lds + W * NS * F::kStage;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* ring = lds + w * NS * F::kStage;
+  const uint32_t ring0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)ring);
+  const int groups = (a.N + 16 * T - 1) / (16 * T), stages = (a.K + kBK - 1) / kBK, tail = a.K % kBK;
+  int s0, s1;
+  part_of(stages, W, w, s0, s1);
+  // a lane's pieces: rows lane / 8 and 8 more of a tile, piece c of them at c ^ (row / 2 mod 8); where a stage ends
+  // within the row, the pieces past it are its first again
+  uint32_t piece[2], cut[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = i * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+    piece[i] = c * 16;
+    cut[i] = tail && c * 8 >= tail ? c * 16 : 0;
+  }
+  uint32_t xo[RT][2], wo[T][2];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) xo[r][i] = (uint32_t)(min(r * 16 + i * 8 + (lane >> 3), a.rows - 1) * a.K * 2) + piece[i];
+  int ig = blockIdx.x, is = s0;  // tile group and stage to load
+  auto at_group = [&] {
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        wo[t][i] = (uint32_t)(min(t * 16 + i * 8 + (lane >> 3), a.N - 1 - ig * 16 * T) * a.K * 2) + piece[i];
+  };
+  at_group();
+  int ahead = 0;  // stages on their way or in the ring
+  auto issue = [&](uint32_t slot) {
+    if (ig >= groups || s0 == s1) return;
+    const bool last = tail && is == stages - 1;
+    const uint32_t dst = ring0 + slot * F::kStage;
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+      const char* p = reinterpret_cast<const char*>(a.w[t / T] + (long)ig * 16 * T * a.K) + (long)is * 128;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) load_lds(p, wo[t % T][i] - (last ? cut[i] : 0), dst + (2 * t + i) * 1024);
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        load_lds(reinterpret_cast<const char*>(a.x) + (long)is * 128, xo[r][i] - (last ? cut[i] : 0), dst + (2 * (TW + r) + i) * 1024);
+    ++ahead;
+    if (++is == s1) {
+      is = s0;
+      ig += gridDim.x;
+      at_group();
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < NS; ++k) issue(k);
+  uint32_t slot = 0;
+  for (int grp = blockIdx.x; grp < groups; grp += gridDim.x) {
+    const int m0 = grp * 16 * T;
+    f32x4 acc[TW][RT];
+#pragma unroll
+    for (int t = 0; t < TW; ++t)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = s0; s < s1; ++s) {
+      if (ahead == NS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * L) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const char* from = ring + slot * F::kStage;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const int row = lane & 15, c = ks * 4 + (lane >> 4);
+        const uint32_t at = row * 128 + ((c ^ ((row >> 1) & 7)) << 4);
+        u32x4 fw[TW], fx[RT];
+#pragma unroll
+        for (int t = 0; t < TW; ++t) fw[t] = *reinterpret_cast<const u32x4*>(from + t * 2048 + at);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) fx[r] = *reinterpret_cast<const u32x4*>(from + (TW + r) * 2048 + at);
+        if (tail && s == stages - 1 && c * 8 >= tail) {  // past the end of k
+#pragma unroll
+          for (int t = 0; t < TW; ++t) fw[t] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int r = 0; r < RT; ++r) fx[r] = u32x4{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[t][r] = mfma(fw[t], fx[r], acc[t][r]);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage is read: its place takes another
+      --ahead;
+      issue(slot);
+      slot = slot + 1 == NS ? 0 : slot + 1;
+    }
+    auto meet = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };  // (not for what is on its way)
+    meet();  // the sums of the tile before are read
+#pragma unroll
+    for (int t = 0; t < TW; ++t)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(sums + (((w * TW + t) * RT + r) * 64 + lane) * 16) = acc[t][r];
+    meet();
+    const int l = threadIdx.x & 63, r = (threadIdx.x >> 6) % RT, t = (threadIdx.x >> 6) / RT, row = r * 16 + (l & 15);
+    const int m = m0 + t * 16 + (l >> 4) * 4;
+    if (t < T && row < a.rows && m < a.N) {  // four columns of a row
+      auto sum = [&](int tile) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < W; ++k) v += *reinterpret_cast<const f32x4*>(sums + (((k * TW + tile) * RT + r) * 64 + l) * 16);
+        return v;
+      };
+      f32x4 v = sum(t), u = v;
+      if constexpr (GATED) u = sum(T + t);
+      const long at = (long)row * a.N + m;
+      auto put = [&](uint16_t* to, f32x4 x) { *reinterpret_cast<uint2*>(to + at) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3])); };
+      if (!GATED && a.bias) v += bf4(a.bias + m);
+      if (a.z[0]) {
+        put(a.z[0], v);
+        if constexpr (GATED) put(a.z[1], u);
+      }
+      with_act(a.act, [&](auto act) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = Activation<act.value>::value(v[e]);
-        if (a.res) v += bf4(a.res + at0 + (long)min(n, nv - 1) * a.N + min(m, mv - 4));
-        put4<TMO>(lds, n, m / 8, h, v);
       });
-    });
+      if constexpr (GATED) v = v * u;
+      else if (a.res) v += bf4(a.res + at);
+      put(a.y, v);
+    }
   }
-  __syncthreads();  // (y may lie on the residual: a tile of it has been read when any of it is written)
-  take<S, TMO>(lds, out_at(a.y));
 }
 
 // a forward product's parts, added in order, and its epilogue; a thread takes 8 columns of a row
@@ -326,8 +523,9 @@ __global__ __launch_bounds__(S::T, 2) void k_dx(Call a) {
   for (int p = 0; p < a.n2; ++p) {
     const int k0 = max(s0 - p * one, 0) * kBK, kn = min((s1 - p * one) * kBK, a.N) - k0;
     if (kn <= 0) continue;
-    product<S, true, false, true>(Operand{a.w[p] + (long)k0 * a.K + m0, a.K, mv, kn}, Operand{a.d[p] + (long)r0 * a.N + k0, a.N, nv, kn}, kn,
-                                  lds, acc, [](Acc<S>&) {});
+    Operand ow{a.w[p] + (long)k0 * a.K + m0, a.K, mv, kn}, od{a.d[p] + (long)r0 * a.N + k0, a.N, nv, kn};
+    ow.s0 = od.s0 = first_stage(kn);
+    product<S, true, false, true>(ow, od, kn, lds, acc, [](Acc<S>&) {});
   }
   const long at = (long)r0 * a.K + m0;
   put_sums<S>(lds, acc, a.parts > 1 ? a.part + (long)ks * a.rows * a.K + at : nullptr, a.dx + at, a.K, nv, mv);
@@ -347,8 +545,9 @@ __global__ __launch_bounds__(S::T, 2) void k_dw(Call a) {
   const int nv = min(a.N - n0, S::TN), mv = min(a.K - m0, S::TM);
   Acc<S> acc;
   clear<S>(acc);
-  product<S, true, true, true>(Operand{a.x + (long)k0 * a.K + m0, a.K, mv, kn}, Operand{a.d[p] + (long)k0 * a.N + n0, a.N, nv, kn}, kn, lds, acc,
-                               [](Acc<S>&) {});
+  Operand ox{a.x + (long)k0 * a.K + m0, a.K, mv, kn}, od{a.d[p] + (long)k0 * a.N + n0, a.N, nv, kn};
+  ox.s0 = od.s0 = first_stage(kn);
+  product<S, true, true, true>(ox, od, kn, lds, acc, [](Acc<S>&) {});
   const long at = (long)n0 * a.K + m0;
   put_sums<S>(lds, acc, a.parts > 1 ? a.part + ((long)ks * a.n2 + p) * a.N * a.K + at : nullptr, a.dw[p] + at, a.K, nv, mv);
 }
@@ -487,8 +686,27 @@ void by_tile(int tile, F&& f) {
 unsigned whole_turns(long groups) { return (unsigned)((groups + 7) / 8 * 8); }  // of the XCDs
 int stages_of(long k) { return (int)((k + kBK - 1) / kBK); }
 
+// the parts' sums of a forward product, as y
+template <bool GATED>
+void finish(const Call& a, hipStream_t st) {
+  if (a.parts == 1) return;
+  const long threads = (long)a.rows * (a.N / 8);
+  hipLaunchKernelGGL((k_finish<GATED>), dim3((unsigned)((threads + kT - 1) / kT)), dim3(kT), 0, st, a);
+}
+constexpr int kFewRows = 32;
+template <bool GATED>
+void forward_few(const Call& a, hipStream_t st) {
+  auto go = [&](auto rt, auto t) {
+    constexpr int RT = decltype(rt)::value, T = decltype(t)::value;
+    hipLaunchKernelGGL((k_few<GATED, RT, T>), dim3(std::min((a.N + 16 * T - 1) / (16 * T), 256)), dim3(512), 0, st, a);
+  };
+  const bool wide = !GATED && a.N > 16 * 256;
+  if (a.rows <= 16) wide ? go(int_c<1>{}, int_c<GATED ? 1 : 2>{}) : go(int_c<1>{}, int_c<1>{});
+  else wide ? go(int_c<2>{}, int_c<GATED ? 1 : 2>{}) : go(int_c<2>{}, int_c<1>{});
+}
 template <bool GATED>
 void forward(Call a, hipStream_t st) {
+  if (a.rows <= kFewRows) return forward_few<GATED>(a, st);
   const long values = (long)a.rows * a.N * a.n2;
   const Plan p = plan_of(GATED ? (a.N + 127l) / 128 * 256 : a.N, GATED ? (a.N + 63l) / 64 * 128 : a.N, a.rows, stages_of(a.K), values, true);
   a.parts = p.parts;
@@ -496,10 +714,7 @@ void forward(Call a, hipStream_t st) {
     using S = decltype(s);
     hipLaunchKernelGGL((k_forward<S, GATED>), dim3(whole_turns(p.groups)), dim3(S::T), 0, st, a);
   });
-  if (p.parts > 1) {
-    const long threads = (long)a.rows * (a.N / 8);
-    hipLaunchKernelGGL((k_finish<GATED>), dim3((unsigned)((threads + kT - 1) / kT)), dim3(kT), 0, st, a);
-  }
+  finish<GATED>(a, st);
 }
 void add_parts(const Call& a, long values, long n0, uint16_t* out0, uint16_t* out1, hipStream_t st) {
   if (a.parts == 1) return;

@@ -62,8 +62,9 @@ __device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
 }
 
-// ROWS: rows (plain) or columns (across) of the operand's tile; W waves load it.  PART: rows of an operand's part, 0: whole
-template <bool ACROSS, int ROWS, int W, int PART = 0>
+// ROWS: rows (plain) or columns (across) of the operand's tile; W waves load it.  TURN: the whole stages of k are taken in
+// turn from stage s0 on.  PART: rows of an operand's part, 0: whole
+template <bool ACROSS, int ROWS, int W, bool TURN = false, int PART = 0>
 struct Loader {
   static_assert(!ACROSS || ROWS % 128 == 0, "the pieces' permutation");
   static constexpr int N = ROWS * kBK * 2 / 1024 / W;  // loads of a wave and stage
@@ -72,15 +73,20 @@ struct Loader {
   uint32_t off[N];  // byte offset of a lane's pieces
   long step;
   int st;
-  __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
+  const char* base;  // TURN: of stage 0
+  int whole;
+  __device__ __forceinline__ void init(const Operand& o, int w, int lane, int whole_) {
     st = o.s0;
-    step = ACROSS ? o.ld * kBK * 2 : o.block - (SB - 1) * kBK * 2;
+    step = ACROSS ? o.ld * kBK * 2 : TURN ? kBK * 2 : o.block - (SB - 1) * kBK * 2;
     const uint16_t* p = o.p;
     if constexpr (PART > 0) {
       static_assert(!ACROSS && PART % (8 * N) == 0, "a wave loads rows of one part");
       if (N * w * 8 / PART & 1) p = o.other;
     }
-    at = reinterpret_cast<const char*>(p) + (ACROSS ? 0 : st / SB * o.block + st % SB * (kBK * 2));
+    base = reinterpret_cast<const char*>(p);
+    whole = whole_;
+    if constexpr (TURN) at = base + st * step;
+    else at = base + (ACROSS ? 0 : st / SB * o.block + st % SB * (kBK * 2));
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if constexpr (!ACROSS) {
@@ -112,8 +118,14 @@ struct Loader {
   __device__ __forceinline__ void issue(uint32_t dst) {
 #pragma unroll
     for (int j = 0; j < N; ++j) load_lds(at, off[j], dst + j * 1024);
-    if constexpr (ACROSS) at += step;
-    else at += (++st % SB == 0) ? step : kBK * 2;
+    if constexpr (TURN) {
+      at += step;
+      if (++st == whole) at = base;
+    } else if constexpr (ACROSS) {
+      at += step;
+    } else {
+      at += (++st % SB == 0) ? step : kBK * 2;
+    }
   }
 };
 
@@ -172,33 +184,36 @@ __device__ __forceinline__ void clear(Acc<S>& acc) {
 // acc = A B^T over k in [0, K); K is rounded up to whole stages, of which operands past kend give zeros times
 // something finite.  start(acc) runs while the first stages are on their way.
 // MASK: acc += A B^T over k in [0, K) alone, kend of both operands being K; what lies past it takes no part (a stage that K
-// ends in comes last, by itself, with both operands' k past the end set to zero).
+// ends in comes last, by itself, with both operands' k past the end set to zero).  The whole stages are taken in turn from s0 on,
+// the same for both operands.
 template <typename S, bool XA, bool XB, bool MASK = false, int PART = 0, typename F>
 __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int K, char* lds, Acc<S>& acc, F&& start) {
-  using LA = Loader<XA, S::TM, S::W, PART>;
-  using LB = Loader<XB, S::TN, S::W>;
+  using LA = Loader<XA, S::TM, S::W, MASK, PART>;
+  using LB = Loader<XB, S::TN, S::W, MASK>;
   constexpr int MT = S::MT, NT = S::NT, Q = MT * NT, R = MT + NT, SB = S::kStageBytes;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   LA la;
   LB lb;
-  la.init(oa, w, lane);
-  lb.init(ob, w, lane);
+  const int nk = (K + kBK - 1) / kBK, whole = MASK ? K / kBK : nk;
+  la.init(oa, w, lane, whole);
+  lb.init(ob, w, lane, whole);
   Reader<XA, S::TM> ra;
   Reader<XB, S::TN> rb;
   ra.init(w % S::WM * MT, lane);
   rb.init(w / S::WM * NT, lane);
   if constexpr (!MASK) clear<S>(acc);
-  const int nk = (K + kBK - 1) / kBK, whole = MASK ? K / kBK : nk;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDSP char*)lds);
   const uint32_t da = lds0 + w * LA::N * 1024, db = lds0 + S::kABytes + w * LB::N * 1024;
   int next = 0;  // stage to load; past the last stage nothing is
   auto issue_a = [&](uint32_t buf) {
     if (next >= nk) return;
+    if (MASK && next == whole) la.at = la.base + whole * la.step;
     if (oa.kend - next * kBK < kBK) la.cut(oa, w, lane, oa.kend - next * kBK);
     la.issue(da + buf);
   };
   auto issue_b = [&](uint32_t buf) {
     if (next < nk) {
+      if (MASK && next == whole) lb.at = lb.base + whole * lb.step;
       if (ob.kend - next * kBK < kBK) lb.cut(ob, w, lane, ob.kend - next * kBK);
       lb.issue(db + buf);
     }

@@ -266,7 +266,8 @@ def products_check(d, ed, x, w, dx, dw, what):
 def linear_check(x, w, bias, res, act, dy, y, z, dx, dw, dbias):
     K = x.shape[1]
     zw = x.double() @ w.double().t() + (0 if bias is None else bias.double())
-    ez = 2 * K * U * (x.double().abs() @ w.double().abs().t()) + 2 * U * zw.abs() + (0 if bias is None else U * bias.double().abs())
+    # (the bias is the first of the K + 1 terms)
+    ez = 2 * (K + 1) * U * (x.double().abs() @ w.double().abs().t() + (0 if bias is None else bias.double().abs()))
     if z is not None:
         within(z, zw, 1.01 * (ez + HALF[BF] * zw.abs()) + LEAST, "z")
     a, _ = act64(act, zw)
