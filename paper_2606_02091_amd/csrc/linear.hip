@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "dflare.h"
 #include "product.h"
@@ -107,8 +108,10 @@ struct Call {
   const uint16_t* d[2];                   // [rows, N] gradients of z, or of g and u
   uint16_t *y, *z[2];                     // [rows, N] outputs: y or h; z, or g and u, or null
   uint16_t *dx, *dw[2];                   // [rows, K], [N, K]
-  float* part;                            // sums of a product's parts
-  int rows, N, K, n2, act, parts;
+  float* part;                            // sums of a product's parts: y's, or dx's
+  float* part_w;                          // and dW's
+  int rows, N, K, n2, act, parts, parts_w;
+  int groups_x;                           // work-groups of dx in the launch of both gradients
 };
 
 // a part's stages of k: [first, past the last) of `stages`
@@ -506,13 +509,12 @@ __device__ __forceinline__ void put_sums(char* lds, const Acc<S>& acc, float* pa
   take<S, S::TM>(lds, [&](int n, int p) { return n < nv && p * 8 < mv ? out + n * ld + p * 8 : nullptr; });
 }
 
-// ---- dx = d W over the rows of W (of both matrices, one after the other) ----
+// dx = d W over the rows of W (of both matrices, one after the other)
 template <typename S>
-__global__ __launch_bounds__(S::T, 2) void k_dx(Call a) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+__device__ __forceinline__ void tile_of_dx(const Call& a, int id, char* lds) {
   const int nb = (a.rows + S::TN - 1) / S::TN, na = (a.K + S::TM - 1) / S::TM;
   int unit, tb;
-  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
+  if (!tile_of(id, na * a.parts, nb, unit, tb)) return;
   const int ks = unit / na, m0 = unit % na * S::TM, r0 = tb * S::TN, one = (a.N + kBK - 1) / kBK;
   int s0, s1;
   part_of(a.n2 * one, a.parts, ks, s0, s1);
@@ -531,16 +533,15 @@ __global__ __launch_bounds__(S::T, 2) void k_dx(Call a) {
   put_sums<S>(lds, acc, a.parts > 1 ? a.part + (long)ks * a.rows * a.K + at : nullptr, a.dx + at, a.K, nv, mv);
 }
 
-// ---- dW = d^T x over the rows, for each matrix ----
+// dW = d^T x over the rows, for each matrix
 template <typename S>
-__global__ __launch_bounds__(S::T, 2) void k_dw(Call a) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+__device__ __forceinline__ void tile_of_dw(const Call& a, int id, char* lds) {
   const int one = (a.N + S::TN - 1) / S::TN, nb = a.n2 * one, na = (a.K + S::TM - 1) / S::TM;
   int unit, tb;
-  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
+  if (!tile_of(id, na * a.parts_w, nb, unit, tb)) return;
   const int ks = unit / na, m0 = unit % na * S::TM, p = tb / one, n0 = tb % one * S::TN;
   int s0, s1;
-  part_of((a.rows + kBK - 1) / kBK, a.parts, ks, s0, s1);
+  part_of((a.rows + kBK - 1) / kBK, a.parts_w, ks, s0, s1);
   const int k0 = s0 * kBK, kn = min(s1 * kBK, a.rows) - k0;
   const int nv = min(a.N - n0, S::TN), mv = min(a.K - m0, S::TM);
   Acc<S> acc;
@@ -549,13 +550,29 @@ __global__ __launch_bounds__(S::T, 2) void k_dw(Call a) {
   ox.s0 = od.s0 = first_stage(kn);
   product<S, true, true, true>(ox, od, kn, lds, acc, [](Acc<S>&) {});
   const long at = (long)n0 * a.K + m0;
-  put_sums<S>(lds, acc, a.parts > 1 ? a.part + ((long)ks * a.n2 + p) * a.N * a.K + at : nullptr, a.dw[p] + at, a.K, nv, mv);
+  put_sums<S>(lds, acc, a.parts_w > 1 ? a.part_w + ((long)ks * a.n2 + p) * a.N * a.K + at : nullptr, a.dw[p] + at, a.K, nv, mv);
 }
 
-// the parts of `values` fp32 sums, added in order; the first `n0` of them go to out0, the others to out1
-__global__ __launch_bounds__(kT) void k_add_parts(const float* part, int parts, long values, long n0, uint16_t* out0, uint16_t* out1) {
-  const long i = (blockIdx.x * (long)kT + threadIdx.x) * 8;
-  if (i >= values) return;
+// ---- both gradients in one launch, dx's tiles first: their sums are the longer ones where rows are few, and the tiles of dW fill
+// the CUs that they leave ----
+template <typename SX, typename SW>
+__global__ __launch_bounds__(SX::T, 2) void k_gradients(Call a) {
+  static_assert(SX::T == SW::T);
+  constexpr int LDS = 2 * (SX::kStageBytes > SW::kStageBytes ? SX::kStageBytes : SW::kStageBytes);
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];
+  if ((int)blockIdx.x < a.groups_x) tile_of_dx<SX>(a, blockIdx.x, lds);
+  else tile_of_dw<SW>(a, blockIdx.x - a.groups_x, lds);
+}
+
+// What is left of the gradients' launch: sums of parts, added in order and rounded, of dx (first `values` of `parts`) and of dW (n0
+// values of each matrix); and the bias' gradient from the chunks' sums.  The work-groups of each come one after another.
+struct Rest {
+  const float *part, *part_w, *sums;
+  uint16_t *dx, *dw[2], *dbias;
+  long values, values_w, n0;
+  int parts, parts_w, chunks, N, groups, groups_w;
+};
+__device__ __forceinline__ u32x4 add_parts(const float* part, int parts, long values, long i) {
   float s[8] = {};
 #pragma unroll 4
   for (int k = 0; k < parts; ++k) {
@@ -567,7 +584,34 @@ __global__ __launch_bounds__(kT) void k_add_parts(const float* part, int parts, 
       s[4 + e] += y[e];
     }
   }
-  *reinterpret_cast<u32x4*>(i < n0 ? out0 + i : out1 + (i - n0)) = pack(s);
+  return pack(s);
+}
+__global__ __launch_bounds__(kT) void k_rest(Rest a) {
+  int id = blockIdx.x;
+  if (id < a.groups) {
+    const long i = (id * (long)kT + threadIdx.x) * 8;
+    if (i < a.values) *reinterpret_cast<u32x4*>(a.dx + i) = add_parts(a.part, a.parts, a.values, i);
+    return;
+  }
+  if ((id -= a.groups) < a.groups_w) {
+    const long i = (id * (long)kT + threadIdx.x) * 8;
+    if (i < a.values_w) *reinterpret_cast<u32x4*>(i < a.n0 ? a.dw[0] + i : a.dw[1] + (i - a.n0)) = add_parts(a.part_w, a.parts_w, a.values_w, i);
+    return;
+  }
+  id -= a.groups_w;
+  __shared__ float s[16][17];  // 16 groups of chunks, then these in order
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = id * 16 + l;
+  float v = 0.f;
+  if (c < a.N) {
+#pragma unroll 8
+    for (int k = g; k < a.chunks; k += 16) v += a.sums[(long)k * a.N + c];
+  }
+  s[g][l] = v;
+  __syncthreads();
+  if (g == 0 && c < a.N) {
+    for (int k = 1; k < 16; ++k) v += s[k][l];
+    a.dbias[c] = (uint16_t)pack2(v, 0.f);
+  }
 }
 
 // ---- gradients of the pre-activations.  A thread takes 8 columns of the rows of a chunk; with a bias it adds them up. ----
@@ -617,23 +661,6 @@ __global__ __launch_bounds__(kT) void k_pre(Pre a) {
   to[1] = f32x4{s[4], s[5], s[6], s[7]};
 }
 
-// the bias' gradient from the chunks' sums (16 groups of them, then these in order)
-__global__ __launch_bounds__(kT) void k_dbias(const float* sums, int chunks, int N, uint16_t* out) {
-  __shared__ float s[16][17];
-  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
-  float v = 0.f;
-  if (c < N) {
-#pragma unroll 8
-    for (int k = g; k < chunks; k += 16) v += sums[(long)k * N + c];
-  }
-  s[g][l] = v;
-  __syncthreads();
-  if (g == 0 && c < N) {
-    for (int k = 1; k < 16; ++k) v += s[k][l];
-    out[c] = (uint16_t)pack2(v, 0.f);
-  }
-}
-
 // ---- host side ----
 constexpr int kMostParts = 128;         // of a product
 constexpr long kPartValues = 1l << 25;  // and most sums of these together
@@ -643,27 +670,62 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 // bytes of the parts of a product of `values` sums, at most (grows with them)
 size_t part_bytes(long values) { return up((size_t)std::min(kPartValues, kMostParts * values) * 4); }
 
-// How a product of m x n over `stages` of k is cut: the tile, and the parts of k.
-struct Plan {
-  int tile, parts;  // 0 large, 1 small, 2 for few rows
-  long groups;
+long over(long a, long b) { return (a + b - 1) / b; }
+// A product of `tiles` over `stages` of k, cut into `parts` of k, and its measured costs in us.  A stage takes 1.55 on the large tile (256
+// work-groups at once); on the smaller ones 0.6 where a work-group has its CU for itself, 0.95 where two share it; a work-group
+// begins and ends in about 5; the parts' sums are written and read at 5 TB/s, by a launch more (3).
+struct Work {
+  long tiles, values;
+  int stages;
+  long groups(int k) const { return tiles * k; }
+  bool can(int k) const { return k == 1 || (stages >= 4 * k && values * k <= kPartValues); }
+  double unit(int k, double stage) const { return tiles ? (double)over(stages, k) * stage + 5.0 : 0.0; }  // of a work-group
+  double sums(int k) const { return k > 1 ? (double)values * k * 8 / 5e6 + 3.0 : 0.0; }
 };
-Plan plan_of(long m_large, long m_small, long n, int stages, long values, bool few) {
-  auto over = [](long a, long b) { return (a + b - 1) / b; };
-  Plan best{};
+double stage_of(int tile, long groups) {
+  return tile == 0 ? 1.55 : 0.6 + 0.35 * (double)std::min(std::max(groups - 256, 0l), 256l) / 256.0;
+}
+// the whole launch: of one product in rounds of work-groups; of two, whose work-groups fill each other's gaps, about half a
+// shorter one more than their sum
+double cost_of(int tile, const Work& x, int kx, const Work& w, int kw) {
+  const long slots = tile == 0 ? 256 : 512, groups = x.groups(kx) + w.groups(kw);
+  const double stage = stage_of(tile, groups), ux = x.unit(kx, stage), uw = w.unit(kw, stage), sums = x.sums(kx) + w.sums(kw);
+  if (!x.tiles || !w.tiles) return (double)over(groups, slots) * (ux + uw) + sums;
+  const double all = ((double)x.groups(kx) * ux + (double)w.groups(kw) * uw) / (double)std::min(groups, slots);
+  return std::max(all, std::max(ux, uw)) + 0.5 * std::min(ux, uw) + sums;
+}
+struct Plan {
+  int tile, kx, kw;  // 0: the large tile, 1: the small one; parts
+};
+// f(tile) gives the two products' work on a tile (the second may be empty).  The parts of one are chosen beside those of the other, in
+// turn, from numbers that come near to any.
+template <typename F>
+Plan plan_of(F&& f) {
+  static constexpr int numbers[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64, 96, kMostParts};
+  Plan best{0, 1, 1};
   double least = 1e300;
-  for (int t = 0; t < 3; ++t) {
-    if ((t == 2) != (few && n <= Few::TN)) continue;
-    const long tn = t == 0 ? Large::TN : t == 1 ? Small::TN : Few::TN;
-    const long tiles = (t == 0 ? over(m_large, Large::TM) : over(m_small, Small::TM)) * over(n, tn), slots = 256l * (t + 1);
-    const double stage = t == 0 ? 1.8 : 1.15;
-    for (int k = 1; k <= kMostParts; ++k) {
-      if (k > 1 && (tiles * k > 2 * slots || stages < 4 * k || values * k > kPartValues)) break;
-      const double cost = over(tiles * k, slots) * (over(stages, k) + 8) * stage + (k > 1 ? 4.0 + (double)values * k * 4 / 4e6 : 0.0);
-      if (cost < least) {
-        least = cost;
-        best = Plan{t, k, tiles * k};
+  for (int t = 0; t < 2; ++t) {
+    const std::pair<Work, Work> p = f(t);
+    int kx = 1, kw = 1;
+    double low = cost_of(t, p.first, 1, p.second, 1);
+    auto search = [&](const Work& own, int& k) {
+      for (int n : numbers) {
+        if (!own.can(n) || (n > 1 && own.groups(n) > 2048)) break;
+        const int was = k;
+        k = n;
+        const double c = cost_of(t, p.first, kx, p.second, kw);
+        if (c < low) low = c;
+        else k = was;
       }
+    };
+    search(p.first, kx);
+    if (p.second.tiles) {
+      search(p.second, kw);
+      search(p.first, kx);
+    }
+    if (low < least) {
+      least = low;
+      best = Plan{t, kx, kw};
     }
   }
   return best;
@@ -677,12 +739,6 @@ int check(int rows, int N, int K, int act) {
   return tiles >= (1l << 23) ? DFLARE_ERR_UNSUPPORTED : DFLARE_OK;
 }
 
-template <typename F>
-void by_tile(int tile, F&& f) {
-  if (tile == 0) f(Large{});
-  else if (tile == 1) f(Small{});
-  else f(Few{});
-}
 unsigned whole_turns(long groups) { return (unsigned)((groups + 7) / 8 * 8); }  // of the XCDs
 int stages_of(long k) { return (int)((k + kBK - 1) / kBK); }
 
@@ -707,44 +763,71 @@ void forward_few(const Call& a, hipStream_t st) {
 template <bool GATED>
 void forward(Call a, hipStream_t st) {
   if (a.rows <= kFewRows) return forward_few<GATED>(a, st);
-  const long values = (long)a.rows * a.N * a.n2;
-  const Plan p = plan_of(GATED ? (a.N + 127l) / 128 * 256 : a.N, GATED ? (a.N + 63l) / 64 * 128 : a.N, a.rows, stages_of(a.K), values, true);
-  a.parts = p.parts;
-  by_tile(p.tile, [&](auto s) {
+  auto go = [&](auto s, long tiles) {
     using S = decltype(s);
-    hipLaunchKernelGGL((k_forward<S, GATED>), dim3(whole_turns(p.groups)), dim3(S::T), 0, st, a);
-  });
-  finish<GATED>(a, st);
-}
-void add_parts(const Call& a, long values, long n0, uint16_t* out0, uint16_t* out1, hipStream_t st) {
-  if (a.parts == 1) return;
-  hipLaunchKernelGGL(k_add_parts, dim3((unsigned)((values / 8 + kT - 1) / kT)), dim3(kT), 0, st, a.part, a.parts, values, n0, out0, out1);
-}
-void gradient_of_x(Call a, hipStream_t st) {
-  const long values = (long)a.rows * a.K;
-  const Plan p = plan_of(a.K, a.K, a.rows, a.n2 * stages_of(a.N), values, true);
-  a.parts = p.parts;
-  by_tile(p.tile, [&](auto s) {
-    using S = decltype(s);
-    hipLaunchKernelGGL((k_dx<S>), dim3(whole_turns(p.groups)), dim3(S::T), 0, st, a);
-  });
-  add_parts(a, values, values, a.dx, nullptr, st);
-}
-void gradient_of_w(Call a, hipStream_t st) {
-  const long one = (long)a.N * a.K;
-  const Plan p = plan_of(a.K, a.K, (long)a.n2 * a.N, stages_of(a.rows), a.n2 * one, false);
-  a.parts = p.parts;
-  auto go = [&](auto s) {  // (operands across have no tiles of 64)
-    using S = decltype(s);
-    const long tiles = (a.K + S::TM - 1l) / S::TM * ((a.N + S::TN - 1l) / S::TN) * a.n2;
-    hipLaunchKernelGGL((k_dw<S>), dim3(whole_turns(tiles * a.parts)), dim3(S::T), 0, st, a);
+    hipLaunchKernelGGL((k_forward<S, GATED>), dim3(whole_turns(tiles * a.parts)), dim3(S::T), 0, st, a);
+    finish<GATED>(a, st);
   };
-  if (p.tile == 0) go(Large{});
-  else go(Small{});
-  add_parts(a, a.n2 * one, one, a.dw[0], a.dw[1], st);
+  auto tiles = [&](auto s) { return over(a.N, s.TM / a.n2) * over(a.rows, s.TN); };
+  auto work = [&](long tiles) { return std::make_pair(Work{tiles, (long)a.rows * a.N * a.n2, stages_of(a.K)}, Work{0, 0, 0}); };
+  // up to 64 rows the small tile's other half would be empty
+  const bool few = a.rows <= Few::TN;
+  const Plan p = plan_of([&](int t) { return work(few ? tiles(Few{}) : t == 0 ? tiles(Large{}) : tiles(Small{})); });
+  a.parts = p.kx;
+  if (few) go(Few{}, tiles(Few{}));
+  else if (p.tile == 0) go(Large{}, tiles(Large{}));
+  else go(Small{}, tiles(Small{}));
+}
+// dx and dW, each where it is wanted, and the bias' gradient from `chunks` sums
+void gradients(Call a, const float* sums, int chunks, uint16_t* dbias, hipStream_t st) {
+  const bool few = a.rows <= Few::TN;
+  const long one = (long)a.N * a.K;
+  auto tiles_x = [&](auto s) { return a.dx ? over(a.K, s.TM) * over(a.rows, s.TN) : 0l; };
+  auto tiles_w = [&](auto s) { return a.dw[0] ? over(a.K, s.TM) * over(a.N, s.TN) * a.n2 : 0l; };
+  auto work = [&](long tx, long tw) {
+    return std::make_pair(Work{tx, (long)a.rows * a.K, a.n2 * stages_of(a.N)}, Work{tw, a.n2 * one, stages_of(a.rows)});
+  };
+  a.parts = a.parts_w = 1;
+  if (a.dx || a.dw[0]) {
+    const Plan p = plan_of([&](int t) {
+      return few ? work(tiles_x(Few{}), tiles_w(Small{})) : t == 0 ? work(tiles_x(Large{}), tiles_w(Large{})) : work(tiles_x(Small{}), tiles_w(Small{}));
+    });
+    auto go = [&](auto sx, auto sw) {
+      using SX = decltype(sx);
+      using SW = decltype(sw);
+      a.parts = a.dx ? p.kx : 1;
+      a.parts_w = a.dw[0] ? p.kw : 1;
+      a.groups_x = (int)whole_turns(tiles_x(sx) * a.parts);
+      hipLaunchKernelGGL((k_gradients<SX, SW>), dim3(a.groups_x + whole_turns(tiles_w(sw) * a.parts_w)), dim3(SX::T), 0, st, a);
+    };
+    if (few) go(Few{}, Small{});
+    else if (p.tile == 0) go(Large{}, Large{});
+    else go(Small{}, Small{});
+  }
+  Rest r{};
+  r.part = a.part;
+  r.part_w = a.part_w;
+  r.sums = sums;
+  r.dx = a.dx;
+  r.dw[0] = a.dw[0];
+  r.dw[1] = a.dw[1];
+  r.dbias = dbias;
+  r.values = (long)a.rows * a.K;
+  r.values_w = a.n2 * one;
+  r.n0 = one;
+  r.parts = a.parts;
+  r.parts_w = a.parts_w;
+  r.chunks = chunks;
+  r.N = a.N;
+  r.groups = a.parts > 1 ? (int)over(r.values / 8, kT) : 0;
+  r.groups_w = a.parts_w > 1 ? (int)over(r.values_w / 8, kT) : 0;
+  const long groups = r.groups + (long)r.groups_w + (dbias ? over(a.N, 16) : 0);
+  if (groups) hipLaunchKernelGGL(k_rest, dim3((unsigned)groups), dim3(kT), 0, st, r);
 }
 // work-groups over 2,048 columns each, and chunks of rows
-int pre_chunks(int rows, int N) { return (int)std::max(1l, std::min<long>(rows, kPreGroups / ((N / 8 + kT - 1) / kT))); }
+int pre_chunks(int rows, int N, bool sums) {
+  return (int)std::max(1l, std::min<long>(sums ? over(rows, 4) : rows, kPreGroups / over(N / 8, kT)));
+}
 template <bool GATED>
 void pre_gradients(const Pre& a, hipStream_t st) {
   const long groups = (long)(a.N / 8 + kT - 1) / kT * a.chunks;
@@ -758,9 +841,9 @@ bool off16(std::initializer_list<const void*> ps) {
 }
 
 struct BwdLayout {
-  size_t d, sums, part, total;
+  size_t d, sums, part, part_w, total;
 };
-// d: n_d gradients of [rows, N]; sums of a bias' gradient; the parts of the larger product
+// d: n_d gradients of [rows, N]; sums of a bias' gradient; the products' parts
 BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx, bool dw) {
   BwdLayout L{};
   size_t o = 0;
@@ -769,7 +852,9 @@ BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx
   L.sums = o;
   if (sums) o += up((size_t)std::min(std::max(rows, 1), kPreGroups) * N * 4);
   L.part = o;
-  o += std::max(dx ? part_bytes((long)rows * K) : 0, dw ? part_bytes((long)n2 * N * K) : 0);
+  if (dx) o += part_bytes((long)rows * K);
+  L.part_w = o;
+  if (dw) o += part_bytes((long)n2 * N * K);
   L.total = std::max<size_t>(o, 256);
   return L;
 }
@@ -855,11 +940,13 @@ int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* 
   a.dx = (uint16_t*)dx;
   a.dw[0] = (uint16_t*)dw;
   a.part = (float*)(ws + L.part);
+  a.part_w = (float*)(ws + L.part_w);
   a.rows = rows;
   a.N = N;
   a.K = K;
   a.n2 = 1;
   a.d[0] = named ? (const uint16_t*)(ws + L.d) : (const uint16_t*)dy;
+  const int chunks = pre_chunks(rows, N, dbias != nullptr);
   if (dbias || (named && (dx || dw))) {
     Pre p{};
     p.dy = (const uint16_t*)dy;
@@ -869,12 +956,10 @@ int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* 
     p.rows = rows;
     p.N = N;
     p.act = act;
-    p.chunks = pre_chunks(rows, N);
+    p.chunks = chunks;
     pre_gradients<false>(p, st);
-    if (dbias) hipLaunchKernelGGL(k_dbias, dim3((N + 15) / 16), dim3(kT), 0, st, p.sums, p.chunks, N, (uint16_t*)dbias);
   }
-  if (dx) gradient_of_x(a, st);
-  if (dw) gradient_of_w(a, st);
+  gradients(a, (const float*)(ws + L.sums), chunks, (uint16_t*)dbias, st);
   return launched();
 }
 
@@ -944,6 +1029,7 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
   a.dw[0] = (uint16_t*)dw_gate;
   a.dw[1] = (uint16_t*)dw_up;
   a.part = (float*)(ws + L.part);
+  a.part_w = (float*)(ws + L.part_w);
   a.rows = rows;
   a.N = F;
   a.K = H;
@@ -957,12 +1043,11 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
   p.rows = rows;
   p.N = F;
   p.act = act;
-  p.chunks = pre_chunks(rows, F);
+  p.chunks = pre_chunks(rows, F, false);
   a.d[0] = p.d[0];
   a.d[1] = p.d[1];
   if (dx || dw_gate) pre_gradients<true>(p, st);
-  if (dx) gradient_of_x(a, st);
-  if (dw_gate) gradient_of_w(a, st);
+  gradients(a, nullptr, 0, nullptr, st);
   return launched();
 }
 
