@@ -5,8 +5,11 @@
 // Clipping takes place here, by the gradients' sum of squares, so that no pass of its own reads and writes them.
 // States in 8 bits: m and sqrt(v) as e4m3 numbers times a scale for each 256 values of a tensor, its largest over 448.  The
 // root, because e4m3 then covers 2^36 of v instead of 2^18; what is above zero stays above zero, so that no step divides a
-// remembered m by eps alone.  Bound by memory: 28 bytes a value (bf16 with an fp32 master and fp32 states), 10 (bf16, 8 bits).
+// remembered m by eps alone.
+// Bound by memory: 28 bytes a value (bf16 with an fp32 master and fp32 states): 402 M values 2,290 us, 4.9 TB/s, a copy's rate on this
+// card; 10 in 8 bits without a master: 912 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -47,22 +50,29 @@ __host__ __device__ inline void set_step(Hyper& h, double lr, double weight_deca
   h.root = (float)(1.0 / sqrt(1.0 - exp(t * ln2)));
 }
 
-// The tensors of a launch, as many as its arguments (4 KB) hold beside the options
+// The tensors of a launch, as many as its arguments (4 KB) hold beside the options.  A tensor's record is read as a whole, and the
+// first chunks by a lane each: the arguments come from far, and every access that waits for another one costs a microsecond
+// (301 tensors, 8 bits, six launches: 7.6 us each; by a binary search over arrays of fields 9.1).
+template <bool MASTER, bool BYTE>
+struct Record {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float* w[MASTER ? 1 : 0];
+  float* scale[BYTE ? 2 : 0];
+  uint32_t n;    // values, the low 32 bits
+  uint32_t tag;  // 1: fp32 parameter; 2: fp32 gradient; 4: a master; the high bits of n above
+  __device__ __forceinline__ long size() const { return (long)n | (long)(tag >> 3) << 32; }
+};
 template <bool MASTER, bool BYTE>
 struct Tab {
-  static constexpr int N = 3850 / ((4 + MASTER + 2 * BYTE) * 8 + 9);
-  void* p[N];
-  const void* g[N];
-  void *m[N], *v[N];
-  float* w[MASTER ? N : 1];
-  float *ms[BYTE ? N : 1], *vs[BYTE ? N : 1];
-  uint32_t n[N];     // values, the low 32 bits
+  using R = Record<MASTER, BYTE>;
+  static constexpr int N = 3880 / (sizeof(R) + 4);
+  R r[N];
   int first[N + 1];  // chunks before the tensor
-  uint8_t tag[N];    // 1: fp32 parameter; 2: fp32 gradient; 4: a master; the high bits of n above
   int count;
-  __device__ __forceinline__ long size(int i) const { return (long)n[i] | (long)(tag[i] >> 3) << 32; }
 };
-static_assert(sizeof(Tab<true, true>) + sizeof(Options) <= 4048 && sizeof(Tab<false, false>) + sizeof(Options) <= 4048, "kernel arguments");
+static_assert(sizeof(Tab<true, true>) + sizeof(Options) <= 4088 && sizeof(Tab<false, false>) + sizeof(Options) <= 4088, "kernel arguments");
 
 // 8 values at any element
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
@@ -140,7 +150,9 @@ __device__ __forceinline__ void store_some(T* p, int left, const float (&x)[8]) 
   }
 }
 
-// x over the scale of its 256 values, which 32 lanes hold, and the scale
+// x over the scale of its 256 values, which 32 lanes hold, and the scale.  ROOT: what is above zero stays at least the smallest number
+// above zero
+template <bool ROOT>
 __device__ __forceinline__ float to_scale(float (&x)[8]) {
   float most = 0.f;
 #pragma unroll
@@ -149,21 +161,25 @@ __device__ __forceinline__ float to_scale(float (&x)[8]) {
   for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
   const float scale = fmaxf(most / kMost, kLeastScale), inv = 1.f / scale;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  for (int e = 0; e < 8; ++e) {
+    const float q = x[e] * inv;
+    x[e] = ROOT && x[e] > 0.f && q < kLeast ? kLeast : q;
+  }
   return scale;
 }
 
 template <bool MASTER, bool BYTE, typename P, typename G>
-__device__ __forceinline__ void chunk(const Tab<MASTER, BYTE>& tab, int i, int c, const Hyper& h, Factor f) {
+__device__ __forceinline__ void chunk(const Record<MASTER, BYTE>& rec, int c, const Hyper& h, Factor f) {
   using S = std::conditional_t<BYTE, e4m3_t, float>;
   const long at = (long)c * kChunk + threadIdx.x * kValues;
-  const int left = (int)max(min(tab.size(i) - at, 8l), 0l);
+  const int left = (int)max(min(rec.size() - at, 8l), 0l);
   if (!BYTE && left == 0) return;
   float p[8], g[8], m[8], v[8];
-  P* param = (P*)tab.p[i] + at;
-  S *pm = (S*)tab.m[i] + at, *pv = (S*)tab.v[i] + at;
-  float* master = MASTER && (tab.tag[i] & 4) ? tab.w[i] + at : nullptr;
-  load_some((const G*)tab.g[i] + at, left, g);
+  P* param = (P*)rec.p + at;
+  S *pm = (S*)rec.m + at, *pv = (S*)rec.v + at;
+  float* master = nullptr;
+  if constexpr (MASTER) master = rec.tag & 4 ? rec.w[0] + at : nullptr;
+  load_some((const G*)rec.g + at, left, g);
   load_some(pm, left, m);
   load_some(pv, left, v);
   if (master) load_some((const float*)master, left, p);
@@ -171,8 +187,8 @@ __device__ __forceinline__ void chunk(const Tab<MASTER, BYTE>& tab, int i, int c
   float *sm = nullptr, *sv = nullptr;
   if constexpr (BYTE) {
     if (left > 0) {
-      sm = tab.ms[i] + at / kScaled;
-      sv = tab.vs[i] + at / kScaled;
+      sm = rec.scale[0] + at / kScaled;
+      sv = rec.scale[1] + at / kScaled;
       const float a = *sm, b = *sv;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -182,23 +198,18 @@ __device__ __forceinline__ void chunk(const Tab<MASTER, BYTE>& tab, int i, int c
       }
     }
   }
+  // (root and reciprocal to a unit in the last place: exact ones take two thirds of all instructions)
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = f.of(g[e]);
     m[e] = fmaf(h.c1, x, h.b1 * m[e]);
     v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
-    const float r = sqrtf(v[e]);
-    p[e] = fmaf(-h.alpha, m[e] / fmaf(r, h.root, h.eps), p[e] * h.decay);
+    const float r = __builtin_amdgcn_sqrtf(v[e]);
+    p[e] = fmaf(-h.alpha, m[e] * __builtin_amdgcn_rcpf(fmaf(r, h.root, h.eps)), p[e] * h.decay);
     if constexpr (BYTE) v[e] = r;
   }
   if constexpr (BYTE) {
-    float r[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = v[e];
-    const float a = to_scale(m), b = to_scale(v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (r[e] > 0.f) v[e] = v[e] < kLeast ? kLeast : v[e];
+    const float a = to_scale<false>(m), b = to_scale<true>(v);
     if (left > 0 && threadIdx.x % 32 == 0) {
       *sm = a;
       *sv = b;
@@ -212,34 +223,40 @@ __device__ __forceinline__ void chunk(const Tab<MASTER, BYTE>& tab, int i, int c
 
 template <bool MASTER, bool BYTE>
 __global__ __launch_bounds__(kT) void k_adamw(Tab<MASTER, BYTE> tab, Options o) {
+  const int total = tab.first[tab.count];
+  int c = (int)((long)total * blockIdx.x / gridDim.x);
+  const int end = (int)((long)total * (blockIdx.x + 1) / gridDim.x);
+  if (c >= end) return;
+  const double sumsq = o.sumsq ? o.sumsq[0] : 0.0;  // (on its way beside the table)
+  // the last tensor whose first chunk is not after c
+  int at = -1;
+  for (int k = 0; k < tab.count; k += 64) {
+    const int i = k + (int)(threadIdx.x & 63);
+    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < tab.count && tab.first[min(i, tab.count)] <= c));
+  }
   Hyper h = o.h;
   if (o.lr_device || o.step_device)
     set_step(h, o.lr_device ? *o.lr_device : o.lr, o.weight_decay, o.ln1, o.ln2, (double)(o.step_device ? *o.step_device : o.step));
   Factor f{1.f, 0};
   if (o.sumsq) {
-    const double norm = sqrt(o.sumsq[0]);
+    const double norm = sqrt(sumsq);
     if (!(norm < (double)INFINITY)) return;  // not finite: the step is left out
     if (norm > (double)o.max_norm) f.m = (float)frexp((double)o.max_norm / norm, &f.e);
   }
-  const long total = tab.first[tab.count];
-  int c = (int)(total * blockIdx.x / gridDim.x);
-  const int end = (int)(total * (blockIdx.x + 1) / gridDim.x);
-  if (c >= end) return;
-  int lo = 0, hi = tab.count - 1;  // the last tensor whose first chunk is not after c
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (tab.first[mid] <= c) lo = mid;
-    else hi = mid - 1;
-  }
-  for (; c < end; ++c) {
-    while (tab.first[lo + 1] <= c) ++lo;
-    const int at = c - tab.first[lo];
-    switch (tab.tag[lo] & 3) {
-      case 0: chunk<MASTER, BYTE, bf16_t, bf16_t>(tab, lo, at, h, f); break;
-      case 1: chunk<MASTER, BYTE, float, bf16_t>(tab, lo, at, h, f); break;
-      case 2: chunk<MASTER, BYTE, bf16_t, float>(tab, lo, at, h, f); break;
-      default: chunk<MASTER, BYTE, float, float>(tab, lo, at, h, f);
+  while (true) {
+    const Record<MASTER, BYTE>& rec = tab.r[at];
+    const int first = tab.first[at], stop = min(tab.first[at + 1], end);
+    auto walk = [&](auto p, auto g) {
+      for (; c < stop; ++c) chunk<MASTER, BYTE, decltype(p), decltype(g)>(rec, c - first, h, f);
+    };
+    switch (rec.tag & 3) {
+      case 0: walk(bf16_t{}, bf16_t{}); break;
+      case 1: walk(float{}, bf16_t{}); break;
+      case 2: walk(bf16_t{}, float{}); break;
+      default: walk(float{}, float{});
     }
+    if (c >= end) return;
+    ++at;
   }
 }
 
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(kT) void k_adamw(Tab<MASTER, BYTE> tab, Options o) 
 int check(const dflare_adamw_tensor* t, int n, const dflare_adamw_options& o) {
   if (n < 0 || (n > 0 && !t)) return DFLARE_ERR_INVALID_ARG;
   if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return DFLARE_ERR_INVALID_ARG;
-  if (!((float)o.eps > 0.f) || !isfinite((float)o.eps) || !(o.weight_decay >= 0.0) || !isfinite(o.weight_decay)) return DFLARE_ERR_INVALID_ARG;
+  if (!((float)o.eps >= FLT_MIN) || !isfinite((float)o.eps) || !(o.weight_decay >= 0.0) || !isfinite(o.weight_decay)) return DFLARE_ERR_INVALID_ARG;
   if (!o.lr_device && (!(o.lr >= 0.0) || !isfinite(o.lr))) return DFLARE_ERR_INVALID_ARG;
   if (!o.step_device && o.step < 1) return DFLARE_ERR_INVALID_ARG;
   if (misplaced(o.lr_device, 8) || misplaced(o.step_device, 8) || misplaced(o.sumsq, 8)) return DFLARE_ERR_INVALID_ARG;
@@ -335,17 +352,18 @@ void launch(const dflare_adamw_tensor* t, int n, const Options& o, hipStream_t s
     const long chunks = (x.n + kChunk - 1) / kChunk;
     if (tab.count == tab.N || (tab.count && tab.first[tab.count] + chunks > (1l << 30))) flush();
     const int k = tab.count++;
-    tab.p[k] = x.param;
-    tab.g[k] = x.grad;
-    tab.m[k] = x.m;
-    tab.v[k] = x.v;
-    if (MASTER) tab.w[k] = x.master;
-    if (BYTE) {
-      tab.ms[k] = x.m_scale;
-      tab.vs[k] = x.v_scale;
+    Record<MASTER, BYTE>& r = tab.r[k];
+    r.p = x.param;
+    r.g = x.grad;
+    r.m = x.m;
+    r.v = x.v;
+    if constexpr (MASTER) r.w[0] = x.master;
+    if constexpr (BYTE) {
+      r.scale[0] = x.m_scale;
+      r.scale[1] = x.v_scale;
     }
-    tab.n[k] = (uint32_t)x.n;
-    tab.tag[k] = (uint8_t)((x.param_dtype == DFLARE_F32) | (x.grad_dtype == DFLARE_F32) << 1 | (x.master != nullptr) << 2 | (x.n >> 32) << 3);
+    r.n = (uint32_t)x.n;
+    r.tag = (uint32_t)((x.param_dtype == DFLARE_F32) | (x.grad_dtype == DFLARE_F32) << 1 | (x.master != nullptr) << 2 | (x.n >> 32) << 3);
     tab.first[k + 1] = tab.first[k] + (int)chunks;
   }
   flush();

@@ -162,7 +162,7 @@ def adam(n=1, tab=True, opt=True, values=600, pt=dfl.BF16, gt=dfl.BF16, lr=1e-3,
 @pytest.mark.parametrize("kw,code", [
     (dict(opt=False), INV), (dict(n=-1), INV), (dict(tab=False), INV), (dict(n=2), INV), (dict(values=-1), INV), (dict(values=(1 << 36) + 1), UNS),
     (dict(pt=2), INV), (dict(gt=-1), INV), (dict(pt=dfl.F32), INV), (dict(lr=-1.0), INV), (dict(lr=NAN), INV), (dict(lr=INF), INV),
-    (dict(b1=1.0), INV), (dict(b1=-0.1), INV), (dict(b2=1.0), INV), (dict(b2=NAN), INV), (dict(eps=0.0), INV), (dict(eps=1e-60), INV),
+    (dict(b1=1.0), INV), (dict(b1=-0.1), INV), (dict(b2=1.0), INV), (dict(b2=NAN), INV), (dict(eps=0.0), INV), (dict(eps=1e-60), INV), (dict(eps=1e-39), INV),
     (dict(eps=INF), INV), (dict(wd=-1.0), INV), (dict(wd=INF), INV), (dict(step=0), INV), (dict(bits=16), INV), (dict(bits=0), INV),
     (dict(sumsq=FAR[8], max_norm=-1.0), INV), (dict(sumsq=FAR[8], max_norm=NAN), INV), (dict(sumsq=FAR[8] + 4), INV), (dict(lrd=FAR[8] + 4), INV),
     (dict(stepd=FAR[8] + 4), INV), (dict(p=None), INV), (dict(g=None), INV), (dict(m=None), INV), (dict(v=None), INV), (dict(ms=None), INV),
