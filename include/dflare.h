@@ -759,9 +759,10 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
  *   param    of type param_dtype;  grad  of type grad_dtype
  *   master   fp32 parameter in whose place param (bf16) is only written, rounded; or NULL: param is the parameter
  *   m, v     the moments, zeros before the first step.  state_bits 32: fp32.  8: e4m3 (OCP, no infinities) numbers times a scale
- *            for each 256 values of a tensor, m_scale and v_scale fp32 [ceil(n / 256)], the scale being the largest of them / 448 (2^-96 at
+ *            for each 256 values of a tensor, m_scale and v_scale fp32 [ceil(n / 256)], the scale being the largest of them times 1 / 448 (2^-96 at
  *            least); v holds the root of the second moment, of which what is above zero is at least the smallest number above
- *            zero.  Numbers are rounded to nearest even; param and master are formed before that.
+ *            zero.  Every operation of the formulas for m and v, the root and the quotients are rounded to fp32 by themselves, the numbers to
+ *            nearest even; param and master are formed before that.
  *   options  HOST: lr, beta1, beta2, eps, weight_decay; step, from 1; lr_device, step_device: DEVICE double and int64, read in their
  *            place by the kernels (a captured step goes on counting), or NULL
  *   sumsq    DEVICE double [1], dflare_grad_norm's, or NULL.  g = grad max_norm / norm where norm = sqrt(*sumsq) is above max_norm,

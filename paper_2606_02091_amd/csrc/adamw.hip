@@ -29,6 +29,7 @@ constexpr int kChunk = kT * kValues;   // values of a work-group's turn
 constexpr int kScaled = 256;           // values that share a scale
 constexpr int kGroups = 2048;          // work-groups of a launch, at most
 constexpr float kMost = 448.f, kLeast = 0.001953125f;  // of e4m3: largest, smallest above zero (2^-9)
+constexpr float kPerMost = 1.f / kMost;
 constexpr float kLeastScale = 1.2621774483536189e-29f;  // 2^-96: scales and their inverses stay inside fp32
 
 struct Hyper {
@@ -159,13 +160,26 @@ __device__ __forceinline__ float to_scale(float (&x)[8]) {
   for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
-  const float scale = fmaxf(most / kMost, kLeastScale), inv = 1.f / scale;
+  const float scale = fmaxf(most * kPerMost, kLeastScale), inv = 1.f / scale;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float q = x[e] * inv;
+    float q = x[e] * inv;
+    if (scale < INFINITY) q = fmaf(fmaf(-q, scale, x[e]), inv, q);  // the quotient, correctly rounded
     x[e] = ROOT && x[e] > 0.f && q < kLeast ? kLeast : q;
   }
   return scale;
+}
+
+// The root, correctly rounded where v is above 2^-90: an estimate y of 1 / sqrt(v), then both v y and y / 2 corrected by
+// 1/2 - (y / 2) (v y), and the root by its remainder (Markstein, "IA-64 and elementary functions", 2000)
+__device__ __forceinline__ float root_of(float v) {
+  const float y = __builtin_amdgcn_rsqf(v);
+  float g = v * y, h = 0.5f * y;
+  const float e = fmaf(-h, g, 0.5f);
+  g = fmaf(g, e, g);
+  h = fmaf(h, e, h);
+  g = fmaf(fmaf(-g, g, v), h, g);
+  return v > 0.f && v < INFINITY ? g : v;  // (a NaN is itself)
 }
 
 template <bool MASTER, bool BYTE, typename P, typename G>
@@ -198,13 +212,22 @@ __device__ __forceinline__ void chunk(const Record<MASTER, BYTE>& rec, int c, co
       }
     }
   }
-  // (root and reciprocal to a unit in the last place: exact ones take two thirds of all instructions)
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = f.of(g[e]);
-    m[e] = fmaf(h.c1, x, h.b1 * m[e]);
-    v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
-    const float r = __builtin_amdgcn_sqrtf(v[e]);
+    float r;
+    if constexpr (BYTE) {
+      // Every operation rounded by itself: a number that lies next to a border between two of e4m3 falls to one side of it by the formula,
+      // not by how a compiler forms it, and a state can be reproduced from its inputs bit by bit
+#pragma clang fp contract(off)
+      m[e] = h.b1 * m[e] + h.c1 * x;
+      v[e] = h.b2 * v[e] + h.c2 * (x * x);
+      r = root_of(v[e]);
+    } else {
+      m[e] = fmaf(h.c1, x, h.b1 * m[e]);
+      v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
+      r = __builtin_amdgcn_sqrtf(v[e]);  // (to a unit in the last place, as the reciprocal)
+    }
     p[e] = fmaf(-h.alpha, m[e] * __builtin_amdgcn_rcpf(fmaf(r, h.root, h.eps)), p[e] * h.decay);
     if constexpr (BYTE) v[e] = r;
   }

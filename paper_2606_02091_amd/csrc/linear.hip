@@ -671,28 +671,40 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 size_t part_bytes(long values) { return up((size_t)std::min(kPartValues, kMostParts * values) * 4); }
 
 long over(long a, long b) { return (a + b - 1) / b; }
-// A product of `tiles` over `stages` of k, cut into `parts` of k, and its measured costs in us.  A stage takes 1.55 on the large tile (256
-// work-groups at once); on the smaller ones 0.6 where a work-group has its CU for itself, 0.95 where two share it; a work-group
-// begins and ends in about 5; the parts' sums are written and read at 5 TB/s, by a launch more (3).
+// A product of `tiles` over `stages` of k, cut into parts of k, and its costs in us, fitted to 34 products and pairs of them under some 25
+// plans each (1 to 8,192 rows, K and N from 256 to 12,288; the plan that is least by them takes 2.4% longer than the best one,
+// at the mean).  A stage takes 1.40 on the large tile (256 work-groups at once); on the smaller ones 0.50 where a work-group has its
+// CU for itself, 0.94 where two share it; a work-group begins and ends in 5 (3); parts are written and read at 6.1 TB/s and
+// added by a launch more (1.9).
 struct Work {
   long tiles, values;
   int stages;
-  long groups(int k) const { return tiles * k; }
   bool can(int k) const { return k == 1 || (stages >= 4 * k && values * k <= kPartValues); }
-  double unit(int k, double stage) const { return tiles ? (double)over(stages, k) * stage + 5.0 : 0.0; }  // of a work-group
-  double sums(int k) const { return k > 1 ? (double)values * k * 8 / 5e6 + 3.0 : 0.0; }
+  double sums(int k) const { return k > 1 ? (double)values * k * 8 / 6.1e6 + 1.9 : 0.0; }
 };
-double stage_of(int tile, long groups) {
-  return tile == 0 ? 1.55 : 0.6 + 0.35 * (double)std::min(std::max(groups - 256, 0l), 256l) / 256.0;
+// When all work-groups have ended: nx that take ux each, then nw that take uw, each where a slot is free first
+double end_of(long nx, double ux, long nw, double uw, long slots, double pole) {
+  if (!nw) return (double)over(nx, slots) * ux;
+  if (!nx) return (double)over(nw, slots) * uw;
+  const long r = nx / slots, late = nx % slots;  // `late` slots have r + 1 of the first, the others r
+  const double t0 = (double)r * ux, t1 = t0 + ux;
+  auto done = [&](double t) {
+    return (slots - late) * (long)std::max(0.0, (t - t0) / uw + 1e-9) + late * (long)std::max(0.0, (t - t1) / uw + 1e-9);
+  };
+  double end = 1e300;
+  for (const double from : {t0, t1}) {
+    double t = from + (double)std::max(0l, (long)(((double)nw + (double)late * (t1 - from) / uw - (double)(slots - late) * (from - t0) / uw) / (double)slots) - 2) * uw;
+    while (done(t) < nw) t += uw;
+    end = std::min(end, t);
+  }
+  return std::max(end, pole * (late ? t1 : t0));
 }
-// the whole launch: of one product in rounds of work-groups; of two, whose work-groups fill each other's gaps, about half a
-// shorter one more than their sum
 double cost_of(int tile, const Work& x, int kx, const Work& w, int kw) {
-  const long slots = tile == 0 ? 256 : 512, groups = x.groups(kx) + w.groups(kw);
-  const double stage = stage_of(tile, groups), ux = x.unit(kx, stage), uw = w.unit(kw, stage), sums = x.sums(kx) + w.sums(kw);
-  if (!x.tiles || !w.tiles) return (double)over(groups, slots) * (ux + uw) + sums;
-  const double all = ((double)x.groups(kx) * ux + (double)w.groups(kw) * uw) / (double)std::min(groups, slots);
-  return std::max(all, std::max(ux, uw)) + 0.5 * std::min(ux, uw) + sums;
+  const long slots = tile == 0 ? 256 : 512, nx = x.tiles * kx, nw = w.tiles * kw;
+  const double stage = tile == 0 ? 1.40 : 0.50 + 0.44 * (double)std::min(std::max(nx + nw - 256, 0l), 256l) / 256.0, ends = tile == 0 ? 5.0 : 3.0;
+  // (the last of dx's work-groups have a small tile's CU for themselves at the end)
+  return end_of(nx, (double)over(x.stages, kx) * stage + ends, nw, (double)over(w.stages, kw) * stage + ends, slots, tile == 0 ? 1.0 : 0.75) +
+         x.sums(kx) + w.sums(kw);
 }
 struct Plan {
   int tile, kx, kw;  // 0: the large tile, 1: the small one; parts
@@ -710,7 +722,7 @@ Plan plan_of(F&& f) {
     double low = cost_of(t, p.first, 1, p.second, 1);
     auto search = [&](const Work& own, int& k) {
       for (int n : numbers) {
-        if (!own.can(n) || (n > 1 && own.groups(n) > 2048)) break;
+        if (!own.can(n) || (n > 1 && own.tiles * n > 2048)) break;
         const int was = k;
         k = n;
         const double c = cost_of(t, p.first, kx, p.second, kw);

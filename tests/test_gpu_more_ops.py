@@ -597,6 +597,31 @@ def test_adamw(bits, masters, clip):
         adamw_check(before, state, grads, step, 1e-2, 0.9, 0.95, 1e-8, 0.1, factor, bits)
 
 
+def test_adamw_8_bit_states_are_the_formula_s_bit_by_bit():
+    """Each operation in fp32 by itself, as tensors' operations are: the same numbers and scales, also after several steps."""
+    n = 1 << 20
+    ps, m, v, ms, vs, _ = state_of([n], [F32], 8, False, seed=3)
+    M, V, MS, VS = (t[0].clone() for t in (m, v, ms, vs))
+    b1, b2 = 0.9, 0.999
+    for step in range(1, 5):
+        g = randn((n,), BF, 70 + step, std=1.0)
+        _, sumsq = dfl.grad_norm([g])
+        dfl.adamw(ps, [g], m, v, step, 1e-3, beta1=b1, beta2=b2, m_scales=ms, v_scales=vs, sumsq=sumsq, max_norm=1.0)
+        f = (1.0 / sumsq.sqrt()).float()
+        x = g.float() * f
+        a = b1 * (M.float().view(-1, 256) * MS[:, None]).view(-1) + (1.0 - b1) * x
+        r = (V.float().view(-1, 256) * VS[:, None]).view(-1)
+        r = (b2 * (r * r) + (1.0 - b2) * (x * x)).sqrt()
+        for t, q, s, got_q, got_s in ((a, M, MS, m[0], ms[0]), (r, V, VS, v[0], vs[0])):
+            t = t.view(-1, 256)
+            s.copy_((t.abs().amax(1) * torch.tensor(1.0 / 448.0, dtype=F32, device="cuda")).clamp_min(2.0 ** -96))
+            k = t / s[:, None]
+            if q is V:
+                k = torch.where(t > 0, k.clamp_min(2.0 ** -9), k)
+            q.copy_(k.view(-1).to(F8))
+            assert torch.equal(got_s, s) and same([got_q], [q]), step
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_from_the_first_step(bits):
     """Zero states; gradients of zero; the first step moves a value by lr against its gradient's sign."""
