@@ -675,7 +675,8 @@ long over(long a, long b) { return (a + b - 1) / b; }
 // plans each (1 to 8,192 rows, K and N from 256 to 12,288; the plan that is least by them takes 2.4% longer than the best one,
 // at the mean).  A stage takes 1.40 on the large tile (256 work-groups at once); on the smaller ones 0.50 where a work-group has its
 // CU for itself, 0.94 where two share it; a work-group begins and ends in 5 (3); parts are written and read at 6.1 TB/s and
-// added by a launch more (1.9).
+// added by a launch more (1.9).  Up to 64 rows the first product's stages wait for memory, 1.3 each (16 rows x 4,096 x 12,288 gated,
+// gradients: 110 us by 0.94, 96 by this).
 struct Work {
   long tiles, values;
   int stages;
@@ -699,33 +700,33 @@ double end_of(long nx, double ux, long nw, double uw, long slots, double pole) {
   }
   return std::max(end, pole * (late ? t1 : t0));
 }
-double cost_of(int tile, const Work& x, int kx, const Work& w, int kw) {
+double cost_of(int tile, bool few, const Work& x, int kx, const Work& w, int kw) {
   const long slots = tile == 0 ? 256 : 512, nx = x.tiles * kx, nw = w.tiles * kw;
   const double stage = tile == 0 ? 1.40 : 0.50 + 0.44 * (double)std::min(std::max(nx + nw - 256, 0l), 256l) / 256.0, ends = tile == 0 ? 5.0 : 3.0;
   // (the last of dx's work-groups have a small tile's CU for themselves at the end)
-  return end_of(nx, (double)over(x.stages, kx) * stage + ends, nw, (double)over(w.stages, kw) * stage + ends, slots, tile == 0 ? 1.0 : 0.75) +
+  return end_of(nx, (double)over(x.stages, kx) * (few ? 1.3 : stage) + ends, nw, (double)over(w.stages, kw) * stage + ends, slots, tile == 0 ? 1.0 : 0.75) +
          x.sums(kx) + w.sums(kw);
 }
 struct Plan {
   int tile, kx, kw;  // 0: the large tile, 1: the small one; parts
 };
-// f(tile) gives the two products' work on a tile (the second may be empty).  The parts of one are chosen beside those of the other, in
+// f(tile) gives the two products' work on a tile (the second may be empty); few: on the small ones alone.  The parts of one are chosen beside those of the other, in
 // turn, from numbers that come near to any.
 template <typename F>
-Plan plan_of(F&& f) {
+Plan plan_of(bool few, F&& f) {
   static constexpr int numbers[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64, 96, kMostParts};
-  Plan best{0, 1, 1};
+  Plan best{few, 1, 1};
   double least = 1e300;
-  for (int t = 0; t < 2; ++t) {
+  for (int t = few; t < 2; ++t) {
     const std::pair<Work, Work> p = f(t);
     int kx = 1, kw = 1;
-    double low = cost_of(t, p.first, 1, p.second, 1);
+    double low = cost_of(t, few, p.first, 1, p.second, 1);
     auto search = [&](const Work& own, int& k) {
       for (int n : numbers) {
         if (!own.can(n) || (n > 1 && own.tiles * n > 2048)) break;
         const int was = k;
         k = n;
-        const double c = cost_of(t, p.first, kx, p.second, kw);
+        const double c = cost_of(t, few, p.first, kx, p.second, kw);
         if (c < low) low = c;
         else k = was;
       }
@@ -784,7 +785,7 @@ void forward(Call a, hipStream_t st) {
   auto work = [&](long tiles) { return std::make_pair(Work{tiles, (long)a.rows * a.N * a.n2, stages_of(a.K)}, Work{0, 0, 0}); };
   // up to 64 rows the small tile's other half would be empty
   const bool few = a.rows <= Few::TN;
-  const Plan p = plan_of([&](int t) { return work(few ? tiles(Few{}) : t == 0 ? tiles(Large{}) : tiles(Small{})); });
+  const Plan p = plan_of(few, [&](int t) { return work(few ? tiles(Few{}) : t == 0 ? tiles(Large{}) : tiles(Small{})); });
   a.parts = p.kx;
   if (few) go(Few{}, tiles(Few{}));
   else if (p.tile == 0) go(Large{}, tiles(Large{}));
@@ -801,7 +802,7 @@ void gradients(Call a, const float* sums, int chunks, uint16_t* dbias, hipStream
   };
   a.parts = a.parts_w = 1;
   if (a.dx || a.dw[0]) {
-    const Plan p = plan_of([&](int t) {
+    const Plan p = plan_of(few, [&](int t) {
       return few ? work(tiles_x(Few{}), tiles_w(Small{})) : t == 0 ? work(tiles_x(Large{}), tiles_w(Large{})) : work(tiles_x(Small{}), tiles_w(Small{}));
     });
     auto go = [&](auto sx, auto sw) {
