@@ -7,7 +7,7 @@
 // root, because e4m3 then covers 2^36 of v instead of 2^18; what is above zero stays above zero, so that no step divides a
 // remembered m by eps alone.
 // Bound by memory: 28 bytes a value (bf16 with an fp32 master and fp32 states): 402 M values 2,290 us, 4.9 TB/s, a copy's rate on this
-// card; 10 in 8 bits without a master: 912 us, 4.4 TB/s.
+// card; 10 in 8 bits without a master: 931 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -51,29 +51,50 @@ __host__ __device__ inline void set_step(Hyper& h, double lr, double weight_deca
   h.root = (float)(1.0 / sqrt(1.0 - exp(t * ln2)));
 }
 
-// The tensors of a launch, as many as its arguments (4 KB) hold beside the options.  A tensor's record is read as a whole, and the
-// first chunks by a lane each: the arguments come from far, and every access that waits for another one costs a microsecond
-// (301 tensors, 8 bits, six launches: 7.6 us each; by a binary search over arrays of fields 9.1).
-template <bool MASTER, bool BYTE>
-struct Record {
-  void* p;
-  const void* g;
-  void *m, *v;
-  float* w[MASTER ? 1 : 0];
-  float* scale[BYTE ? 2 : 0];
-  uint32_t n;    // values, the low 32 bits
-  uint32_t tag;  // 1: fp32 parameter; 2: fp32 gradient; 4: a master; the high bits of n above
-  __device__ __forceinline__ long size() const { return (long)n | (long)(tag >> 3) << 32; }
-};
+// The tensors of a launch, as many as its arguments (4 KB) hold beside the options: 87 with masters and scales.  A tensor's addresses are
+// distances of 40 bits from those of the launch's first tensor less 2^39.  The arguments come from far, and every access that
+// waits for another one costs a microsecond, so a record is read as a whole, and the first chunks by a lane each (301 tensors, 8 bits: four
+// launches of 7-9 us; as 57 records of whole addresses six, and with a binary search over arrays of fields six of 9).
+constexpr long kReach = 1l << 39;
 template <bool MASTER, bool BYTE>
 struct Tab {
-  using R = Record<MASTER, BYTE>;
-  static constexpr int N = 3880 / (sizeof(R) + 4);
-  R r[N];
+  static constexpr int K = 4 + MASTER + 2 * BYTE;  // parameter, gradient, m, v; master; scales
+  static constexpr int N = 3840 / (4 * K + 16);
+  struct Record {
+    uint32_t lo[K];
+    uint32_t hi[2];  // bits from 32 on of address k in byte k; byte 7: 1: fp32 parameter; 2: fp32 gradient; 4: a master; the high bits of n above
+    uint32_t n;      // values, the low 32 bits
+  };
+  uint64_t base[K];
+  Record r[N];
   int first[N + 1];  // chunks before the tensor
   int count;
 };
 static_assert(sizeof(Tab<true, true>) + sizeof(Options) <= 4088 && sizeof(Tab<false, false>) + sizeof(Options) <= 4088, "kernel arguments");
+// a tensor of it
+template <bool MASTER, bool BYTE>
+struct Tensor {
+  void *p, *m, *v;
+  const void* g;
+  float *w, *ms, *vs;
+  long n;
+  int tag;
+  __device__ __forceinline__ Tensor(const Tab<MASTER, BYTE>& t, int i) {
+    const auto r = t.r[i];
+    auto address = [&](int k) {
+      return (void*)(t.base[k] + ((uint64_t)((r.hi[k / 4] >> (8 * (k % 4))) & 255u) << 32 | r.lo[k]));
+    };
+    p = address(0);
+    g = address(1);
+    m = address(2);
+    v = address(3);
+    w = MASTER ? (float*)address(4) : nullptr;
+    ms = BYTE ? (float*)address(4 + MASTER) : nullptr;
+    vs = BYTE ? (float*)address(5 + MASTER) : nullptr;
+    tag = (int)(r.hi[1] >> 24);
+    n = (long)r.n | (long)(tag >> 3) << 32;
+  }
+};
 
 // 8 values at any element
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
@@ -183,17 +204,16 @@ __device__ __forceinline__ float root_of(float v) {
 }
 
 template <bool MASTER, bool BYTE, typename P, typename G>
-__device__ __forceinline__ void chunk(const Record<MASTER, BYTE>& rec, int c, const Hyper& h, Factor f) {
+__device__ __forceinline__ void chunk(const Tensor<MASTER, BYTE>& t, int c, const Hyper& h, Factor f) {
   using S = std::conditional_t<BYTE, e4m3_t, float>;
   const long at = (long)c * kChunk + threadIdx.x * kValues;
-  const int left = (int)max(min(rec.size() - at, 8l), 0l);
+  const int left = (int)max(min(t.n - at, 8l), 0l);
   if (!BYTE && left == 0) return;
   float p[8], g[8], m[8], v[8];
-  P* param = (P*)rec.p + at;
-  S *pm = (S*)rec.m + at, *pv = (S*)rec.v + at;
-  float* master = nullptr;
-  if constexpr (MASTER) master = rec.tag & 4 ? rec.w[0] + at : nullptr;
-  load_some((const G*)rec.g + at, left, g);
+  P* param = (P*)t.p + at;
+  S *pm = (S*)t.m + at, *pv = (S*)t.v + at;
+  float* master = MASTER && (t.tag & 4) ? t.w + at : nullptr;
+  load_some((const G*)t.g + at, left, g);
   load_some(pm, left, m);
   load_some(pv, left, v);
   if (master) load_some((const float*)master, left, p);
@@ -201,8 +221,8 @@ __device__ __forceinline__ void chunk(const Record<MASTER, BYTE>& rec, int c, co
   float *sm = nullptr, *sv = nullptr;
   if constexpr (BYTE) {
     if (left > 0) {
-      sm = rec.scale[0] + at / kScaled;
-      sv = rec.scale[1] + at / kScaled;
+      sm = t.ms + at / kScaled;
+      sv = t.vs + at / kScaled;
       const float a = *sm, b = *sv;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -267,12 +287,12 @@ __global__ __launch_bounds__(kT) void k_adamw(Tab<MASTER, BYTE> tab, Options o) 
     if (norm > (double)o.max_norm) f.m = (float)frexp((double)o.max_norm / norm, &f.e);
   }
   while (true) {
-    const Record<MASTER, BYTE>& rec = tab.r[at];
+    const Tensor<MASTER, BYTE> t(tab, at);
     const int first = tab.first[at], stop = min(tab.first[at + 1], end);
     auto walk = [&](auto p, auto g) {
-      for (; c < stop; ++c) chunk<MASTER, BYTE, decltype(p), decltype(g)>(rec, c - first, h, f);
+      for (; c < stop; ++c) chunk<MASTER, BYTE, decltype(p), decltype(g)>(t, c - first, h, f);
     };
-    switch (rec.tag & 3) {
+    switch (t.tag & 3) {
       case 0: walk(bf16_t{}, bf16_t{}); break;
       case 1: walk(float{}, bf16_t{}); break;
       case 2: walk(bf16_t{}, float{}); break;
@@ -307,62 +327,74 @@ int check(const dflare_adamw_tensor* t, int n, const dflare_adamw_options& o) {
   return DFLARE_OK;
 }
 
-// INVALID_ARG where what is written (parameters, masters, states) overlaps anything else.  The lists of a call are
-// mostly in the order of their addresses: each is sorted only if it is not, then they are merged.
+// INVALID_ARG where what is written (parameters, masters, states) overlaps anything else.  The lists of a call are mostly in the
+// order of their addresses: a list is cut into ascending runs, and where these are few and lie apart as wholes (views of
+// flat buffers), that is all; otherwise everything is sorted.
 int all_apart(const dflare_adamw_tensor* t, int n, const dflare_adamw_options& o) try {
   struct Span {
     uintptr_t a, b;
     bool out;
   };
-  const auto before = [](const Span& x, const Span& y) { return x.a < y.a; };
-  std::vector<Span> all, list, both;
-  all.reserve(7 * (size_t)n + 3);
-  both.reserve(7 * (size_t)n + 3);
-  list.reserve((size_t)n + 3);
-  auto add = [&](const void* p, size_t bytes, bool out) {
-    if (p && bytes) list.push_back({(uintptr_t)p, (uintptr_t)p + bytes, out});
-  };
-  auto merge = [&] {
-    if (!std::is_sorted(list.begin(), list.end(), before)) std::sort(list.begin(), list.end(), before);
-    both.clear();
-    std::merge(all.begin(), all.end(), list.begin(), list.end(), std::back_inserter(both), before);
-    all.swap(both);
-    list.clear();
-  };
-  add(o.lr_device, 8, false);
-  add(o.step_device, 8, false);
-  add(o.sumsq, 8, false);
-  merge();
   const bool byte = o.state_bits == 8;
   const size_t state = byte ? 1 : 4;
+  // f(address, bytes, written) for every tensor, list by list
   auto each = [&](auto f) {
-    for (int i = 0; i < n; ++i)
-      if (t[i].n > 0) f(t[i], (size_t)t[i].n);
-    merge();
+    f(o.lr_device, 8, false);
+    f(o.step_device, 8, false);
+    f(o.sumsq, 8, false);
+    for (int i = 0; i < n; ++i) f(t[i].param, (size_t)t[i].n * size_of(t[i].param_dtype), true);
+    for (int i = 0; i < n; ++i) f(t[i].grad, (size_t)t[i].n * size_of(t[i].grad_dtype), false);
+    for (int i = 0; i < n; ++i) f(t[i].master, (size_t)t[i].n * 4, true);
+    for (int i = 0; i < n; ++i) f(t[i].m, (size_t)t[i].n * state, true);
+    for (int i = 0; i < n; ++i) f(t[i].v, (size_t)t[i].n * state, true);
+    if (!byte) return;
+    for (int i = 0; i < n; ++i) f(t[i].m_scale, ((size_t)t[i].n + kScaled - 1) / kScaled * 4, true);
+    for (int i = 0; i < n; ++i) f(t[i].v_scale, ((size_t)t[i].n + kScaled - 1) / kScaled * 4, true);
   };
-  each([&](const auto& x, size_t k) { add(x.param, k * size_of(x.param_dtype), true); });
-  each([&](const auto& x, size_t k) { add(x.grad, k * size_of(x.grad_dtype), false); });
-  each([&](const auto& x, size_t k) { add(x.master, k * 4, true); });
-  each([&](const auto& x, size_t k) { add(x.m, k * state, true); });
-  each([&](const auto& x, size_t k) { add(x.v, k * state, true); });
-  if (byte) {
-    each([&](const auto& x, size_t k) { add(x.m_scale, (k + kScaled - 1) / kScaled * 4, true); });
-    each([&](const auto& x, size_t k) { add(x.v_scale, (k + kScaled - 1) / kScaled * 4, true); });
+  auto before = [](const Span& x, const Span& y) { return x.a < y.a; };
+  auto clear = [](const Span* s, const Span* end) {
+    uintptr_t end_out = 0, end_any = 0;
+    for (; s != end; ++s) {
+      if (s->a < end_out || (s->out && s->a < end_any)) return false;
+      end_any = std::max(end_any, s->b);
+      if (s->out) end_out = std::max(end_out, s->b);
+    }
+    return true;
+  };
+  constexpr int RUNS = 48;
+  Span runs[RUNS];
+  int count = 0;
+  bool few = true;
+  each([&](const void* p, size_t bytes, bool out) {
+    const uintptr_t a = (uintptr_t)p;
+    if (!p || !bytes || !few) return;
+    if (count && runs[count - 1].out == out && a >= runs[count - 1].b) {
+      runs[count - 1].b = a + bytes;
+    } else if (count < RUNS) {
+      runs[count++] = Span{a, a + bytes, out};
+    } else {
+      few = false;
+    }
+  });
+  if (few) {
+    std::sort(runs, runs + count, before);
+    if (clear(runs, runs + count)) return DFLARE_OK;
   }
-  uintptr_t end_out = 0, end_any = 0;
-  for (const Span& x : all) {
-    if (x.a < end_out || (x.out && x.a < end_any)) return DFLARE_ERR_INVALID_ARG;
-    end_any = std::max(end_any, x.b);
-    if (x.out) end_out = std::max(end_out, x.b);
-  }
-  return DFLARE_OK;
+  std::vector<Span> all;
+  all.reserve(7 * (size_t)n + 3);
+  each([&](const void* p, size_t bytes, bool out) {
+    if (p && bytes) all.push_back({(uintptr_t)p, (uintptr_t)p + bytes, out});
+  });
+  std::sort(all.begin(), all.end(), before);
+  return clear(all.data(), all.data() + all.size()) ? DFLARE_OK : DFLARE_ERR_INVALID_ARG;
 } catch (const std::bad_alloc&) {
   return DFLARE_ERR_OUT_OF_MEMORY;
 }
 
 template <bool MASTER, bool BYTE>
 void launch(const dflare_adamw_tensor* t, int n, const Options& o, hipStream_t st) {
-  Tab<MASTER, BYTE> tab;
+  using T = Tab<MASTER, BYTE>;
+  T tab;
   tab.count = 0;
   tab.first[0] = 0;
   auto flush = [&] {
@@ -372,22 +404,32 @@ void launch(const dflare_adamw_tensor* t, int n, const Options& o, hipStream_t s
   for (int i = 0; i < n; ++i) {
     const dflare_adamw_tensor& x = t[i];
     if (!x.n) continue;
+    uint64_t at[7] = {(uint64_t)x.param, (uint64_t)x.grad, (uint64_t)x.m, (uint64_t)x.v};
+    if (MASTER) at[4] = (uint64_t)x.master;
+    if (BYTE) {
+      at[4 + MASTER] = (uint64_t)x.m_scale;
+      at[5 + MASTER] = (uint64_t)x.v_scale;
+    }
     const long chunks = (x.n + kChunk - 1) / kChunk;
-    if (tab.count == tab.N || (tab.count && tab.first[tab.count] + chunks > (1l << 30))) flush();
-    const int k = tab.count++;
-    Record<MASTER, BYTE>& r = tab.r[k];
-    r.p = x.param;
-    r.g = x.grad;
-    r.m = x.m;
-    r.v = x.v;
-    if constexpr (MASTER) r.w[0] = x.master;
-    if constexpr (BYTE) {
-      r.scale[0] = x.m_scale;
-      r.scale[1] = x.v_scale;
+    bool fits = tab.count < T::N && (!tab.count || tab.first[tab.count] + chunks <= (1l << 30));
+    for (int k = 0; tab.count && k < T::K; ++k) {
+      if (MASTER && k == 4 && !x.master) continue;  // (its address is not read)
+      fits = fits && at[k] - tab.base[k] < (uint64_t)(2 * kReach);
+    }
+    if (!fits) flush();
+    if (!tab.count)
+      for (int k = 0; k < T::K; ++k) tab.base[k] = at[k] - kReach;
+    const int j = tab.count++;
+    typename T::Record& r = tab.r[j];
+    r.hi[0] = 0;
+    r.hi[1] = (uint32_t)((x.param_dtype == DFLARE_F32) | (x.grad_dtype == DFLARE_F32) << 1 | (x.master != nullptr) << 2 | (x.n >> 32) << 3) << 24;
+    for (int k = 0; k < T::K; ++k) {
+      const uint64_t far = at[k] - tab.base[k];
+      r.lo[k] = (uint32_t)far;
+      r.hi[k / 4] |= (uint32_t)((far >> 32) & 255u) << (8 * (k % 4));
     }
     r.n = (uint32_t)x.n;
-    r.tag = (uint32_t)((x.param_dtype == DFLARE_F32) | (x.grad_dtype == DFLARE_F32) << 1 | (x.master != nullptr) << 2 | (x.n >> 32) << 3);
-    tab.first[k + 1] = tab.first[k] + (int)chunks;
+    tab.first[j + 1] = tab.first[j] + (int)chunks;
   }
   flush();
 }

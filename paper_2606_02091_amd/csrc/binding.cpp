@@ -53,7 +53,7 @@ int type_code(const at::Tensor& t) {
   type_error("expected a bf16 or fp32 tensor");
 }
 const at::Tensor& tensor(PyObject* o) {
-  if (!THPVariable_Check(o)) type_error("expected a device tensor");
+  if (!THPVariable_CheckExact(o) && !THPVariable_Check(o)) type_error("expected a device tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) type_error("expected a device tensor");
   return t;
@@ -476,10 +476,12 @@ PyObject* adamw(PyObject* const* a) {
     }
   }
   dflare_adamw_options o{};
-  if (THPVariable_Check(a[7])) o.step_device = (const int64_t*)like(a[7], "step", {1}, first, at::kLong);
-  else o.step = PyLong_AsLongLong(a[7]);
-  if (THPVariable_Check(a[8])) o.lr_device = (const double*)like(a[8], "lr", {1}, first, at::kDouble);
-  else o.lr = PyFloat_AsDouble(a[8]);
+  const bool step_there = THPVariable_Check(a[7]), lr_there = THPVariable_Check(a[8]);
+  if (step_there) o.step_device = (const int64_t*)like(a[7], "step", {1}, first, at::kLong);
+  if (lr_there) o.lr_device = (const double*)like(a[8], "lr", {1}, first, at::kDouble);
+  if (!step_there) o.step = PyLong_AsLongLong(a[7]);
+  if (!PyErr_Occurred() && !lr_there) o.lr = PyFloat_AsDouble(a[8]);
+  if (PyErr_Occurred()) return nullptr;
   o.beta1 = PyFloat_AsDouble(a[9]);
   o.beta2 = PyFloat_AsDouble(a[10]);
   o.eps = PyFloat_AsDouble(a[11]);

@@ -887,3 +887,94 @@ def test_a_training_step_of_a_draft_layer():
         flat = [t.view(-1) for t in grads]
         adamw_check([t and [x.view(-1) for x in t] for t in before], [t and [x.view(-1) for x in t] for t in (ps, m, v, ms, vs, masters)],
                     flat, 1, 1e-3, 0.9, 0.999, 1e-8, 0.01, min(1.0, 1.0 / float(sumsq.sqrt())), bits)
+
+
+def test_adamw_of_tensors_that_lie_far_apart():
+    """Parameters and masters in turn with tensors that have none; addresses in any order, also where gigabytes lie between."""
+    big = torch.empty(3 << 30, dtype=torch.uint8, device="cuda")
+    spots = [torch.empty(0)] * 3
+    for i, at in enumerate(((3 << 30) - (1 << 20), 1 << 30, 0)):
+        spots[i] = big[at:at + 4000].view(F32)
+    ps = [spots[0], randn((500,), BF, 1), spots[1], randn((600,), BF, 2), spots[2]]
+    for i, p in enumerate(ps):
+        p.copy_(randn(p.shape, F32, 10 + i))
+    masters = [None, ps[1].float(), None, ps[3].float(), None]
+    grads = [randn(p.shape, BF, 20 + i) for i, p in enumerate(ps)]
+    m, v, _, _ = dfl.adamw_state(ps)
+    before = ([p.clone() for p in ps], [t.clone() for t in m], [t.clone() for t in v], None, None,
+              [None if t is None else t.clone() for t in masters])
+    dfl.adamw(ps, grads, m, v, 2, 1e-2, masters=masters)
+    adamw_check(before, (ps, m, v, None, None, masters), grads, 2, 1e-2, 0.9, 0.999, 1e-8, 0.01, 1.0, 32)
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    x, w = randn((8, 64)), randn((72, 64))
+    dy, z = randn((8, 72)), randn((8, 72))
+    for f in (lambda: dfl.linear_fwd(x, randn((72, 56))), lambda: dfl.linear_fwd(x, w, randn((64,))), lambda: dfl.linear_fwd(x, w, residual=x),
+              lambda: dfl.linear_fwd(x.t(), w), lambda: dfl.linear_bwd(x, x, w), lambda: dfl.gated_fwd(x, w, randn((64, 64))),
+              lambda: dfl.gated_bwd(dy, x, z, x, w, w), lambda: dfl.qk_norm_rope_fwd(x.view(8, 1, 64), randn((32,)), torch.zeros(32, dtype=F64, device="cuda")),
+              lambda: dfl.qk_norm_rope_fwd((x.view(8, 1, 64),), (None, None), torch.zeros(32, dtype=F64, device="cuda")),
+              lambda: dfl.linear_fwd(x.view(2, 4, 64), w)):
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: dfl.linear_fwd(x.float(), w.float()), lambda: dfl.linear_fwd(x, w.float()), lambda: dfl.linear_bwd(None, x, w),
+              lambda: dfl.gated_bwd(dy, x, None, z, w, w), lambda: dfl.linear_fwd(x, w, act="silu"),
+              lambda: dfl.qk_norm_rope_fwd(x.view(8, 1, 64), None, torch.zeros(32, device="cuda")),
+              lambda: dfl.adamw([x], [x], [x], [x], 1, 0.1), lambda: dfl.adamw([x], [x], [x.float()], [x.float()], 1.5, 0.1)):
+        with pytest.raises(TypeError):
+            f()
+    for f, status in ((lambda: dfl.linear_fwd(x, w, act=9), dfl.ERR_INVALID_ARG), (lambda: dfl.linear_bwd(dy, x, w, act=dfl.ACT_SILU), dfl.ERR_INVALID_ARG),
+                      (lambda: dfl.linear_fwd(randn((4, 60)), randn((8, 60))), dfl.ERR_UNSUPPORTED),
+                      (lambda: dfl.linear_fwd(randn((520,))[4:516].view(8, 64), w), dfl.ERR_INVALID_ARG),
+                      (lambda: dfl.adamw([x], [x], [x.float()], [x.float()], 0, 0.1), dfl.ERR_INVALID_ARG)):
+        with pytest.raises(dfl.DFlareError) as e:
+            f()
+        assert e.value.status == status
+    m, v, ms, vs = dfl.adamw_state([x], 8)
+    for f in (lambda: dfl.adamw([x], [x], m, v, 1, 0.1, m_scales=[ms[0][:1]], v_scales=vs),
+              lambda: dfl.adamw([x], [x, x], m, v, 1, 0.1, m_scales=ms, v_scales=vs), lambda: dfl.adamw([x], [dy], m, v, 1, 0.1, m_scales=ms, v_scales=vs),
+              lambda: dfl.adamw([x], [x], [x.float()], [x.float()], 1, 0.1, m_scales=ms, v_scales=vs)):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(dfl.DFlareError):  # 8-bit moments without scales
+        dfl.adamw([x], [x], m, v, 1, 0.1)
+
+
+def test_two_graphs_in_turn():
+    """Two captured graphs of the same calls on other inputs, replayed in turn with eager calls between."""
+    made = []
+    for seed in (0, 500):
+        calls, inputs = operators(seed)
+        for f in calls:
+            f()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = [f() for f in calls]
+        made.append((calls, inputs, graph, outs))
+    for turn in range(3):
+        for k, (calls, inputs, graph, outs) in enumerate(made):
+            inputs[1].copy_(randn(inputs[1].shape, seed=turn * 10 + k))
+            graph.replay()
+        for calls, inputs, graph, outs in made:
+            want = [f() for f in calls]
+            torch.cuda.synchronize()
+            assert all(same(a, b) for a, b in zip(outs, want))
+
+
+def test_calls_of_two_streams_at_once():
+    """Each call has a workspace of its own."""
+    calls, _ = operators()
+    more, _ = operators(900)
+    want, want2 = [f() for f in calls], [f() for f in more]
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in (a, b):
+        s.wait_stream(torch.cuda.current_stream())
+    got = {}
+    for turn in range(5):
+        with torch.cuda.stream(a):
+            got[0] = [f() for f in calls]
+        with torch.cuda.stream(b):
+            got[1] = [f() for f in more]
+    torch.cuda.synchronize()
+    assert all(same(x, y) for x, y in zip(got[0], want)) and all(same(x, y) for x, y in zip(got[1], want2))
