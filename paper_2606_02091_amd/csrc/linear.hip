@@ -114,7 +114,7 @@ struct Call {
   float* part;                            // sums of a product's parts: y's, or dx's
   float* part_w;                          // and dW's
   int rows, N, K, n2, act, parts, parts_w;
-  int groups_x;                           // work-groups of dx in the launch of both gradients
+  int groups_x, split;                    // work-groups of dx in the launch of both gradients; of the rows before `split`
 };
 
 // a part's stages of k: [first, past the last) of `stages`
@@ -202,19 +202,18 @@ __device__ __forceinline__ void finish_tile(char* lds, const Acc<S>& acc, int ac
   }
 }
 
-// ---- z = x W^T, a tile of rows x TM rows of W, and its epilogue; or a part's sums ----
+// z = x W^T, tile `id` of those over `rows` rows of x from row0 on x TM rows of W, and its epilogue; or a part's sums
 template <typename S, bool GATED>
-__global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+__device__ __forceinline__ void tile_of_y(const std::conditional_t<GATED, const Call&, Call> a, int id, char* lds, int row0, int rows) {
   constexpr int MT = S::MT, NT = S::NT, HT = GATED ? MT / 2 : MT;  // HT: a wave's 32-row tiles of one matrix
   constexpr int PART = GATED ? HT * 32 : 0, TMO = GATED ? S::TM / 2 : S::TM;
-  const int nb = (a.rows + S::TN - 1) / S::TN, na = (a.N + TMO - 1) / TMO;
+  const int nb = (rows + S::TN - 1) / S::TN, na = (a.N + TMO - 1) / TMO;
   int unit, tb;
-  if (!tile_of(blockIdx.x, na * a.parts, nb, unit, tb)) return;
-  const int ks = unit / na, m0 = unit % na * TMO, r0 = tb * S::TN;
+  if (!tile_of(id, na * a.parts, nb, unit, tb)) return;
+  const int ks = unit / na, m0 = unit % na * TMO, r0 = row0 + tb * S::TN;
   int s0, s1;
   part_of((a.K + kBK - 1) / kBK, a.parts, ks, s0, s1);
-  const int k0 = s0 * kBK, kn = min(s1 * kBK, a.K) - k0, nv = min(a.rows - r0, S::TN), mv = min(a.N - m0, TMO);
+  const int k0 = s0 * kBK, kn = min(s1 * kBK, a.K) - k0, nv = min(row0 + rows - r0, S::TN), mv = min(a.N - m0, TMO);
   const long wo = (long)m0 * a.K + k0;
   Operand ow{a.w[0] + wo, a.K, mv, kn}, ox{a.x + (long)r0 * a.K + k0, a.K, nv, kn};
   if constexpr (GATED) ow.other = a.w[1] + wo;
@@ -294,6 +293,21 @@ __global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
   }
   __syncthreads();
   take<S, TMO>(lds, out_at(a.y));
+}
+
+// ---- forward products on one tile ----
+template <typename S, bool GATED>
+__global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+  tile_of_y<S, GATED>(a, blockIdx.x, lds, 0, a.rows);
+}
+// on small tiles, and on halves of them from row `split` on: where there are more small tiles than CUs but not twice as many, some CUs
+// would take two and others one
+template <bool GATED>
+__global__ __launch_bounds__(Small::T, 2) void k_forward_halves(Call a) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * Small::kStageBytes];
+  if ((int)blockIdx.x < a.groups_x) tile_of_y<Small, GATED>(a, blockIdx.x, lds, 0, a.split);
+  else tile_of_y<Few, GATED>(a, blockIdx.x - a.groups_x, lds, a.split, a.rows - a.split);
 }
 
 // ---- the same for up to 32 rows, bound by the way of W from memory (16 rows x 4,096 x 12,288 gated: 37 us, on tiles of 128 x 64 with parts
@@ -710,13 +724,38 @@ double end_of(long nx, double ux, long nw, double uw, long slots, double pole) {
   }
   return std::max(end, pole * (late ? t1 : t0));
 }
+// The last of a product's turns of work-groups over the CUs, us a stage, of n: the large tile's alone on a CU, the small one's in pairs
+// where there are more than CUs
+double last_stage(int tile, double n) {
+  const double f = n / 256.0;
+  return n == 0 ? 0.0 : tile == 0 ? 1.07 + 0.36 * f * f : f <= 1.0 ? 0.58 + 0.09 * f : 0.80 + 0.17 * (f - 1.0);
+}
 double cost_of(int tile, bool few, const Work& x, int kx, const Work& w, int kw) {
   const long slots = tile == 0 ? 256 : 512, nx = x.tiles * kx, nw = w.tiles * kw;
+  if (!nw && !few) {
+    const double s = (double)over(x.stages, kx);
+    return (double)(nx / slots) * (tile == 0 ? 1.40 * s + 2.0 : 0.97 * s + 1.0) + last_stage(tile, (double)(nx % slots)) * s + (tile == 0 ? 5.0 : 3.0) + x.sums(kx);
+  }
   const double stage = tile == 0 ? 1.40 : 0.50 + 0.44 * (double)std::min(std::max(nx + nw - 256, 0l), 256l) / 256.0, ends = tile == 0 ? 5.0 : 3.0;
   // (the last of dx's work-groups have a small tile's CU for themselves at the end)
   return end_of(nx, (double)over(x.stages, kx) * (few ? 1.3 : stage) + ends, nw, (double)over(w.stages, kw) * stage + ends, slots, tile == 0 ? 1.0 : 0.75) +
          x.sums(kx) + w.sums(kw);
 }
+// A forward product's rows that go to small tiles, where there are more of these than CUs and at most two to a CU: some CUs would take
+// two (0.9 us a stage) and others one (0.6), so the fewest of the rows behind them go to halves of the tile that leave at most one to
+// each CU, and two work-groups as before (1,003 gated rows of 2,880 x 2,880 45.6 -> 41.0 us, 777 x 5,120 x 2,880 40.6 -> 33.9).
+// All rows: no halves.
+int rows_before_halves(long columns, int rows) {
+  const long halves = over(rows, Few::TN);
+  if (columns * over(rows, Small::TN) > 512) return rows;
+  for (long b = 0; b <= halves; ++b) {
+    const long big = columns * ((halves - b) / 2);
+    if ((halves - b) % 2 || big > 256) continue;
+    return b && big + columns * b <= 512 ? (int)(halves - b) * Few::TN : rows;
+  }
+  return rows;
+}
+
 struct Plan {
   int tile, kx, kw;  // 0: the large tile, 1: the small one; parts
 };
@@ -797,6 +836,15 @@ void forward(Call a, hipStream_t st) {
   const bool few = a.rows <= Few::TN;
   const Plan p = plan_of(few, [&](int t) { return work(few ? tiles(Few{}) : t == 0 ? tiles(Large{}) : tiles(Small{})); });
   a.parts = p.kx;
+  const long columns = over(a.N, Small::TM / a.n2);
+  if (!few && p.tile == 1 && a.parts == 1) {
+    a.split = rows_before_halves(columns, a.rows);
+    if (a.split < a.rows) {
+      a.groups_x = (int)whole_turns(columns * (a.split / Small::TN));
+      hipLaunchKernelGGL((k_forward_halves<GATED>), dim3(a.groups_x + whole_turns(columns * over(a.rows - a.split, Few::TN))), dim3(Small::T), 0, st, a);
+      return;
+    }
+  }
   if (few) go(Few{}, tiles(Few{}));
   else if (p.tile == 0) go(Large{}, tiles(Large{}));
   else go(Small{}, tiles(Small{}));

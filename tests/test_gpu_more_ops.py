@@ -369,6 +369,21 @@ def test_products_on_the_large_tile(kind):
         gated_check(x, w, w2, "silu", dy, h, g, u, *dfl.gated_bwd(dy, x, g, u, w, w2))
 
 
+@pytest.mark.parametrize("rows,N,K", [(777, 5096, 136), (1003, 5120, 72), (300, 12040, 200), (4095, 2040, 1032), (2496, 2888, 328)])
+def test_products_on_tiles_of_two_sizes(rows, N, K):
+    """More small tiles than CUs and less than twice as many (a part of the rows on halves of them), and a gated block's large tile."""
+    x, w, w2 = randn((rows, K), seed=1), randn((N, K), seed=2, std=K ** -0.5), randn((N, K), seed=3, std=K ** -0.5)
+    dy, res = randn((rows, N), seed=4), randn((rows, N), seed=5)
+    y, z = dfl.linear_fwd(x, w, res[0].contiguous(), residual=res, act=dfl.ACT_GELU, save=True)
+    linear_check(x, w, res[0], res, "gelu", dy, y, z, *dfl.linear_bwd(dy, x, w, z, act=dfl.ACT_GELU, need_dbias=True))
+    half = N // 16 * 8
+    for F in (half, N):
+        u, v = w[:F].contiguous(), w2[:F].contiguous()
+        dh = dy[:, :F].contiguous()
+        h, gate, up = dfl.gated_fwd(x, u, v, act=dfl.ACT_SILU, save=True)
+        gated_check(x, u, v, "silu", dh, h, gate, up, *dfl.gated_bwd(dh, x, gate, up, u, v, act=dfl.ACT_SILU))
+
+
 @pytest.mark.parametrize("rows,N,K", [(1, 8, 8), (67, 200, 72), (300, 520, 136)])
 def test_products_without_rows_and_values_beside_them(rows, N, K):
     """Inputs between NaN, outputs between values that stay: nothing past a tensor's end is read into a result or written."""
