@@ -202,7 +202,9 @@ __device__ __forceinline__ void finish_tile(char* lds, const Acc<S>& acc, int ac
   }
 }
 
-// z = x W^T, tile `id` of those over `rows` rows of x from row0 on x TM rows of W, and its epilogue; or a part's sums
+// z = x W^T, tile `id` of those over `rows` rows of x from row0 on x TM rows of W, and its epilogue; or a part's sums.  (A gated block's
+// call by reference: a copy's two matrices would be chosen from in registers.  The other's by value: by reference the large tile needs 43
+// registers more than there are.)
 template <typename S, bool GATED>
 __device__ __forceinline__ void tile_of_y(const std::conditional_t<GATED, const Call&, Call> a, int id, char* lds, int row0, int rows) {
   constexpr int MT = S::MT, NT = S::NT, HT = GATED ? MT / 2 : MT;  // HT: a wave's 32-row tiles of one matrix
