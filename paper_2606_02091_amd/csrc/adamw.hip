@@ -191,16 +191,30 @@ __device__ __forceinline__ float to_scale(float (&x)[8]) {
   return scale;
 }
 
-// The root, correctly rounded where v is above 2^-90: an estimate y of 1 / sqrt(v), then both v y and y / 2 corrected by
+// The card's roots take numbers below 2^-126 for zero: a v below 2^-90 (a gradient below 1e-13) is multiplied by 2^64 first, its root by 2^-32
+struct Scaled {
+  float v, back;
+  __device__ __forceinline__ explicit Scaled(float x) {
+    const bool small = x < 0x1p-90f;
+    v = small ? x * 0x1p64f : x;
+    back = small ? 0x1p-32f : 1.f;
+  }
+};
+// The root, correctly rounded: an estimate y of 1 / sqrt(v), then both v y and y / 2 corrected by
 // 1/2 - (y / 2) (v y), and the root by its remainder (Markstein, "IA-64 and elementary functions", 2000)
 __device__ __forceinline__ float root_of(float v) {
-  const float y = __builtin_amdgcn_rsqf(v);
-  float g = v * y, h = 0.5f * y;
+  const Scaled s(v);
+  const float y = __builtin_amdgcn_rsqf(s.v);
+  float g = s.v * y, h = 0.5f * y;
   const float e = fmaf(-h, g, 0.5f);
   g = fmaf(g, e, g);
   h = fmaf(h, e, h);
-  g = fmaf(fmaf(-g, g, v), h, g);
-  return v > 0.f && v < INFINITY ? g : v;  // (a NaN is itself)
+  g = fmaf(fmaf(-g, g, s.v), h, g);
+  return v > 0.f && v < INFINITY ? g * s.back : v;  // (a NaN is itself)
+}
+__device__ __forceinline__ float near_root_of(float v) {  // to a unit in the last place
+  const Scaled s(v);
+  return __builtin_amdgcn_sqrtf(s.v) * s.back;
 }
 
 template <bool MASTER, bool BYTE, typename P, typename G>
@@ -246,7 +260,7 @@ __device__ __forceinline__ void chunk(const Tensor<MASTER, BYTE>& t, int c, cons
     } else {
       m[e] = fmaf(h.c1, x, h.b1 * m[e]);
       v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
-      r = __builtin_amdgcn_sqrtf(v[e]);  // (to a unit in the last place, as the reciprocal)
+      r = near_root_of(v[e]);  // (to a unit in the last place, as the reciprocal)
     }
     p[e] = fmaf(-h.alpha, m[e] * __builtin_amdgcn_rcpf(fmaf(r, h.root, h.eps)), p[e] * h.decay);
     if constexpr (BYTE) v[e] = r;

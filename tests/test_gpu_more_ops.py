@@ -638,6 +638,39 @@ def test_adamw_8_bit_states_are_the_formula_s_bit_by_bit():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-8, 1e-30])
+def test_adamw_of_gradients_whose_squares_are_hardly_there(bits, eps):
+    """Second moments down to the smallest number in fp32, whose root is no special case of the formula."""
+    b1, b2, lr, n = 0.9, 0.95, 1e-3, 700
+    for mag in (1e-26, 1e-20, 1e-19, 1e-18, 1e-17, 1e-16, 1e-14, 1e-10, 1e10, 1e17):
+        p = torch.zeros(n, dtype=F32, device="cuda")
+        (m,), (v,), ms, vs = dfl.adamw_state([p], bits)
+        ms, vs = (ms or [None])[0], (vs or [None])[0]
+        for step in (1, 2, 3):
+            g = (randn((n,), F32, step).sign() * (0.5 + randn((n,), F32, 9 + step).abs().clamp_max(2.0))) * mag
+            value = [t.double() if bits == 32 else t.double() * spread(s, n) for t, s in ((m, ms), (v, vs))]
+            mw, vw = b1 * value[0] + (1 - b1) * g.double(), b2 * (value[1] if bits == 32 else value[1] ** 2) + (1 - b2) * g.double() ** 2
+            # the products and their sum within units of their terms, and each within half of the smallest number besides
+            em, ev = 6 * U * (b1 * value[0].abs() + (1 - b1) * g.double().abs()) + 2.0 ** -147, 8 * U * vw + 2.0 ** -147
+            root, old = vw.sqrt(), p.double()
+            er = torch.where(vw > 2 * ev, ev / root.clamp_min(1e-200), (vw + ev).sqrt())
+            den = root / math.sqrt(1 - b2 ** step) + eps
+            low = (root - er).clamp_min(0) / math.sqrt(1 - b2 ** step) + eps
+            k = lr / (1 - b1 ** step)
+            dfl.adamw([p], [g], [m], [v], step, lr, beta1=b1, beta2=b2, eps=eps, weight_decay=0.0, m_scales=None if ms is None else [ms],
+                      v_scales=None if vs is None else [vs])
+            bound = k * (mw.abs() + em) / low * (1 + 16 * U) - k * mw.abs() / den + 4 * U * old.abs() + 2.0 ** -147
+            within(p, old - k * mw / den, 1.01 * bound, f"parameter at {mag}")
+            if bits == 32:
+                within(m, mw, 1.01 * em, "m")
+                within(v, vw, 1.01 * ev, "v")
+            else:
+                for q, s, t, e in ((m, ms, mw, em), (v, vs, root, er)):
+                    # half a step of e4m3 with its scale's own rounding, and a root above zero at least the smallest number
+                    within(q.double() * spread(s, n), t, 1.01 * (2.0 ** -4 * (t.abs() + e) + 2.0 ** -9 * spread(s, n) + e), "8-bit state")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_from_the_first_step(bits):
     """Zero states; gradients of zero; the first step moves a value by lr against its gradient's sign."""
     state = state_of([600], [F32], bits, False, fresh=True)
