@@ -201,6 +201,26 @@ def test_qk_norm_rope_of_nothing_and_of_zeros():
     assert torch.isfinite(dx.float()).all() and not dgain.any()
 
 
+def test_qk_norm_rope_of_a_head_whose_squares_are_hardly_there():
+    """Without an eps the root mean square is a head's size, however small."""
+    freq, _ = dfl.rope_frequencies(64, 1e4)
+    x, dy, gain = randn((9, 3, 64), F32, 1) * 2.0 ** -66, randn((9, 3, 64), F32, 2), randn((64,), F32, 3, mean=1.0)
+    y, (dx, dgain) = dfl.qk_norm_rope_fwd(x, gain, freq, eps=0.0), dfl.qk_norm_rope_bwd(dy, x, gain, freq, eps=0.0)
+    pos = torch.arange(9, device="cuda")
+    rstd = x.double().square().mean(-1, keepdim=True).rsqrt()
+    n, g = x.double() * rstd, gain.double()
+    want, size = turned(n * g, pos, freq, True, 1.0)
+    # 64 sums and a product of numbers near 2^-132, each within 2^-150: 2^-19 of their mean at most, half of that of the root; and the
+    # units of test_qk_norm_rope
+    k = 2.0 ** -19 + (64 + 32) * U
+    within(y, want, k * size, "y")
+    d, ds = turned(dy.double(), pos, freq, True, 1.0, inverse=True)
+    e = d * g
+    mean, es = (e * n).mean(-1, keepdim=True), ds * g.abs()
+    within(dx, rstd * (e - n * mean), 4 * k * rstd * (es + n.abs() * (es * n.abs()).mean(-1, keepdim=True)), "dx")
+    within(dgain, (d * n).sum((0, 1)), 4 * k * (ds * n.abs()).sum((0, 1)), "dgain")
+
+
 def test_qk_norm_rope_keeps_nan_in_its_head():
     freq, _ = dfl.rope_frequencies(64, 1e6)
     x, dy, gain = randn((30, 5, 64), seed=1), randn((30, 5, 64), seed=2), randn((64,), seed=3, mean=1.0)
