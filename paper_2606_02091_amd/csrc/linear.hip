@@ -307,6 +307,7 @@ __global__ __launch_bounds__(S::T, 2) void k_forward(Call a) {
 // would take two and others one
 template <bool GATED>
 __global__ __launch_bounds__(Small::T, 2) void k_forward_halves(Call a) {
+  static_assert(Small::T == Few::T && Small::TM == Few::TM && Small::kStageBytes >= Few::kStageBytes);
   __shared__ __attribute__((aligned(1024))) char lds[2 * Small::kStageBytes];
   if ((int)blockIdx.x < a.groups_x) tile_of_y<Small, GATED>(a, blockIdx.x, lds, 0, a.split);
   else tile_of_y<Few, GATED>(a, blockIdx.x - a.groups_x, lds, a.split, a.rows - a.split);
@@ -923,7 +924,7 @@ BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx
   L.d = o;
   o += n_d * up((size_t)rows * N * 2);
   L.sums = o;
-  if (sums) o += up((size_t)std::min(std::max(rows, 1), kPreGroups) * N * 4);
+  if (sums) o += up((size_t)pre_chunks(rows, N, true) * N * 4);
   L.part = o;
   if (dx) o += part_bytes((long)rows * K);
   L.part_w = o;
