@@ -924,7 +924,8 @@ BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx
   L.d = o;
   o += n_d * up((size_t)rows * N * 2);
   L.sums = o;
-  if (sums) o += up((size_t)pre_chunks(rows, N, true) * N * 4);
+  // (pre_chunks' at most, but growing with N)
+  if (sums) o += up((size_t)std::min(std::max(over(rows, 4), 1l) * N, kPreGroups * 8l * kT) * 4);
   L.part = o;
   if (dx) o += part_bytes((long)rows * K);
   L.part_w = o;

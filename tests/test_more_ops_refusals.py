@@ -146,6 +146,21 @@ def test_workspaces_of_products_grow_with_every_size():
             assert 0 < f(*small) <= f(*big)
 
 
+def test_workspace_of_a_bias_gradient_grows_across_its_chunks():
+    """The rows are cut into fewer chunks where columns take more work-groups; the space does not shrink there."""
+    f = dfl.lib().dflare_linear_bwd_workspace
+    for rows in (1, 5, 1000, 8192, 1 << 20):
+        last = 0
+        for N in (8, 2040, 2048, 2056, 4096, 4104, 12288, 12296, 65536, 65544, 1 << 18):
+            now = f(rows, N, 64, 0, 0, 0, 1)
+            if now == 0:  # about 2^35 values
+                break
+            assert now >= last
+            last = now
+            chunks = max(1, min(-(-rows // 4), 2048 // -(-N // 2048)))
+            assert now >= chunks * N * 4
+
+
 # ---- AdamW ----
 
 ADAM = dict(p=FAR[0], g=FAR[1], w=FAR[2], m=FAR[3], v=FAR[4], ms=FAR[5], vs=FAR[6])
