@@ -388,6 +388,14 @@ void launch(Args& a, int n_tensors, int dtype, int layout, hipStream_t st) {
       const long all = (long)a.rows * (a.t[0].heads + (n_tensors == 2 ? a.t[1].heads : 0));
       for (int k = 0; k < n_tensors; ++k) {
         const long n = (long)a.rows * a.t[k].heads, turns = (n + kT / L - 1) / (kT / L);
+        // forward: whole turns, up to six where that leaves 1,024 work-groups, so that some do not take one and others two, and the
+        // angles of a work-group's rows are formed for more than a few heads (2,048 rows x 40 heads x 128 14.1 -> 11.6 us, 1,024 rows 9.3
+        // -> 7.9; up to 4 or 8 turns 0 to +6%; backward no change)
+        if (!BACK) {
+          const long total = (all + kT / L - 1) / (kT / L), each = std::max(std::clamp(total / 1024, 1l, 6l), (total + most - 1) / most);
+          a.t[k].groups = (int)((turns + each - 1) / each);
+          continue;
+        }
         a.t[k].groups = (int)std::min(turns, n ? std::max(1l, most * n / all) : 0l);
       }
       const int groups = a.t[0].groups + (n_tensors == 2 ? a.t[1].groups : 0);
