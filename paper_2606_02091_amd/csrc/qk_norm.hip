@@ -3,7 +3,7 @@
 //   n = x / sqrt(mean of x^2 + eps),  y = scale R(p) (n g)
 //   d = scale R(-p) dy, e = d g,  dx = (e - n mean(e n)) / sqrt(mean of x^2 + eps),  dg = sum of d n over rows and heads
 // Bound by memory: a head is read and written once (twice read, x and dy, going back); everything between stays in registers.
-// 8,192 rows x 40 heads x 128 bf16: forward 35 us (168 MB, 4.8 TB/s), backward 52 (252 MB, 4.9 TB/s), a copy's rate on this card.
+// 8,192 rows x 40 heads x 128 bf16: forward 35 to 37 us (168 MB, 4.6 TB/s), backward 52 (252 MB, 4.9 TB/s), a copy's rate on this card.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
