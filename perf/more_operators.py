@@ -28,8 +28,8 @@ def listed():
         # one token of each of 32 sequences, 64-wide heads: latency
         dict(name="qk_token", kind="qk", rows=32, block=1, n_q=64, n_kv=8, hd=64, rot=64, layout="half",
              dtype="bf16", scale=1.0, far=8192, backward=False),
-        # fp32, a part of each head turned in pairs whose number fits no wide access, far positions
-        dict(name="qk_odd", kind="qk", rows=4001, block=4001, n_q=16, n_kv=3, hd=80, rot=36, layout="half",
+        # fp32, a part of each head turned in interleaved pairs whose number fits no wide access, far positions
+        dict(name="qk_odd", kind="qk", rows=4001, block=4001, n_q=16, n_kv=3, hd=80, rot=36, layout="interleaved",
              dtype="f32", scale=1.25, far=1000000, backward=True),
         # the feed-forward block of a draft layer over 512 blocks of 16 positions, with all gradients
         dict(name="gated_train", kind="gated", rows=8192, hidden=4096, ffn=12288, act="silu", backward=True),
