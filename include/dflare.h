@@ -674,7 +674,8 @@ int dflare_clip_grads(const dflare_grad_tensor* tensors, int32_t n, const double
  *   dx       of type dtype; may be x or dy, with the same strides
  *   dgain    fp32 [head_dim] out, or NULL: summed over rows and heads in a fixed order in fp32 (zeros without any)
  *   workspace  16-byte aligned, at least dflare_qk_norm_rope_bwd_workspace(rows, head_dim, n_tensors) bytes
- * A head with NaN or infinities is what the formula gives; other heads' results are not touched, dgain aside.
+ * A head with NaN or infinities is what the formula gives; other heads' results are not touched, dgain aside.  eps may be 0: the squares are
+ * added in fp32, which holds heads of 512 values of up to 2^59 at root mean square, and of 2^-66 with 2^-19 of the root.
  * rows = 0 does nothing, but for dgain.  head_dim > 512 or n_heads head_dim > 2^20: UNSUPPORTED.  Any alignment and strides, as in dflare_rope.
  */
 typedef struct {

@@ -30,15 +30,7 @@ struct Args {
   const double* freq;
   float* part;  // [work-groups][hd] sums of the gains' gradients
   int rows, B, hd, rot, table_rows;  // table_rows: rows whose cosines and sines LDS holds
-  float scale, inv, eps, back;  // 1 / sqrt(mean + eps) is back / sqrt(sum inv + eps)
-  // The card's root takes numbers below 2^-126 for zero.  Without an eps that keeps from them the mean is scaled by 2^24 (a mean above
-  // 2^104, of values above 10^15, then comes to infinity); by selects in the kernel 8,192 rows x 40 heads x 128 both ways take 2 to 3% longer
-  void norm_of(int head_dim, float e) {
-    const bool small = e < 0x1p-90f;
-    inv = (small ? 0x1p24f : 1.f) / (float)head_dim;
-    eps = small ? e * 0x1p24f : e;
-    back = small ? 0x1p12f : 1.f;
-  }
+  float scale, inv, eps;        // inv: 1 / hd
 };
 
 // VE elements of type T at any element, in one access
@@ -177,9 +169,20 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
+// 1 / sqrt(sum / hd + eps).  The card's root takes numbers below 2^-126 for zero.  BARE: eps is below 2^-90 and does not keep from them, so
+// a sum below 2^-90 is multiplied by 2^64 first and the result by 2^32.  (Kernels of their own: with selects for every head 8,192 rows x
+// 40 heads x 128 both ways take 2 to 3% longer, with a branch that is one way for the whole launch 3.6% backward.)
+template <bool BARE>
+__device__ __forceinline__ float rstd_of(const Args& a, float sum) {
+  if constexpr (!BARE) return __builtin_amdgcn_rsqf(fmaf(sum, a.inv, a.eps));
+  const bool small = sum < 0x1p-90f;
+  const float up = small ? 0x1p64f : 1.f;
+  return __builtin_amdgcn_rsqf(fmaf(sum * up, a.inv, a.eps * up)) * (small ? 0x1p32f : 1.f);
+}
+
 // A head is held by L lanes, S items each; the next one's is on its way while it is worked on.  BACK: dx and the work-group's
 // sums of the gain's gradient; otherwise y.
-template <typename T, int VE, bool HALF, int L, int S, bool BACK>
+template <typename T, int VE, bool HALF, int L, int S, bool BACK, bool BARE>
 __global__ __launch_bounds__(kT, 1) void k_qk(Args a) {
   using I = Item<T, VE, HALF>;
   extern __shared__ float tab[];
@@ -227,7 +230,6 @@ __global__ __launch_bounds__(kT, 1) void k_qk(Args a) {
       for (int e = 0; e < I::E; ++e) dg[i][e] = 0.f;
     }
   }
-  const float inv = 1.f / (float)a.hd;
   const int row_end = (int)((last + heads - 1) / heads);
   for (int row0 = (int)(first / heads); row0 < row_end; row0 += a.table_rows) {
     const int nr = min(a.table_rows, row_end - row0);
@@ -262,9 +264,9 @@ __global__ __launch_bounds__(kT, 1) void k_qk(Args a) {
           if constexpr (BACK) p = fmaf(d[i][e] * g[e], v[i][e], p);
         }
       }
-      const float rstd = __builtin_amdgcn_rsqf(fmaf(head_sum<L>(q), a.inv, a.eps)) * a.back;
+      const float rstd = rstd_of<BARE>(a, head_sum<L>(q));
       float mean = 0.f;
-      if constexpr (BACK) mean = head_sum<L>(p) * rstd * inv;
+      if constexpr (BACK) mean = head_sum<L>(p) * rstd * a.inv;
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         const I it(lane + i * L, items, half, a.rot);
@@ -404,8 +406,12 @@ void launch(Args& a, int n_tensors, int dtype, int layout, hipStream_t st) {
       const long rows = std::max(over_groups(a, 0), n_tensors == 2 ? over_groups(a, 1) : 0l);
       a.table_rows = (int)std::min<long>(a.table_rows, rows);
       const size_t lds = std::max((size_t)a.table_rows * half * 8, BACK ? (size_t)a.hd * 16 : 0);
-      if (layout == DFLARE_ROPE_HALF) hipLaunchKernelGGL((k_qk<T, VE, true, L, S, BACK>), dim3(groups), dim3(kT), lds, st, a);
-      else hipLaunchKernelGGL((k_qk<T, VE, false, L, S, BACK>), dim3(groups), dim3(kT), lds, st, a);
+      auto go = [&](auto half_c, auto bare) {
+        hipLaunchKernelGGL((k_qk<T, VE, decltype(half_c)::value, L, S, BACK, decltype(bare)::value>), dim3(groups), dim3(kT), lds, st, a);
+      };
+      const bool bare = a.eps < 0x1p-90f;
+      if (layout == DFLARE_ROPE_HALF) bare ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+      else bare ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
     });
   });
 }
@@ -458,7 +464,8 @@ int dflare_qk_norm_rope_fwd(const dflare_qk_tensor* tensors, int32_t n_tensors, 
   a.hd = head_dim;
   a.rot = rotary_dim;
   a.scale = scale;
-  a.norm_of(head_dim, eps);
+  a.inv = 1.f / (float)head_dim;
+  a.eps = eps;
   launch<false>(a, n_tensors, dtype, layout, (hipStream_t)stream);
   return launched();
 }
@@ -519,7 +526,8 @@ int dflare_qk_norm_rope_bwd(const dflare_qk_grad* tensors, int32_t n_tensors, co
   a.hd = head_dim;
   a.rot = rotary_dim;
   a.scale = scale;
-  a.norm_of(head_dim, eps);
+  a.inv = 1.f / (float)head_dim;
+  a.eps = eps;
   a.part = (float*)workspace;
   if (rows > 0) launch<true>(a, n_tensors, dtype, layout, (hipStream_t)stream);
   hipLaunchKernelGGL(k_qk_cols, dim3((head_dim + 15) / 16 * n_tensors), dim3(1024), 0, (hipStream_t)stream, a.part, a.t[0].groups, a.t[1].groups,

@@ -1046,3 +1046,16 @@ def test_calls_of_two_streams_at_once():
             got[1] = [f() for f in more]
     torch.cuda.synchronize()
     assert all(same(x, y) for x, y in zip(got[0], want)) and all(same(x, y) for x, y in zip(got[1], want2))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("eps", [0.0, 1e-30])
+def test_qk_norm_rope_of_small_and_large_heads_without_an_eps(dtype, eps):
+    """Heads of one call from 2^-55 to 2^58 at root mean square: the squares' sums are inside fp32 for all of them."""
+    freq, _ = dfl.rope_frequencies(64, 1e4)
+    size = torch.tensor([2.0 ** k for k in (-55, -48, -20, 0, 30, 52, 53, 58)], device="cuda")[:, None]
+    x, dy = (randn((9, 8, 64), F32, 1) * size).to(dtype), randn((9, 8, 64), dtype, 2)
+    gain = randn((64,), dtype, 3, mean=1.0, std=0.3)
+    kw = dict(layout=dfl.ROPE_HALF, eps=eps)
+    y, (dx, dgain) = dfl.qk_norm_rope_fwd(x, gain, freq, **kw), dfl.qk_norm_rope_bwd(dy, x, gain, freq, **kw)
+    qk_check(x, gain, torch.arange(9, device="cuda"), freq, True, 1.0, eps, y, dy, dx, dgain)
