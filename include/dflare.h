@@ -756,7 +756,8 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
  * dflare_adamw -- one AdamW step over n tensors, in place.  With the clipped gradient g:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
- * formed in fp32 (the factors in double) and rounded once where stored.
+ * formed in fp32 (the factors, lr weight_decay among them, in double, and then rounded) and rounded once where stored: p less the sum of its
+ * decay and its update.
  *   param    of type param_dtype;  grad  of type grad_dtype
  *   master   fp32 parameter in whose place param (bf16) is only written, rounded; or NULL: param is the parameter
  *   m, v     the moments, zeros before the first step.  state_bits 32: fp32.  8: e4m3 (OCP, no infinities) numbers times a scale

@@ -33,7 +33,7 @@ constexpr float kPerMost = 1.f / kMost;
 constexpr float kLeastScale = 1.2621774483536189e-29f;  // 2^-96: scales and their inverses stay inside fp32
 
 struct Hyper {
-  float decay, alpha, root;  // 1 - lr w, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float decay, alpha, root;  // lr w, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   float b1, c1, b2, c2, eps; // c: 1 - b
 };
 struct Options {
@@ -46,7 +46,7 @@ struct Options {
   Hyper h;
 };
 __host__ __device__ inline void set_step(Hyper& h, double lr, double weight_decay, double ln1, double ln2, double t) {
-  h.decay = (float)(1.0 - lr * weight_decay);
+  h.decay = (float)(lr * weight_decay);
   h.alpha = (float)(lr / (1.0 - exp(t * ln1)));
   h.root = (float)(1.0 / sqrt(1.0 - exp(t * ln2)));
 }
@@ -262,7 +262,10 @@ __device__ __forceinline__ void chunk(const Tensor<MASTER, BYTE>& t, int c, cons
       v[e] = fmaf(h.c2 * x, x, h.b2 * v[e]);
       r = near_root_of(v[e]);  // (to a unit in the last place, as the reciprocal)
     }
-    p[e] = fmaf(-h.alpha, m[e] * __builtin_amdgcn_rcpf(fmaf(r, h.root, h.eps)), p[e] * h.decay);
+    // Decay and update are taken off together, and p is rounded once: 1 - lr w in fp32 is a multiple of 2^-24, 19% off at lr w = 1e-7 and no
+    // decay below 3e-8, step after step to the same side.  (An infinite p stays what it is.)
+    const float kept = fabsf(p[e]) < INFINITY ? p[e] : 0.f;
+    p[e] -= fmaf(h.decay, kept, h.alpha * (m[e] * __builtin_amdgcn_rcpf(fmaf(r, h.root, h.eps))));
     if constexpr (BYTE) v[e] = r;
   }
   if constexpr (BYTE) {

@@ -1059,3 +1059,44 @@ def test_qk_norm_rope_of_small_and_large_heads_without_an_eps(dtype, eps):
     kw = dict(layout=dfl.ROPE_HALF, eps=eps)
     y, (dx, dgain) = dfl.qk_norm_rope_fwd(x, gain, freq, **kw), dfl.qk_norm_rope_bwd(dy, x, gain, freq, **kw)
     qk_check(x, gain, torch.arange(9, device="cuda"), freq, True, 1.0, eps, y, dy, dx, dgain)
+
+
+@pytest.mark.parametrize("masters", [True, False])
+@pytest.mark.parametrize("lr,decay", [(1e-6, 0.1), (1e-6, 0.01)])
+def test_adamw_decay_of_small_rates_adds_up(masters, lr, decay):
+    """lr weight_decay of 1e-7 and 1e-8, next to and below fp32's steps under 1: what 64 steps take off a million values at the mean."""
+    n, steps, b1, b2 = 1 << 20, 64, 0.9, 0.95
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty(n, device="cuda").uniform_(1.1, 1.9, generator=g)
+    p = w.to(BF) if masters else w
+    m, v = randn((n,), F32, 2), torch.empty(n, device="cuda").uniform_(0.5, 1.5, generator=g)
+    want, mw, vw = w.double(), m.double(), v.double()
+    for step in range(50, 50 + steps):
+        x = randn((n,), F32, step)
+        dfl.adamw([p], [x], [m], [v], step, lr, beta1=b1, beta2=b2, weight_decay=decay, masters=[w] if masters else None)
+        mw = b1 * mw + (1 - b1) * x.double()
+        vw = b2 * vw + (1 - b2) * x.double() ** 2
+        want = want * (1 - lr * decay) - lr / (1 - b1 ** step) * mw / ((vw / (1 - b2 ** step)).sqrt() + 1e-8)
+    # A step rounds each value to half of 2^-23 at most, the update (several times that, another one for each value) deciding the
+    # side: 2^-23 / sqrt(12) at root mean square, which n values times `steps` bring down to 2.7e-10 at the mean; 30 of these.  Errors
+    # of the update itself are 2^-22 of 1e-6 a step.
+    off = float((w.double() - want).mean())
+    assert abs(off) <= 30 * 2.0 ** -23 / math.sqrt(12) * math.sqrt(steps / n) + steps * 2.0 ** -22 * lr, off
+    assert not masters or torch.equal(p, w.to(BF))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_decay_of_what_is_no_number(bits):
+    """Infinite and undefined parameters stay what they are, beside others that are not touched by it."""
+    p = randn((300,), F32, 1)
+    p[5], p[6], p[7] = float("inf"), -float("inf"), float("nan")
+    q = p.clone()
+    q[5:8] = 1.0
+    x = randn((300,), F32, 2)
+    for t in (p, q):
+        m, v, ms, vs = dfl.adamw_state([t], bits)
+        dfl.adamw([t], [x], m, v, 1, 1e-2, weight_decay=0.1, m_scales=ms, v_scales=vs)
+    assert p[5] == float("inf") and p[6] == -float("inf") and p[7].isnan()
+    keep = torch.ones(300, dtype=torch.bool, device="cuda")
+    keep[5:8] = False
+    assert torch.equal(p[keep], q[keep])
