@@ -769,7 +769,8 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
  *            place by the kernels (a captured step goes on counting), or NULL
  *   sumsq    DEVICE double [1], dflare_grad_norm's, or NULL.  g = grad max_norm / norm where norm = sqrt(*sumsq) is above max_norm,
  *            as dflare_clip_grads gives it, but for its rounding; where *sumsq is not finite the step is left out: nothing is written.
- * Without sumsq a gradient that is not finite makes its value, and with 8 bits its 256 values of the states, what the formulas give.
+ * Without sumsq a gradient that is not finite makes its value, and with 8 bits its 256 values of the states, what the formulas give (their
+ * largest, and with it the scale, is NaN or infinite).
  * beta outside [0, 1), eps below fp32's normal numbers, lr or weight_decay negative or not finite, step < 1, max_norm < 0 beside a sumsq,
  * state_bits neither 8 nor 32: INVALID_ARG; more than 2^36 values in one tensor: UNSUPPORTED.  Tensors need the alignment of their elements alone.
  */

@@ -172,16 +172,16 @@ __device__ __forceinline__ void store_some(T* p, int left, const float (&x)[8]) 
   }
 }
 
-// x over the scale of its 256 values, which 32 lanes hold, and the scale.  ROOT: what is above zero stays at least the smallest number
-// above zero
+// x over the scale of its 256 values, which 32 lanes hold, and the scale.  A NaN among them is their largest, and so all 256 are NaN, as
+// the formula has it.  ROOT: what is above zero stays at least the smallest number above zero
 template <bool ROOT>
 __device__ __forceinline__ float to_scale(float (&x)[8]) {
   float most = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+  for (int e = 0; e < 8; ++e) most = __builtin_elementwise_maximum(most, fabsf(x[e]));
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
-  const float scale = fmaxf(most * kPerMost, kLeastScale), inv = 1.f / scale;
+  for (int off = 16; off > 0; off >>= 1) most = __builtin_elementwise_maximum(most, __shfl_xor(most, off));
+  const float scale = __builtin_elementwise_maximum(most * kPerMost, kLeastScale), inv = 1.f / scale;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     float q = x[e] * inv;

@@ -1100,3 +1100,32 @@ def test_adamw_decay_of_what_is_no_number(bits):
     keep = torch.ones(300, dtype=torch.bool, device="cuda")
     keep[5:8] = False
     assert torch.equal(p[keep], q[keep])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_adamw_8_bit_states_of_gradients_that_are_not_finite(bad):
+    """The 256 values that share a scale with such a one are what the formula gives; the others are what they are without it."""
+    n, at = 1000, 300
+    state, clean = (state_of([n], [F32], 8, False, seed=3) for _ in range(2))
+    M, V, MS, VS = (state[k][0].clone() for k in (1, 2, 3, 4))
+    g = randn((n,), F32, 9)
+    dfl.adamw(clean[0], [g], clean[1], clean[2], 4, 1e-3, m_scales=clean[3], v_scales=clean[4])
+    g[at] = bad
+    dfl.adamw(state[0], [g], state[1], state[2], 4, 1e-3, m_scales=state[3], v_scales=state[4])
+    pad = lambda t: torch.nn.functional.pad(t, (0, -n % 256)).view(-1, 256)  # noqa: E731
+    a = 0.9 * (pad(M.float()) * MS[:, None]) + (1.0 - 0.9) * pad(g)
+    r = (pad(V.float()) * VS[:, None])
+    r = (0.999 * (r * r) + (1.0 - 0.999) * (pad(g) * pad(g))).sqrt()
+    for t, q, s, q0, s0, root in ((a, state[1][0], state[3][0], clean[1][0], clean[3][0], False),
+                                  (r, state[2][0], state[4][0], clean[2][0], clean[4][0], True)):
+        scale = (t.abs().amax(1) * torch.tensor(1.0 / 448.0, dtype=F32, device="cuda")).clamp_min(2.0 ** -96)
+        k = t / scale[:, None]
+        if root:
+            k = torch.where(t > 0, k.clamp_min(2.0 ** -9), k)
+        want, got = k.to(F8).float() * scale[:, None], pad(q.float()) * s[:, None]
+        assert torch.equal(s.nan_to_num(1.25, 2.5, -2.5), scale.nan_to_num(1.25, 2.5, -2.5))
+        assert torch.equal(got[1].nan_to_num(1.25, 2.5, -2.5), want[1].nan_to_num(1.25, 2.5, -2.5)) and not torch.isfinite(got[1]).any()
+        others = torch.arange(n, device="cuda") // 256 != at // 256
+        assert torch.equal(q.view(torch.uint8)[others], q0.view(torch.uint8)[others]) and torch.equal(s[[0, 2, 3]], s0[[0, 2, 3]])
+    keep = torch.arange(n, device="cuda") != at
+    assert torch.equal(state[0][0][keep], clean[0][0][keep])
