@@ -766,7 +766,8 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
  *            zero.  Every operation of the formulas for m and v, the root and the quotients are rounded to fp32 by themselves, the numbers to
  *            nearest even; param and master are formed before that.
  *   options  HOST: lr, beta1, beta2, eps, weight_decay; step, from 1; lr_device, step_device: DEVICE double and int64, read in their
- *            place by the kernels (a captured step goes on counting), or NULL
+ *            place by the kernels (a captured step goes on counting), or NULL; with a step below 1, or a rate that is negative or not
+ *            finite there, the step is left out: nothing is written
  *   sumsq    DEVICE double [1], dflare_grad_norm's, or NULL.  g = grad max_norm / norm where norm = sqrt(*sumsq) is above max_norm,
  *            as dflare_clip_grads gives it, but for its rounding; where *sumsq is not finite the step is left out: nothing is written.
  * Without sumsq a gradient that is not finite makes its value, and with 8 bits its 256 values of the states, what the formulas give (their

@@ -295,8 +295,12 @@ __global__ __launch_bounds__(kT) void k_adamw(Tab<MASTER, BYTE> tab, Options o) 
     at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < tab.count && tab.first[min(i, tab.count)] <= c));
   }
   Hyper h = o.h;
-  if (o.lr_device || o.step_device)
-    set_step(h, o.lr_device ? *o.lr_device : o.lr, o.weight_decay, o.ln1, o.ln2, (double)(o.step_device ? *o.step_device : o.step));
+  if (o.lr_device || o.step_device) {
+    const double lr = o.lr_device ? *o.lr_device : o.lr;
+    const int64_t step = o.step_device ? *o.step_device : o.step;
+    if (!(lr >= 0.0 && lr < (double)INFINITY) || step < 1) return;  // the host refuses such numbers: the step is left out
+    set_step(h, lr, o.weight_decay, o.ln1, o.ln2, (double)step);
+  }
   Factor f{1.f, 0};
   if (o.sumsq) {
     const double norm = sqrt(sumsq);

@@ -639,8 +639,8 @@ def adamw(params, grads, m, v, step, lr, beta1: float = 0.9, beta2: float = 0.99
           masters=None, m_scales=None, v_scales=None, sumsq=None, max_norm: float = float("inf"), stream=None) -> None:
     """One AdamW step over lists of parameters (bf16 or fp32), in place (include/dflare.h).  m, v: fp32, or float8_e4m3fn
     with the scales of adamw_state; masters: fp32 parameters of the bf16 ones, or None; step (from 1) and lr: numbers, or device
-    tensors of one int64 and one fp64, which the kernels read; sumsq: grad_norm's, by which gradients are clipped to max_norm
-    (a step whose sumsq is not finite is left out)."""
+    tensors of one int64 and one fp64, which the kernels read (below 1, negative or not finite there: the step is left out); sumsq:
+    grad_norm's, by which gradients are clipped to max_norm (a step whose sumsq is not finite is left out)."""
     params = list(params)
     if not params:
         return

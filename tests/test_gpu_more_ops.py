@@ -1129,3 +1129,26 @@ def test_adamw_8_bit_states_of_gradients_that_are_not_finite(bad):
         assert torch.equal(q.view(torch.uint8)[others], q0.view(torch.uint8)[others]) and torch.equal(s[[0, 2, 3]], s0[[0, 2, 3]])
     keep = torch.arange(n, device="cuda") != at
     assert torch.equal(state[0][0][keep], clean[0][0][keep])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("step,lr", [(0, 1e-2), (-3, 1e-2), (2, float("nan")), (2, -1e-2), (2, float("inf")), (0, None), (None, -1e-2)])
+def test_adamw_leaves_out_a_step_whose_number_or_rate_is_none(bits, step, lr):
+    """On the device, where the call cannot refuse them; the next step, with others in their place, is taken."""
+    state = state_of([3000, 10, 300], [BF, F32, BF], bits, True)
+    ps, m, v, ms, vs, w = state
+    grads = [randn((n,), BF, 1 + n) for n in (3000, 10, 300)]
+    before = [[None if x is None else x.clone() for x in t] for t in state if t is not None]
+    at = torch.full((1,), 2 if step is None else step, dtype=torch.int64, device="cuda") if step is not None else 2
+    rate = torch.full((1,), lr, dtype=F64, device="cuda") if lr is not None else 1e-2
+    dfl.adamw(ps, grads, m, v, at, rate, masters=w, m_scales=ms, v_scales=vs)
+    for a, b in zip(before, [t for t in state if t is not None]):
+        assert same(a, b)
+    if step is not None:
+        at.fill_(2)
+    if lr is not None:
+        rate.fill_(1e-2)
+    other = [None if t is None else [None if x is None else x.clone() for x in t] for t in state]
+    dfl.adamw(ps, grads, m, v, at, rate, masters=w, m_scales=ms, v_scales=vs)
+    dfl.adamw(other[0], grads, other[1], other[2], 2, 1e-2, masters=other[5], m_scales=other[3], v_scales=other[4])
+    assert all(same(a, b) for a, b in zip(state, other) if a is not None) and not same(state[0], before[0])
