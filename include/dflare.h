@@ -710,19 +710,34 @@ int dflare_qk_norm_rope_bwd(const dflare_qk_grad* tensors, int32_t n_tensors, co
 enum { DFLARE_ACT_NONE = 0, DFLARE_ACT_RELU = 1, DFLARE_ACT_SILU = 2, DFLARE_ACT_GELU = 3, DFLARE_ACT_GELU_TANH = 4 };
 
 /*
+ * What a call of the projections or the gated block with these sizes does (no GPU call).  The choice is the library's own and may
+ * change with it; the results' roundings hang on it, nothing else.
+ *   tiles    of the output, columns x rows: DFLARE_TILES_NONE (up to 32 rows forward: columns in turn, the weights read once), _64 (128 x 64; dw
+ *            128 x 128), _128 (128 x 128), _128_64 (128 x 128, 128 x 64 from row `split` on), _256 (256 x 256)
+ *   parts    of the sums of y (both of the gated block's products) or dx, which are added in a launch of their own; parts_w: of dw
+ *   workspace  bytes that the call takes
+ */
+enum { DFLARE_TILES_NONE = 0, DFLARE_TILES_64 = 1, DFLARE_TILES_128 = 2, DFLARE_TILES_128_64 = 3, DFLARE_TILES_256 = 4 };
+typedef struct {
+  int32_t tiles, parts, parts_w, split;
+  size_t workspace;
+} dflare_product_plan;
+
+/*
  * dflare_linear_fwd -- a projection with its epilogue: z = x w^T + bias, y = act(z) + residual.
  *   x  bf16 [rows, K];  w  bf16 [N, K];  bias  bf16 [N] or NULL;  residual  bf16 [rows, N] or NULL
  *   y  bf16 [rows, N] out; may be residual;  z  bf16 [rows, N] out, what the backward pass through an activation takes, or NULL: not wanted
- *   workspace  at least dflare_linear_fwd_workspace(rows, N, K) bytes
+ *   workspace  dflare_linear_fwd_workspace(rows, N, K) bytes are enough, also for every call of smaller sizes; the plan's, fewer mostly, for
+ *              this one (dflare_linear_plan)
  * dflare_linear_bwd -- its gradients for the output gradient dy (which is also residual's), dz = dy act'(z):
  *   z      of the forward pass; not read without an activation
  *   dx     bf16 [rows, K] out: dz w;  dw  bf16 [N, K] out: dz^T x;  dbias  bf16 [N] out: dz added over the rows; each may be NULL: not
  *          wanted (x is read for dw alone, w for dx alone)
- *   workspace  at least dflare_linear_bwd_workspace(rows, N, K, act, dx wanted, dw wanted, dbias wanted) bytes
+ *   workspace  as above, of dflare_linear_bwd_workspace(rows, N, K, act, dx wanted, dw wanted, dbias wanted) bytes or the plan's
  * Products run on the bf16 matrix cores with fp32 sums; everything up to y is formed in fp32 and rounded once.  The gradients are those at
  * the stored z; dz is rounded to bf16 as an operand of dx and dw (dbias adds it unrounded).  All tensors 16-byte aligned.
  * rows = 0 writes zeros to dw and dbias.  N or K not a multiple of 8 or above 2^18, more than 2^22 rows, or about 2^35 values of y or
- * of w: UNSUPPORTED (a workspace is then 0 bytes).  Each workspace grows with rows, N and K.
+ * of w: UNSUPPORTED (a workspace is then 0 bytes).  What the workspace functions give grows with rows, N and K.
  * NaN and infinities stay in the rows of y and dx, and the rows and columns of dw, whose sums they belong to.
  */
 size_t dflare_linear_fwd_workspace(int32_t rows, int32_t N, int32_t K);
@@ -731,16 +746,18 @@ int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void
 size_t dflare_linear_bwd_workspace(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias);
 int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* z, int32_t rows, int32_t N, int32_t K, int32_t act,
                       void* dx, void* dw, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+int dflare_linear_plan(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias, dflare_product_plan* fwd,
+                       dflare_product_plan* bwd); /* either may be NULL: not wanted */
 
 /*
  * dflare_gated_fwd -- the gated feed-forward block up to its down projection, in one product: gate = x w_gate^T, up = x w_up^T,
  * h = act(gate) up.
  *   x  bf16 [rows, H];  w_gate, w_up  bf16 [F, H];  h  bf16 [rows, F] out
  *   gate, up  bf16 [rows, F] out, what the backward pass takes, or both NULL: not wanted
- *   workspace  at least dflare_gated_fwd_workspace(rows, H, F) bytes
+ *   workspace  dflare_gated_fwd_workspace(rows, H, F) bytes or the plan's, as for the projections
  * dflare_gated_bwd -- its gradients for dh, dgate = dh up act'(gate), dup = dh act(gate):
  *   dx  bf16 [rows, H] out: dgate w_gate + dup w_up, or NULL;  dw_gate, dw_up  bf16 [F, H] out: dgate^T x, dup^T x, or both NULL
- *   workspace  at least dflare_gated_bwd_workspace(rows, H, F, dx wanted, dw wanted) bytes
+ *   workspace  dflare_gated_bwd_workspace(rows, H, F, dx wanted, dw wanted) bytes or the plan's
  * Roundings, alignment, sizes, rows = 0, NaN and infinities as for the projections (N = F, K = H): gate and up are used unrounded in h, and as
  * stored in the gradients; dgate and dup are rounded to bf16 as operands.
  */
@@ -751,6 +768,7 @@ size_t dflare_gated_bwd_workspace(int32_t rows, int32_t H, int32_t F, int32_t dx
 int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void* up, const void* w_gate, const void* w_up, int32_t rows,
                      int32_t H, int32_t F, int32_t act, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
                      void* stream);
+int dflare_gated_plan(int32_t rows, int32_t H, int32_t F, int32_t dx, int32_t dw, dflare_product_plan* fwd, dflare_product_plan* bwd);
 
 /*
  * dflare_adamw -- one AdamW step over n tensors, in place.  With the clipped gradient g:

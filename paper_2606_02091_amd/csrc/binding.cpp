@@ -26,13 +26,11 @@ decltype(&dflare_clip_grads) p_clip_grads;
 decltype(&dflare_qk_norm_rope_fwd) p_qk_norm_rope_fwd;
 decltype(&dflare_qk_norm_rope_bwd_workspace) p_qk_norm_rope_bwd_workspace;
 decltype(&dflare_qk_norm_rope_bwd) p_qk_norm_rope_bwd;
-decltype(&dflare_linear_fwd_workspace) p_linear_fwd_workspace;
+decltype(&dflare_linear_plan) p_linear_plan;
 decltype(&dflare_linear_fwd) p_linear_fwd;
-decltype(&dflare_linear_bwd_workspace) p_linear_bwd_workspace;
 decltype(&dflare_linear_bwd) p_linear_bwd;
-decltype(&dflare_gated_fwd_workspace) p_gated_fwd_workspace;
+decltype(&dflare_gated_plan) p_gated_plan;
 decltype(&dflare_gated_fwd) p_gated_fwd;
-decltype(&dflare_gated_bwd_workspace) p_gated_bwd_workspace;
 decltype(&dflare_gated_bwd) p_gated_bwd;
 decltype(&dflare_adamw) p_adamw;
 PyObject* p_raw_stream;     // device index -> address of its current stream
@@ -368,7 +366,9 @@ PyObject* linear_fwd(PyObject* const* a) {
   if (PyErr_Occurred()) return nullptr;
   const bool save = truth(a[5]);
   const Here here(p.x.device());
-  const size_t bytes = p_linear_fwd_workspace(p.rows, p.N, p.K);
+  dflare_product_plan plan{};  // (of sizes that are refused below: 0 bytes)
+  p_linear_plan(p.rows, p.N, p.K, act, 0, 0, 0, &plan, nullptr);
+  const size_t bytes = plan.workspace;
   const at::Tensor ws = scratch(bytes, p.x), y = fresh({p.rows, p.N}, p.x, p.x.scalar_type());
   const at::Tensor z = save ? fresh({p.rows, p.N}, p.x, p.x.scalar_type()) : at::Tensor();
   const int rc = unlocked([&] {
@@ -387,7 +387,9 @@ PyObject* linear_bwd(PyObject* const* a) {
   tensor(a[0]);
   const int need_dx = truth(a[5]), need_dw = truth(a[6]), need_dbias = truth(a[7]);
   const Here here(p.x.device());
-  const size_t bytes = p_linear_bwd_workspace(p.rows, p.N, p.K, act, need_dx, need_dw, need_dbias);
+  dflare_product_plan plan{};
+  p_linear_plan(p.rows, p.N, p.K, act, need_dx, need_dw, need_dbias, nullptr, &plan);
+  const size_t bytes = plan.workspace;
   const auto type = p.x.scalar_type();
   const at::Tensor ws = scratch(bytes, p.x), dx = need_dx ? fresh(p.x.sizes(), p.x, type) : at::Tensor();
   const at::Tensor dw = need_dw ? fresh(p.w.sizes(), p.x, type) : at::Tensor(), dbias = need_dbias ? fresh({p.N}, p.x, type) : at::Tensor();
@@ -407,7 +409,9 @@ PyObject* gated_fwd(PyObject* const* a) {
   if (PyErr_Occurred()) return nullptr;
   const bool save = truth(a[4]);
   const Here here(p.x.device());
-  const size_t bytes = p_gated_fwd_workspace(p.rows, p.K, p.N);
+  dflare_product_plan plan{};
+  p_gated_plan(p.rows, p.K, p.N, 0, 0, &plan, nullptr);
+  const size_t bytes = plan.workspace;
   auto rows_of = [&] { return fresh({p.rows, p.N}, p.x, p.x.scalar_type()); };
   const at::Tensor ws = scratch(bytes, p.x), h = rows_of(), gate = save ? rows_of() : at::Tensor(), up = save ? rows_of() : at::Tensor();
   const int rc = unlocked([&] {
@@ -427,7 +431,9 @@ PyObject* gated_bwd(PyObject* const* a) {
   for (int k : {0, 2, 3, 5}) tensor(a[k]);
   const int need_dx = truth(a[7]), need_dw = truth(a[8]);
   const Here here(p.x.device());
-  const size_t bytes = p_gated_bwd_workspace(p.rows, p.K, p.N, need_dx, need_dw);
+  dflare_product_plan plan{};
+  p_gated_plan(p.rows, p.K, p.N, need_dx, need_dw, nullptr, &plan);
+  const size_t bytes = plan.workspace;
   const auto type = p.x.scalar_type();
   auto weights = [&] { return need_dw ? fresh(p.w.sizes(), p.x, type) : at::Tensor(); };
   const at::Tensor ws = scratch(bytes, p.x), dx = need_dx ? fresh(p.x.sizes(), p.x, type) : at::Tensor(), dg = weights(), du = weights();
@@ -516,15 +522,15 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
-constexpr int kBound = 21;
+constexpr int kBound = 19;
 // bind(addresses of the entry points in the order below, function from a device index to its current stream's address,
 // torch's out-of-memory exception)
 PyObject* bind(PyObject* const* a) {
   void** to[] = {(void**)&p_norm_fwd, (void**)&p_norm_bwd_workspace, (void**)&p_norm_bwd, (void**)&p_rope,
                  (void**)&p_grad_norm_workspace, (void**)&p_grad_norm, (void**)&p_clip_grads,
                  (void**)&p_qk_norm_rope_fwd, (void**)&p_qk_norm_rope_bwd_workspace, (void**)&p_qk_norm_rope_bwd,
-                 (void**)&p_linear_fwd_workspace, (void**)&p_linear_fwd, (void**)&p_linear_bwd_workspace, (void**)&p_linear_bwd,
-                 (void**)&p_gated_fwd_workspace, (void**)&p_gated_fwd, (void**)&p_gated_bwd_workspace, (void**)&p_gated_bwd, (void**)&p_adamw};
+                 (void**)&p_linear_plan, (void**)&p_linear_fwd, (void**)&p_linear_bwd, (void**)&p_gated_plan, (void**)&p_gated_fwd,
+                 (void**)&p_gated_bwd, (void**)&p_adamw};
   constexpr int n = sizeof(to) / sizeof(to[0]);
   static_assert(n + 2 == kBound);
   for (int k = 0; k < n; ++k) *to[k] = PyLong_AsVoidPtr(a[k]);

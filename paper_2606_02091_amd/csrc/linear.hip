@@ -694,8 +694,16 @@ constexpr long kPartValues = 1l << 25;  // and most sums of these together
 constexpr int kPreGroups = 2048;        // work-groups of k_pre, about
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
-// bytes of the parts of a product of `values` sums, at most (grows with them)
-size_t part_bytes(long values) { return up((size_t)std::min(kPartValues, kMostParts * values) * 4); }
+constexpr int kPartStages = 4;          // of a part, at least
+constexpr int kPartGroups = 2048;       // work-groups of a product in parts, at most
+// bytes of the parts of any product of up to `values` sums over up to `stages` of k: grows with all three.  Up to 64 rows the work-groups are
+// of tiles of 128 columns, and so there are 2^18 sums of a row at most.
+size_t part_bytes(int rows, long values, long stages) {
+  const long parts = std::min<long>(kMostParts, stages / kPartStages), sums = std::min(kPartValues, parts * values);
+  return parts < 2 ? 0 : up((size_t)(rows <= Few::TN ? std::min(sums, (long)rows * kPartGroups * Few::TM) : sums) * 4);
+}
+// and of those that a product is cut into
+size_t own_bytes(int parts, long values) { return parts < 2 ? 0 : up((size_t)values * parts * 4); }
 
 long over(long a, long b) { return (a + b - 1) / b; }
 // A product of `tiles` over `stages` of k, cut into parts of k, and its costs in us, fitted to 34 products and pairs of them under some 25
@@ -707,7 +715,7 @@ long over(long a, long b) { return (a + b - 1) / b; }
 struct Work {
   long tiles, values;
   int stages;
-  bool can(int k) const { return k == 1 || (stages >= 4 * k && values * k <= kPartValues); }
+  bool can(int k) const { return k == 1 || (stages >= kPartStages * k && values * k <= kPartValues); }
   double sums(int k) const { return k > 1 ? (double)values * k * 8 / 6.1e6 + 1.9 : 0.0; }
 };
 // When all work-groups have ended: nx that take ux each, then nw that take uw, each where a slot is free first
@@ -775,7 +783,7 @@ Plan plan_of(bool few, F&& f) {
     double low = cost_of(t, few, p.first, 1, p.second, 1);
     auto search = [&](const Work& own, int& k) {
       for (int n : numbers) {
-        if (!own.can(n) || (n > 1 && own.tiles * n > 2048)) break;
+        if (!own.can(n) || (n > 1 && own.tiles * n > kPartGroups)) break;
         const int was = k;
         k = n;
         const double c = cost_of(t, few, p.first, kx, p.second, kw);
@@ -807,6 +815,41 @@ int check(int rows, int N, int K, int act) {
 unsigned whole_turns(long groups) { return (unsigned)((groups + 7) / 8 * 8); }  // of the XCDs
 int stages_of(long k) { return (int)((k + kBK - 1) / kBK); }
 
+// What a call's products run on, and their parts.  split: rows before the halves
+struct Chosen {
+  int tiles, parts, parts_w, split;
+};
+constexpr int kFewRows = 32;
+Chosen forward_plan(int rows, int N, int K, int n2) {
+  if (rows <= kFewRows) return {DFLARE_TILES_NONE, 1, 1, rows};
+  auto work = [&](auto s) {
+    return std::make_pair(Work{over(N, s.TM / n2) * over(rows, s.TN), (long)rows * N * n2, stages_of(K)}, Work{0, 0, 0});
+  };
+  // up to 64 rows the small tile's other half would be empty
+  const bool few = rows <= Few::TN;
+  const Plan p = plan_of(few, [&](int t) { return few ? work(Few{}) : t == 0 ? work(Large{}) : work(Small{}); });
+  if (few || p.tile == 0) return {few ? DFLARE_TILES_64 : DFLARE_TILES_256, p.kx, 1, rows};
+  const int split = p.kx == 1 ? rows_before_halves(over(N, Small::TM / n2), rows) : rows;
+  return {split < rows ? DFLARE_TILES_128_64 : DFLARE_TILES_128, p.kx, 1, split};
+}
+long tiles_of_dx(long rows, long K, int tn, int tm) { return over(K, tm) * over(rows, tn); }
+long tiles_of_dw(long N, long K, int n2, int tn, int tm) { return over(K, tm) * over(N, tn) * n2; }
+// dx and dW, each where it is wanted
+Chosen gradients_plan(int rows, int N, int K, int n2, bool dx, bool dw) {
+  const bool few = rows <= Few::TN;
+  Chosen c{few ? DFLARE_TILES_64 : DFLARE_TILES_128, 1, 1, rows};
+  if (!rows || !(dx || dw)) return c;
+  auto work = [&](auto sx, auto sw) {
+    return std::make_pair(Work{dx ? tiles_of_dx(rows, K, sx.TN, sx.TM) : 0l, (long)rows * K, n2 * stages_of(N)},
+                          Work{dw ? tiles_of_dw(N, K, n2, sw.TN, sw.TM) : 0l, (long)n2 * N * K, stages_of(rows)});
+  };
+  const Plan p = plan_of(few, [&](int t) { return few ? work(Few{}, Small{}) : t == 0 ? work(Large{}, Large{}) : work(Small{}, Small{}); });
+  if (p.tile == 0) c.tiles = DFLARE_TILES_256;
+  if (dx) c.parts = p.kx;
+  if (dw) c.parts_w = p.kw;
+  return c;
+}
+
 // the parts' sums of a forward product, as y
 template <bool GATED>
 void finish(const Call& a, hipStream_t st) {
@@ -814,7 +857,6 @@ void finish(const Call& a, hipStream_t st) {
   const long threads = (long)a.rows * (a.N / 8);
   hipLaunchKernelGGL((k_finish<GATED>), dim3((unsigned)((threads + kT - 1) / kT)), dim3(kT), 0, st, a);
 }
-constexpr int kFewRows = 32;
 template <bool GATED>
 void forward_few(const Call& a, hipStream_t st) {
   auto go = [&](auto rt, auto t) {
@@ -826,56 +868,40 @@ void forward_few(const Call& a, hipStream_t st) {
   else wide ? go(int_c<2>{}, int_c<GATED ? 1 : 2>{}) : go(int_c<2>{}, int_c<1>{});
 }
 template <bool GATED>
-void forward(Call a, hipStream_t st) {
-  if (a.rows <= kFewRows) return forward_few<GATED>(a, st);
-  auto go = [&](auto s, long tiles) {
+void forward(Call a, const Chosen& c, hipStream_t st) {
+  a.parts = c.parts;
+  a.split = c.split;
+  auto go = [&](auto s) {
     using S = decltype(s);
+    const long tiles = over(a.N, S::TM / a.n2) * over(a.rows, S::TN);
     hipLaunchKernelGGL((k_forward<S, GATED>), dim3(whole_turns(tiles * a.parts)), dim3(S::T), 0, st, a);
     finish<GATED>(a, st);
   };
-  auto tiles = [&](auto s) { return over(a.N, s.TM / a.n2) * over(a.rows, s.TN); };
-  auto work = [&](long tiles) { return std::make_pair(Work{tiles, (long)a.rows * a.N * a.n2, stages_of(a.K)}, Work{0, 0, 0}); };
-  // up to 64 rows the small tile's other half would be empty
-  const bool few = a.rows <= Few::TN;
-  const Plan p = plan_of(few, [&](int t) { return work(few ? tiles(Few{}) : t == 0 ? tiles(Large{}) : tiles(Small{})); });
-  a.parts = p.kx;
   const long columns = over(a.N, Small::TM / a.n2);
-  if (!few && p.tile == 1 && a.parts == 1) {
-    a.split = rows_before_halves(columns, a.rows);
-    if (a.split < a.rows) {
-      a.groups_x = (int)whole_turns(columns * (a.split / Small::TN));
-      hipLaunchKernelGGL((k_forward_halves<GATED>), dim3(a.groups_x + whole_turns(columns * over(a.rows - a.split, Few::TN))), dim3(Small::T), 0, st, a);
-      return;
-    }
+  switch (c.tiles) {
+    case DFLARE_TILES_NONE: return forward_few<GATED>(a, st);
+    case DFLARE_TILES_64: return go(Few{});
+    case DFLARE_TILES_128: return go(Small{});
+    case DFLARE_TILES_256: return go(Large{});
   }
-  if (few) go(Few{}, tiles(Few{}));
-  else if (p.tile == 0) go(Large{}, tiles(Large{}));
-  else go(Small{}, tiles(Small{}));
+  a.groups_x = (int)whole_turns(columns * (a.split / Small::TN));
+  hipLaunchKernelGGL((k_forward_halves<GATED>), dim3(a.groups_x + whole_turns(columns * over(a.rows - a.split, Few::TN))), dim3(Small::T), 0, st, a);
 }
-// dx and dW, each where it is wanted, and the bias' gradient from `chunks` sums
-void gradients(Call a, const float* sums, int chunks, uint16_t* dbias, hipStream_t st) {
-  const bool few = a.rows <= Few::TN;
+// dx and dW, and the bias' gradient from `chunks` sums
+void gradients(Call a, const Chosen& c, const float* sums, int chunks, uint16_t* dbias, hipStream_t st) {
   const long one = (long)a.N * a.K;
-  auto tiles_x = [&](auto s) { return a.dx ? over(a.K, s.TM) * over(a.rows, s.TN) : 0l; };
-  auto tiles_w = [&](auto s) { return a.dw[0] ? over(a.K, s.TM) * over(a.N, s.TN) * a.n2 : 0l; };
-  auto work = [&](long tx, long tw) {
-    return std::make_pair(Work{tx, (long)a.rows * a.K, a.n2 * stages_of(a.N)}, Work{tw, a.n2 * one, stages_of(a.rows)});
-  };
-  a.parts = a.parts_w = 1;
+  a.parts = c.parts;
+  a.parts_w = c.parts_w;
   if (a.dx || a.dw[0]) {
-    const Plan p = plan_of(few, [&](int t) {
-      return few ? work(tiles_x(Few{}), tiles_w(Small{})) : t == 0 ? work(tiles_x(Large{}), tiles_w(Large{})) : work(tiles_x(Small{}), tiles_w(Small{}));
-    });
     auto go = [&](auto sx, auto sw) {
       using SX = decltype(sx);
       using SW = decltype(sw);
-      a.parts = a.dx ? p.kx : 1;
-      a.parts_w = a.dw[0] ? p.kw : 1;
-      a.groups_x = (int)whole_turns(tiles_x(sx) * a.parts);
-      hipLaunchKernelGGL((k_gradients<SX, SW>), dim3(a.groups_x + whole_turns(tiles_w(sw) * a.parts_w)), dim3(SX::T), 0, st, a);
+      a.groups_x = a.dx ? (int)whole_turns(tiles_of_dx(a.rows, a.K, SX::TN, SX::TM) * a.parts) : 0;
+      const long tiles = a.dw[0] ? tiles_of_dw(a.N, a.K, a.n2, SW::TN, SW::TM) : 0;
+      hipLaunchKernelGGL((k_gradients<SX, SW>), dim3(a.groups_x + whole_turns(tiles * a.parts_w)), dim3(SX::T), 0, st, a);
     };
-    if (few) go(Few{}, Small{});
-    else if (p.tile == 0) go(Large{}, Large{});
+    if (c.tiles == DFLARE_TILES_64) go(Few{}, Small{});
+    else if (c.tiles == DFLARE_TILES_256) go(Large{}, Large{});
     else go(Small{}, Small{});
   }
   Rest r{};
@@ -914,24 +940,31 @@ bool off16(std::initializer_list<const void*> ps) {
   return false;
 }
 
-struct BwdLayout {
+// A call's workspace.  d: n_d gradients of [rows, N]; sums of a bias' gradient; the products' parts
+struct Layout {
   size_t d, sums, part, part_w, total;
+  Layout(size_t d_bytes, size_t sum_bytes, size_t x_bytes, size_t w_bytes)
+      : d(0), sums(d_bytes), part(sums + sum_bytes), part_w(part + x_bytes), total(std::max<size_t>(part_w + w_bytes, 256)) {}
 };
-// d: n_d gradients of [rows, N]; sums of a bias' gradient; the products' parts
-BwdLayout bwd_layout(int rows, int N, int K, int n2, int n_d, bool sums, bool dx, bool dw) {
-  BwdLayout L{};
-  size_t o = 0;
-  L.d = o;
-  o += n_d * up((size_t)rows * N * 2);
-  L.sums = o;
-  // (pre_chunks' at most, but growing with N)
-  if (sums) o += up((size_t)std::min(std::max(over(rows, 4), 1l) * N, kPreGroups * 8l * kT) * 4);
-  L.part = o;
-  if (dx) o += part_bytes((long)rows * K);
-  L.part_w = o;
-  if (dw) o += part_bytes((long)n2 * N * K);
-  L.total = std::max<size_t>(o, 256);
-  return L;
+Layout forward_layout(const Chosen& c, int rows, int N, int n2) { return Layout(0, 0, own_bytes(c.parts, (long)rows * N * n2), 0); }
+Layout backward_layout(const Chosen& c, int rows, int N, int K, int n2, int n_d, bool sums) {
+  return Layout(n_d * up((size_t)rows * N * 2), sums ? up((size_t)pre_chunks(rows, N, true) * N * 4) : 0, own_bytes(c.parts, (long)rows * K),
+                own_bytes(c.parts_w, (long)n2 * N * K));
+}
+// what any call of up to these sizes takes: grows with each of them
+size_t forward_most(int rows, int N, int K, int n2) {
+  return Layout(0, 0, rows <= kFewRows ? 0 : part_bytes(rows, (long)rows * N * n2, stages_of(K)), 0).total;
+}
+size_t backward_most(int rows, int N, int K, int n2, int n_d, bool sums, bool dx, bool dw) {
+  // (sums: pre_chunks' at most, but growing with N)
+  return Layout(n_d * up((size_t)rows * N * 2),
+                sums ? up((size_t)std::min(std::max(over(rows, 4), 1l) * N, kPreGroups * 8l * kT) * 4) : 0,
+                dx ? part_bytes(rows, (long)rows * K, (long)n2 * stages_of(N)) : 0,
+                dw ? part_bytes(INT_MAX, (long)n2 * N * K, stages_of(rows)) : 0)
+      .total;
+}
+void describe(const Chosen& c, const Layout& L, dflare_product_plan* to) {
+  *to = dflare_product_plan{c.tiles, c.parts, c.parts_w, c.split, L.total};
 }
 // zeros by a kernel (a memset node of a captured graph is not relied upon)
 __global__ __launch_bounds__(kT) void k_zero(u32x4* p, long n) {
@@ -951,7 +984,7 @@ using namespace dflare;
 extern "C" {
 
 size_t dflare_linear_fwd_workspace(int32_t rows, int32_t N, int32_t K) {
-  return check(rows, N, K, 0) == DFLARE_OK ? std::max<size_t>(part_bytes((long)rows * N), 256) : 0;
+  return check(rows, N, K, 0) == DFLARE_OK ? forward_most(rows, N, K, 1) : 0;
 }
 
 int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, int32_t rows, int32_t N, int32_t K, int32_t act,
@@ -959,8 +992,9 @@ int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void
   int rc = check(rows, N, K, act);
   if (rc != DFLARE_OK) return rc;
   if (!w || !workspace || (rows > 0 && (!x || !y))) return DFLARE_ERR_INVALID_ARG;
-  if (off16({x, w, bias, residual, y, z, workspace}) || workspace_bytes < dflare_linear_fwd_workspace(rows, N, K)) return DFLARE_ERR_INVALID_ARG;
-  const size_t xb = (size_t)rows * K * 2, wb = (size_t)N * K * 2, yb = (size_t)rows * N * 2, ws = dflare_linear_fwd_workspace(rows, N, K);
+  const Chosen c = forward_plan(rows, N, K, 1);
+  const size_t xb = (size_t)rows * K * 2, wb = (size_t)N * K * 2, yb = (size_t)rows * N * 2, ws = forward_layout(c, rows, N, 1).total;
+  if (off16({x, w, bias, residual, y, z, workspace}) || workspace_bytes < ws) return DFLARE_ERR_INVALID_ARG;
   if (!apart({{y, yb}, {z, yb}, {workspace, ws}}, {{x, xb}, {w, wb}, {bias, (size_t)N * 2}}) ||
       !apart({{z, yb}, {workspace, ws}}, {{residual, yb}}) || !same_or_apart(y, residual, yb))
     return DFLARE_ERR_INVALID_ARG;
@@ -979,13 +1013,13 @@ int dflare_linear_fwd(const void* x, const void* w, const void* bias, const void
   a.K = K;
   a.n2 = 1;
   a.act = act;
-  forward<false>(a, (hipStream_t)stream);
+  forward<false>(a, c, (hipStream_t)stream);
   return launched();
 }
 
 size_t dflare_linear_bwd_workspace(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias) {
   if (check(rows, N, K, act) != DFLARE_OK) return 0;
-  return bwd_layout(rows, N, K, 1, act != DFLARE_ACT_NONE, dbias != 0, dx != 0, dw != 0).total;
+  return backward_most(rows, N, K, 1, act != DFLARE_ACT_NONE, dbias != 0, dx != 0, dw != 0);
 }
 
 int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* z, int32_t rows, int32_t N, int32_t K, int32_t act, void* dx,
@@ -995,7 +1029,8 @@ int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* 
   const bool named = act != DFLARE_ACT_NONE;
   if (!workspace || (rows > 0 && (!dy || (named && !z) || (dx && !w) || (dw && !x)))) return DFLARE_ERR_INVALID_ARG;
   if (off16({dy, x, w, z, dx, dw, dbias, workspace})) return DFLARE_ERR_INVALID_ARG;
-  const BwdLayout L = bwd_layout(rows, N, K, 1, named, dbias != nullptr, dx != nullptr, dw != nullptr);
+  const Chosen c = gradients_plan(rows, N, K, 1, dx != nullptr, dw != nullptr);
+  const Layout L = backward_layout(c, rows, N, K, 1, named, dbias != nullptr);
   if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
   const size_t xb = (size_t)rows * K * 2, wb = (size_t)N * K * 2, yb = (size_t)rows * N * 2;
   if (!apart({{dx, xb}, {dw, wb}, {dbias, (size_t)N * 2}, {workspace, L.total}},
@@ -1034,12 +1069,41 @@ int dflare_linear_bwd(const void* dy, const void* x, const void* w, const void* 
     p.chunks = chunks;
     pre_gradients<false>(p, st);
   }
-  gradients(a, (const float*)(ws + L.sums), chunks, (uint16_t*)dbias, st);
+  gradients(a, c, (const float*)(ws + L.sums), chunks, (uint16_t*)dbias, st);
   return launched();
 }
 
+int dflare_linear_plan(int32_t rows, int32_t N, int32_t K, int32_t act, int32_t dx, int32_t dw, int32_t dbias, dflare_product_plan* fwd,
+                       dflare_product_plan* bwd) {
+  const int rc = check(rows, N, K, act);
+  if (rc != DFLARE_OK) return rc;
+  if (fwd) {
+    const Chosen c = forward_plan(rows, N, K, 1);
+    describe(c, forward_layout(c, rows, N, 1), fwd);
+  }
+  if (bwd) {
+    const Chosen c = gradients_plan(rows, N, K, 1, dx != 0, dw != 0);
+    describe(c, backward_layout(c, rows, N, K, 1, act != DFLARE_ACT_NONE, dbias != 0), bwd);
+  }
+  return DFLARE_OK;
+}
+
+int dflare_gated_plan(int32_t rows, int32_t H, int32_t F, int32_t dx, int32_t dw, dflare_product_plan* fwd, dflare_product_plan* bwd) {
+  const int rc = check(rows, F, H, 0);
+  if (rc != DFLARE_OK) return rc;
+  if (fwd) {
+    const Chosen c = forward_plan(rows, F, H, 2);
+    describe(c, forward_layout(c, rows, F, 2), fwd);
+  }
+  if (bwd) {
+    const Chosen c = gradients_plan(rows, F, H, 2, dx != 0, dw != 0);
+    describe(c, backward_layout(c, rows, F, H, 2, 2, false), bwd);
+  }
+  return DFLARE_OK;
+}
+
 size_t dflare_gated_fwd_workspace(int32_t rows, int32_t H, int32_t F) {
-  return check(rows, F, H, 0) == DFLARE_OK ? std::max<size_t>(part_bytes(2l * rows * F), 256) : 0;
+  return check(rows, F, H, 0) == DFLARE_OK ? forward_most(rows, F, H, 2) : 0;
 }
 
 int dflare_gated_fwd(const void* x, const void* w_gate, const void* w_up, int32_t rows, int32_t H, int32_t F, int32_t act, void* h, void* gate,
@@ -1047,9 +1111,11 @@ int dflare_gated_fwd(const void* x, const void* w_gate, const void* w_up, int32_
   int rc = check(rows, F, H, act);
   if (rc != DFLARE_OK) return rc;
   if (!w_gate || !w_up || !workspace || (rows > 0 && (!x || !h)) || !gate != !up) return DFLARE_ERR_INVALID_ARG;
-  if (off16({x, w_gate, w_up, h, gate, up, workspace}) || workspace_bytes < dflare_gated_fwd_workspace(rows, H, F)) return DFLARE_ERR_INVALID_ARG;
+  const Chosen c = forward_plan(rows, F, H, 2);
+  const size_t ws = forward_layout(c, rows, F, 2).total;
+  if (off16({x, w_gate, w_up, h, gate, up, workspace}) || workspace_bytes < ws) return DFLARE_ERR_INVALID_ARG;
   const size_t xb = (size_t)rows * H * 2, wb = (size_t)F * H * 2, yb = (size_t)rows * F * 2;
-  if (!apart({{h, yb}, {gate, yb}, {up, yb}, {workspace, dflare_gated_fwd_workspace(rows, H, F)}}, {{x, xb}, {w_gate, wb}, {w_up, wb}}))
+  if (!apart({{h, yb}, {gate, yb}, {up, yb}, {workspace, ws}}, {{x, xb}, {w_gate, wb}, {w_up, wb}}))
     return DFLARE_ERR_INVALID_ARG;
   if (rows == 0) return DFLARE_OK;
   if ((rc = stream_ok(stream)) != DFLARE_OK) return rc;
@@ -1066,12 +1132,12 @@ int dflare_gated_fwd(const void* x, const void* w_gate, const void* w_up, int32_
   a.K = H;
   a.n2 = 2;
   a.act = act;
-  forward<true>(a, (hipStream_t)stream);
+  forward<true>(a, c, (hipStream_t)stream);
   return launched();
 }
 
 size_t dflare_gated_bwd_workspace(int32_t rows, int32_t H, int32_t F, int32_t dx, int32_t dw) {
-  return check(rows, F, H, 0) == DFLARE_OK ? bwd_layout(rows, F, H, 2, 2, false, dx != 0, dw != 0).total : 0;
+  return check(rows, F, H, 0) == DFLARE_OK ? backward_most(rows, F, H, 2, 2, false, dx != 0, dw != 0) : 0;
 }
 
 int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void* up_, const void* w_gate, const void* w_up, int32_t rows,
@@ -1082,7 +1148,8 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
   if (!workspace || !dw_gate != !dw_up) return DFLARE_ERR_INVALID_ARG;
   if (rows > 0 && (!dh || !gate || !up_ || (dx && (!w_gate || !w_up)) || (dw_gate && !x))) return DFLARE_ERR_INVALID_ARG;
   if (off16({dh, x, gate, up_, w_gate, w_up, dx, dw_gate, dw_up, workspace})) return DFLARE_ERR_INVALID_ARG;
-  const BwdLayout L = bwd_layout(rows, F, H, 2, 2, false, dx != nullptr, dw_gate != nullptr);
+  const Chosen c = gradients_plan(rows, F, H, 2, dx != nullptr, dw_gate != nullptr);
+  const Layout L = backward_layout(c, rows, F, H, 2, 2, false);
   if (workspace_bytes < L.total) return DFLARE_ERR_INVALID_ARG;
   const size_t xb = (size_t)rows * H * 2, wb = (size_t)F * H * 2, yb = (size_t)rows * F * 2;
   if (!apart({{dx, xb}, {dw_gate, wb}, {dw_up, wb}, {workspace, L.total}},
@@ -1122,7 +1189,7 @@ int dflare_gated_bwd(const void* dh, const void* x, const void* gate, const void
   a.d[0] = p.d[0];
   a.d[1] = p.d[1];
   if (dx || dw_gate) pre_gradients<true>(p, st);
-  gradients(a, nullptr, 0, nullptr, st);
+  gradients(a, c, nullptr, 0, nullptr, st);
   return launched();
 }
 

@@ -38,6 +38,7 @@ EXPORTED = (
     "dflare_clip_grads", "dflare_qk_norm_rope_fwd", "dflare_qk_norm_rope_bwd_workspace", "dflare_qk_norm_rope_bwd",
     "dflare_linear_fwd_workspace", "dflare_linear_fwd", "dflare_linear_bwd_workspace", "dflare_linear_bwd",
     "dflare_gated_fwd_workspace", "dflare_gated_fwd", "dflare_gated_bwd_workspace", "dflare_gated_bwd", "dflare_adamw",
+    "dflare_linear_plan", "dflare_gated_plan",
 )
 K_QKV, K_ATTN, K_O, K_GATE_UP, K_DOWN, K_LM_HEAD, K_FUSE, K_KV_T, K_DRAFT = range(1, 10)
 (K_B_QKV, K_B_ATTN, K_B_O, K_B_GATE_UP, K_B_DOWN, K_B_LM_HEAD, K_B_KV_T, K_B_EPI, K_B_FUSE, K_B_DRAFT,
@@ -89,6 +90,10 @@ class dflare_qk_grad(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dy", "dx", "gain", "dgain")] + [
         (n, ctypes.c_int64) for n in ("x_row", "x_head", "dy_row", "dy_head", "dx_row", "dx_head")] + [
         ("n_heads", ctypes.c_int32)]
+
+
+class dflare_product_plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tiles", "parts", "parts_w", "split")] + [("workspace", ctypes.c_size_t)]
 
 
 class dflare_adamw_tensor(ctypes.Structure):
@@ -173,6 +178,8 @@ def lib() -> ctypes.CDLL:
         "dflare_gated_fwd": ([vp] * 3 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
         "dflare_gated_bwd_workspace": ([i32] * 5, ctypes.c_size_t),
         "dflare_gated_bwd": ([vp] * 6 + [i32] * 4 + [vp] * 4 + [ctypes.c_size_t, vp], ctypes.c_int),
+        "dflare_linear_plan": ([i32] * 7 + [ctypes.POINTER(dflare_product_plan)] * 2, ctypes.c_int),
+        "dflare_gated_plan": ([i32] * 5 + [ctypes.POINTER(dflare_product_plan)] * 2, ctypes.c_int),
         "dflare_adamw": ([vp, i32, vp, vp], ctypes.c_int),
         "dflare_context_len_seq": ([vp, i32, ctypes.POINTER(i32)], ctypes.c_int),
         "dflare_debug_read_seq": ([vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
@@ -200,8 +207,8 @@ def _native():
         loader.exec_module(mod)
         mod.bind(*(ctypes.cast(getattr(lib(), "dflare_" + f), ctypes.c_void_p).value for f in (
             "norm_fwd", "norm_bwd_workspace", "norm_bwd", "rope", "grad_norm_workspace", "grad_norm", "clip_grads",
-            "qk_norm_rope_fwd", "qk_norm_rope_bwd_workspace", "qk_norm_rope_bwd", "linear_fwd_workspace", "linear_fwd",
-            "linear_bwd_workspace", "linear_bwd", "gated_fwd_workspace", "gated_fwd", "gated_bwd_workspace", "gated_bwd", "adamw")),
+            "qk_norm_rope_fwd", "qk_norm_rope_bwd_workspace", "qk_norm_rope_bwd", "linear_plan", "linear_fwd", "linear_bwd",
+            "gated_plan", "gated_fwd", "gated_bwd", "adamw")),
                  _current_raw, torch.OutOfMemoryError)
         _binding = mod
     return _binding
@@ -596,6 +603,7 @@ def qk_norm_rope_bwd(dy, x, gain, inv_freq: torch.Tensor, positions=None, B: int
 
 
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
+TILES_NONE, TILES_64, TILES_128, TILES_128_64, TILES_256 = range(5)
 
 
 def linear_fwd(x, w, bias=None, residual=None, act: int = ACT_NONE, save: bool = False, stream=None):

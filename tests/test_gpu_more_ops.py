@@ -1152,3 +1152,27 @@ def test_adamw_leaves_out_a_step_whose_number_or_rate_is_none(bits, step, lr):
     dfl.adamw(ps, grads, m, v, at, rate, masters=w, m_scales=ms, v_scales=vs)
     dfl.adamw(other[0], grads, other[1], other[2], 2, 1e-2, masters=other[5], m_scales=other[3], v_scales=other[4])
     assert all(same(a, b) for a, b in zip(state, other) if a is not None) and not same(state[0], before[0])
+
+
+@pytest.mark.parametrize("rows,N,K", [(5, 264, 520), (63, 264, 2056), (300, 520, 2056), (1000, 72, 4096)])
+def test_products_stay_inside_the_workspace_of_their_plan(rows, N, K):
+    """A workspace of just the plan's bytes between others that stay; the results do not hang on what lay in it."""
+    lib, st = dfl.lib(), torch.cuda.current_stream().cuda_stream
+    x, w, u, dy = randn((rows, K), seed=1), randn((N, K), seed=2, std=K ** -0.5), randn((N, K), seed=3, std=K ** -0.5), randn((rows, N), seed=4)
+    y, z = dfl.linear_fwd(x, w, act=dfl.ACT_SILU, save=True)
+    h, gate, up = dfl.gated_fwd(x, w, u, save=True)
+    want = [(y,), dfl.linear_bwd(dy, x, w, z, act=dfl.ACT_SILU, need_dbias=True), (h,), dfl.gated_bwd(dy, x, gate, up, w, u)]
+    plan = [dfl.dflare_product_plan() for _ in range(4)]
+    assert lib.dflare_linear_plan(rows, N, K, 2, 1, 1, 1, plan[0], plan[1]) == lib.dflare_gated_plan(rows, K, N, 1, 1, plan[2], plan[3]) == dfl.OK
+    for k, p in enumerate(plan):
+        n = p.workspace
+        buf = torch.full((n + 8192,), 255, dtype=torch.uint8, device="cuda")  # (NaN as fp32 and as bf16)
+        ws, got = buf.data_ptr() + 4096, [torch.empty_like(t) for t in want[k]]
+        o = [t.data_ptr() for t in got]
+        rc = (lambda: lib.dflare_linear_fwd(x.data_ptr(), w.data_ptr(), None, None, rows, N, K, 2, o[0], None, ws, n, st),
+              lambda: lib.dflare_linear_bwd(dy.data_ptr(), x.data_ptr(), w.data_ptr(), z.data_ptr(), rows, N, K, 2, *o, ws, n, st),
+              lambda: lib.dflare_gated_fwd(x.data_ptr(), w.data_ptr(), u.data_ptr(), rows, K, N, 2, o[0], None, None, ws, n, st),
+              lambda: lib.dflare_gated_bwd(dy.data_ptr(), x.data_ptr(), gate.data_ptr(), up.data_ptr(), w.data_ptr(), u.data_ptr(), rows, K, N,
+                                           2, *o, ws, n, st))[k]()
+        assert rc == dfl.OK and same(got, want[k]), k
+        assert (buf[:4096] == 255).all() and (buf[4096 + n:] == 255).all(), k

@@ -241,3 +241,58 @@ def test_binding_refuses_what_is_not_on_a_device():
     assert dfl.adamw([], [], [], [], 1, 0.1) is None
     m, v, ms, vs = dfl.adamw_state([torch.zeros(3, 100), torch.zeros(0)], 8)
     assert m[0].shape == (3, 100) and m[0].dtype == torch.float8_e4m3fn and ms[0].shape == (2,) and vs[1].shape == (0,)
+
+
+def plans(kind, rows, N, K, act=2, dx=1, dw=1, dbias=1):
+    """(forward, backward) plan of a projection or the gated block."""
+    L, fwd, bwd = dfl.lib(), dfl.dflare_product_plan(), dfl.dflare_product_plan()
+    rc = (L.dflare_linear_plan(rows, N, K, act, dx, dw, dbias, fwd, bwd) if kind == "linear" else
+          L.dflare_gated_plan(rows, K, N, dx, dw, fwd, bwd))
+    assert rc == OK
+    return fwd, bwd
+
+
+def test_workspace_of_a_call_is_what_its_plan_takes():
+    L = dfl.lib()
+    # none for what has no parts: few rows, and more values than parts may have
+    for rows, N, K in ((1, 4096, 4096), (16, 12288, 4096), (32, 6144, 2560), (8192, 12288, 4096)):
+        assert plans("linear", rows, N, K)[0].workspace == plans("gated", rows, N, K)[0].workspace == 256
+    assert L.dflare_linear_fwd_workspace(32, 6144, 2560) == L.dflare_gated_fwd_workspace(16, 4096, 12288) == 256
+    assert plans("gated", 8192, 12288, 4096)[1].workspace == 2 * 8192 * 12288 * 2  # (dgate and dup)
+    rng = np.random.default_rng(5)
+    for _ in range(3000):
+        rows, N, K = int(2 ** rng.uniform(0, 14)), 8 * int(2 ** rng.uniform(0, 11)), 8 * int(2 ** rng.uniform(0, 11))
+        act, dx, dw, dbias = (int(v) for v in (rng.integers(0, 2) * 2, *rng.integers(0, 2, 3)))
+        up = lambda n: -(-n // 256) * 256  # noqa: E731
+        for kind, n2 in (("linear", 1), ("gated", 2)):
+            f, b = plans(kind, rows, N, K, act, dx, dw, dbias)
+            assert f.workspace == max(256, up(rows * N * n2 * f.parts * 4) if f.parts > 1 else 0) and f.parts_w == 1
+            d = n2 if n2 == 2 or act else 0
+            sums = max(1, min(-(-rows // 4), 2048 // -(-N // 2048))) * N * 4 if n2 == 1 and dbias else 0
+            assert b.workspace == max(256, d * up(rows * N * 2) + up(sums) + (up(rows * K * b.parts * 4) if b.parts > 1 else 0) + (
+                up(n2 * N * K * b.parts_w * 4) if b.parts_w > 1 else 0))
+            assert (dx or b.parts == 1) and (dw or b.parts_w == 1)
+            most = ((L.dflare_linear_fwd_workspace(rows, N, K), L.dflare_linear_bwd_workspace(rows, N, K, act, dx, dw, dbias)) if n2 == 1 else
+                    (L.dflare_gated_fwd_workspace(rows, K, N), L.dflare_gated_bwd_workspace(rows, K, N, dx, dw)))
+            assert f.workspace <= most[0] and b.workspace <= most[1]
+
+
+def test_plans_of_sizes_that_are_refused():
+    L, p = dfl.lib(), dfl.dflare_product_plan()
+    for kw, code in ((dict(rows=-1), INV), (dict(N=0), INV), (dict(N=12), UNS), (dict(K=12), UNS), (dict(N=1 << 18, K=1 << 18), UNS)):
+        a = {**dict(rows=40, N=136, K=64), **kw}
+        assert L.dflare_linear_plan(a["rows"], a["N"], a["K"], 0, 1, 1, 1, p, p) == L.dflare_gated_plan(a["rows"], a["K"], a["N"], 1, 1, p, p) == code
+    assert L.dflare_linear_plan(40, 136, 64, 5, 1, 1, 1, p, p) == INV
+    assert L.dflare_linear_plan(40, 136, 64, 0, 1, 1, 1, None, None) == L.dflare_gated_plan(40, 64, 136, 1, 1, None, None) == OK
+
+
+def test_products_refuse_a_byte_less_than_their_plan():
+    for rows, N, K in ((40, 136, 64), (64, 1032, 2056), (1000, 72, 4096)):
+        (lf, lb), (gf, gb) = plans("linear", rows, N, K), plans("gated", rows, N, K)
+        far = [(i + 1) << 44 for i in range(10)]
+        for k, ws in enumerate((lf, lb, gf, gb)):
+            call = (lambda n: lin(rows, N, K, 2, *far[:7], n), lambda n: lin_bwd(rows, N, K, 2, *far[:8], n),
+                    lambda n: gate(rows, K, N, 2, *far[:7], n), lambda n: gate_bwd(rows, K, N, 2, *far[:10], n))[k]
+            assert call(ws.workspace - 1) == INV, (rows, N, K, k)
+            if not torch.cuda.is_available():
+                assert call(ws.workspace) == dfl.ERR_HIP, (rows, N, K, k)
