@@ -11,6 +11,7 @@ import pytest
 import torch
 
 from paper_2606_02091_amd import dflare as dfl
+from product_shapes import WAYS
 
 pytestmark = pytest.mark.gpu
 
@@ -1176,3 +1177,64 @@ def test_products_stay_inside_the_workspace_of_their_plan(rows, N, K):
                                            2, *o, ws, n, st))[k]()
         assert rc == dfl.OK and same(got, want[k]), k
         assert (buf[:4096] == 255).all() and (buf[4096 + n:] == 255).all(), k
+
+
+@pytest.mark.parametrize("kind,rows,N,K,fwd,bwd", WAYS)
+def test_products_on_each_of_their_ways(kind, rows, N, K, fwd, bwd):
+    """Every tile, whole and in parts, with each epilogue; and both gradients beside one of them alone."""
+    print(f"[more ops] {kind} {(rows, N, K, fwd, bwd)}", flush=True)
+    x, w, dy = randn((rows, K), seed=1), randn((N, K), seed=2, std=K ** -0.5), randn((rows, N), seed=4)
+    if kind == "linear":
+        res, bias = randn((rows, N), seed=5), randn((N,), seed=6)
+        for act, b, r, save in (("none", None, None, False), ("none", bias, None, True), ("none", None, res, False), ("silu", bias, None, True),
+                                ("gelu", None, res, True)):
+            code = ACTS[act]
+            y, z = dfl.linear_fwd(x, w, b, residual=r, act=code, save=save)
+            grads = dfl.linear_bwd(dy, x, w, z, act=code, need_dbias=b is not None)
+            linear_check(x, w, b, r, act, dy, y, z, *grads)
+            for part in ((True, False), (False, True)):
+                one = dfl.linear_bwd(dy, x, w, z, act=code, need_dx=part[0], need_dw=part[1])
+                linear_check(x, w, b, r, act, dy, y, z, *one)
+        return
+    u = randn((N, K), seed=3, std=K ** -0.5)
+    for act, save in (("silu", True), ("none", True), ("gelu_tanh", False)):
+        h, gate, up = dfl.gated_fwd(x, w, u, act=ACTS[act], save=save)
+        if not save:
+            gated_check(x, w, u, act, None, h, gate, up, None, None, None)
+            continue
+        gated_check(x, w, u, act, dy, h, gate, up, *dfl.gated_bwd(dy, x, gate, up, w, u, act=ACTS[act]))
+        for part in ((True, False), (False, True)):
+            one = dfl.gated_bwd(dy, x, gate, up, w, u, act=ACTS[act], need_dx=part[0], need_dw=part[1])
+            gated_check(x, w, u, act, dy, h, gate, up, *one)
+
+
+@pytest.mark.parametrize("half", [True, False])
+def test_qk_norm_rope_of_work_groups_that_take_many_rows(half):
+    """Each work-group walks a part of the heads with many fills of its table: distinct rows, checked around the ends of the parts of
+    any number of work-groups up to those of a launch, and the gains' gradients over all of them."""
+    rows, hd, B = 70_001, 512, 7
+    x, dy = randn((rows, 1, hd), seed=1), randn((rows, 1, hd), seed=2)
+    gain = randn((hd,), seed=3, mean=1.0, std=0.3)
+    freq, _ = dfl.rope_frequencies(hd, 1e6)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    starts = torch.randint(0, 100_000, (-(-rows // B),), generator=g, device="cuda", dtype=torch.int32)
+    kw = dict(B=B, layout=dfl.ROPE_HALF if half else dfl.ROPE_INTERLEAVED)
+    y, (dx, dgain) = dfl.qk_norm_rope_fwd(x, gain, freq, starts, **kw), dfl.qk_norm_rope_bwd(dy, x, gain, freq, starts, **kw)
+    pos = starts.repeat_interleave(B)[:rows].long() + torch.arange(rows, device="cuda") % B
+    for first in range(0, rows, 10_000):  # (all rows, some at a time)
+        at = slice(first, min(first + 10_000, rows))
+        u = x[at].double()
+        n = u * (u.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+        want, size = turned(n * gain.double(), pos[at], freq, half, 1.0)
+        k = (hd + 32) * U
+        within(y[at], want, 1.01 * (HALF[BF] * want.abs() + k * size) + 1e-38, "y")
+        d, size = turned(dy[at].double(), pos[at], freq, half, 1.0, inverse=True)
+        part, terms = (d * n).sum((0, 1)), (size * n.abs()).sum((0, 1))
+        total, sizes = (part, terms) if first == 0 else (total + part, sizes + terms)
+        e, es = d * gain.double(), size * gain.double().abs()
+        rstd = (u.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+        want = rstd * (e - n * (e * n).mean(-1, keepdim=True))
+        err = es + n.abs() * (es * n.abs()).mean(-1, keepdim=True)
+        within(dx[at], want, 1.01 * (HALF[BF] * want.abs() + 2 * k * rstd * err) + 1e-38, "dx")
+    # (no chain of additions is longer than 4,160 of them: see qk_check)
+    within(dgain, total, ((hd + 32) * U + 4160 * U) * sizes + 1e-38, "dgain")

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2606_02091_amd import dflare as dfl
+from product_shapes import WAYS
 
 INV, UNS, OK = dfl.ERR_INVALID_ARG, dfl.ERR_UNSUPPORTED, dfl.OK
 INF, NAN = float("inf"), float("nan")
@@ -296,3 +297,24 @@ def test_products_refuse_a_byte_less_than_their_plan():
             assert call(ws.workspace - 1) == INV, (rows, N, K, k)
             if not torch.cuda.is_available():
                 assert call(ws.workspace) == dfl.ERR_HIP, (rows, N, K, k)
+
+
+@pytest.mark.parametrize("kind,rows,N,K,fwd,bwd", WAYS)
+def test_products_take_the_ways_that_are_tested(kind, rows, N, K, fwd, bwd):
+    f, b = plans(kind, rows, N, K)
+    assert (f.tiles, f.parts > 1) == fwd and (b.tiles, b.parts > 1, b.parts_w > 1) == bwd
+
+
+def test_every_way_of_a_product_is_among_the_tested_ones():
+    """Of sizes over the whole range none takes another kernel, or the same one in parts where only its whole is tested."""
+    rng = np.random.default_rng(11)
+    ways = {(kind, *w) for kind, _, _, _, fwd, bwd in WAYS for w in (fwd, bwd)}
+    # (a gradient that is not cut beside one that is takes what it takes beside one that is not)
+    halves = {(kind, t, k, cut) for kind, t, *cuts in ways if len(cuts) == 2 for k, cut in enumerate(cuts)}
+    for _ in range(4000):
+        rows, N, K = int(2 ** rng.uniform(0, 14)), 8 * int(2 ** rng.uniform(0, 11)), 8 * int(2 ** rng.uniform(0, 11))
+        for kind in ("linear", "gated"):
+            f, b = plans(kind, rows, N, K)
+            assert (f.tiles == dfl.TILES_NONE) == (rows <= 32)
+            assert rows <= 32 or (kind, f.tiles, f.parts > 1) in ways, (kind, rows, N, K)
+            assert {(kind, b.tiles, 0, b.parts > 1), (kind, b.tiles, 1, b.parts_w > 1)} <= halves, (kind, rows, N, K)
