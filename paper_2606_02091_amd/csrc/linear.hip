@@ -123,7 +123,8 @@ __device__ __forceinline__ void part_of(int stages, int parts, int ks, int& s0, 
   s1 = (int)((long)stages * (ks + 1) / parts);
 }
 
-// the stage of k that a work-group begins with: another one on each XCD
+// the stage of k that a work-group begins with: another one on each XCD, whose requests then meet fewer others for the same lines (from k = 0
+// on all of them, by turns over 12 products of 2,048 and 8,192 rows: 1.4% faster to 1.9% slower)
 __device__ __forceinline__ int first_stage(int kn) { return (int)(blockIdx.x % 8) * (kn / kBK) / 8; }
 
 // 4 values as bf16 into LDS rows of TMO values; piece p of row n at p ^ (n mod the pieces)
@@ -133,7 +134,8 @@ __device__ __forceinline__ void put4(char* lds, int n, int p, int h, f32x4 v) {
       make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
 }
 // and from there, 16 bytes at a time, to to(row, piece) where that is not null.  The large tile's are streamed: there are many of
-// them, and the operands keep their places in L2 (8,192 rows x 4,096 x 12,288 gated with three outputs 1,297 -> 1,250 us).
+// them, and the operands keep their places in L2 (8,192 rows gated with three outputs, the two by turns:
+// x 4,096 x 12,288 1,332 -> 1,305 us, x 4,096 x 4,096 447 -> 431).
 template <typename S, int TMO, typename F>
 __device__ __forceinline__ void take(const char* lds, F&& to) {
   constexpr int P = TMO / 8, RW = S::TN / S::W;
@@ -314,7 +316,8 @@ __global__ __launch_bounds__(Small::T, 2) void k_forward_halves(Call a) {
 }
 
 // ---- the same for up to 32 rows, bound by the way of W from memory (16 rows x 4,096 x 12,288 gated: 37 us, on tiles of 128 x 64 with parts
-// of k and their sums 41; 4,096 x 4,096: 9.0 and 13.4; 33 to 64 rows are faster on tiles).  A work-group per CU walks tiles of 16 T rows of each matrix.
+// of k and their sums 41; 4,096 x 4,096: 9.0 and 13.4; for more than 32 rows LDS does
+// not hold two stages of such rings, but of one matrix for up to 48).  A work-group per CU walks tiles of 16 T rows of each matrix.
 // Its eight waves take a part of k each, all of it through rings of NS stages of 64 k in LDS that are a wave's own, so that none
 // waits for another while a tile lasts and the stages of the next tile are on their way at the end of one.  There the waves' sums
 // meet in LDS, in order. ----

@@ -263,7 +263,7 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     step(f1, f0, buf, 2);
     step(f0, f1, buf, 3);
     // in the midst of the stage's last products: the next stage is here, and all waves have read this one, whose
-    // buffer takes the one after the next (after a quarter of them on the large tile: dx and dW 1% faster than after half)
+    // buffer takes the one after the next (after a quarter of them on the large tile: at 8,192 rows, by turns, 0.2 to 3.4% faster than after half)
     constexpr int B = MASK && Q > 4 ? Q / 4 : Q / 2;
 #pragma unroll
     for (int n = 0; n < Q; ++n) {

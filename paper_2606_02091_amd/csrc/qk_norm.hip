@@ -169,7 +169,8 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
-// 1 / sqrt(sum / hd + eps).  The card's root takes numbers below 2^-126 for zero.  BARE: eps is below 2^-90 and does not keep from them, so
+// 1 / sqrt(sum / hd + eps), to a unit in the last place (fp32 heads come out 2e-7 off in the 2-norm, with a correctly rounded root
+// 1e-7).  The card's root takes numbers below 2^-126 for zero.  BARE: eps is below 2^-90 and does not keep from them, so
 // a sum below 2^-90 is multiplied by 2^64 first and the result by 2^32.  (Kernels of their own: with selects for every head 8,192 rows x
 // 40 heads x 128 both ways take 2 to 3% longer, with a branch that is one way for the whole launch 3.6% backward.)
 template <bool BARE>
