@@ -712,8 +712,9 @@ enum { DFLARE_ACT_NONE = 0, DFLARE_ACT_RELU = 1, DFLARE_ACT_SILU = 2, DFLARE_ACT
 /*
  * What a call of the projections or the gated block with these sizes does (no GPU call).  The choice is the library's own and may
  * change with it; the results' roundings hang on it, nothing else.
- *   tiles    of the output, columns x rows: DFLARE_TILES_NONE (up to 32 rows forward: columns in turn, the weights read once), _64 (128 x 64; dw
- *            128 x 128), _128 (128 x 128), _128_64 (128 x 128, 128 x 64 from row `split` on), _256 (256 x 256)
+ *   tiles    of the output, columns (the gated block's forward: half of them of each matrix) x rows: DFLARE_TILES_NONE (up to 32 rows forward:
+ *            columns in turn, the weights read once), _64 (128 x 64; dw 128 x 128), _128 (128 x 128), _128_64 (128 x 128, and 128 x 64
+ *            from row `split` on), _256 (256 x 256)
  *   parts    of the sums of y (both of the gated block's products) or dx, which are added in a launch of their own; parts_w: of dw
  *   workspace  bytes that the call takes
  */
